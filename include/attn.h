@@ -348,6 +348,51 @@ attn_status_t attn_fwd_splitkv(const void* q, const void* k, const void* v, void
                                int n_splits, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * attn_bwd -- gradients of the attention forward pass (Section 2.2's operation; the paper times the
+ * forward pass only).  With S = scale Q K^T, P = exp(S - LSE), 0 where the mask hides a key, and
+ * delta_i = sum_d dO_id O_id - dLSE_i:
+ *
+ *     dV = P^T dO,   dP = dO V^T,   dS = P o (dP - delta),   dQ = scale dS K,   dK = scale dS^T Q
+ *
+ * The probabilities are recomputed from q, k and lse.  A key head shared by several query heads
+ * (GQA) gets the sum of their contributions.
+ *
+ *   dout    BF16 [B, Sq, Hq, D]   gradient with respect to o                        (read)
+ *   q, k, v, o, lse               inputs and results of attn_fwd; lse is required    (read)
+ *   dlse    FP32 [B, Hq, Sq]      gradient with respect to lse; may be NULL (zero)   (read)
+ *   dq      BF16 [B, Sq, Hq, D]                                                      (written)
+ *   dk, dv  BF16 [B, Sk, Hkv, D]                                                     (written)
+ *   workspace  device memory, 16-byte aligned, owned by the caller, at least
+ *           attn_bwd_workspace_bytes(...) bytes; its contents are undefined before and after
+ *   shapes, causal, scale, alignment, stream: as for attn_fwd
+ *
+ * Rows that see no key (causal, Sq > Sk; their lse is -infinity) have dq = 0 and contribute nothing,
+ * whatever their dlse.  dout must be finite, also in such rows.  dq, dk, dv and workspace must not
+ * overlap each other or any input.  S, dP and the gradients accumulate in fp32 on the tensor cores
+ * and each output is rounded once; P and dS are rounded to BF16 before the products that read them.
+ * Every sum has a fixed order: the same call gives the same bits.  Asynchronous on `stream`, no
+ * state is kept between calls: any number of calls may run at once, each with its own
+ * workspace, and calls can be captured into a CUDA graph (after a first call on the device outside
+ * capture); replays that may overlap need workspaces of their own.
+ * Errors: those of attn_fwd; ATTN_ERR_TOO_LARGE if the workspace is too small.
+ */
+size_t attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal); /* 0: sizes attn_bwd refuses */
+attn_status_t attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
+                       const float* dlse, void* dq, void* dk, void* dv, int B, int Hq, int Hkv, int Sq, int Sk, int D,
+                       int causal, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * attn_bwd_strided -- attn_bwd on strided views; the strides follow attn_fwd_strided's rules, for
+ * every tensor (rows of dq, of dk and of dv must not overlap; lse and dlse are contiguous).
+ */
+attn_status_t attn_bwd_strided(const void* dout, const void* q, const void* k, const void* v, const void* o,
+                               const float* lse, const float* dlse, void* dq, void* dk, void* dv, int B, int Hq, int Hkv,
+                               int Sq, int Sk, int D, const long long* dout_strides, const long long* q_strides,
+                               const long long* k_strides, const long long* v_strides, const long long* o_strides,
+                               const long long* dq_strides, const long long* dk_strides, const long long* dv_strides,
+                               int causal, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * attn_selftest_wait_timeout -- exercises the bounded waits every kernel of this library uses
  * between its warp roles (the paper's kernels hand work between MMA, softmax, correction and
  * load warps "with barrier-based signaling", Section 2.2; here every such wait has a time limit).

@@ -23,7 +23,8 @@ STATUS_NAMES = {
     5: "ATTN_ERR_CUDA", 6: "ATTN_ERR_ARCH", 7: "ATTN_ERR_TIMEOUT", 8: "ATTN_ERR_TOO_LARGE",
 }
 EXPORTED_SYMBOLS = ("attn_fwd", "attn_fwd_strided", "attn_fwd_host", "attn_fwd_noalloc", "attn_merge", "attn_merge_n",
-                    "attn_fwd_splitkv", "attn_splitkv_workspace_bytes", "attn_release_host_staging", "attn_set_option",
+                    "attn_fwd_splitkv", "attn_splitkv_workspace_bytes", "attn_bwd", "attn_bwd_strided", "attn_bwd_workspace_bytes",
+                    "attn_release_host_staging", "attn_set_option",
                     "attn_get_option",
                     "attn_plan", "attn_plan_item", "attn_plan_item_pair", "attn_last_launch_clock", "attn_launch_clocks", "attn_selftest_wait_timeout", "attn_status_str", "attn_version",
                     "attn_last_device_status")
@@ -77,6 +78,13 @@ def load_library() -> ctypes.CDLL:
     lib.attn_splitkv_workspace_bytes.restype = ctypes.c_size_t
     lib.attn_fwd_splitkv.argtypes = fwd_args[:13] + [ci, vp, ctypes.c_size_t, vp]
     lib.attn_fwd_splitkv.restype = ci
+    bwd_args = [vp] * 10 + [ci] * 6
+    lib.attn_bwd.argtypes = bwd_args + [ci, cf, vp, ctypes.c_size_t, vp]
+    lib.attn_bwd.restype = ci
+    lib.attn_bwd_strided.argtypes = bwd_args + [ll3] * 8 + [ci, cf, vp, ctypes.c_size_t, vp]
+    lib.attn_bwd_strided.restype = ci
+    lib.attn_bwd_workspace_bytes.argtypes = [ci] * 7
+    lib.attn_bwd_workspace_bytes.restype = ctypes.c_size_t
     lib.attn_selftest_wait_timeout.argtypes = [ci, vp]
     lib.attn_selftest_wait_timeout.restype = ci
     lib.attn_status_str.argtypes = [ci]
@@ -334,6 +342,75 @@ def attn_fwd_splitkv(q, k, v, o, lse, causal: bool, scale: float, n_splits: int,
         raise AttnError(st, "attn_fwd_splitkv")
 
 
+def attn_bwd_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Sk: int, D: int, causal: bool) -> int:
+    return int(load_library().attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, int(bool(causal))))
+
+
+def _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, strided):
+    named = (("dout", dout), ("q", q), ("k", k), ("v", v), ("o", o), ("dq", dq), ("dk", dk), ("dv", dv))
+    dev = q.device
+    for name, t in named:
+        if t.dtype != torch.bfloat16 or t.dim() != 4 or t.device.type != "cuda" or t.device != dev \
+                or not (t.stride(3) == 1 if strided else t.is_contiguous()):
+            layout = "with a contiguous last axis" if strided else "that is contiguous"
+            raise ValueError(f"{name} must be a 4-D bfloat16 tensor [B, S, H, D] {layout}, all on one cuda device")
+    B, Sq, Hq, D = q.shape
+    Bk, Sk, Hkv, Dk = k.shape
+    if v.shape != k.shape or o.shape != q.shape or dout.shape != q.shape or dq.shape != q.shape or dk.shape != k.shape \
+            or dv.shape != k.shape or Bk != B or Dk != D:
+        raise ValueError("inconsistent q/k/v/o/dout/dq/dk/dv shapes")
+    for name, t in (("lse", lse), ("dlse", dlse)):
+        if t is None and name == "dlse":
+            continue
+        if t is None or t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (B, Hq, Sq) or t.device != dev:
+            raise ValueError(f"{name} must be a contiguous float32 tensor [B, Hq, Sq] on q's device")
+    lib = load_library()
+    if workspace is None:
+        need = lib.attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, int(bool(causal)))
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+    elif not workspace.is_contiguous() or workspace.device != dev:
+        raise ValueError("workspace must be a contiguous tensor on q's device")
+    ptrs = [t.data_ptr() for t in (dout, q, k, v, o, lse)] + [None if dlse is None else dlse.data_ptr()] \
+        + [t.data_ptr() for t in (dq, dk, dv)] + [B, Hq, Hkv, Sq, Sk, D]
+    with torch.cuda.device(dev):
+        if stream is None:
+            stream = torch.cuda.current_stream(dev).cuda_stream
+        tail = (int(bool(causal)), float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+        if strided:
+            return lib.attn_bwd_strided(*ptrs, *[_strides3(t) for _, t in named], *tail)
+        return lib.attn_bwd(*ptrs, *tail)
+
+
+def attn_bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal: bool, scale: float, dlse=None, workspace=None,
+                    stream=None) -> int:
+    """Calls ``attn_bwd`` on CUDA tensors and returns its raw status code.  ``workspace`` is a contiguous
+    cuda tensor (allocated here when None)."""
+    return _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, False)
+
+
+def attn_bwd(dout, q, k, v, o, lse, dq, dk, dv, causal: bool, scale: float, dlse=None, workspace=None, stream=None) -> None:
+    """``attn_bwd`` of the C ABI: the gradients dq, dk, dv (written) of ``attn_fwd`` from its inputs q, k, v, its
+    results o, lse and the gradients dout (and dlse, may be None) with respect to them."""
+    st = attn_bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_bwd")
+
+
+def attn_bwd_strided_status(dout, q, k, v, o, lse, dq, dk, dv, causal: bool, scale: float, dlse=None, workspace=None,
+                            stream=None) -> int:
+    """Calls ``attn_bwd_strided`` on CUDA tensors of shape [B, S, H, D] with arbitrary batch, sequence and
+    head strides (the head dimension must be contiguous); returns the raw status."""
+    return _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, True)
+
+
+def attn_bwd_strided(dout, q, k, v, o, lse, dq, dk, dv, causal: bool, scale: float, dlse=None, workspace=None,
+                     stream=None) -> None:
+    """``attn_bwd_strided`` of the C ABI: ``attn_bwd`` on views (see ``attn_fwd_strided``)."""
+    st = attn_bwd_strided_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_bwd_strided")
+
+
 def attn_selftest_wait_timeout(limit_ms: int, device=0, stream=None) -> None:
     """Launches the bounded-wait self-test (see include/attn.h); read the outcome with
     ``attn_last_device_status``."""
@@ -393,3 +470,20 @@ def attention_forward(q, k, v, causal: bool = False, scale: float | None = None,
         if return_lse else None
     attn_fwd(q, k, v, o, lse, causal, scale)
     return (o, lse) if return_lse else o
+
+
+def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float | None = None, dlse=None):
+    """Gradients (dq, dk, dv) of ``attention_forward(q, k, v, causal, scale)`` from its results ``o``, ``lse`` and the
+    gradient ``dout`` with respect to ``o`` (and ``dlse`` with respect to ``lse``).  Inputs may be views as in
+    ``attn_fwd_strided``; a ``dout`` without an order of its own (the expanded gradient of a sum) is copied first.
+    The gradients are new contiguous tensors."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1])
+    if dout.dim() == 4 and not dout.is_contiguous() and (dout.stride(3) != 1 or 0 in dout.stride()):
+        dout = dout.contiguous()
+    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    if all(t.is_contiguous() for t in (dout, q, k, v, o)):
+        attn_bwd(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse)
+    else:
+        attn_bwd_strided(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse)
+    return dq, dk, dv

@@ -1,5 +1,6 @@
 // Host side of the C ABI declared in include/attn.h: argument checks, TMA descriptors,
-// persistent-grid set-up and the launch of attn_fwd_kernel.
+// persistent-grid set-up and the launch of attn_fwd_kernel.  The backward entry points are in
+// attn_bwd_api.cuh, included at the end.
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -12,6 +13,7 @@
 #include "attn_fwd_pair.cuh"
 #include "attn_fwd_w16.cuh"
 #include "attn_merge_kernel.cuh"
+#include "attn_bwd_kernel.cuh"
 
 namespace {
 
@@ -126,6 +128,8 @@ DeviceState* device_state(attn_status_t* st) {
                            attn::pair::kSmemBytes2) != cudaSuccess ||
       cudaFuncSetAttribute(attn::w16::attn_fwd_w16_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::kSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||
       cudaMalloc(&d.status, 2 * sizeof(int)) != cudaSuccess ||
       cudaMemset(d.status, 0, 2 * sizeof(int)) != cudaSuccess ||
@@ -950,3 +954,5 @@ attn_status_t attn_last_device_status(int* code, int* detail) {
 }
 
 }  // extern "C"
+
+#include "attn_bwd_api.cuh"

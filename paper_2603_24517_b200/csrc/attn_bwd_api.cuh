@@ -1,0 +1,124 @@
+// Host side of the backward entry points: argument checks, plan, TMA descriptors, launches.
+// Included by attn_api.cu (uses its device state and descriptor helpers).
+#pragma once
+
+namespace {
+
+using attn::bwd::BwdParams;
+
+// Bytes of one row-statistics array: fp32 [B * Hq][ceil(Sq / 128) * 128].
+size_t bwd_stat_bytes(int B, int Hq, int Sq) {
+  const size_t padded = (static_cast<size_t>(Sq) + attn::kTile - 1) / attn::kTile * attn::kTile;
+  return static_cast<size_t>(B) * Hq * padded * sizeof(float);
+}
+
+// Problem geometry and launch order (no device access).  False if the launch grid cannot hold the items.
+bool fill_bwd_plan(BwdParams* p, int B, int Hq, int Hkv, int Sq, int Sk, int causal) {
+  std::memset(p, 0, sizeof(*p));
+  p->B = B; p->Hq = Hq; p->Hkv = Hkv; p->Sq = Sq; p->Sk = Sk;
+  p->group = Hq / Hkv;
+  p->causal = causal ? 1 : 0;
+  p->off = Sk - Sq;
+  p->n_qt = (Sq + attn::kTile - 1) / attn::kTile;
+  p->n_kt = (Sk + attn::kTile - 1) / attn::kTile;
+  const long long keys = static_cast<long long>(B) * Hkv * p->n_kt, queries = static_cast<long long>(B) * Hq * p->n_qt;
+  if (keys + queries > 0x7fffffffLL) return false;
+  p->n_key_items = static_cast<int>(keys);
+  return true;
+}
+
+struct BwdTensors {
+  const void *dout, *q, *k, *v, *o;
+  const float *lse, *dlse;
+  void *dq, *dk, *dv;
+};
+struct BwdStrides {
+  Strides3 dout, q, k, v, o, dq, dk, dv;
+};
+
+attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, int Sk, int D, const BwdStrides& ts,
+                         int causal, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+  if (t.dout == nullptr || t.lse == nullptr || t.dq == nullptr || t.dk == nullptr || t.dv == nullptr ||
+      workspace == nullptr)
+    return ATTN_ERR_NULL;
+  attn_status_t st = check_args(t.q, t.k, t.v, const_cast<void*>(t.o), t.lse, B, Hq, Hkv, Sq, Sk, D, causal, scale, true);
+  if (st != ATTN_OK) return st;
+  BwdParams p;
+  if (!fill_bwd_plan(&p, B, Hq, Hkv, Sq, Sk, causal)) return ATTN_ERR_UNSUPPORTED;
+  const void* aligned[] = {t.dout, t.dq, t.dk, t.dv, workspace};
+  for (const void* a : aligned) {
+    if (reinterpret_cast<uintptr_t>(a) & 15) return ATTN_ERR_ALIGN;
+  }
+  if (t.dlse != nullptr && (reinterpret_cast<uintptr_t>(t.dlse) & 3)) return ATTN_ERR_ALIGN;
+  if (workspace_bytes < attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, causal)) return ATTN_ERR_TOO_LARGE;
+  DeviceState* dev = device_state(&st);
+  if (dev == nullptr) return st;
+
+  CUtensorMap tm_q, tm_k, tm_v, tm_do, tm_dq, tm_dk, tm_dv;
+  if (!make_tensor_map(&tm_q, t.q, B, Sq, Hq, ts.q) || !make_tensor_map(&tm_k, t.k, B, Sk, Hkv, ts.k) ||
+      !make_tensor_map(&tm_v, t.v, B, Sk, Hkv, ts.v) || !make_tensor_map(&tm_do, t.dout, B, Sq, Hq, ts.dout) ||
+      !make_tensor_map(&tm_dq, t.dq, B, Sq, Hq, ts.dq) || !make_tensor_map(&tm_dk, t.dk, B, Sk, Hkv, ts.dk) ||
+      !make_tensor_map(&tm_dv, t.dv, B, Sk, Hkv, ts.dv))
+    return ATTN_ERR_CUDA;
+
+  float* neg_lse2 = static_cast<float*>(workspace);
+  float* delta = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + bwd_stat_bytes(B, Hq, Sq));
+  p.scale = scale;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.neg_lse2 = neg_lse2;
+  p.delta = delta;
+  p.status = dev->status;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int padded = p.n_qt * attn::kTile;
+  const long long n_rows = static_cast<long long>(B) * Hq * padded;
+  long long blocks = (n_rows + attn::bwd::kPrepThreads / 16 - 1) / (attn::bwd::kPrepThreads / 16);
+  const long long cap = static_cast<long long>(dev->sm_count) * 8;
+  if (blocks > cap) blocks = cap;
+  attn::bwd::attn_bwd_prep_kernel<<<static_cast<int>(blocks), attn::bwd::kPrepThreads, 0, s>>>(
+      static_cast<const uint16_t*>(t.o), static_cast<const uint16_t*>(t.dout),
+      attn::bwd::RowStrides{ts.o.b, ts.o.s, ts.o.h}, attn::bwd::RowStrides{ts.dout.b, ts.dout.s, ts.dout.h}, t.lse, t.dlse,
+      neg_lse2, delta, Hq, Sq, padded, n_rows);
+  if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
+  const int grid = p.n_key_items + B * Hq * p.n_qt;
+  attn::bwd::attn_bwd_kernel<<<grid, attn::bwd::kBwdThreads, attn::bwd::kSmemBwdBytes, s>>>(tm_q, tm_k, tm_v, tm_do, tm_dq,
+                                                                                       tm_dk, tm_dv, p);
+  return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal) {
+  int dummy = 0;
+  if (check_args(&dummy, &dummy, &dummy, &dummy, nullptr, B, Hq, Hkv, Sq, Sk, D, causal, 1.0f, false) != ATTN_OK) return 0;
+  return 2 * bwd_stat_bytes(B, Hq, Sq);
+}
+
+attn_status_t attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
+                       const float* dlse, void* dq, void* dk, void* dv, int B, int Hq, int Hkv, int Sq, int Sk, int D,
+                       int causal, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+  const Strides3 sq = contiguous_strides(Sq, Hq), sk = contiguous_strides(Sk, Hkv);
+  return bwd_device(BwdTensors{dout, q, k, v, o, lse, dlse, dq, dk, dv}, B, Hq, Hkv, Sq, Sk, D,
+                    BwdStrides{sq, sq, sk, sk, sq, sq, sk, sk}, causal, scale, workspace, workspace_bytes, stream);
+}
+
+attn_status_t attn_bwd_strided(const void* dout, const void* q, const void* k, const void* v, const void* o,
+                               const float* lse, const float* dlse, void* dq, void* dk, void* dv, int B, int Hq, int Hkv,
+                               int Sq, int Sk, int D, const long long* dout_strides, const long long* q_strides,
+                               const long long* k_strides, const long long* v_strides, const long long* o_strides,
+                               const long long* dq_strides, const long long* dk_strides, const long long* dv_strides,
+                               int causal, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+  const long long* all[8] = {dout_strides, q_strides, k_strides, v_strides, o_strides, dq_strides, dk_strides, dv_strides};
+  Strides3 s[8];
+  for (int i = 0; i < 8; ++i) {
+    const attn_status_t st = check_strides(all[i]);
+    if (st != ATTN_OK) return st;
+    s[i] = Strides3{all[i][0], all[i][1], all[i][2]};
+  }
+  return bwd_device(BwdTensors{dout, q, k, v, o, lse, dlse, dq, dk, dv}, B, Hq, Hkv, Sq, Sk, D,
+                    BwdStrides{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}, causal, scale, workspace, workspace_bytes,
+                    stream);
+}
+
+}  // extern "C"
