@@ -393,6 +393,68 @@ attn_status_t attn_bwd_strided(const void* dout, const void* q, const void* k, c
                                int causal, float scale, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * attn_qk_norm_rope -- what stands between the query / key projection and attn_fwd: every head's
+ * query and key is divided by its root mean square, scaled by a learned weight and rotated by the
+ * position of its token, in one pass.  (The paper times attention alone; Section 2.2's q and k are
+ * this call's outputs.)  Per row x of 128 values, at position m:
+ *
+ *     n = x / sqrt(mean(x^2) + eps) * weight
+ *     y[a] = n[a] cos[m][i] - n[b] sin[m][i],   y[b] = n[b] cos[m][i] + n[a] sin[m][i]
+ *
+ * for the pairs (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) if `interleaved`, i < rot_dim / 2;
+ * y = n from rot_dim on.  Computed in fp32, rounded once.
+ *
+ *   q, k        BF16 [B, S, Hq, D], [B, S, Hkv, D]  (read)     any Hq, Hkv >= 1
+ *   q_weight, k_weight  [D], weight_type 0: FP32, 1: BF16; each may be NULL (all ones)
+ *   cos_table, sin_table  FP32 [n_positions, rot_dim / 2], contiguous
+ *   positions   the tokens' rows in the tables, position_type 0: int32, 1: int64, at element
+ *               b * position_strides[0] + s * position_strides[1] (NULL strides: contiguous [B, S];
+ *               strides may be 0).  NULL: token s is at position s, S <= n_positions
+ *   q_out, k_out  BF16, shapes of q and k (written); may be q and k themselves (same address and strides)
+ *   D           must be 128;  rot_dim  a multiple of 16 from 16 to 128;  eps  finite and > 0
+ *   *_strides   as in attn_fwd_strided; NULL: contiguous.  An output may be a slice of a key cache
+ *
+ * A position outside the tables reads nothing there: that token's outputs are NaN.  Each row is
+ * computed by itself: infinities and NaN stay in their row.  Pointers 16-byte aligned (positions: their size).
+ * Asynchronous on `stream`, one launch, no state; any number of calls may run at once, and after a first call
+ * on the device calls can be captured.  Overlaps other than the one named are not allowed.
+ * Errors: ATTN_ERR_NULL, ATTN_ERR_SHAPE (a size or stride <= 0, S > n_positions without positions),
+ * ATTN_ERR_UNSUPPORTED (D, rot_dim, eps, a type; an output at its input's address with other strides),
+ * ATTN_ERR_ALIGN, ATTN_ERR_CUDA, ATTN_ERR_ARCH.
+ */
+attn_status_t attn_qk_norm_rope(const void* q, const void* k, const void* q_weight, const void* k_weight, int weight_type,
+                                const float* cos_table, const float* sin_table, const void* positions, int position_type,
+                                const long long* position_strides, void* q_out, void* k_out, int B, int S, int Hq, int Hkv,
+                                int D, int rot_dim, int n_positions, int interleaved, float eps, const long long* q_strides,
+                                const long long* k_strides, const long long* q_out_strides, const long long* k_out_strides,
+                                void* stream);
+
+/*
+ * attn_qk_norm_rope_bwd -- its gradient.  With g = dq_out (dk_out) rotated back and r = 1 / sqrt(mean(x^2) + eps):
+ *
+ *     dx = r (g weight - x r^2 mean(g weight x)),     dweight = sum over all rows of g x r
+ *
+ *   dq_out, dk_out   BF16, gradients with respect to q_out, k_out          (read)
+ *   q, k, weights, tables, positions, eps: as given to attn_qk_norm_rope    (read)
+ *   dq, dk           BF16 (written); each may be dq_out / dk_out or q / k itself (same address and strides)
+ *   dq_weight, dk_weight  FP32 [D] (written); each may be NULL
+ *   workspace        device memory, 16-byte aligned, attn_qk_norm_rope_bwd_workspace_bytes() bytes; may be NULL
+ *                    when neither weight gradient is wanted
+ * The weight sums run in fp32 in a fixed order: the same call gives the same bits.  A token whose position lies
+ * outside the tables has NaN in dx and makes the weight gradients NaN.  Otherwise as attn_qk_norm_rope;
+ * calls that may overlap need workspaces of their own, replays of one captured call too.
+ */
+size_t attn_qk_norm_rope_bwd_workspace_bytes(void);
+attn_status_t attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k, const void* q_weight,
+                                    const void* k_weight, int weight_type, const float* cos_table, const float* sin_table,
+                                    const void* positions, int position_type, const long long* position_strides, void* dq,
+                                    void* dk, float* dq_weight, float* dk_weight, int B, int S, int Hq, int Hkv, int D,
+                                    int rot_dim, int n_positions, int interleaved, float eps, const long long* dq_out_strides,
+                                    const long long* dk_out_strides, const long long* q_strides, const long long* k_strides,
+                                    const long long* dq_strides, const long long* dk_strides, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/*
  * attn_selftest_wait_timeout -- exercises the bounded waits every kernel of this library uses
  * between its warp roles (the paper's kernels hand work between MMA, softmax, correction and
  * load warps "with barrier-based signaling", Section 2.2; here every such wait has a time limit).

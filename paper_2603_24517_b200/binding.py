@@ -24,6 +24,7 @@ STATUS_NAMES = {
 }
 EXPORTED_SYMBOLS = ("attn_fwd", "attn_fwd_strided", "attn_fwd_host", "attn_fwd_noalloc", "attn_merge", "attn_merge_n",
                     "attn_fwd_splitkv", "attn_splitkv_workspace_bytes", "attn_bwd", "attn_bwd_strided", "attn_bwd_workspace_bytes",
+                    "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes",
                     "attn_release_host_staging", "attn_set_option",
                     "attn_get_option",
                     "attn_plan", "attn_plan_item", "attn_plan_item_pair", "attn_last_launch_clock", "attn_launch_clocks", "attn_selftest_wait_timeout", "attn_status_str", "attn_version",
@@ -85,6 +86,13 @@ def load_library() -> ctypes.CDLL:
     lib.attn_bwd_strided.restype = ci
     lib.attn_bwd_workspace_bytes.argtypes = [ci] * 7
     lib.attn_bwd_workspace_bytes.restype = ctypes.c_size_t
+    rope_in = [vp, vp, vp, vp, ci, vp, vp, vp, ci, ctypes.POINTER(ctypes.c_longlong)]
+    lib.attn_qk_norm_rope.argtypes = rope_in + [vp, vp] + [ci] * 8 + [cf] + [ll3] * 4 + [vp]
+    lib.attn_qk_norm_rope.restype = ci
+    lib.attn_qk_norm_rope_bwd.argtypes = [vp, vp] + rope_in + [vp] * 4 + [ci] * 8 + [cf] + [ll3] * 6 + [vp, ctypes.c_size_t, vp]
+    lib.attn_qk_norm_rope_bwd.restype = ci
+    lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = []
+    lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
     lib.attn_selftest_wait_timeout.argtypes = [ci, vp]
     lib.attn_selftest_wait_timeout.restype = ci
     lib.attn_status_str.argtypes = [ci]
@@ -411,6 +419,114 @@ def attn_bwd_strided(dout, q, k, v, o, lse, dq, dk, dv, causal: bool, scale: flo
         raise AttnError(st, "attn_bwd_strided")
 
 
+def _rope_args(q, k, q_weight, k_weight, cos, sin, positions, others):
+    """Checks the tensors and marshals what both directions share: (leading arguments, sizes)."""
+    dev = q.device
+    for name, t in (("q", q), ("k", k)) + others:
+        if t.dtype != torch.bfloat16 or t.dim() != 4 or t.stride(3) != 1 or t.device != dev or dev.type != "cuda":
+            raise ValueError(f"{name} must be a 4-D bfloat16 tensor [B, S, H, D] with a contiguous last axis, "
+                             "all on one cuda device")
+    B, S, Hq, D = q.shape
+    Hkv = k.shape[2]
+    if k.shape != (B, S, Hkv, D):
+        raise ValueError("inconsistent q/k shapes")
+    for name, t in others:
+        if t.shape != (q if "q" in name else k).shape:
+            raise ValueError(f"inconsistent shape of {name}")
+    weight_type = -1
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if w.dtype not in (torch.float32, torch.bfloat16) or w.shape != (D,) or not w.is_contiguous() or w.device != dev:
+            raise ValueError(f"{name} must be a contiguous float32 or bfloat16 tensor [D] on q's device")
+        kind = int(w.dtype == torch.bfloat16)
+        if weight_type not in (-1, kind):
+            raise ValueError("q_weight and k_weight must have one type")
+        weight_type = kind
+    if cos.dtype != torch.float32 or cos.dim() != 2 or not cos.is_contiguous() or cos.device != dev \
+            or sin.dtype != torch.float32 or sin.shape != cos.shape or not sin.is_contiguous() or sin.device != dev:
+        raise ValueError("cos and sin must be contiguous float32 tensors [positions, rot_dim / 2] on q's device")
+    pos_ptr, pos_type, pos_strides = None, 0, None
+    if positions is not None:
+        if positions.dtype not in (torch.int32, torch.int64) or positions.device != dev \
+                or positions.shape not in ((B, S), (S,)):
+            raise ValueError("positions must be an int32 or int64 tensor [B, S] or [S] on q's device")
+        pos_ptr, pos_type = positions.data_ptr(), int(positions.dtype == torch.int64)
+        if positions.dim() == 1 or not positions.is_contiguous():
+            pos_strides = (ctypes.c_longlong * 2)(*((0, positions.stride(0)) if positions.dim() == 1 else positions.stride()))
+    lead = (q.data_ptr(), k.data_ptr(), None if q_weight is None else q_weight.data_ptr(),
+            None if k_weight is None else k_weight.data_ptr(), max(weight_type, 0), cos.data_ptr(), sin.data_ptr(),
+            pos_ptr, pos_type, pos_strides)
+    return lead, (B, S, Hq, Hkv, D, 2 * cos.shape[1], cos.shape[0])
+
+
+def _strides3_or_none(t):
+    return None if t.is_contiguous() else _strides3(t)
+
+
+def attn_qk_norm_rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6,
+                             interleaved: bool = False, stream=None) -> int:
+    """Calls ``attn_qk_norm_rope`` on CUDA tensors and returns its raw status code."""
+    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, (("q_out", q_out), ("k_out", k_out)))
+    with torch.cuda.device(q.device):
+        if stream is None:
+            stream = torch.cuda.current_stream(q.device).cuda_stream
+        return load_library().attn_qk_norm_rope(*lead, q_out.data_ptr(), k_out.data_ptr(), *sizes, int(bool(interleaved)),
+                                                float(eps), *[_strides3_or_none(t) for t in (q, k, q_out, k_out)], stream)
+
+
+def attn_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6,
+                      interleaved: bool = False, stream=None) -> None:
+    """``attn_qk_norm_rope`` of the C ABI: per-head root-mean-square norm and rotation of q [B,S,Hq,D] and k [B,S,Hkv,D]
+    into q_out and k_out (which may be q and k, or views of a cache).  Tables ``cos``, ``sin`` [positions, rot_dim / 2],
+    ``positions`` [B,S] or [S] (None: 0 .. S-1), weights [D] or None."""
+    st = attn_qk_norm_rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved, stream)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_qk_norm_rope")
+
+
+def attn_qk_norm_rope_bwd_workspace_bytes() -> int:
+    return int(load_library().attn_qk_norm_rope_bwd_workspace_bytes())
+
+
+def attn_qk_norm_rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight,
+                                 positions=None, eps: float = 1e-6, interleaved: bool = False, workspace=None,
+                                 stream=None) -> int:
+    """Calls ``attn_qk_norm_rope_bwd``; ``workspace`` is a contiguous cuda tensor (allocated here when None)."""
+    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions,
+                             (("dq_out", dq_out), ("dk_out", dk_out), ("dq", dq), ("dk", dk)))
+    for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
+        if t is not None and (t.dtype != torch.float32 or t.shape != q.shape[3:] or not t.is_contiguous()
+                              or t.device != q.device):
+            raise ValueError(f"{name} must be a contiguous float32 tensor [D] on q's device")
+    lib = load_library()
+    if workspace is None:
+        if dq_weight is not None or dk_weight is not None:
+            workspace = torch.empty(lib.attn_qk_norm_rope_bwd_workspace_bytes(), dtype=torch.uint8, device=q.device)
+    elif not workspace.is_contiguous() or workspace.device != q.device:
+        raise ValueError("workspace must be a contiguous tensor on q's device")
+    with torch.cuda.device(q.device):
+        if stream is None:
+            stream = torch.cuda.current_stream(q.device).cuda_stream
+        return lib.attn_qk_norm_rope_bwd(dq_out.data_ptr(), dk_out.data_ptr(), *lead, dq.data_ptr(), dk.data_ptr(),
+                                         None if dq_weight is None else dq_weight.data_ptr(),
+                                         None if dk_weight is None else dk_weight.data_ptr(), *sizes,
+                                         int(bool(interleaved)), float(eps),
+                                         *[_strides3_or_none(t) for t in (dq_out, dk_out, q, k, dq, dk)],
+                                         None if workspace is None else workspace.data_ptr(),
+                                         0 if workspace is None else workspace.numel() * workspace.element_size(), stream)
+
+
+def attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions=None,
+                          eps: float = 1e-6, interleaved: bool = False, workspace=None, stream=None) -> None:
+    """``attn_qk_norm_rope_bwd`` of the C ABI: gradients of ``attn_qk_norm_rope`` with respect to q, k (BF16) and both weights
+    (FP32 [D], each may be None)."""
+    st = attn_qk_norm_rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight,
+                                      positions, eps, interleaved, workspace, stream)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_qk_norm_rope_bwd")
+
+
 def attn_selftest_wait_timeout(limit_ms: int, device=0, stream=None) -> None:
     """Launches the bounded-wait self-test (see include/attn.h); read the outcome with
     ``attn_last_device_status``."""
@@ -472,6 +588,13 @@ def attention_forward(q, k, v, causal: bool = False, scale: float | None = None,
     return (o, lse) if return_lse else o
 
 
+def _ordered(grad):
+    """A gradient as it comes: one that is expanded (of a sum or a mean) or turned is copied into an order of its own."""
+    if grad.dim() == 4 and not grad.is_contiguous() and (grad.stride(3) != 1 or 0 in grad.stride()):
+        return grad.contiguous()
+    return grad
+
+
 def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float | None = None, dlse=None):
     """Gradients (dq, dk, dv) of ``attention_forward(q, k, v, causal, scale)`` from its results ``o``, ``lse`` and the
     gradient ``dout`` with respect to ``o`` (and ``dlse`` with respect to ``lse``).  Inputs may be views as in
@@ -479,11 +602,30 @@ def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float
     The gradients are new contiguous tensors."""
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1])
-    if dout.dim() == 4 and not dout.is_contiguous() and (dout.stride(3) != 1 or 0 in dout.stride()):
-        dout = dout.contiguous()
+    dout = _ordered(dout)
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
     if all(t.is_contiguous() for t in (dout, q, k, v, o)):
         attn_bwd(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse)
     else:
         attn_bwd_strided(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse)
     return dq, dk, dv
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: float = 1e-6, interleaved: bool = False):
+    """Convenience wrapper: the normed and rotated queries and keys as new contiguous tensors (see ``attn_qk_norm_rope``),
+    ready for ``attention_forward``."""
+    q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    attn_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved)
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, positions=None, eps: float = 1e-6,
+                          interleaved: bool = False):
+    """Gradients (dq, dk, dq_weight, dk_weight) of ``qk_norm_rope``; a weight that is None has the gradient None."""
+    dq_out, dk_out = _ordered(dq_out), _ordered(dk_out)
+    dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    dq_weight, dk_weight = (None if w is None else torch.empty(w.shape, dtype=torch.float32, device=w.device)
+                            for w in (q_weight, k_weight))
+    attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions, eps,
+                          interleaved)
+    return dq, dk, dq_weight, dk_weight

@@ -9,7 +9,7 @@ _CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libattn_b200.so")
 SOURCES = ["attn_api.cu"]
 HEADERS = ["ptx.cuh", "attn_fwd_kernel.cuh", "attn_fwd_sb3.cuh", "attn_fwd_pair.cuh", "attn_fwd_w16.cuh", "attn_merge_kernel.cuh", "attn_bwd_kernel.cuh", "attn_bwd_api.cuh",
-           os.path.join("..", "..", "include", "attn.h")]
+           "qk_norm_rope_kernel.cuh", "qk_norm_rope_api.cuh",           os.path.join("..", "..", "include", "attn.h")]
 
 
 def _nvcc() -> str:

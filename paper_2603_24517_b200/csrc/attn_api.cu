@@ -1,6 +1,6 @@
 // Host side of the C ABI declared in include/attn.h: argument checks, TMA descriptors,
-// persistent-grid set-up and the launch of attn_fwd_kernel.  The backward entry points are in
-// attn_bwd_api.cuh, included at the end.
+// persistent-grid set-up and the launch of attn_fwd_kernel.  The backward pass and the norm with
+// rotation have their entry points in attn_bwd_api.cuh and qk_norm_rope_api.cuh, included at the end.
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -14,6 +14,7 @@
 #include "attn_fwd_w16.cuh"
 #include "attn_merge_kernel.cuh"
 #include "attn_bwd_kernel.cuh"
+#include "qk_norm_rope_kernel.cuh"
 
 namespace {
 
@@ -956,3 +957,4 @@ attn_status_t attn_last_device_status(int* code, int* detail) {
 }  // extern "C"
 
 #include "attn_bwd_api.cuh"
+#include "qk_norm_rope_api.cuh"
