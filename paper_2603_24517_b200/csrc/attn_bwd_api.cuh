@@ -62,11 +62,11 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
     return ATTN_ERR_CUDA;
 
   float* neg_lse2 = static_cast<float*>(workspace);
-  float* delta = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + bwd_stat_bytes(B, Hq, Sq));
+  float* neg_delta = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + bwd_stat_bytes(B, Hq, Sq));
   p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.neg_lse2 = neg_lse2;
-  p.delta = delta;
+  p.neg_delta = neg_delta;
   p.status = dev->status;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int padded = p.n_qt * attn::kTile;
@@ -77,7 +77,7 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
   attn::bwd::attn_bwd_prep_kernel<<<static_cast<int>(blocks), attn::bwd::kPrepThreads, 0, s>>>(
       static_cast<const uint16_t*>(t.o), static_cast<const uint16_t*>(t.dout),
       attn::bwd::RowStrides{ts.o.b, ts.o.s, ts.o.h}, attn::bwd::RowStrides{ts.dout.b, ts.dout.s, ts.dout.h}, t.lse, t.dlse,
-      neg_lse2, delta, Hq, Sq, padded, n_rows);
+      neg_lse2, neg_delta, Hq, Sq, padded, n_rows);
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
   const int grid = p.n_key_items + B * Hq * p.n_qt;
   attn::bwd::attn_bwd_kernel<<<grid, attn::bwd::kBwdThreads, attn::bwd::kSmemBwdBytes, s>>>(tm_q, tm_k, tm_v, tm_do, tm_dq,
