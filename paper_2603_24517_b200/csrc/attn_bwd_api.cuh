@@ -21,9 +21,28 @@ bool fill_bwd_plan(BwdParams* p, int B, int Hq, int Hkv, int Sq, int Sk, int cau
   p->off = Sk - Sq;
   p->n_qt = (Sq + attn::kTile - 1) / attn::kTile;
   p->n_kt = (Sk + attn::kTile - 1) / attn::kTile;
-  const long long keys = static_cast<long long>(B) * Hkv * p->n_kt, queries = static_cast<long long>(B) * Hq * p->n_qt;
-  if (keys + queries > 0x7fffffffLL) return false;
-  p->n_key_items = static_cast<int>(keys);
+  const long long units = static_cast<long long>(B) * Hkv;
+  // Parts of an item's stream: with fewer items than SMs an item is cut into parts of 8 tiles or more, so that the
+  // items fill the GPU.
+  p->key_splits = p->qry_splits = 1;
+  const long long items = units * (static_cast<long long>(p->n_kt) * p->key_splits +
+                                   static_cast<long long>(p->group) * p->n_qt * p->qry_splits);
+  if (items > 0x3fffffffLL) return false;
+  p->n_items = static_cast<int>(items);
+  // Causal: as many units in a run as keep their q, dout, k and v within 64 MB of L2.  Non-causal items are all alike:
+  // one unit after the other.
+  long long run = 1;
+  if (p->causal) {
+    run = (64LL << 20) / (512LL * (static_cast<long long>(Sq) * p->group + Sk));
+    if (run < 1) run = 1;
+    if (run > 64) run = 64;
+    if (run > units) run = units;
+  }
+  // runs of nearly equal size, so that the last one is not a small remainder
+  const int runs = static_cast<int>((units + run - 1) / run);
+  const int base = static_cast<int>(units) / runs, extra = static_cast<int>(units) % runs;
+  p->run = extra == 0 ? base : base + 1;
+  p->run_extra = extra == 0 ? runs : extra;
   return true;
 }
 
@@ -79,7 +98,7 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
       attn::bwd::RowStrides{ts.o.b, ts.o.s, ts.o.h}, attn::bwd::RowStrides{ts.dout.b, ts.dout.s, ts.dout.h}, t.lse, t.dlse,
       neg_lse2, neg_delta, Hq, Sq, padded, n_rows);
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-  const int grid = p.n_key_items + B * Hq * p.n_qt;
+  const int grid = p.n_items;
   attn::bwd::attn_bwd_kernel<<<grid, attn::bwd::kBwdThreads, attn::bwd::kSmemBwdBytes, s>>>(tm_q, tm_k, tm_v, tm_do, tm_dq,
                                                                                        tm_dk, tm_dv, p);
   return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;

@@ -3,24 +3,37 @@
 //
 //     dV = P^T dO,   dP = dO V^T,   dS = P o (dP - delta),   dQ = scale dS K,   dK = scale dS^T Q.
 //
-// P is recomputed from Q, K and LSE tile by tile.  Two kinds of CTAs in one launch, so that every sum
+// P is recomputed from Q, K and LSE tile by tile.  Two kinds of work items in one launch, so that every sum
 // has one owner and a fixed order (no atomics, the same bits on every run):
 //
-//   key CTAs    one 128-key tile of one KV head: K and V stay in shared memory, the query tiles (Q, dO) of
-//               every query head that shares the KV head stream past, dK and dV accumulate in tensor memory
-//               (products per tile pair: K Q^T, V dO^T, P^T dO, dS^T Q);
-//   query CTAs  one 128-row query tile of one head: Q and dO stay, the K / V tiles stream past, dQ accumulates
-//               in tensor memory (products per tile pair: Q K^T, dO V^T, dS K).
+//   key items    one 128-key tile of one KV head: K and V stay in shared memory, the query tiles (Q, dO) of
+//                every query head that shares the KV head stream past, dK and dV accumulate in tensor memory
+//                (products per tile pair: K Q^T, V dO^T, P^T dO, dS^T Q);
+//   query items  one 128-row query tile of one head: Q and dO stay, the K / V tiles stream past, dQ accumulates
+//                in tensor memory (products per tile pair: Q K^T, dO V^T, dS K).
 //
-// That is seven products where five would do if dQ were added up across CTAs, but those additions would
-// either come in any order or wait for one another.  Each CTA (576 threads, one per SM):
+// That is seven products where five would do if dQ were added up across key tiles, but those additions would
+// either come in any order or wait for one another.  A long item of a problem with few tiles can be split along its
+// stream; its parts leave fp32 partial sums that attn_bwd_join_kernel adds up in order.
 //
-//   warps 0-15  softmax: lane quarter w % 4 of the tile, 32 of its 128 columns (w / 4); a thread per row and quarter
-//   warp  16    MMA issue (tcgen05.mma by an elected lane)
-//   warps 17-18 loaders (TMA), one for each of the two streams: a ring of three 32 KB tiles for the one whose tiles
-//               are read by the first and the last product of a pair (Q or K), of two for the other (dO or V)
+// One CTA per SM (640 threads) works through items: the grid has a CTA per item, and a running CTA takes over CTAs
+// that have not started yet (clusterlaunchcontrol), so the hardware's own queue balances the work and nothing is
+// left in memory between launches.  Roles:
 //
-// Transposed tiles in key CTAs (rows are keys) let P^T and dS^T go back to tensor memory as the left
+//   warps 0-15  softmax: lane quarter w % 4 of the tile, 32 of its 128 columns (w / 4); a thread per row and quarter;
+//               the accumulators' way out (tensor memory -> BF16 -> shared memory)
+//   warps 16-17 MMA issue (tcgen05.mma by an elected lane).  Barrier polls and commits take a warp longer than the few
+//               instructions that the tensor pipe queues behind an issuer last, so one warp alone leaves the pipe
+//               idle; two warps feed it by turns.  Products that must keep an order share a warp:
+//               16: scores and the products that read P (key items) or dS (query items); 17: dP, and dK
+//   warp  18    loader (TMA).  Stream A (Q or K), whose tiles are read by the first and the last product of a pair, has
+//               a ring of three 32 KB tiles, stream B (dO or V) one of two; it also fetches the next item
+//   warp  19    TMA stores of the results
+//
+// The results are staged in ring slots, which the loader sets aside at the end of an item, so the next
+// item's tiles are already on their way while the results leave.
+//
+// Transposed tiles in key items (rows are keys) let P^T and dS^T go back to tensor memory as the left
 // operand of the second products, so nothing is transposed through shared memory.
 #pragma once
 
@@ -32,7 +45,10 @@ namespace bwd {
 constexpr int kParts = 4;                 // softmax threads per row
 constexpr int kCols = kTile / kParts;     // columns of a tile each of them handles
 constexpr int kSoftmaxWarps = 4 * kParts;
-constexpr int kBwdThreads = (kSoftmaxWarps + 3) * 32;
+constexpr int kBwdThreads = (kSoftmaxWarps + 4) * 32;
+// Registers a thread after the re-split (setmaxnreg): the block is launched with 96 each.
+constexpr int kRegsSoftmax = 104, kRegsOther = 56;
+static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsOther <= kBwdThreads / 32 * 96, "register split");
 constexpr int kRingA = 3, kRingB = 2;     // slots of the two streams: Q and dO, or K and V
 constexpr int kRingSlots = kRingA + kRingB;
 constexpr int kStatStages = 2;
@@ -42,8 +58,11 @@ constexpr int kSmemFixed = 0;  // two resident tiles
 constexpr int kSmemRing = 2 * kTileBytes;
 constexpr int kSmemStat = kSmemRing + kRingSlots * kTileBytes;  // [kStatStages][2][128]: -LSE log2(e), -delta
 constexpr int kSmemBwdBars = kSmemStat + kStatStages * 2 * kStatBytes;
-constexpr int kBwdBars = 1 + 2 * kRingSlots + 2 * kStatStages + 2 + 1 + 1 + 2 + 4 + 1 + 2;
-constexpr int kSmemBwdMisc = kSmemBwdBars + kBwdBars * 8;  // tensor memory base, abort flag
+constexpr int kBwdBars = 4 + 2 * kRingSlots + 2 * kStatStages + 2 + 1 + 1 + 2 + 4 + 2 + 2 + 2 + 4 + 2;
+constexpr int kItemInts = 12;
+constexpr int kSmemBwdClc = (kSmemBwdBars + kBwdBars * 8 + 15) / 16 * 16;  // [2] 16-byte answers of the launch queue
+constexpr int kSmemBwdItems = kSmemBwdClc + 32;                            // [2][kItemInts] mailbox of work items
+constexpr int kSmemBwdMisc = kSmemBwdItems + 2 * kItemInts * 4;            // tensor memory base, abort flag
 constexpr int kSmemBwdBytes = kSmemBwdMisc + 8;
 static_assert(kSmemBwdBytes <= 232448, "shared memory budget of one CTA");
 
@@ -53,35 +72,45 @@ struct BwdParams {
   int causal;
   int off;                // Sk - Sq: key j is visible to row i iff j <= i + off
   int n_qt, n_kt;         // 128-row query tiles, 128-key tiles
-  int n_key_items;        // CTAs [0, n_key_items) are key CTAs, the rest query CTAs
+  int key_splits, qry_splits;  // parts of a key / query item's stream
+  int n_items;            // B * Hkv * (n_kt * key_splits + group * n_qt * qry_splits)
+  int run, run_extra;     // launch order, see decode_item
   float scale, scale_log2;
   const float* neg_lse2;  // [B * Hq][n_qt * 128], -LSE * log2(e); -inf in rows that see no key or do not exist
   const float* neg_delta; // same layout, -delta, 0 in those rows
+  float *dq_part, *dk_part, *dv_part;  // fp32 partial sums of split items, [split][head of the batch][padded rows][128]
   int* status;
 };
 
 // codes of expired waits: role << 8 | barrier (roles continue the forward kernels' numbering)
 enum : int {
-  kRoleBwdLoad = 10 << 8, kRoleBwdMma = 11 << 8, kRoleBwdSoftmax = 12 << 8,
+  kRoleBwdLoad = 10 << 8, kRoleBwdMma = 11 << 8, kRoleBwdSoftmax = 12 << 8, kRoleBwdStore = 13 << 8, kRoleBwdMma2 = 14 << 8,
   kBarFixed = 1, kBarRingFull = 2, kBarRingEmpty = 3, kBarStat = 4, kBarStatEmpty = 5, kBarS = 6, kBarDp = 7,
-  kBarDpRead = 8, kBarP = 9, kBarDs = 10, kBarAcc = 11, kBarStage = 12
+  kBarDpRead = 8, kBarP = 9, kBarDs = 10, kBarAcc = 11, kBarAccEmpty = 12, kBarStageReady = 13, kBarStage = 14, kBarItem = 15,
+  kBarItemEmpty = 16, kBarClc = 17, kBarFixedEmpty = 18
 };
 
 struct BwdBarriers {
-  uint64_t* fixed_full;  // loader (TMA) -> MMA
+  uint64_t* fixed_full;  // [2]  loader (TMA) -> MMA: K or Q, V or dO
+  uint64_t* fixed_empty; // [2]  MMA commit after an item's last use -> loader
   uint64_t* a_full;      // [kRingA]  loader (TMA) -> MMA
-  uint64_t* a_empty;     // [kRingA]  MMA commit -> loader
+  uint64_t* a_empty;     // [kRingA]  two MMA commits, one for each product that reads the tile -> loader
   uint64_t* b_full;      // [kRingB]
   uint64_t* b_empty;     // [kRingB]
-  uint64_t* stat_full;   // [kStatStages]  loader (bulk copy) -> softmax (key CTAs)
+  uint64_t* stat_full;   // [kStatStages]  loader (bulk copy) -> softmax (key items)
   uint64_t* stat_empty;  // [kStatStages]  softmax (all warps) -> loader
-  uint64_t* s_full;      // [2]  MMA commit -> softmax (key CTAs use the first)
+  uint64_t* s_full;      // [2]  MMA commit -> softmax (key items use the first)
   uint64_t* dp_full;     // MMA commit -> softmax
-  uint64_t* dp_read;     // softmax (all warps) -> MMA: dP is in registers (query CTAs)
-  uint64_t* p_full;      // [2]  softmax warps of a half tile: its 64 columns of P are in tensor memory (key CTAs)
-  uint64_t* ds_full;     // [4]  the same for dS; query CTAs alternate two pairs, one for each score buffer
-  uint64_t* acc_full;    // MMA commit: the accumulators are final
-  uint64_t* stage_full;  // [2]  softmax warps of a half tile: its staging area is written
+  uint64_t* dp_read;     // softmax (all warps) -> MMA: dP is in registers (query items)
+  uint64_t* p_full;      // [2]  softmax warps of a half tile: its 64 columns of P are in tensor memory (key items)
+  uint64_t* ds_full;     // [4]  the same for dS; query items alternate two pairs, one for each score buffer
+  uint64_t* acc_full;    // commits of both MMA warps: the accumulators are final
+  uint64_t* acc_empty;   // softmax (all warps) -> MMA: they are in registers
+  uint64_t* stage_ready; // [2]  loader and store warp -> softmax: a slot of stream A / B is set aside for results
+  uint64_t* stage_full;  // [2]  softmax warps of a half tile -> store warp
+  uint64_t* item_full;   // [2]  loader -> everybody else: the next item is in the mailbox
+  uint64_t* item_empty;  // [2]
+  uint64_t* clc_full;    // [2]  the launch queue's answer has arrived
 };
 
 // Untiled copy of `bytes` (a multiple of 16) from global to shared memory, counted on `bar`.
@@ -92,62 +121,134 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
                : "memory");
 }
 
-// A CTA's item: which tile it owns and which tiles stream past it.
+// The launch queue: asks for a CTA that has not started yet (16-byte answer, counted on `bar`), and reads the answer:
+// the index of the CTA taken over, or -1 if none is left.
+__device__ __forceinline__ void clc_request(void* answer, uint64_t* bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                   smem_u32(answer)),
+               "r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ int clc_answer(const void* answer) {
+  uint32_t got, x;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      ".reg .b128 r;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "ld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t"
+      "}\n"
+      : "=r"(got), "=r"(x)
+      : "r"(smem_u32(answer))
+      : "memory");
+  return got != 0 ? static_cast<int>(x) : -1;
+}
+
+// A work item: the tile it owns and the tiles that stream past it.  Streamed tile t (t0 <= t < t0 + n) is tile
+// first + t % per_head of the t / per_head-th head of the group (key items), or tile t (query items).
 struct BwdItem {
-  int b, h;     // batch entry; KV head (key CTA) or query head (query CTA)
-  int row0;     // first key / query row of the owned tile
-  int first;    // first streamed tile of a head
-  int per_head; // streamed tiles per head
-  int n;        // streamed tiles in all (0: a query tile whose rows see no key)
+  int keys;         // 1: key item, 0: query item
+  int b, h;         // batch entry; KV head (key item) or query head (query item)
+  int row0;         // first key / query row of the owned tile
+  int first, per_head;
+  int t0, n;        // n = 0: nothing streams past, the result is 0
+  int split;        // which part of the stream this is, of key_splits / qry_splits
 };
 
-// Launch order: tile-major over (batch, head) with the longest items first under the causal mask.
-__host__ __device__ __forceinline__ BwdItem key_item(const BwdParams& p, int w) {
-  BwdItem it;
-  const int heads = p.B * p.Hkv;
-  int kt, bh;
-  if (p.causal) {  // early keys are seen by the most queries
-    kt = w / heads;
-    bh = w - kt * heads;
+// Launch order.  A unit is a (batch, KV head) with its query heads: n_kt key tiles and group * n_qt query tiles, each
+// in its number of parts.  Units are taken in runs of `run` (the first `run_extra` runs) or run - 1 units whose
+// streams together fit L2; in a run come first all key items, then all query items, rank by rank over its units,
+// under the causal mask the longest ranks (early keys, late rows) first, so that every run ends on short items.
+__host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int w) {
+  const int unit_keys = p.n_kt * p.key_splits;
+  const int per_unit = unit_keys + p.group * p.n_qt * p.qry_splits;
+  const int big = p.run * per_unit;
+  int first, g, rem;
+  if (w < p.run_extra * big) {
+    first = w / big;
+    rem = w - first * big;
+    first *= p.run;
+    g = p.run;
   } else {
-    bh = w / p.n_kt;
-    kt = w - bh * p.n_kt;
+    const int small = big - per_unit;
+    const int n = (w - p.run_extra * big) / small;
+    rem = (w - p.run_extra * big) - n * small;
+    first = p.run_extra * p.run + n * (p.run - 1);
+    g = p.run - 1;
   }
-  it.b = bh / p.Hkv;
-  it.h = bh - it.b * p.Hkv;
-  it.row0 = kt * kTile;
-  const int first_row = p.causal && it.row0 > p.off ? it.row0 - p.off : 0;  // < Sq: the last row sees every key
-  it.first = first_row / kTile;
-  it.per_head = p.n_qt - it.first;
-  it.n = it.per_head * p.group;
+  BwdItem it;
+  it.keys = rem < g * unit_keys ? 1 : 0;
+  int splits;
+  if (it.keys) {
+    splits = p.key_splits;
+    const int rank = rem / g, unit = first + rem - rank * g;
+    const int kt = rank / splits;
+    it.split = rank - kt * splits;
+    it.b = unit / p.Hkv;
+    it.h = unit - it.b * p.Hkv;
+    it.row0 = kt * kTile;
+    const int first_row = p.causal && it.row0 > p.off ? it.row0 - p.off : 0;  // < Sq: the last row sees every key
+    it.first = first_row / kTile;
+    it.per_head = p.n_qt - it.first;
+    it.n = it.per_head * p.group;
+  } else {
+    splits = p.qry_splits;
+    rem -= g * unit_keys;
+    const int wide = g * p.group;
+    const int rank = rem / wide, x = rem - rank * wide;
+    const int unit = first + x / p.group;
+    const int qt = rank / splits;
+    it.split = rank - qt * splits;
+    it.b = unit / p.Hkv;
+    it.h = (unit - it.b * p.Hkv) * p.group + x % p.group;
+    it.row0 = (p.causal ? p.n_qt - 1 - qt : qt) * kTile;
+    it.first = 0;
+    it.per_head = p.n_kt;
+    if (p.causal) {
+      const int row_end = it.row0 + kTile < p.Sq ? it.row0 + kTile : p.Sq;
+      const int last_key = row_end - 1 + p.off;
+      const int need = last_key < 0 ? 0 : last_key / kTile + 1;
+      if (need < it.per_head) it.per_head = need;
+    }
+    it.n = it.per_head;
+  }
+  it.t0 = 0;
+  if (splits > 1) {  // equal parts of this item's own stream
+    const long long n = it.n;
+    it.t0 = static_cast<int>(n * it.split / splits);
+    it.n = static_cast<int>(n * (it.split + 1) / splits) - it.t0;
+  }
   return it;
 }
-__host__ __device__ __forceinline__ BwdItem query_item(const BwdParams& p, int w) {
-  BwdItem it;
-  const int heads = p.B * p.Hq;
-  int qt, bh;
-  if (p.causal) {  // late rows see the most keys
-    qt = w / heads;
-    bh = w - qt * heads;
-    qt = p.n_qt - 1 - qt;
-  } else {
-    bh = w / p.n_qt;
-    qt = w - bh * p.n_qt;
-  }
-  it.b = bh / p.Hq;
-  it.h = bh - it.b * p.Hq;
-  it.row0 = qt * kTile;
-  it.first = 0;
-  it.per_head = p.n_kt;
-  if (p.causal) {
-    const int row_end = it.row0 + kTile < p.Sq ? it.row0 + kTile : p.Sq;
-    const int last_key = row_end - 1 + p.off;
-    const int need = last_key < 0 ? 0 : last_key / kTile + 1;
-    if (need < it.per_head) it.per_head = need;
-  }
-  it.n = it.per_head;
-  return it;
+// Whether the item's result goes out as BF16 through a staging slot (else as an fp32 partial sum).
+__device__ __forceinline__ bool staged(const BwdParams& p, const BwdItem& it) {
+  return (it.keys ? p.key_splits : p.qry_splits) == 1;
 }
+
+__device__ __forceinline__ void put_item(volatile int* slot, const BwdItem& it) {
+  slot[1] = it.keys; slot[2] = it.b; slot[3] = it.h; slot[4] = it.row0; slot[5] = it.first; slot[6] = it.per_head;
+  slot[7] = it.t0; slot[8] = it.n; slot[9] = it.split;
+}
+
+// Item number k of this CTA for a consuming warp: false when there are no more, or after an expired wait.  One
+// arrival per warp hands the mailbox slot back.
+__device__ __forceinline__ bool next_item(const BwdBarriers& bars, const volatile int* box, int k, WaitCtx ctx, int role,
+                                          bool whole_warp, bool arrives, BwdItem& it) {
+  bool ok = mbar_wait(&bars.item_full[k & 1], (k >> 1) & 1, ctx, role | kBarItem);
+  if (whole_warp) ok = __all_sync(0xffffffffu, ok);
+  if (!ok) return false;
+  const int* slot = const_cast<const int*>(box) + (k & 1) * kItemInts;
+  const int valid = slot[0];
+  it.keys = slot[1]; it.b = slot[2]; it.h = slot[3]; it.row0 = slot[4]; it.first = slot[5]; it.per_head = slot[6];
+  it.t0 = slot[7]; it.n = slot[8]; it.split = slot[9];
+  if (whole_warp) __syncwarp();
+  if (arrives) mbar_arrive(&bars.item_empty[k & 1]);
+  return valid != 0;
+}
+constexpr int kItemConsumers = kSoftmaxWarps + 3;  // softmax warps, MMA warps, store warp
 
 // D[128 x 128] (+)= A[tmem] B for 64 of the 128 contraction rows.  A (BF16) was written over fp32 columns, by each
 // softmax thread over the first half of its own kCols; B is MN-major (16 contraction rows are 2048 bytes).
@@ -164,7 +265,7 @@ __device__ __forceinline__ void issue_ts_half(bool leader, uint32_t tmem_d, uint
   }
 }
 
-// Tensor memory columns.  Key CTAs: S (then P over it), dP (then dS over it), dV, dK.  Query CTAs: two score buffers
+// Tensor memory columns.  Key items: S (then P over it), dP (then dS over it), dV, dK.  Query items: two score buffers
 // (dS over the scores it comes from), dP, dQ.
 constexpr uint32_t kTmS = 0, kTmDp = kTile, kTmDv = 2 * kTile, kTmDk = 3 * kTile;
 constexpr uint32_t kTmQryS = 0, kTmQryDp = 2 * kTile, kTmDq = 3 * kTile;  // score buffer j % 2 at kTmQryS + (j % 2) * kTile
@@ -174,152 +275,399 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, u
   tma_load_4d(dst + kHalfBytes, tm, bar, 64, head, row, b);
 }
 
-// Stream A (kA: Q in key CTAs, K in query CTAs) and the resident tiles, or stream B (dO, V).  Key CTAs' stream A also
-// brings the row statistics of its tiles.
-template <bool kKeys, bool kA>
-__device__ __forceinline__ void bwd_loader(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, uint8_t* smem,
-                                           WaitCtx ctx, const CUtensorMap* tm_fixed, const CUtensorMap* tm_stream) {
-  constexpr int kSlots = kA ? kRingA : kRingB;
-  uint64_t* full = kA ? bars.a_full : bars.b_full;
-  uint64_t* empty = kA ? bars.a_empty : bars.b_empty;
-  uint8_t* ring = smem + kSmemRing + (kA ? 0 : kRingA * kTileBytes);
-  // each loader brings one resident tile: K or Q with stream A, V or dO with stream B
-  mbar_arrive_expect_tx(bars.fixed_full, kTileBytes);
-  load_tile(smem + kSmemFixed + (kA ? 0 : kTileBytes), tm_fixed, bars.fixed_full, it.h, it.row0, it.b);
-  int head = kKeys ? it.h * p.group : it.h / p.group;
-  int tile = it.first;
+// The loader's counts: ring positions, resident tiles, statistics tiles so far.
+struct LoaderState {
+  uint32_t a = 0, b = 0, fixed = 0, stats = 0;
+};
+
+// A slot of a ring, for the next position.
+template <int kSlots>
+__device__ __forceinline__ bool wait_slot(uint64_t* empty, uint32_t pos, WaitCtx ctx) {
+  return mbar_wait(&empty[pos % kSlots], ((pos / kSlots) & 1) ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty);
+}
+
+// One item's tiles: the resident ones, then the streams, pair by pair; key items' stream A also brings the row
+// statistics of its tiles.  False after an expired wait.
+__device__ __forceinline__ bool load_item(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, uint8_t* smem,
+                                          WaitCtx ctx, const CUtensorMap* fixed_a, const CUtensorMap* fixed_b,
+                                          const CUtensorMap* stream_a, const CUtensorMap* stream_b, LoaderState& ls,
+                                          void* clc_buf, uint64_t* clc_bar) {
+  uint8_t* ring_a = smem + kSmemRing;
+  uint8_t* ring_b = ring_a + kRingA * kTileBytes;
+  const int head0 = it.keys ? it.h * p.group : it.h / p.group;
+  int head = head0 + it.t0 / (it.per_head > 0 ? it.per_head : 1);
+  int tile = it.first + it.t0 - (head - head0) * it.per_head;
   for (int i = 0; i < it.n; ++i) {
-    const int slot = i % kSlots;
-    if (!mbar_wait(&empty[slot], ((i / kSlots) & 1) ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return;
-    mbar_arrive_expect_tx(&full[slot], kTileBytes);
-    load_tile(ring + slot * kTileBytes, tm_stream, &full[slot], head, tile * kTile, it.b);
-    if (kKeys && kA) {
-      const int st = i & 1;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      if (i == 0) {  // the resident tile of the product that comes first
+        if (!mbar_wait(&bars.fixed_empty[x], (ls.fixed & 1) ^ 1, ctx, kRoleBwdLoad | kBarFixedEmpty)) return false;
+        mbar_arrive_expect_tx(&bars.fixed_full[x], kTileBytes);
+        load_tile(smem + kSmemFixed + x * kTileBytes, x == 0 ? fixed_a : fixed_b, &bars.fixed_full[x], it.h, it.row0, it.b);
+      }
+      if (x == 0) {
+        if (!wait_slot<kRingA>(bars.a_empty, ls.a, ctx)) return false;
+        const uint32_t slot = ls.a % kRingA;
+        mbar_arrive_expect_tx(&bars.a_full[slot], kTileBytes);
+        load_tile(ring_a + slot * kTileBytes, stream_a, &bars.a_full[slot], head, tile * kTile, it.b);
+        ++ls.a;
+      } else {
+        if (!wait_slot<kRingB>(bars.b_empty, ls.b, ctx)) return false;
+        const uint32_t slot = ls.b % kRingB;
+        mbar_arrive_expect_tx(&bars.b_full[slot], kTileBytes);
+        load_tile(ring_b + slot * kTileBytes, stream_b, &bars.b_full[slot], head, tile * kTile, it.b);
+        ++ls.b;
+      }
+    }
+    if (it.keys) {
+      const uint32_t st = ls.stats & 1;
       float* dst = reinterpret_cast<float*>(smem + kSmemStat) + st * 2 * kTile;
       const size_t at = (static_cast<size_t>(it.b) * p.Hq + head) * p.n_qt * kTile + static_cast<size_t>(tile) * kTile;
-      if (!mbar_wait(&bars.stat_empty[st], ((i >> 1) & 1) ^ 1, ctx, kRoleBwdLoad | kBarStatEmpty)) return;
+      if (!mbar_wait(&bars.stat_empty[st], ((ls.stats >> 1) & 1) ^ 1, ctx, kRoleBwdLoad | kBarStatEmpty)) return false;
       mbar_arrive_expect_tx(&bars.stat_full[st], 2 * kStatBytes);
       bulk_load(dst, p.neg_lse2 + at, kStatBytes, &bars.stat_full[st]);
       bulk_load(dst + kTile, p.neg_delta + at, kStatBytes, &bars.stat_full[st]);
+      ++ls.stats;
     }
     if (++tile == it.first + it.per_head) {
       tile = it.first;
       ++head;
     }
   }
-}
-
-// Shared-memory address of tile i of a stream, and the wait for it.
-__device__ __forceinline__ uint32_t a_tile(uint32_t base, int i) { return base + kSmemRing + (i % kRingA) * kTileBytes; }
-__device__ __forceinline__ uint32_t b_tile(uint32_t base, int i) {
-  return base + kSmemRing + (kRingA + i % kRingB) * kTileBytes;
-}
-__device__ __forceinline__ bool wait_a(const BwdBarriers& bars, int i, WaitCtx ctx) {
-  return mbar_wait_warp(&bars.a_full[i % kRingA], (i / kRingA) & 1, ctx, kRoleBwdMma | kBarRingFull);
-}
-__device__ __forceinline__ bool wait_b(const BwdBarriers& bars, int i, WaitCtx ctx) {
-  return mbar_wait_warp(&bars.b_full[i % kRingB], (i / kRingB) & 1, ctx, kRoleBwdMma | kBarRingFull);
-}
-
-// Tensor pipe order in a key CTA, per query tile i:  P(i)^T dO(i) | K Q(i+1)^T | dS(i)^T Q(i) | V dO(i+1)^T.
-// P(i+1) is exponentiated beside the last two, dS(i+1) is formed beside the next two.  P aliases the
-// scores it comes from and dS the dP it comes from: a later product into the same columns is issued behind the one
-// that reads them, on a pipe that executes in order.
-__device__ __forceinline__ void key_mma(const BwdItem& it, const BwdBarriers& bars, uint8_t* smem, WaitCtx ctx,
-                                        uint32_t tmem) {
-  const bool leader = elect_one();
-  const uint32_t base = smem_u32(smem);
-  const uint64_t k_desc = kmajor_desc(base + kSmemFixed), v_desc = kmajor_desc(base + kSmemFixed + kTileBytes);
-  if (!mbar_wait_warp(bars.fixed_full, 0, ctx, kRoleBwdMma | kBarFixed)) return;
-  if (!wait_a(bars, 0, ctx)) return;
-  tc_fence_after_sync();
-  issue_qk(leader, tmem + kTmS, k_desc, kmajor_desc(a_tile(base, 0)));
-  if (leader) mma_commit(bars.s_full);
-  if (!wait_b(bars, 0, ctx)) return;
-  tc_fence_after_sync();
-  issue_qk(leader, tmem + kTmDp, v_desc, kmajor_desc(b_tile(base, 0)));
-  if (leader) mma_commit(bars.dp_full);
-  for (int i = 0; i < it.n; ++i) {
-    const bool next = i + 1 < it.n;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (!mbar_wait_warp(&bars.p_full[h], i & 1, ctx, kRoleBwdMma | kBarP)) return;
-      tc_fence_after_sync();
-      issue_ts_half(leader, tmem + kTmDv, tmem + kTmS, vtile_desc(b_tile(base, i)), h, i > 0 || h > 0);
-    }
-    if (leader) mma_commit(&bars.b_empty[i % kRingB]);
-    if (next) {
-      if (!wait_a(bars, i + 1, ctx)) return;
-      tc_fence_after_sync();
-      issue_qk(leader, tmem + kTmS, k_desc, kmajor_desc(a_tile(base, i + 1)));
-      if (leader) mma_commit(bars.s_full);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (!mbar_wait_warp(&bars.ds_full[h], i & 1, ctx, kRoleBwdMma | kBarDs)) return;
-      tc_fence_after_sync();
-      issue_ts_half(leader, tmem + kTmDk, tmem + kTmDp, vtile_desc(a_tile(base, i)), h, i > 0 || h > 0);
-    }
-    if (leader) mma_commit(&bars.a_empty[i % kRingA]);
-    if (next) {
-      if (!wait_b(bars, i + 1, ctx)) return;
-      tc_fence_after_sync();
-      issue_qk(leader, tmem + kTmDp, v_desc, kmajor_desc(b_tile(base, i + 1)));
-      if (leader) mma_commit(bars.dp_full);
+  if (it.n > 0) ++ls.fixed;
+  // Ask for the next item only now that this one's last tiles are on their way (two tile pairs or so are still to be
+  // computed, longer than the answer takes): a CTA that reserved it earlier would keep others from it.
+  fence_proxy_async_smem();  // the answer this one overwrites was read through the generic proxy
+  mbar_arrive_expect_tx(clc_bar, 16);
+  clc_request(clc_buf, clc_bar);
+  if (staged(p, it)) {
+    // The slots behind the last tiles take the results.  The `full` barriers go through these positions too, so that
+    // they keep the phases of the `empty` ones.
+    if (!wait_slot<kRingA>(bars.a_empty, ls.a, ctx)) return false;
+    mbar_arrive(&bars.a_full[ls.a % kRingA]);
+    mbar_arrive(&bars.stage_ready[0]);
+    ++ls.a;
+    if (it.keys) {
+      if (!wait_slot<kRingB>(bars.b_empty, ls.b, ctx)) return false;
+      mbar_arrive(&bars.b_full[ls.b % kRingB]);
+      mbar_arrive(&bars.stage_ready[1]);
+      ++ls.b;
     }
   }
-  if (leader) mma_commit(bars.acc_full);
+  return true;
 }
 
-// Tensor pipe order in a query CTA, per key tile j:  Q K(j+1)^T | dO V(j+1)^T | dS(j) K(j).  The scores of tile j + 1 are
-// computed while tile j's are exponentiated (two score buffers; dS(j) goes over the scores of tile j, and S(j+2)
-// into the same columns is issued behind dS(j) K(j)); dP has one buffer, free as soon as it is in registers.
-__device__ __forceinline__ void query_mma(const BwdItem& it, const BwdBarriers& bars, uint8_t* smem, WaitCtx ctx,
-                                          uint32_t tmem) {
-  const bool leader = elect_one();
-  const uint32_t base = smem_u32(smem);
-  const uint64_t q_desc = kmajor_desc(base + kSmemFixed), do_desc = kmajor_desc(base + kSmemFixed + kTileBytes);
-  if (!mbar_wait_warp(bars.fixed_full, 0, ctx, kRoleBwdMma | kBarFixed)) return;
-  for (int j = -1; j < it.n; ++j) {
-    const int n = j + 1;
-    if (n < it.n) {  // scores and dP of the next tile
-      if (!wait_a(bars, n, ctx)) return;
+__device__ __forceinline__ void role_loader(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem, volatile int* box,
+                                            WaitCtx ctx, const CUtensorMap* tm_q, const CUtensorMap* tm_k,
+                                            const CUtensorMap* tm_v, const CUtensorMap* tm_do) {
+  LoaderState ls;
+  BwdItem it = decode_item(p, static_cast<int>(blockIdx.x));
+  put_item(box, it);
+  box[0] = 1;
+  mbar_arrive(&bars.item_full[0]);
+  for (int k = 0;; ++k) {
+    uint8_t* answer = smem + kSmemBwdClc + (k & 1) * 16;
+    uint64_t* clc_bar = &bars.clc_full[k & 1];
+    const bool ok = it.keys ? load_item(p, it, bars, smem, ctx, tm_k, tm_v, tm_q, tm_do, ls, answer, clc_bar)
+                            : load_item(p, it, bars, smem, ctx, tm_q, tm_do, tm_k, tm_v, ls, answer, clc_bar);
+    if (!ok || !mbar_wait(clc_bar, (k >> 1) & 1, ctx, kRoleBwdLoad | kBarClc)) return;
+    const int w = clc_answer(answer);
+    const int n = k + 1;
+    if (!mbar_wait(&bars.item_empty[n & 1], ((n >> 1) & 1) ^ 1, ctx, kRoleBwdLoad | kBarItemEmpty)) return;
+    volatile int* slot = box + (n & 1) * kItemInts;
+    if (w >= 0) {
+      it = decode_item(p, w);
+      put_item(slot, it);
+    }
+    slot[0] = w >= 0 ? 1 : 0;
+    mbar_arrive(&bars.item_full[n & 1]);
+    if (w < 0) return;
+  }
+}
+
+// TMA stores of the staged results; hands the slots back to the loader once they have been read.
+__device__ __forceinline__ void role_store(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem,
+                                           const volatile int* box, WaitCtx ctx, const CUtensorMap* tm_dq,
+                                           const CUtensorMap* tm_dk, const CUtensorMap* tm_dv) {
+  uint32_t pos_a = 0, pos_b = 0, stores = 0;
+  BwdItem it;
+  for (int k = 0; next_item(bars, box, k, ctx, kRoleBwdStore, false, true, it); ++k) {
+    pos_a += it.n;
+    pos_b += it.n;
+    if (!staged(p, it)) continue;
+    uint8_t* slot_a = smem + kSmemRing + (pos_a % kRingA) * kTileBytes;
+    uint8_t* slot_b = smem + kSmemRing + (kRingA + pos_b % kRingB) * kTileBytes;
+    // ready for this item's results: keeps the softmax warps from running two items ahead of this warp
+    mbar_arrive(&bars.stage_ready[0]);
+    if (it.keys) mbar_arrive(&bars.stage_ready[1]);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (!mbar_wait(&bars.stage_full[half], stores & 1, ctx, kRoleBwdStore | kBarStage)) return;
+      if (it.keys) {  // half 0: dV in stream B's slot, half 1: dK in stream A's
+        const CUtensorMap* tm = half == 0 ? tm_dv : tm_dk;
+        uint8_t* src = half == 0 ? slot_b : slot_a;
+        tma_store_4d(tm, src, 0, it.h, it.row0, it.b);
+        tma_store_4d(tm, src + kHalfBytes, 64, it.h, it.row0, it.b);
+      } else {
+        tma_store_4d(tm_dq, slot_a + half * kHalfBytes, half * 64, it.h, it.row0, it.b);
+      }
+      tma_store_commit();
+    }
+    ++stores;
+    tma_store_wait_read0();
+    // in the place of the two products that read a tile
+    mbar_arrive(&bars.a_empty[pos_a % kRingA]);
+    mbar_arrive(&bars.a_empty[pos_a % kRingA]);
+    ++pos_a;
+    if (it.keys) {
+      mbar_arrive(&bars.b_empty[pos_b % kRingB]);
+      mbar_arrive(&bars.b_empty[pos_b % kRingB]);
+      ++pos_b;
+    }
+  }
+}
+
+// Shared-memory address of ring position `pos` of a stream, and the wait for it.
+__device__ __forceinline__ uint32_t a_tile(uint32_t base, uint32_t pos) { return base + kSmemRing + (pos % kRingA) * kTileBytes; }
+__device__ __forceinline__ uint32_t b_tile(uint32_t base, uint32_t pos) {
+  return base + kSmemRing + (kRingA + pos % kRingB) * kTileBytes;
+}
+__device__ __forceinline__ bool wait_a(const BwdBarriers& bars, uint32_t pos, WaitCtx ctx, int role) {
+  return mbar_wait_warp(&bars.a_full[pos % kRingA], (pos / kRingA) & 1, ctx, role | kBarRingFull);
+}
+__device__ __forceinline__ bool wait_b(const BwdBarriers& bars, uint32_t pos, WaitCtx ctx, int role) {
+  return mbar_wait_warp(&bars.b_full[pos % kRingB], (pos / kRingB) & 1, ctx, role | kBarRingFull);
+}
+
+// Phases of the barriers that count tile pairs across items; every role that waits for them keeps its own copy.
+struct Phases {
+  uint32_t s = 0;    // bit x: uses of score buffer x so far (s_full[x], ds_full[2 x], ds_full[2 x + 1])
+  uint32_t dp = 0;   // tile pairs so far (dp_full)
+  uint32_t key = 0;  // tile pairs of key items (p_full, stat_full, stat_empty)
+  uint32_t qry = 0;  // tile pairs of query items (dp_read)
+};
+
+// What both MMA warps know of the item they work on.
+struct MmaItem {
+  uint32_t base, tmem;
+  uint32_t pos_a, pos_b, fixed;  // ring positions of its first tiles, resident tiles before it
+  uint32_t k;                    // its number
+  bool leader;
+  bool after_other;              // the item before was of the other kind
+};
+
+// Key item, first MMA warp:  S(0) | P(i)^T dO(i), S(i+1) | ...    (S = K Q^T)
+// Key item, second MMA warp: dP(0) | dS(i)^T Q(i), dP(i+1) | ...  (dP = V dO^T)
+// P(i+1) is exponentiated beside the second warp's products, dS(i+1) is formed beside the first warp's.  P aliases the
+// scores it comes from and dS the dP it comes from: a later product into the same columns is issued behind the one
+// that reads them by the same warp, and the pipe executes in order.  Waits that are over early (the tiles) come while
+// there is nothing to issue.  Across items the same order holds between items of one kind; products into columns that
+// the item before used otherwise, and into its accumulators, wait until its results have left tensor memory
+// (acc_empty).
+__device__ __forceinline__ bool key_mma_1(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+  constexpr int kRole = kRoleBwdMma;
+  const uint64_t k_desc = kmajor_desc(m.base + kSmemFixed);
+  uint32_t pos_a = m.pos_a, pos_b = m.pos_b;
+  if (!mbar_wait_warp(&bars.fixed_full[0], m.fixed & 1, ctx, kRole | kBarFixed) || !wait_a(bars, pos_a, ctx, kRole)) return false;
+  tc_fence_after_sync();
+  issue_qk(m.leader, m.tmem + kTmS, k_desc, kmajor_desc(a_tile(m.base, pos_a)));
+  if (m.leader) {
+    mma_commit(&bars.s_full[0]);
+    mma_commit(&bars.a_empty[pos_a % kRingA]);
+    if (it.n == 1) mma_commit(&bars.fixed_empty[0]);  // that was the last use of K
+  }
+  if (!mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
+  for (int i = 0; i < it.n; ++i, ++pos_a, ++pos_b) {
+    const bool next = i + 1 < it.n;
+    if (!wait_b(bars, pos_b, ctx, kRole)) return false;
+    if (next && !wait_a(bars, pos_a + 1, ctx, kRole)) return false;
+    const uint64_t do_desc = vtile_desc(b_tile(m.base, pos_b));
+    const uint64_t q_desc = kmajor_desc(a_tile(m.base, pos_a + 1));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (!mbar_wait_warp(&bars.p_full[h], ph.key & 1, ctx, kRole | kBarP)) return false;
       tc_fence_after_sync();
-      issue_qk(leader, tmem + kTmQryS + (n & 1) * kTile, q_desc, kmajor_desc(a_tile(base, n)));
-      if (leader) mma_commit(&bars.s_full[n & 1]);
-      if (!wait_b(bars, n, ctx)) return;
-      if (j >= 0 && !mbar_wait_warp(bars.dp_read, j & 1, ctx, kRoleBwdMma | kBarDpRead)) return;
-      tc_fence_after_sync();
-      issue_qk(leader, tmem + kTmQryDp, do_desc, kmajor_desc(b_tile(base, n)));
-      if (leader) {
-        mma_commit(bars.dp_full);
-        mma_commit(&bars.b_empty[n % kRingB]);
+      issue_ts_half(m.leader, m.tmem + kTmDv, m.tmem + kTmS, do_desc, h, i > 0 || h > 0);
+    }
+    if (next) {
+      issue_qk(m.leader, m.tmem + kTmS, k_desc, q_desc);
+      if (m.leader) {
+        mma_commit(&bars.s_full[0]);
+        mma_commit(&bars.a_empty[(pos_a + 1) % kRingA]);
+        if (i + 2 == it.n) mma_commit(&bars.fixed_empty[0]);
       }
     }
-    if (j >= 0) {
+    if (m.leader) mma_commit(&bars.b_empty[pos_b % kRingB]);
+    ++ph.key;
+  }
+  ph.s ^= it.n & 1;  // the other warp waits for dS
+  return true;
+}
+__device__ __forceinline__ bool key_mma_2(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+  constexpr int kRole = kRoleBwdMma2;
+  const uint64_t v_desc = kmajor_desc(m.base + kSmemFixed + kTileBytes);
+  uint32_t pos_a = m.pos_a, pos_b = m.pos_b;
+  // dP's columns were a score buffer of a query item, which the first MMA warp's products read
+  if (m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
+  if (!mbar_wait_warp(&bars.fixed_full[1], m.fixed & 1, ctx, kRole | kBarFixed) || !wait_b(bars, pos_b, ctx, kRole)) return false;
+  tc_fence_after_sync();
+  issue_qk(m.leader, m.tmem + kTmDp, v_desc, kmajor_desc(b_tile(m.base, pos_b)));
+  if (m.leader) {
+    mma_commit(bars.dp_full);
+    mma_commit(&bars.b_empty[pos_b % kRingB]);
+    if (it.n == 1) mma_commit(&bars.fixed_empty[1]);  // that was the last use of V
+  }
+  if (!m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
+  for (int i = 0; i < it.n; ++i, ++pos_a, ++pos_b) {
+    const bool next = i + 1 < it.n;
+    if (next && !wait_b(bars, pos_b + 1, ctx, kRole)) return false;
+    const uint64_t q_desc = vtile_desc(a_tile(m.base, pos_a));
+    const uint64_t do_desc = kmajor_desc(b_tile(m.base, pos_b + 1));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (!mbar_wait_warp(&bars.ds_full[h], ph.s & 1, ctx, kRole | kBarDs)) return false;
+      tc_fence_after_sync();
+      issue_ts_half(m.leader, m.tmem + kTmDk, m.tmem + kTmDp, q_desc, h, i > 0 || h > 0);
+    }
+    if (next) {
+      issue_qk(m.leader, m.tmem + kTmDp, v_desc, do_desc);
+      if (m.leader) {
+        mma_commit(bars.dp_full);
+        mma_commit(&bars.b_empty[(pos_b + 1) % kRingB]);
+        if (i + 2 == it.n) mma_commit(&bars.fixed_empty[1]);
+      }
+    }
+    if (m.leader) mma_commit(&bars.a_empty[pos_a % kRingA]);
+    ph.s ^= 1u;
+  }
+  return true;
+}
+
+// Query item, first MMA warp:  S(0), S(1) | dS(j) K(j), S(j+2) | ...  (S = Q K^T).  The scores of tile j + 1 are computed
+// while tile j's are exponentiated: two score buffers, dS(j) goes over the scores of tile j, and S(j+2) into the same
+// columns is issued behind dS(j) K(j).
+// Second MMA warp: dP(j) = dO V(j)^T into one buffer, free as soon as the softmax warps have it in registers.
+__device__ __forceinline__ bool query_mma_1(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+  constexpr int kRole = kRoleBwdMma;
+  const uint64_t q_desc = kmajor_desc(m.base + kSmemFixed);
+  const uint32_t pos = m.pos_a;
+  if (!mbar_wait_warp(&bars.fixed_full[0], m.fixed & 1, ctx, kRole | kBarFixed)) return false;
+  for (int j = -2; j < it.n; ++j) {
+    const int n = j + 2;
+    const uint32_t scores = m.tmem + kTmQryS + (n & 1) * kTile;  // buffer of tiles j and j + 2
+    const uint64_t k_desc = kmajor_desc(a_tile(m.base, pos + n));
+    // buffer 1 was a key item's dP, which the second MMA warp's products read
+    if (j == -1 && m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
+    if (j >= 0) {  // dQ += dS(j) K(j)
+      if (j == 0 && !m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
+      const int x = j & 1;
+      const uint64_t kv_desc = vtile_desc(a_tile(m.base, pos + j));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (!mbar_wait_warp(&bars.ds_full[(j & 1) * 2 + h], (j >> 1) & 1, ctx, kRoleBwdMma | kBarDs)) return;
+        if (!mbar_wait_warp(&bars.ds_full[2 * x + h], (ph.s >> x) & 1, ctx, kRole | kBarDs)) return false;
         tc_fence_after_sync();
-        issue_ts_half(leader, tmem + kTmDq, tmem + kTmQryS + (j & 1) * kTile, vtile_desc(a_tile(base, j)), h, j > 0 || h > 0);
+        issue_ts_half(m.leader, m.tmem + kTmDq, scores, kv_desc, h, j > 0 || h > 0);
       }
-      if (leader) mma_commit(&bars.a_empty[j % kRingA]);
+      ph.s ^= 1u << x;
+    }
+    if (n < it.n) {
+      if (!wait_a(bars, pos + n, ctx, kRole)) return false;
+      tc_fence_after_sync();
+      issue_qk(m.leader, scores, q_desc, k_desc);
+      if (m.leader) {
+        mma_commit(&bars.s_full[n & 1]);
+        mma_commit(&bars.a_empty[(pos + n) % kRingA]);
+        if (n + 1 == it.n) mma_commit(&bars.fixed_empty[0]);
+      }
+    }
+    if (j >= 0 && m.leader) mma_commit(&bars.a_empty[(pos + j) % kRingA]);
+  }
+  return true;
+}
+__device__ __forceinline__ bool query_mma_2(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+  constexpr int kRole = kRoleBwdMma2;
+  const uint64_t do_desc = kmajor_desc(m.base + kSmemFixed + kTileBytes);
+  uint32_t pos = m.pos_b;
+  if (!mbar_wait_warp(&bars.fixed_full[1], m.fixed & 1, ctx, kRole | kBarFixed) ||
+      !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty))
+    return false;
+  for (int j = 0; j < it.n; ++j, ++pos) {
+    if (!wait_b(bars, pos, ctx, kRole)) return false;
+    if (j > 0) {  // dP(j - 1) has been read
+      if (!mbar_wait_warp(bars.dp_read, ph.qry & 1, ctx, kRole | kBarDpRead)) return false;
+      ++ph.qry;
+    }
+    tc_fence_after_sync();
+    issue_qk(m.leader, m.tmem + kTmQryDp, do_desc, kmajor_desc(b_tile(m.base, pos)));
+    if (m.leader) {
+      mma_commit(bars.dp_full);
+      mma_commit(&bars.b_empty[pos % kRingB]);
+      mma_commit(&bars.b_empty[pos % kRingB]);  // the tile's only reader stands for two
+      if (j + 1 == it.n) mma_commit(&bars.fixed_empty[1]);
     }
   }
-  if (leader) mma_commit(bars.acc_full);
+  ++ph.qry;  // the last tile's phase: over by the time that the next item gets past acc_empty
+  ph.s ^= (((it.n + 1) >> 1) & 1) | (((it.n >> 1) & 1) << 1);  // the other warp waits for dS
+  return true;
 }
 
-// 32 fp32 columns of one row -> BF16 chunks of a 128-byte-swizzled [128][64] half tile; `chunk0` is the
-// first 16-byte chunk (0 or 4) in the half tile's row.
-__device__ __forceinline__ void stage_row32(uint8_t* half_tile, int row, int chunk0, const uint32_t* o, float factor) {
+template <bool kFirst>
+__device__ __forceinline__ void role_mma(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem, const volatile int* box,
+                                         WaitCtx ctx, uint32_t tmem, int lane) {
+  constexpr int kRole = kFirst ? kRoleBwdMma : kRoleBwdMma2;
+  MmaItem m;
+  m.base = smem_u32(smem);
+  m.tmem = tmem;
+  m.pos_a = m.pos_b = m.fixed = 0;
+  m.leader = elect_one();
+  Phases ph;
+  BwdItem it;
+  int kind_before = -1;
+  for (int k = 0; next_item(bars, box, k, ctx, kRole, true, lane == 0, it); ++k) {
+    m.k = k;
+    m.after_other = k > 0 && it.keys != kind_before;
+    if (it.n > 0) {
+      bool ok;
+      if (kFirst) {
+        ok = it.keys ? key_mma_1(it, m, bars, ctx, ph) : query_mma_1(it, m, bars, ctx, ph);
+      } else {
+        ok = it.keys ? key_mma_2(it, m, bars, ctx, ph) : query_mma_2(it, m, bars, ctx, ph);
+      }
+      if (!ok) return;
+      ++m.fixed;
+      kind_before = it.keys;
+    } else if (!mbar_wait_warp(bars.acc_empty, (k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) {
+      return;
+    }
+    if (m.leader) mma_commit(bars.acc_full);
+    m.pos_a += it.n;
+    m.pos_b += it.n;
+    if (staged(p, it)) {
+      ++m.pos_a;
+      if (it.keys) ++m.pos_b;
+    }
+  }
+}
+
+// 32 fp32 columns of one row, times `factor`, as BF16 words.
+__device__ __forceinline__ void pack_row32(const uint32_t* o, float factor, uint32_t* pk) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) pk[e] = pack_bf16x2(__uint_as_float(o[2 * e]) * factor, __uint_as_float(o[2 * e + 1]) * factor);
+}
+// Four 16-byte chunks of a row of a 128-byte-swizzled [128][64] half tile; `chunk0` is the first (0 or 4).
+__device__ __forceinline__ void stage_row32(uint8_t* half_tile, int row, int chunk0, const uint32_t* pk) {
 #pragma unroll
   for (int ch = 0; ch < 4; ++ch) {
-    uint4 val;
-    val.x = pack_bf16x2(__uint_as_float(o[ch * 8 + 0]) * factor, __uint_as_float(o[ch * 8 + 1]) * factor);
-    val.y = pack_bf16x2(__uint_as_float(o[ch * 8 + 2]) * factor, __uint_as_float(o[ch * 8 + 3]) * factor);
-    val.z = pack_bf16x2(__uint_as_float(o[ch * 8 + 4]) * factor, __uint_as_float(o[ch * 8 + 5]) * factor);
-    val.w = pack_bf16x2(__uint_as_float(o[ch * 8 + 6]) * factor, __uint_as_float(o[ch * 8 + 7]) * factor);
-    *reinterpret_cast<uint4*>(half_tile + row * 128 + (((chunk0 + ch) ^ (row & 7)) << 4)) = val;
+    *reinterpret_cast<uint4*>(half_tile + row * 128 + (((chunk0 + ch) ^ (row & 7)) << 4)) =
+        make_uint4(pk[ch * 4], pk[ch * 4 + 1], pk[ch * 4 + 2], pk[ch * 4 + 3]);
+  }
+}
+// The same columns as an fp32 partial sum of a split item.
+__device__ __forceinline__ void store_part32(float* dst, const uint32_t* o, float factor) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) {
+    *reinterpret_cast<float4*>(dst + e) = make_float4(__uint_as_float(o[e]) * factor, __uint_as_float(o[e + 1]) * factor,
+                                                      __uint_as_float(o[e + 2]) * factor, __uint_as_float(o[e + 3]) * factor);
   }
 }
 
@@ -351,28 +699,28 @@ __device__ __forceinline__ void exp_row(uint32_t* x, float2 c2, NegLse neg_lse, 
   }
 }
 
-// One softmax thread: row `row` of the tile, columns [part * kCols, (part + 1) * kCols).
-__device__ __forceinline__ void key_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, uint8_t* smem,
-                                            WaitCtx ctx, uint32_t tmem, int part, int row, int lane,
-                                            const CUtensorMap* tm_dk, const CUtensorMap* tm_dv) {
+// One softmax thread of a key item: row `row` of the tile (a key), columns [part * kCols, (part + 1) * kCols).
+__device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars,
+                                            const uint8_t* smem, WaitCtx ctx, uint32_t tmem_row, int part, int row, int lane,
+                                            Phases& ph) {
   const int half = part / (kParts / 2);
-  const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
-  const uint32_t t_s = tmem + lane_sel + kTmS + part * kCols, t_dp = tmem + lane_sel + kTmDp + part * kCols;
+  const uint32_t t_s = tmem_row + kTmS + part * kCols, t_dp = tmem_row + kTmDp + part * kCols;
   const float2 c2 = make_float2(p.scale_log2, p.scale_log2);
-  int tile = it.first;
+  int tile = it.first + it.t0 % it.per_head;
   for (int i = 0; i < it.n; ++i) {
-    const float* nl = reinterpret_cast<const float*>(smem + kSmemStat) + (i & 1) * 2 * kTile + part * kCols;
+    const uint32_t st = ph.key & 1;
+    const float* nl = reinterpret_cast<const float*>(smem + kSmemStat) + st * 2 * kTile + part * kCols;
     const float* neg_delta = nl + kTile;
-    bool ok = mbar_wait(&bars.stat_full[i & 1], (i >> 1) & 1, ctx, kRoleBwdSoftmax | kBarStat) &&
-              mbar_wait(bars.s_full, i & 1, ctx, kRoleBwdSoftmax | kBarS);
-    if (!__all_sync(0xffffffffu, ok)) return;
+    bool ok = mbar_wait(&bars.stat_full[st], (ph.key >> 1) & 1, ctx, kRoleBwdSoftmax | kBarStat) &&
+              mbar_wait(&bars.s_full[0], ph.s & 1, ctx, kRoleBwdSoftmax | kBarS);
+    if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
     uint32_t x[kCols], pk[kCols / 2];
     tmem_ld_x32(t_s, x);
     tmem_wait_ld();
     // the key is visible to the queries of columns `seen_from` on
     const int seen_from = it.row0 + row - p.off - tile * kTile - part * kCols;
-    const bool masked = p.causal && it.row0 + kTile - 1 > tile * kTile + p.off;  // CTA-uniform
+    const bool masked = p.causal && it.row0 + kTile - 1 > tile * kTile + p.off;  // the same for the whole CTA
     exp_row(x, c2, [&](int e) { return *reinterpret_cast<const float2*>(nl + e); }, masked, seen_from, kCols);
 #pragma unroll
     for (int e = 0; e < kCols / 2; ++e) pk[e] = pack_bf16x2(ATTN_F(x, 2 * e), ATTN_F(x, 2 * e + 1));
@@ -381,8 +729,8 @@ __device__ __forceinline__ void key_softmax(const BwdParams& p, const BwdItem& i
     tc_fence_before_sync();
     __syncwarp();
     if (lane == 0) mbar_arrive(&bars.p_full[half]);
-    ok = mbar_wait(bars.dp_full, i & 1, ctx, kRoleBwdSoftmax | kBarDp);
-    if (!__all_sync(0xffffffffu, ok)) return;
+    ok = mbar_wait(bars.dp_full, ph.dp & 1, ctx, kRoleBwdSoftmax | kBarDp);
+    if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
     uint32_t d[kCols];
     tmem_ld_x32(t_dp, d);
@@ -399,44 +747,21 @@ __device__ __forceinline__ void key_softmax(const BwdParams& p, const BwdItem& i
     __syncwarp();
     if (lane == 0) {
       mbar_arrive(&bars.ds_full[half]);
-      mbar_arrive(&bars.stat_empty[i & 1]);
+      mbar_arrive(&bars.stat_empty[st]);
     }
+    ph.s ^= 1u;
+    ++ph.dp;
+    ++ph.key;
     if (++tile == it.first + it.per_head) tile = it.first;
   }
-  // Epilogue: half 0 stores dV (through V's tile in shared memory), half 1 dK (through K's); no product reads them now.
-  bool ok = mbar_wait(bars.acc_full, 0, ctx, kRoleBwdSoftmax | kBarAcc);
-  if (!__all_sync(0xffffffffu, ok)) return;
-  tc_fence_after_sync();
-  uint8_t* stage = smem + kSmemFixed + (half == 0 ? kTileBytes : 0);
-  const int col0 = (part % (kParts / 2)) * 2 * kCols;  // this thread's 2 kCols columns of its accumulator
-  const uint32_t t_acc = tmem + lane_sel + (half == 0 ? kTmDv : kTmDk) + col0;
-  const float factor = half == 0 ? 1.f : p.scale;
-#pragma unroll
-  for (int cc = 0; cc < 2 * kCols / 32; ++cc) {
-    uint32_t o[32];
-    tmem_ld_x32(t_acc + cc * 32, o);
-    tmem_wait_ld();
-    const int c = col0 + cc * 32;
-    stage_row32(stage + (c >> 6) * kHalfBytes, row, (c & 63) / 8, o, factor);
-  }
-  fence_proxy_async_smem();
-  __syncwarp();
-  if (lane == 0) mbar_arrive(&bars.stage_full[half]);
-  if (row == 0 && part % (kParts / 2) == 0 && mbar_wait(&bars.stage_full[half], 0, ctx, kRoleBwdSoftmax | kBarStage)) {
-    const CUtensorMap* tm = half == 0 ? tm_dv : tm_dk;
-    tma_store_4d(tm, stage, 0, it.h, it.row0, it.b);
-    tma_store_4d(tm, stage + kHalfBytes, 64, it.h, it.row0, it.b);
-    tma_store_commit();
-    tma_store_wait_all0();
-  }
+  return true;
 }
 
-__device__ __forceinline__ void query_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, uint8_t* smem,
-                                              WaitCtx ctx, uint32_t tmem, int part, int row, int lane,
-                                              const CUtensorMap* tm_dq) {
+// The same for a query item: row `row` is a query, the columns are keys.
+__device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, WaitCtx ctx,
+                                              uint32_t tmem_row, int part, int row, int lane, Phases& ph) {
   const int half = part / (kParts / 2);
-  const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
-  const uint32_t t_dp = tmem + lane_sel + kTmQryDp + part * kCols;
+  const uint32_t t_dp = tmem_row + kTmQryDp + part * kCols;
   const float2 c2 = make_float2(p.scale_log2, p.scale_log2);
   const size_t at = (static_cast<size_t>(it.b) * p.Hq + it.h) * p.n_qt * kTile + it.row0 + row;
   const float nl = __ldg(p.neg_lse2 + at), ndl = __ldg(p.neg_delta + at);
@@ -444,18 +769,19 @@ __device__ __forceinline__ void query_softmax(const BwdParams& p, const BwdItem&
   const int row_limit = p.causal ? min(p.Sk, it.row0 + row + p.off + 1) : p.Sk;   // keys this row may see
   const int tile_clear = p.causal ? min(p.Sk, it.row0 + p.off + 1) : p.Sk;        // keys every row of the tile sees
   for (int j = 0; j < it.n; ++j) {
-    bool ok = mbar_wait(&bars.s_full[j & 1], (j >> 1) & 1, ctx, kRoleBwdSoftmax | kBarS);
-    if (!__all_sync(0xffffffffu, ok)) return;
+    const int x_buf = j & 1;
+    bool ok = mbar_wait(&bars.s_full[x_buf], (ph.s >> x_buf) & 1, ctx, kRoleBwdSoftmax | kBarS);
+    if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
-    const uint32_t t_s = tmem + lane_sel + kTmQryS + (j & 1) * kTile + part * kCols;
+    const uint32_t t_s = tmem_row + kTmQryS + x_buf * kTile + part * kCols;
     uint32_t x[kCols];
     tmem_ld_x32(t_s, x);
     tmem_wait_ld();
     // keys beyond Sk are masked too: their scores are 0, and exp2(nl) may be infinite
-    const bool masked = (j + 1) * kTile > tile_clear;  // CTA-uniform
-    exp_row(x, c2, [&](int) { return nl2; }, masked, 0, row_limit - j * kTile - part * kCols);
-    ok = mbar_wait(bars.dp_full, j & 1, ctx, kRoleBwdSoftmax | kBarDp);
-    if (!__all_sync(0xffffffffu, ok)) return;
+    const bool masked = (it.t0 + j + 1) * kTile > tile_clear;  // the same for the whole CTA
+    exp_row(x, c2, [&](int) { return nl2; }, masked, 0, row_limit - (it.t0 + j) * kTile - part * kCols);
+    ok = mbar_wait(bars.dp_full, ph.dp & 1, ctx, kRoleBwdSoftmax | kBarDp);
+    if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
     uint32_t d[kCols], pk[kCols / 2];
     tmem_ld_x32(t_dp, d);
@@ -473,29 +799,95 @@ __device__ __forceinline__ void query_softmax(const BwdParams& p, const BwdItem&
     tmem_wait_st();
     tc_fence_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&bars.ds_full[(j & 1) * 2 + half]);
+    if (lane == 0) mbar_arrive(&bars.ds_full[2 * x_buf + half]);
+    ph.s ^= 1u << x_buf;
+    ++ph.dp;
   }
-  // Epilogue: each thread stores kCols columns of dQ through Q's tile, each half tile by itself.
-  bool ok = mbar_wait(bars.acc_full, 0, ctx, kRoleBwdSoftmax | kBarAcc);
-  if (!__all_sync(0xffffffffu, ok)) return;
+  return true;
+}
+
+// The results' way out.  Key items: half 0 takes dV, half 1 dK, 64 columns a thread; query items: 32 columns of dQ.
+// `staged_a`, `staged_b`: items that used a slot of stream A / B so far; pos_a, pos_b: ring positions of the slots.
+__device__ __forceinline__ bool write_results(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, uint8_t* smem,
+                                              WaitCtx ctx, uint32_t tmem_row, int part, int row, int lane, int item,
+                                              uint32_t pos_a, uint32_t pos_b, uint32_t staged_a, uint32_t staged_b) {
+  const int half = part / (kParts / 2);
+  const int n32 = it.keys ? 2 : 1;  // 32-column pieces of this thread
+  const int col0 = it.keys ? (part % (kParts / 2)) * 64 : part * kCols;
+  const uint32_t t_acc = tmem_row + (it.keys ? (half == 0 ? kTmDv : kTmDk) : kTmDq) + col0;
+  const float factor = it.keys && half == 0 ? 1.f : p.scale;
+  bool ok = mbar_wait(bars.acc_full, item & 1, ctx, kRoleBwdSoftmax | kBarAcc);
+  if (!__all_sync(0xffffffffu, ok)) return false;
   tc_fence_after_sync();
-  uint8_t* stage = smem + kSmemFixed + half * kHalfBytes;
-  uint32_t o[kCols];
-  if (it.n > 0) {
-    tmem_ld_x32(tmem + lane_sel + kTmDq + part * kCols, o);
-    tmem_wait_ld();
-  } else {  // no row of the tile sees a key: dQ is 0, and tensor memory holds nothing of ours
-#pragma unroll
-    for (int e = 0; e < kCols; ++e) o[e] = 0u;
+  const bool out_bf16 = staged(p, it);
+  float* part_dst = nullptr;
+  if (!out_bf16) {
+    const int heads = it.keys ? p.Hkv : p.Hq, rows = (it.keys ? p.n_kt : p.n_qt) * kTile;
+    float* buf = it.keys ? (half == 0 ? p.dv_part : p.dk_part) : p.dq_part;
+    part_dst = buf + (((static_cast<size_t>(it.split) * p.B + it.b) * heads + it.h) * rows + it.row0 + row) * kHeadDim + col0;
   }
-  stage_row32(stage, row, (part % (kParts / 2)) * kCols / 8, o, p.scale);
+  uint32_t pk[32];
+#pragma unroll
+  for (int cc = 0; cc < 2; ++cc) {
+    if (cc < n32) {
+      uint32_t o[32];
+      if (it.n > 0) {
+        tmem_ld_x32(t_acc + cc * 32, o);
+        tmem_wait_ld();
+      } else {  // nothing streamed past: the result is 0, and tensor memory holds nothing of this item
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = 0u;
+      }
+      if (out_bf16) {
+        pack_row32(o, factor, pk + cc * 16);
+      } else {
+        store_part32(part_dst + cc * 32, o, factor);
+      }
+    }
+  }
+  tc_fence_before_sync();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bars.acc_empty);
+  if (!out_bf16) return true;
+  ok = mbar_wait(&bars.stage_ready[0], staged_a & 1, ctx, kRoleBwdSoftmax | kBarStageReady) &&
+       (!it.keys || mbar_wait(&bars.stage_ready[1], staged_b & 1, ctx, kRoleBwdSoftmax | kBarStageReady));
+  if (!__all_sync(0xffffffffu, ok)) return false;
+  uint8_t* slot_a = smem + kSmemRing + (pos_a % kRingA) * kTileBytes;
+  uint8_t* slot_b = smem + kSmemRing + (kRingA + pos_b % kRingB) * kTileBytes;
+  uint8_t* stage = (it.keys && half == 0 ? slot_b : slot_a) + (col0 >> 6) * kHalfBytes;
+#pragma unroll
+  for (int cc = 0; cc < 2; ++cc) {
+    if (cc < n32) stage_row32(stage, row, ((col0 & 63) + cc * 32) / 8, pk + cc * 16);
+  }
   fence_proxy_async_smem();
   __syncwarp();
   if (lane == 0) mbar_arrive(&bars.stage_full[half]);
-  if (row == 0 && part % (kParts / 2) == 0 && mbar_wait(&bars.stage_full[half], 0, ctx, kRoleBwdSoftmax | kBarStage)) {
-    tma_store_4d(tm_dq, stage, half * 64, it.h, it.row0, it.b);
-    tma_store_commit();
-    tma_store_wait_all0();
+  return true;
+}
+
+__device__ __forceinline__ void role_softmax(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem, const volatile int* box,
+                                             WaitCtx ctx, uint32_t tmem, int part, int row, int lane) {
+  const uint32_t tmem_row = tmem + (static_cast<uint32_t>(row & ~31) << 16);
+  uint32_t pos_a = 0, pos_b = 0, staged_a = 0, staged_b = 0;
+  Phases ph;
+  BwdItem it;
+  for (int k = 0; next_item(bars, box, k, ctx, kRoleBwdSoftmax, true, lane == 0, it); ++k) {
+    bool ok = true;
+    if (it.n > 0) {
+      ok = it.keys ? key_softmax(p, it, bars, smem, ctx, tmem_row, part, row, lane, ph)
+                   : query_softmax(p, it, bars, ctx, tmem_row, part, row, lane, ph);
+    }
+    pos_a += it.n;
+    pos_b += it.n;
+    if (!ok || !write_results(p, it, bars, smem, ctx, tmem_row, part, row, lane, k, pos_a, pos_b, staged_a, staged_b)) return;
+    if (staged(p, it)) {
+      ++pos_a;
+      ++staged_a;
+      if (it.keys) {
+        ++pos_b;
+        ++staged_b;
+      }
+    }
   }
 }
 
@@ -508,7 +900,8 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + kSmemBwdBars);
   BwdBarriers bars;
   bars.fixed_full = bar;
-  bars.a_full = bars.fixed_full + 1;
+  bars.fixed_empty = bars.fixed_full + 2;
+  bars.a_full = bars.fixed_empty + 2;
   bars.a_empty = bars.a_full + kRingA;
   bars.b_full = bars.a_empty + kRingA;
   bars.b_empty = bars.b_full + kRingB;
@@ -520,7 +913,13 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   bars.p_full = bars.dp_read + 1;
   bars.ds_full = bars.p_full + 2;
   bars.acc_full = bars.ds_full + 4;
-  bars.stage_full = bars.acc_full + 1;
+  bars.acc_empty = bars.acc_full + 1;
+  bars.stage_ready = bars.acc_empty + 1;
+  bars.stage_full = bars.stage_ready + 2;
+  bars.item_full = bars.stage_full + 2;
+  bars.item_empty = bars.item_full + 2;
+  bars.clc_full = bars.item_empty + 2;
+  volatile int* box = reinterpret_cast<volatile int*>(smem + kSmemBwdItems);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kSmemBwdMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kSmemBwdMisc + 4);
   const WaitCtx ctx{abort_flag, p.status, kWaitLimitNs};
@@ -530,26 +929,32 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     return;
   }
   if (tid == 0) {
-    mbar_init(bars.fixed_full, 2);
     for (int i = 0; i < kRingA; ++i) {
       mbar_init(&bars.a_full[i], 1);
-      mbar_init(&bars.a_empty[i], 1);
+      mbar_init(&bars.a_empty[i], 2);
     }
     for (int i = 0; i < kRingB; ++i) {
       mbar_init(&bars.b_full[i], 1);
-      mbar_init(&bars.b_empty[i], 1);
+      mbar_init(&bars.b_empty[i], 2);
     }
     mbar_init(bars.dp_full, 1);
     mbar_init(bars.dp_read, kSoftmaxWarps);
-    mbar_init(bars.acc_full, 1);
+    mbar_init(bars.acc_full, 2);
+    mbar_init(bars.acc_empty, kSoftmaxWarps);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.fixed_full[i], 1);
+      mbar_init(&bars.fixed_empty[i], 1);
       mbar_init(&bars.stat_full[i], 1);
       mbar_init(&bars.stat_empty[i], kSoftmaxWarps);
       mbar_init(&bars.s_full[i], 1);
       mbar_init(&bars.p_full[i], kSoftmaxWarps / 2);
       mbar_init(&bars.ds_full[i], kSoftmaxWarps / 2);
       mbar_init(&bars.ds_full[2 + i], kSoftmaxWarps / 2);
+      mbar_init(&bars.stage_ready[i], 2);
       mbar_init(&bars.stage_full[i], kSoftmaxWarps / 2);
+      mbar_init(&bars.item_full[i], 1);
+      mbar_init(&bars.item_empty[i], kItemConsumers);
+      mbar_init(&bars.clc_full[i], 1);
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -562,33 +967,24 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
-  const bool keys = static_cast<int>(blockIdx.x) < p.n_key_items;  // CTA-uniform
-  const BwdItem it = keys ? key_item(p, blockIdx.x) : query_item(p, static_cast<int>(blockIdx.x) - p.n_key_items);
 
   if (warp < kSoftmaxWarps) {
-    if (keys) {
-      key_softmax(p, it, bars, smem, ctx, tmem, warp >> 2, tid & 127, lane, &tm_dk, &tm_dv);
+    reg_alloc<kRegsSoftmax>();
+    role_softmax(p, bars, smem, box, ctx, tmem, warp >> 2, tid & 127, lane);
+  } else {
+    reg_dealloc<kRegsOther>();
+    if (warp == kSoftmaxWarps) {
+      role_mma<true>(p, bars, smem, box, ctx, tmem, lane);
+    } else if (warp == kSoftmaxWarps + 1) {
+      role_mma<false>(p, bars, smem, box, ctx, tmem, lane);
+    } else if (lane != 0) {
+      // the loader and the store warp are one thread each
+    } else if (warp == kSoftmaxWarps + 2) {
+      role_loader(p, bars, smem, box, ctx, &tm_q, &tm_k, &tm_v, &tm_do);
     } else {
-      query_softmax(p, it, bars, smem, ctx, tmem, warp >> 2, tid & 127, lane, &tm_dq);
+      role_store(p, bars, smem, box, ctx, &tm_dq, &tm_dk, &tm_dv);
     }
-  } else if (warp == kSoftmaxWarps) {
-    if (keys) {
-      key_mma(it, bars, smem, ctx, tmem);
-    } else {
-      query_mma(it, bars, smem, ctx, tmem);
-    }
-  } else if (lane == 0) {
-    const bool stream_a = warp == kSoftmaxWarps + 1;
-    if (keys && stream_a) {
-      bwd_loader<true, true>(p, it, bars, smem, ctx, &tm_k, &tm_q);
-    } else if (keys) {
-      bwd_loader<true, false>(p, it, bars, smem, ctx, &tm_v, &tm_do);
-    } else if (stream_a) {
-      bwd_loader<false, true>(p, it, bars, smem, ctx, &tm_q, &tm_k);
-    } else {
-      bwd_loader<false, false>(p, it, bars, smem, ctx, &tm_do, &tm_v);
-    }
-    if (*abort_flag) {  // let loads in flight land before the CTA's shared memory is released
+    if (lane == 0 && *abort_flag) {  // let copies in flight land before the CTA's shared memory is released
       const uint64_t t0 = global_timer_ns();
       while (global_timer_ns() - t0 < 1000000ull) {
       }
@@ -646,6 +1042,29 @@ attn_bwd_prep_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict_
 }
 
 #undef ATTN_F
+
+// Adds up the fp32 partial sums of split items in order and rounds once: one warp a row of 128, rows in the
+// order of the output [B][S][H].  HBM-bound, and small: only problems with few tiles are split.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads)
+attn_bwd_join_kernel(const float* __restrict__ part, int splits, uint16_t* out, RowStrides so, int H, int S, int padded,
+                     long long n_rows, long long part_stride) {
+  const int lane = threadIdx.x & 31;
+  const long long step = static_cast<long long>(gridDim.x) * (kJoinThreads / 32);
+  for (long long r = static_cast<long long>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); r < n_rows; r += step) {
+    const int h = static_cast<int>(r % H);
+    const long long t = r / H;
+    const long long s = t % S, b = t / S;
+    const float* src = part + ((b * H + h) * padded + s) * kHeadDim + lane * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < splits; ++i) {
+      const float4 x = __ldg(reinterpret_cast<const float4*>(src + i * part_stride));
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    *reinterpret_cast<uint2*>(out + b * so.b + s * so.s + h * so.h + lane * 4) =
+        make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+  }
+}
 
 }  // namespace bwd
 }  // namespace attn
