@@ -160,8 +160,10 @@ struct BwdItem {
 
 // Launch order.  A unit is a (batch, KV head) with its query heads: n_kt key tiles and group * n_qt query tiles, each
 // in its number of parts.  Units are taken in runs of `run` (the first `run_extra` runs) or run - 1 units whose
-// streams together fit L2; in a run come first all key items, then all query items, rank by rank over its units,
-// under the causal mask the longest ranks (early keys, late rows) first, so that every run ends on short items.
+// tensors together fit L2; in a run come first all key items, then all query items.  Under the causal mask each kind
+// goes rank by rank over the run's units, longest ranks (early keys, late rows) first, so that a run ends on
+// short items.  Without it items are alike and go unit by unit: neighbours then read the same stream at about the same
+// time, which the L2 answers with fewer requests (8 heads of 16384: 3 % over a mixed order).
 __host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int w) {
   const int unit_keys = p.n_kt * p.key_splits;
   const int per_unit = unit_keys + p.group * p.n_qt * p.qry_splits;
@@ -184,7 +186,8 @@ __host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int 
   int splits;
   if (it.keys) {
     splits = p.key_splits;
-    const int rank = rem / g, unit = first + rem - rank * g;
+    const int u = p.causal ? rem % g : rem / unit_keys;
+    const int rank = p.causal ? rem / g : rem - u * unit_keys, unit = first + u;
     const int kt = rank / splits;
     it.split = rank - kt * splits;
     it.b = unit / p.Hkv;
@@ -197,8 +200,9 @@ __host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int 
   } else {
     splits = p.qry_splits;
     rem -= g * unit_keys;
-    const int wide = g * p.group;
-    const int rank = rem / wide, x = rem - rank * wide;
+    const int wide = g * p.group, per_head = p.n_qt * splits;
+    const int x = p.causal ? rem % wide : rem / per_head;  // which head of the run
+    const int rank = p.causal ? rem / wide : rem - x * per_head;
     const int unit = first + x / p.group;
     const int qt = rank / splits;
     it.split = rank - qt * splits;
@@ -275,16 +279,31 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, u
   tma_load_4d(dst + kHalfBytes, tm, bar, 64, head, row, b);
 }
 
+// A position in a ring of N slots: the slot and the parity of its current phase.
+template <int N>
+struct RingPos {
+  uint32_t slot = 0, par = 0;
+  __device__ __forceinline__ void next() {
+    if (++slot == N) {
+      slot = 0;
+      par ^= 1u;
+    }
+  }
+  __device__ __forceinline__ void skip(uint32_t n) {
+    const uint32_t c = (par * N + slot + n) % (2 * N);
+    par = c >= N ? 1u : 0u;
+    slot = c - par * N;
+  }
+};
+typedef RingPos<kRingA> RingPosA;
+typedef RingPos<kRingB> RingPosB;
+
 // The loader's counts: ring positions, resident tiles, statistics tiles so far.
 struct LoaderState {
-  uint32_t a = 0, b = 0, fixed = 0, stats = 0;
+  RingPosA a;
+  RingPosB b;
+  uint32_t fixed = 0, stats = 0;
 };
-
-// A slot of a ring, for the next position.
-template <int kSlots>
-__device__ __forceinline__ bool wait_slot(uint64_t* empty, uint32_t pos, WaitCtx ctx) {
-  return mbar_wait(&empty[pos % kSlots], ((pos / kSlots) & 1) ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty);
-}
 
 // One item's tiles: the resident ones, then the streams, pair by pair; key items' stream A also brings the row
 // statistics of its tiles.  False after an expired wait.
@@ -306,17 +325,15 @@ __device__ __forceinline__ bool load_item(const BwdParams& p, const BwdItem& it,
         load_tile(smem + kSmemFixed + x * kTileBytes, x == 0 ? fixed_a : fixed_b, &bars.fixed_full[x], it.h, it.row0, it.b);
       }
       if (x == 0) {
-        if (!wait_slot<kRingA>(bars.a_empty, ls.a, ctx)) return false;
-        const uint32_t slot = ls.a % kRingA;
-        mbar_arrive_expect_tx(&bars.a_full[slot], kTileBytes);
-        load_tile(ring_a + slot * kTileBytes, stream_a, &bars.a_full[slot], head, tile * kTile, it.b);
-        ++ls.a;
+        if (!mbar_wait(&bars.a_empty[ls.a.slot], ls.a.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
+        mbar_arrive_expect_tx(&bars.a_full[ls.a.slot], kTileBytes);
+        load_tile(ring_a + ls.a.slot * kTileBytes, stream_a, &bars.a_full[ls.a.slot], head, tile * kTile, it.b);
+        ls.a.next();
       } else {
-        if (!wait_slot<kRingB>(bars.b_empty, ls.b, ctx)) return false;
-        const uint32_t slot = ls.b % kRingB;
-        mbar_arrive_expect_tx(&bars.b_full[slot], kTileBytes);
-        load_tile(ring_b + slot * kTileBytes, stream_b, &bars.b_full[slot], head, tile * kTile, it.b);
-        ++ls.b;
+        if (!mbar_wait(&bars.b_empty[ls.b.slot], ls.b.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
+        mbar_arrive_expect_tx(&bars.b_full[ls.b.slot], kTileBytes);
+        load_tile(ring_b + ls.b.slot * kTileBytes, stream_b, &bars.b_full[ls.b.slot], head, tile * kTile, it.b);
+        ls.b.next();
       }
     }
     if (it.keys) {
@@ -343,15 +360,15 @@ __device__ __forceinline__ bool load_item(const BwdParams& p, const BwdItem& it,
   if (staged(p, it)) {
     // The slots behind the last tiles take the results.  The `full` barriers go through these positions too, so that
     // they keep the phases of the `empty` ones.
-    if (!wait_slot<kRingA>(bars.a_empty, ls.a, ctx)) return false;
-    mbar_arrive(&bars.a_full[ls.a % kRingA]);
+    if (!mbar_wait(&bars.a_empty[ls.a.slot], ls.a.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
+    mbar_arrive(&bars.a_full[ls.a.slot]);
     mbar_arrive(&bars.stage_ready[0]);
-    ++ls.a;
+    ls.a.next();
     if (it.keys) {
-      if (!wait_slot<kRingB>(bars.b_empty, ls.b, ctx)) return false;
-      mbar_arrive(&bars.b_full[ls.b % kRingB]);
+      if (!mbar_wait(&bars.b_empty[ls.b.slot], ls.b.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
+      mbar_arrive(&bars.b_full[ls.b.slot]);
       mbar_arrive(&bars.stage_ready[1]);
-      ++ls.b;
+      ls.b.next();
     }
   }
   return true;
@@ -427,16 +444,16 @@ __device__ __forceinline__ void role_store(const BwdParams& p, const BwdBarriers
   }
 }
 
-// Shared-memory address of ring position `pos` of a stream, and the wait for it.
-__device__ __forceinline__ uint32_t a_tile(uint32_t base, uint32_t pos) { return base + kSmemRing + (pos % kRingA) * kTileBytes; }
-__device__ __forceinline__ uint32_t b_tile(uint32_t base, uint32_t pos) {
-  return base + kSmemRing + (kRingA + pos % kRingB) * kTileBytes;
+// Shared-memory address of the tile at a ring position, and the wait for it.
+__device__ __forceinline__ uint32_t tile_at(uint32_t base, const RingPosA& r) { return base + kSmemRing + r.slot * kTileBytes; }
+__device__ __forceinline__ uint32_t tile_at(uint32_t base, const RingPosB& r) {
+  return base + kSmemRing + (kRingA + r.slot) * kTileBytes;
 }
-__device__ __forceinline__ bool wait_a(const BwdBarriers& bars, uint32_t pos, WaitCtx ctx, int role) {
-  return mbar_wait_warp(&bars.a_full[pos % kRingA], (pos / kRingA) & 1, ctx, role | kBarRingFull);
+__device__ __forceinline__ bool wait_tile(const BwdBarriers& bars, const RingPosA& r, WaitCtx ctx, int role) {
+  return mbar_wait_warp(&bars.a_full[r.slot], r.par, ctx, role | kBarRingFull);
 }
-__device__ __forceinline__ bool wait_b(const BwdBarriers& bars, uint32_t pos, WaitCtx ctx, int role) {
-  return mbar_wait_warp(&bars.b_full[pos % kRingB], (pos / kRingB) & 1, ctx, role | kBarRingFull);
+__device__ __forceinline__ bool wait_tile(const BwdBarriers& bars, const RingPosB& r, WaitCtx ctx, int role) {
+  return mbar_wait_warp(&bars.b_full[r.slot], r.par, ctx, role | kBarRingFull);
 }
 
 // Phases of the barriers that count tile pairs across items; every role that waits for them keeps its own copy.
@@ -450,7 +467,9 @@ struct Phases {
 // What both MMA warps know of the item they work on.
 struct MmaItem {
   uint32_t base, tmem;
-  uint32_t pos_a, pos_b, fixed;  // ring positions of its first tiles, resident tiles before it
+  RingPosA a;                    // ring positions: of its first tiles, and behind its last ones afterwards
+  RingPosB b;
+  uint32_t fixed;                // resident tiles before it
   uint32_t k;                    // its number
   bool leader;
   bool after_other;              // the item before was of the other kind
@@ -464,25 +483,25 @@ struct MmaItem {
 // there is nothing to issue.  Across items the same order holds between items of one kind; products into columns that
 // the item before used otherwise, and into its accumulators, wait until its results have left tensor memory
 // (acc_empty).
-__device__ __forceinline__ bool key_mma_1(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+__device__ __forceinline__ bool key_mma_1(const BwdItem& it, MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
   constexpr int kRole = kRoleBwdMma;
   const uint64_t k_desc = kmajor_desc(m.base + kSmemFixed);
-  uint32_t pos_a = m.pos_a, pos_b = m.pos_b;
-  if (!mbar_wait_warp(&bars.fixed_full[0], m.fixed & 1, ctx, kRole | kBarFixed) || !wait_a(bars, pos_a, ctx, kRole)) return false;
+  if (!mbar_wait_warp(&bars.fixed_full[0], m.fixed & 1, ctx, kRole | kBarFixed) || !wait_tile(bars, m.a, ctx, kRole)) return false;
   tc_fence_after_sync();
-  issue_qk(m.leader, m.tmem + kTmS, k_desc, kmajor_desc(a_tile(m.base, pos_a)));
+  issue_qk(m.leader, m.tmem + kTmS, k_desc, kmajor_desc(tile_at(m.base, m.a)));
   if (m.leader) {
     mma_commit(&bars.s_full[0]);
-    mma_commit(&bars.a_empty[pos_a % kRingA]);
+    mma_commit(&bars.a_empty[m.a.slot]);
     if (it.n == 1) mma_commit(&bars.fixed_empty[0]);  // that was the last use of K
   }
+  m.a.next();
   if (!mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
-  for (int i = 0; i < it.n; ++i, ++pos_a, ++pos_b) {
+  for (int i = 0; i < it.n; ++i) {
     const bool next = i + 1 < it.n;
-    if (!wait_b(bars, pos_b, ctx, kRole)) return false;
-    if (next && !wait_a(bars, pos_a + 1, ctx, kRole)) return false;
-    const uint64_t do_desc = vtile_desc(b_tile(m.base, pos_b));
-    const uint64_t q_desc = kmajor_desc(a_tile(m.base, pos_a + 1));
+    if (!wait_tile(bars, m.b, ctx, kRole)) return false;             // dO(i)
+    if (next && !wait_tile(bars, m.a, ctx, kRole)) return false;     // Q(i + 1)
+    const uint64_t do_desc = vtile_desc(tile_at(m.base, m.b));
+    const uint64_t q_desc = kmajor_desc(tile_at(m.base, m.a));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (!mbar_wait_warp(&bars.p_full[h], ph.key & 1, ctx, kRole | kBarP)) return false;
@@ -493,36 +512,38 @@ __device__ __forceinline__ bool key_mma_1(const BwdItem& it, const MmaItem& m, c
       issue_qk(m.leader, m.tmem + kTmS, k_desc, q_desc);
       if (m.leader) {
         mma_commit(&bars.s_full[0]);
-        mma_commit(&bars.a_empty[(pos_a + 1) % kRingA]);
+        mma_commit(&bars.a_empty[m.a.slot]);
         if (i + 2 == it.n) mma_commit(&bars.fixed_empty[0]);
       }
+      m.a.next();
     }
-    if (m.leader) mma_commit(&bars.b_empty[pos_b % kRingB]);
+    if (m.leader) mma_commit(&bars.b_empty[m.b.slot]);
+    m.b.next();
     ++ph.key;
   }
   ph.s ^= it.n & 1;  // the other warp waits for dS
   return true;
 }
-__device__ __forceinline__ bool key_mma_2(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+__device__ __forceinline__ bool key_mma_2(const BwdItem& it, MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
   constexpr int kRole = kRoleBwdMma2;
   const uint64_t v_desc = kmajor_desc(m.base + kSmemFixed + kTileBytes);
-  uint32_t pos_a = m.pos_a, pos_b = m.pos_b;
   // dP's columns were a score buffer of a query item, which the first MMA warp's products read
   if (m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
-  if (!mbar_wait_warp(&bars.fixed_full[1], m.fixed & 1, ctx, kRole | kBarFixed) || !wait_b(bars, pos_b, ctx, kRole)) return false;
+  if (!mbar_wait_warp(&bars.fixed_full[1], m.fixed & 1, ctx, kRole | kBarFixed) || !wait_tile(bars, m.b, ctx, kRole)) return false;
   tc_fence_after_sync();
-  issue_qk(m.leader, m.tmem + kTmDp, v_desc, kmajor_desc(b_tile(m.base, pos_b)));
+  issue_qk(m.leader, m.tmem + kTmDp, v_desc, kmajor_desc(tile_at(m.base, m.b)));
   if (m.leader) {
     mma_commit(bars.dp_full);
-    mma_commit(&bars.b_empty[pos_b % kRingB]);
+    mma_commit(&bars.b_empty[m.b.slot]);
     if (it.n == 1) mma_commit(&bars.fixed_empty[1]);  // that was the last use of V
   }
+  m.b.next();
   if (!m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
-  for (int i = 0; i < it.n; ++i, ++pos_a, ++pos_b) {
+  for (int i = 0; i < it.n; ++i) {
     const bool next = i + 1 < it.n;
-    if (next && !wait_b(bars, pos_b + 1, ctx, kRole)) return false;
-    const uint64_t q_desc = vtile_desc(a_tile(m.base, pos_a));
-    const uint64_t do_desc = kmajor_desc(b_tile(m.base, pos_b + 1));
+    if (next && !wait_tile(bars, m.b, ctx, kRole)) return false;     // dO(i + 1)
+    const uint64_t q_desc = vtile_desc(tile_at(m.base, m.a));        // Q(i): dS(i) comes from its scores
+    const uint64_t do_desc = kmajor_desc(tile_at(m.base, m.b));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (!mbar_wait_warp(&bars.ds_full[h], ph.s & 1, ctx, kRole | kBarDs)) return false;
@@ -533,11 +554,13 @@ __device__ __forceinline__ bool key_mma_2(const BwdItem& it, const MmaItem& m, c
       issue_qk(m.leader, m.tmem + kTmDp, v_desc, do_desc);
       if (m.leader) {
         mma_commit(bars.dp_full);
-        mma_commit(&bars.b_empty[(pos_b + 1) % kRingB]);
+        mma_commit(&bars.b_empty[m.b.slot]);
         if (i + 2 == it.n) mma_commit(&bars.fixed_empty[1]);
       }
+      m.b.next();
     }
-    if (m.leader) mma_commit(&bars.a_empty[pos_a % kRingA]);
+    if (m.leader) mma_commit(&bars.a_empty[m.a.slot]);
+    m.a.next();
     ph.s ^= 1u;
   }
   return true;
@@ -547,67 +570,70 @@ __device__ __forceinline__ bool key_mma_2(const BwdItem& it, const MmaItem& m, c
 // while tile j's are exponentiated: two score buffers, dS(j) goes over the scores of tile j, and S(j+2) into the same
 // columns is issued behind dS(j) K(j).
 // Second MMA warp: dP(j) = dO V(j)^T into one buffer, free as soon as the softmax warps have it in registers.
-__device__ __forceinline__ bool query_mma_1(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+__device__ __forceinline__ bool query_mma_1(const BwdItem& it, MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
   constexpr int kRole = kRoleBwdMma;
   const uint64_t q_desc = kmajor_desc(m.base + kSmemFixed);
-  const uint32_t pos = m.pos_a;
+  RingPosA done = m.a;  // position of K(j); m.a: of K(j + 2)
   if (!mbar_wait_warp(&bars.fixed_full[0], m.fixed & 1, ctx, kRole | kBarFixed)) return false;
   for (int j = -2; j < it.n; ++j) {
     const int n = j + 2;
     const uint32_t scores = m.tmem + kTmQryS + (n & 1) * kTile;  // buffer of tiles j and j + 2
-    const uint64_t k_desc = kmajor_desc(a_tile(m.base, pos + n));
     // buffer 1 was a key item's dP, which the second MMA warp's products read
     if (j == -1 && m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
     if (j >= 0) {  // dQ += dS(j) K(j)
       if (j == 0 && !m.after_other && !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty)) return false;
       const int x = j & 1;
-      const uint64_t kv_desc = vtile_desc(a_tile(m.base, pos + j));
+      const uint64_t kv_desc = vtile_desc(tile_at(m.base, done));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if (!mbar_wait_warp(&bars.ds_full[2 * x + h], (ph.s >> x) & 1, ctx, kRole | kBarDs)) return false;
         tc_fence_after_sync();
         issue_ts_half(m.leader, m.tmem + kTmDq, scores, kv_desc, h, j > 0 || h > 0);
       }
+      if (m.leader) mma_commit(&bars.a_empty[done.slot]);
+      done.next();
       ph.s ^= 1u << x;
     }
     if (n < it.n) {
-      if (!wait_a(bars, pos + n, ctx, kRole)) return false;
+      if (!wait_tile(bars, m.a, ctx, kRole)) return false;
       tc_fence_after_sync();
-      issue_qk(m.leader, scores, q_desc, k_desc);
+      issue_qk(m.leader, scores, q_desc, kmajor_desc(tile_at(m.base, m.a)));
       if (m.leader) {
         mma_commit(&bars.s_full[n & 1]);
-        mma_commit(&bars.a_empty[(pos + n) % kRingA]);
+        mma_commit(&bars.a_empty[m.a.slot]);
         if (n + 1 == it.n) mma_commit(&bars.fixed_empty[0]);
       }
+      m.a.next();
     }
-    if (j >= 0 && m.leader) mma_commit(&bars.a_empty[(pos + j) % kRingA]);
   }
+  m.b.skip(it.n);
   return true;
 }
-__device__ __forceinline__ bool query_mma_2(const BwdItem& it, const MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
+__device__ __forceinline__ bool query_mma_2(const BwdItem& it, MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
   constexpr int kRole = kRoleBwdMma2;
   const uint64_t do_desc = kmajor_desc(m.base + kSmemFixed + kTileBytes);
-  uint32_t pos = m.pos_b;
   if (!mbar_wait_warp(&bars.fixed_full[1], m.fixed & 1, ctx, kRole | kBarFixed) ||
       !mbar_wait_warp(bars.acc_empty, (m.k & 1) ^ 1, ctx, kRole | kBarAccEmpty))
     return false;
-  for (int j = 0; j < it.n; ++j, ++pos) {
-    if (!wait_b(bars, pos, ctx, kRole)) return false;
+  for (int j = 0; j < it.n; ++j) {
+    if (!wait_tile(bars, m.b, ctx, kRole)) return false;
     if (j > 0) {  // dP(j - 1) has been read
       if (!mbar_wait_warp(bars.dp_read, ph.qry & 1, ctx, kRole | kBarDpRead)) return false;
       ++ph.qry;
     }
     tc_fence_after_sync();
-    issue_qk(m.leader, m.tmem + kTmQryDp, do_desc, kmajor_desc(b_tile(m.base, pos)));
+    issue_qk(m.leader, m.tmem + kTmQryDp, do_desc, kmajor_desc(tile_at(m.base, m.b)));
     if (m.leader) {
       mma_commit(bars.dp_full);
-      mma_commit(&bars.b_empty[pos % kRingB]);
-      mma_commit(&bars.b_empty[pos % kRingB]);  // the tile's only reader stands for two
+      mma_commit(&bars.b_empty[m.b.slot]);
+      mma_commit(&bars.b_empty[m.b.slot]);  // the tile's only reader stands for two
       if (j + 1 == it.n) mma_commit(&bars.fixed_empty[1]);
     }
+    m.b.next();
   }
   ++ph.qry;  // the last tile's phase: over by the time that the next item gets past acc_empty
   ph.s ^= (((it.n + 1) >> 1) & 1) | (((it.n >> 1) & 1) << 1);  // the other warp waits for dS
+  m.a.skip(it.n);
   return true;
 }
 
@@ -618,7 +644,7 @@ __device__ __forceinline__ void role_mma(const BwdParams& p, const BwdBarriers& 
   MmaItem m;
   m.base = smem_u32(smem);
   m.tmem = tmem;
-  m.pos_a = m.pos_b = m.fixed = 0;
+  m.fixed = 0;
   m.leader = elect_one();
   Phases ph;
   BwdItem it;
@@ -640,11 +666,9 @@ __device__ __forceinline__ void role_mma(const BwdParams& p, const BwdBarriers& 
       return;
     }
     if (m.leader) mma_commit(bars.acc_full);
-    m.pos_a += it.n;
-    m.pos_b += it.n;
     if (staged(p, it)) {
-      ++m.pos_a;
-      if (it.keys) ++m.pos_b;
+      m.a.next();
+      if (it.keys) m.b.next();
     }
   }
 }
@@ -1044,24 +1068,34 @@ attn_bwd_prep_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict_
 #undef ATTN_F
 
 // Adds up the fp32 partial sums of split items in order and rounds once: one warp a row of 128, rows in the
-// order of the output [B][S][H].  HBM-bound, and small: only problems with few tiles are split.
+// order of the output [B][S][H]; blockIdx.y picks the output.  HBM-bound, and small: only problems with few tiles are
+// split.
 constexpr int kJoinThreads = 256;
-__global__ void __launch_bounds__(kJoinThreads)
-attn_bwd_join_kernel(const float* __restrict__ part, int splits, uint16_t* out, RowStrides so, int H, int S, int padded,
-                     long long n_rows, long long part_stride) {
+struct JoinOut {
+  const float* part;  // [splits][B][H][padded][128]
+  uint16_t* out;
+  RowStrides strides;
+  int splits, H, S, padded;
+  long long n_rows, part_stride;
+};
+struct JoinParams {
+  JoinOut o[3];
+};
+__global__ void __launch_bounds__(kJoinThreads) attn_bwd_join_kernel(const __grid_constant__ JoinParams p) {
+  const JoinOut& j = p.o[blockIdx.y];
   const int lane = threadIdx.x & 31;
   const long long step = static_cast<long long>(gridDim.x) * (kJoinThreads / 32);
-  for (long long r = static_cast<long long>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); r < n_rows; r += step) {
-    const int h = static_cast<int>(r % H);
-    const long long t = r / H;
-    const long long s = t % S, b = t / S;
-    const float* src = part + ((b * H + h) * padded + s) * kHeadDim + lane * 4;
+  for (long long r = static_cast<long long>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); r < j.n_rows; r += step) {
+    const int h = static_cast<int>(r % j.H);
+    const long long t = r / j.H;
+    const long long s = t % j.S, b = t / j.S;
+    const float* src = j.part + ((b * j.H + h) * j.padded + s) * kHeadDim + lane * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < splits; ++i) {
-      const float4 x = __ldg(reinterpret_cast<const float4*>(src + i * part_stride));
+    for (int i = 0; i < j.splits; ++i) {
+      const float4 x = __ldg(reinterpret_cast<const float4*>(src + i * j.part_stride));
       v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
     }
-    *reinterpret_cast<uint2*>(out + b * so.b + s * so.s + h * so.h + lane * 4) =
+    *reinterpret_cast<uint2*>(j.out + b * j.strides.b + s * j.strides.s + h * j.strides.h + lane * 4) =
         make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
   }
 }
