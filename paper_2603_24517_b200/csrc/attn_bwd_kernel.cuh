@@ -20,8 +20,9 @@
 // that have not started yet (clusterlaunchcontrol), so the hardware's own queue balances the work and nothing is
 // left in memory between launches.  Roles:
 //
-//   warps 0-15  softmax: lane quarter w % 4 of the tile, 32 of its 128 columns (w / 4); a thread per row and quarter;
-//               the accumulators' way out (tensor memory -> BF16 -> shared memory)
+//   warps 0-15  softmax: lane quarter w % 4 of the tile, 16 columns of each half of it (part w / 4); four threads a row.
+//               All warps do their share of the first half, hand it over, and do the second while the product that
+//               reads the first already runs.  Also the accumulators' way out (tensor memory -> BF16 -> shared memory)
 //   warps 16-17 MMA issue (tcgen05.mma by an elected lane).  Barrier polls and commits take a warp longer than the few
 //               instructions that the tensor pipe queues behind an issuer last, so one warp alone leaves the pipe
 //               idle; two warps feed it by turns.  Products that must keep an order share a warp:
@@ -43,7 +44,7 @@ namespace attn {
 namespace bwd {
 
 constexpr int kParts = 4;                 // softmax threads per row
-constexpr int kCols = kTile / kParts;     // columns of a tile each of them handles
+constexpr int kCols = kTile / kParts / 2; // columns of each half tile that each of them handles
 constexpr int kSoftmaxWarps = 4 * kParts;
 constexpr int kBwdThreads = (kSoftmaxWarps + 4) * 32;
 // Registers a thread after the re-split (setmaxnreg): the block is launched with 96 each.
@@ -102,7 +103,7 @@ struct BwdBarriers {
   uint64_t* s_full;      // [2]  MMA commit -> softmax (key items use the first)
   uint64_t* dp_full;     // MMA commit -> softmax
   uint64_t* dp_read;     // softmax (all warps) -> MMA: dP is in registers (query items)
-  uint64_t* p_full;      // [2]  softmax warps of a half tile: its 64 columns of P are in tensor memory (key items)
+  uint64_t* p_full;      // [2]  softmax (all warps): a half tile's columns of P are in tensor memory (key items)
   uint64_t* ds_full;     // [4]  the same for dS; query items alternate two pairs, one for each score buffer
   uint64_t* acc_full;    // commits of both MMA warps: the accumulators are final
   uint64_t* acc_empty;   // softmax (all warps) -> MMA: they are in registers
@@ -254,16 +255,14 @@ __device__ __forceinline__ bool next_item(const BwdBarriers& bars, const volatil
 }
 constexpr int kItemConsumers = kSoftmaxWarps + 3;  // softmax warps, MMA warps, store warp
 
-// D[128 x 128] (+)= A[tmem] B for 64 of the 128 contraction rows.  A (BF16) was written over fp32 columns, by each
-// softmax thread over the first half of its own kCols; B is MN-major (16 contraction rows are 2048 bytes).
+// D[128 x 128] (+)= A[tmem] B for one half (64) of the contraction rows.  A (BF16) was written over fp32 columns, by each
+// softmax thread over the first half of its own 16; B is MN-major (16 contraction rows are 2048 bytes).
 __device__ __forceinline__ void issue_ts_half(bool leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t b_desc, int half,
                                               bool accumulate) {
   if (leader) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      const int k16 = half * 4 + kk;           // 16 contraction rows: 8 columns of A
-      const int part = k16 * 16 / kCols;
-      mma_ts(tmem_d, tmem_a + part * kCols + (k16 * 8 - part * (kCols / 2)), desc_advance(b_desc, k16 * 2048), kIdescPV,
+      mma_ts(tmem_d, tmem_a + half * 64 + kk * kCols, desc_advance(b_desc, (half * 4 + kk) * 2048), kIdescPV,
              (accumulate || kk > 0) ? 1u : 0u);
     }
   }
@@ -696,22 +695,22 @@ __device__ __forceinline__ void store_part32(float* dst, const uint32_t* o, floa
 }
 
 // Both softmax roles: P = exp2(S * scale log2(e) - LSE log2(e)) on pairs of columns; of every eight pairs
-// kBwdPolyPairs take the polynomial on the FMA pipe, the others the special-function unit.
-#ifndef ATTN_BWD_POLY_PAIRS
-#define ATTN_BWD_POLY_PAIRS 2
-#endif
-constexpr int kBwdPolyPairs = ATTN_BWD_POLY_PAIRS;
+// kPolyPairs take the polynomial on the FMA pipe, the others the special-function unit.  Key items wait for P with the
+// tensor pipe idle behind them, so both units share the work; query items have the next scores ready and want the fewest
+// instructions (8 heads of 16384, each kind by itself, 1 / 2 / 4 of eight: key items 1545 / 1509 / 1489 us, query
+// items 1142 / 1191 / 1205 us).
+constexpr int kKeyPolyPairs = 4, kQryPolyPairs = 1;
 #define ATTN_F(r, i) __uint_as_float((r)[(i)])
 
 // exp2 of kCols score columns in place, given per pair of columns the pair of -LSE log2(e).  Columns outside
 // [seen_from, seen_to) become 0 where `masked`.
-template <typename NegLse>
+template <int kPolyPairs, typename NegLse>
 __device__ __forceinline__ void exp_row(uint32_t* x, float2 c2, NegLse neg_lse, bool masked, int seen_from, int seen_to) {
 #pragma unroll
   for (int pr = 0; pr < kCols / 2; ++pr) {
     const int e = pr * 2;
     const float2 y = fma2(make_float2(ATTN_F(x, e), ATTN_F(x, e + 1)), c2, neg_lse(e));
-    const float2 w = (pr & 7) < kBwdPolyPairs ? exp2_poly2(y) : make_float2(ex2_approx(y.x), ex2_approx(y.y));
+    const float2 w = (pr & 7) < kPolyPairs ? exp2_poly2(y) : make_float2(ex2_approx(y.x), ex2_approx(y.y));
     x[e] = __float_as_uint(w.x);
     x[e + 1] = __float_as_uint(w.y);
   }
@@ -723,11 +722,29 @@ __device__ __forceinline__ void exp_row(uint32_t* x, float2 c2, NegLse neg_lse, 
   }
 }
 
-// One softmax thread of a key item: row `row` of the tile (a key), columns [part * kCols, (part + 1) * kCols).
+// dS = P o (dP - delta) of kCols columns, as BF16 words, given per pair of columns the pair of -delta.
+template <typename NegDelta>
+__device__ __forceinline__ void ds_row(const uint32_t* x, const uint32_t* d, NegDelta neg_delta, uint32_t* pk) {
+#pragma unroll
+  for (int e = 0; e < kCols; e += 2) {
+    const float2 t = add2(make_float2(ATTN_F(d, e), ATTN_F(d, e + 1)), neg_delta(e));
+    const float2 w = mul2(make_float2(ATTN_F(x, e), ATTN_F(x, e + 1)), t);
+    pk[e / 2] = pack_bf16x2(w.x, w.y);
+  }
+}
+// kCols / 2 words of a finished operand into tensor memory, and the word to the MMA warp that waits for it.
+__device__ __forceinline__ void hand_over(uint32_t taddr, const uint32_t* pk, uint64_t* bar, int lane) {
+  tmem_st_x8(taddr, pk);
+  tmem_wait_st();
+  tc_fence_before_sync();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+}
+
+// One softmax thread of a key item: row `row` of the tile (a key), columns part * kCols + [0, kCols) of each half.
 __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars,
                                             const uint8_t* smem, WaitCtx ctx, uint32_t tmem_row, int part, int row, int lane,
                                             Phases& ph) {
-  const int half = part / (kParts / 2);
   const uint32_t t_s = tmem_row + kTmS + part * kCols, t_dp = tmem_row + kTmDp + part * kCols;
   const float2 c2 = make_float2(p.scale_log2, p.scale_log2);
   int tile = it.first + it.t0 % it.per_head;
@@ -739,40 +756,33 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
               mbar_wait(&bars.s_full[0], ph.s & 1, ctx, kRoleBwdSoftmax | kBarS);
     if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
-    uint32_t x[kCols], pk[kCols / 2];
-    tmem_ld_x32(t_s, x);
+    uint32_t x[2][kCols], d[2][kCols], pk[kCols / 2];
+    tmem_ld_x16(t_s, x[0]);
+    tmem_ld_x16(t_s + 64, x[1]);
     tmem_wait_ld();
     // the key is visible to the queries of columns `seen_from` on
     const int seen_from = it.row0 + row - p.off - tile * kTile - part * kCols;
     const bool masked = p.causal && it.row0 + kTile - 1 > tile * kTile + p.off;  // the same for the whole CTA
-    exp_row(x, c2, [&](int e) { return *reinterpret_cast<const float2*>(nl + e); }, masked, seen_from, kCols);
 #pragma unroll
-    for (int e = 0; e < kCols / 2; ++e) pk[e] = pack_bf16x2(ATTN_F(x, 2 * e), ATTN_F(x, 2 * e + 1));
-    tmem_st_x16(t_s, pk);
-    tmem_wait_st();
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&bars.p_full[half]);
+    for (int h = 0; h < 2; ++h) {
+      exp_row<kKeyPolyPairs>(x[h], c2, [&](int e) { return *reinterpret_cast<const float2*>(nl + h * 64 + e); }, masked,
+                             seen_from - h * 64, kCols);
+#pragma unroll
+      for (int e = 0; e < kCols / 2; ++e) pk[e] = pack_bf16x2(ATTN_F(x[h], 2 * e), ATTN_F(x[h], 2 * e + 1));
+      hand_over(t_s + h * 64, pk, &bars.p_full[h], lane);
+    }
     ok = mbar_wait(bars.dp_full, ph.dp & 1, ctx, kRoleBwdSoftmax | kBarDp);
     if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
-    uint32_t d[kCols];
-    tmem_ld_x32(t_dp, d);
+    tmem_ld_x16(t_dp, d[0]);
+    tmem_ld_x16(t_dp + 64, d[1]);
     tmem_wait_ld();
 #pragma unroll
-    for (int e = 0; e < kCols; e += 2) {
-      const float2 t = add2(make_float2(ATTN_F(d, e), ATTN_F(d, e + 1)), *reinterpret_cast<const float2*>(neg_delta + e));
-      const float2 w = mul2(make_float2(ATTN_F(x, e), ATTN_F(x, e + 1)), t);
-      pk[e / 2] = pack_bf16x2(w.x, w.y);
+    for (int h = 0; h < 2; ++h) {  // over this thread's own columns, which are in registers
+      ds_row(x[h], d[h], [&](int e) { return *reinterpret_cast<const float2*>(neg_delta + h * 64 + e); }, pk);
+      hand_over(t_dp + h * 64, pk, &bars.ds_full[h], lane);
     }
-    tmem_st_x16(t_dp, pk);  // over this thread's own columns, which are in registers
-    tmem_wait_st();
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) {
-      mbar_arrive(&bars.ds_full[half]);
-      mbar_arrive(&bars.stat_empty[st]);
-    }
+    if (lane == 0) mbar_arrive(&bars.stat_empty[st]);
     ph.s ^= 1u;
     ++ph.dp;
     ++ph.key;
@@ -784,7 +794,6 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
 // The same for a query item: row `row` is a query, the columns are keys.
 __device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, WaitCtx ctx,
                                               uint32_t tmem_row, int part, int row, int lane, Phases& ph) {
-  const int half = part / (kParts / 2);
   const uint32_t t_dp = tmem_row + kTmQryDp + part * kCols;
   const float2 c2 = make_float2(p.scale_log2, p.scale_log2);
   const size_t at = (static_cast<size_t>(it.b) * p.Hq + it.h) * p.n_qt * kTile + it.row0 + row;
@@ -798,32 +807,30 @@ __device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem&
     if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
     const uint32_t t_s = tmem_row + kTmQryS + x_buf * kTile + part * kCols;
-    uint32_t x[kCols];
-    tmem_ld_x32(t_s, x);
+    uint32_t x[2][kCols], d[2][kCols], pk[kCols / 2];
+    tmem_ld_x16(t_s, x[0]);
+    tmem_ld_x16(t_s + 64, x[1]);
     tmem_wait_ld();
     // keys beyond Sk are masked too: their scores are 0, and exp2(nl) may be infinite
     const bool masked = (it.t0 + j + 1) * kTile > tile_clear;  // the same for the whole CTA
-    exp_row(x, c2, [&](int) { return nl2; }, masked, 0, row_limit - (it.t0 + j) * kTile - part * kCols);
+    const int seen_to = row_limit - (it.t0 + j) * kTile - part * kCols;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      exp_row<kQryPolyPairs>(x[h], c2, [&](int) { return nl2; }, masked, 0, seen_to - h * 64);
     ok = mbar_wait(bars.dp_full, ph.dp & 1, ctx, kRoleBwdSoftmax | kBarDp);
     if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
-    uint32_t d[kCols], pk[kCols / 2];
-    tmem_ld_x32(t_dp, d);
+    tmem_ld_x16(t_dp, d[0]);
+    tmem_ld_x16(t_dp + 64, d[1]);
     tmem_wait_ld();
     tc_fence_before_sync();
     __syncwarp();
     if (lane == 0) mbar_arrive(bars.dp_read);
 #pragma unroll
-    for (int e = 0; e < kCols; e += 2) {
-      const float2 t = add2(make_float2(ATTN_F(d, e), ATTN_F(d, e + 1)), ndl2);
-      const float2 w = mul2(make_float2(ATTN_F(x, e), ATTN_F(x, e + 1)), t);
-      pk[e / 2] = pack_bf16x2(w.x, w.y);
+    for (int h = 0; h < 2; ++h) {  // over this thread's own scores, read above
+      ds_row(x[h], d[h], [&](int) { return ndl2; }, pk);
+      hand_over(t_s + h * 64, pk, &bars.ds_full[2 * x_buf + h], lane);
     }
-    tmem_st_x16(t_s, pk);  // over this thread's own scores, read above
-    tmem_wait_st();
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&bars.ds_full[2 * x_buf + half]);
     ph.s ^= 1u << x_buf;
     ++ph.dp;
   }
@@ -837,7 +844,7 @@ __device__ __forceinline__ bool write_results(const BwdParams& p, const BwdItem&
                                               uint32_t pos_a, uint32_t pos_b, uint32_t staged_a, uint32_t staged_b) {
   const int half = part / (kParts / 2);
   const int n32 = it.keys ? 2 : 1;  // 32-column pieces of this thread
-  const int col0 = it.keys ? (part % (kParts / 2)) * 64 : part * kCols;
+  const int col0 = it.keys ? (part % (kParts / 2)) * 64 : part * 32;
   const uint32_t t_acc = tmem_row + (it.keys ? (half == 0 ? kTmDv : kTmDk) : kTmDq) + col0;
   const float factor = it.keys && half == 0 ? 1.f : p.scale;
   bool ok = mbar_wait(bars.acc_full, item & 1, ctx, kRoleBwdSoftmax | kBarAcc);
@@ -971,9 +978,9 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       mbar_init(&bars.stat_full[i], 1);
       mbar_init(&bars.stat_empty[i], kSoftmaxWarps);
       mbar_init(&bars.s_full[i], 1);
-      mbar_init(&bars.p_full[i], kSoftmaxWarps / 2);
-      mbar_init(&bars.ds_full[i], kSoftmaxWarps / 2);
-      mbar_init(&bars.ds_full[2 + i], kSoftmaxWarps / 2);
+      mbar_init(&bars.p_full[i], kSoftmaxWarps);
+      mbar_init(&bars.ds_full[i], kSoftmaxWarps);
+      mbar_init(&bars.ds_full[2 + i], kSoftmaxWarps);
       mbar_init(&bars.stage_ready[i], 2);
       mbar_init(&bars.stage_full[i], kSoftmaxWarps / 2);
       mbar_init(&bars.item_full[i], 1);
