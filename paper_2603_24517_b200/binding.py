@@ -354,39 +354,53 @@ def attn_bwd_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Sk: int, D: int
     return int(load_library().attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, int(bool(causal))))
 
 
+def _raw_stream(dev, stream):
+    """cudaStream_t of ``stream``, or of torch's current stream on ``dev`` when None."""
+    return torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream
+
+
+def _on_device(dev, fn, *args):
+    """fn(*args) with ``dev`` current; switching devices costs more than a call that need not."""
+    if torch.cuda.current_device() == dev.index:
+        return fn(*args)
+    with torch.cuda.device(dev):
+        return fn(*args)
+
+
 def _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, strided):
-    named = (("dout", dout), ("q", q), ("k", k), ("v", v), ("o", o), ("dq", dq), ("dk", dk), ("dv", dv))
+    tensors = (dout, q, k, v, o, dq, dk, dv)
     dev = q.device
-    for name, t in named:
-        if t.dtype != torch.bfloat16 or t.dim() != 4 or t.device.type != "cuda" or t.device != dev \
-                or not (t.stride(3) == 1 if strided else t.is_contiguous()):
+    shape, kv_shape = q.shape, k.shape
+    if len(shape) != 4 or len(kv_shape) != 4 or dev.type != "cuda":
+        raise ValueError("q and k must be 4-D cuda tensors [B, S, H, D]")
+    for i, t in enumerate(tensors):
+        if t.dtype is not torch.bfloat16 or t.device != dev or t.shape != (kv_shape if i in (2, 3, 6, 7) else shape) \
+                or not (t.is_contiguous() or strided and t.stride(3) == 1):
+            name = ("dout", "q", "k", "v", "o", "dq", "dk", "dv")[i]
             layout = "with a contiguous last axis" if strided else "that is contiguous"
-            raise ValueError(f"{name} must be a 4-D bfloat16 tensor [B, S, H, D] {layout}, all on one cuda device")
-    B, Sq, Hq, D = q.shape
-    Bk, Sk, Hkv, Dk = k.shape
-    if v.shape != k.shape or o.shape != q.shape or dout.shape != q.shape or dq.shape != q.shape or dk.shape != k.shape \
-            or dv.shape != k.shape or Bk != B or Dk != D:
-        raise ValueError("inconsistent q/k/v/o/dout/dq/dk/dv shapes")
+            raise ValueError(f"{name} must be a bfloat16 tensor {layout}, of the shape [B, S, H, D] of "
+                             f"{'k' if i in (2, 3, 6, 7) else 'q'}, on q's device")
+    B, Sq, Hq, D = shape
+    Bk, Sk, Hkv, Dk = kv_shape
+    if Bk != B or Dk != D:
+        raise ValueError("inconsistent q/k shapes")
     for name, t in (("lse", lse), ("dlse", dlse)):
         if t is None and name == "dlse":
             continue
-        if t is None or t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (B, Hq, Sq) or t.device != dev:
+        if t is None or t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != (B, Hq, Sq) or t.device != dev:
             raise ValueError(f"{name} must be a contiguous float32 tensor [B, Hq, Sq] on q's device")
     lib = load_library()
+    causal = int(bool(causal))
     if workspace is None:
-        need = lib.attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, int(bool(causal)))
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        workspace = q.new_empty(max(lib.attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, causal), 16), dtype=torch.uint8)
     elif not workspace.is_contiguous() or workspace.device != dev:
         raise ValueError("workspace must be a contiguous tensor on q's device")
-    ptrs = [t.data_ptr() for t in (dout, q, k, v, o, lse)] + [None if dlse is None else dlse.data_ptr()] \
-        + [t.data_ptr() for t in (dq, dk, dv)] + [B, Hq, Hkv, Sq, Sk, D]
-    with torch.cuda.device(dev):
-        if stream is None:
-            stream = torch.cuda.current_stream(dev).cuda_stream
-        tail = (int(bool(causal)), float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
-        if strided:
-            return lib.attn_bwd_strided(*ptrs, *[_strides3(t) for _, t in named], *tail)
-        return lib.attn_bwd(*ptrs, *tail)
+    args = (dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+            None if dlse is None else dlse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Hq, Hkv, Sq, Sk, D)
+    tail = (causal, float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(dev, stream))
+    if strided:
+        return _on_device(dev, lib.attn_bwd_strided, *args, *[_strides3(t) for t in tensors], *tail)
+    return _on_device(dev, lib.attn_bwd, *args, *tail)
 
 
 def attn_bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal: bool, scale: float, dlse=None, workspace=None,
@@ -420,44 +434,44 @@ def attn_bwd_strided(dout, q, k, v, o, lse, dq, dk, dv, causal: bool, scale: flo
 
 
 def _rope_args(q, k, q_weight, k_weight, cos, sin, positions, others):
-    """Checks the tensors and marshals what both directions share: (leading arguments, sizes)."""
-    dev = q.device
-    for name, t in (("q", q), ("k", k)) + others:
-        if t.dtype != torch.bfloat16 or t.dim() != 4 or t.stride(3) != 1 or t.device != dev or dev.type != "cuda":
-            raise ValueError(f"{name} must be a 4-D bfloat16 tensor [B, S, H, D] with a contiguous last axis, "
-                             "all on one cuda device")
-    B, S, Hq, D = q.shape
-    Hkv = k.shape[2]
-    if k.shape != (B, S, Hkv, D):
-        raise ValueError("inconsistent q/k shapes")
-    for name, t in others:
-        if t.shape != (q if "q" in name else k).shape:
-            raise ValueError(f"inconsistent shape of {name}")
-    weight_type = -1
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+    """Checks the tensors and marshals what both directions share: (leading arguments, sizes).  ``others``: pairs of
+    tensors shaped like (q, k)."""
+    dev, shape, kv_shape = q.device, q.shape, k.shape
+    if dev.type != "cuda" or len(shape) != 4 or len(kv_shape) != 4 or kv_shape[:2] != shape[:2] or kv_shape[3] != shape[3]:
+        raise ValueError("q and k must be cuda tensors [B, S, Hq, D] and [B, S, Hkv, D]")
+    for pair in ((q, k), *others):
+        for t, want in zip(pair, (shape, kv_shape)):
+            if t.dtype is not torch.bfloat16 or t.shape != want or t.stride(3) != 1 or t.device != dev:
+                raise ValueError("queries, keys, their outputs and gradients must be bfloat16 tensors [B, S, H, D] of q's and "
+                                 "k's shapes with a contiguous last axis, all on q's device")
+    B, S, Hq, D = shape
+    weight_type, weights = 0, []
+    for w in (q_weight, k_weight):
         if w is None:
+            weights.append(None)
             continue
         if w.dtype not in (torch.float32, torch.bfloat16) or w.shape != (D,) or not w.is_contiguous() or w.device != dev:
-            raise ValueError(f"{name} must be a contiguous float32 or bfloat16 tensor [D] on q's device")
-        kind = int(w.dtype == torch.bfloat16)
-        if weight_type not in (-1, kind):
-            raise ValueError("q_weight and k_weight must have one type")
-        weight_type = kind
-    if cos.dtype != torch.float32 or cos.dim() != 2 or not cos.is_contiguous() or cos.device != dev \
-            or sin.dtype != torch.float32 or sin.shape != cos.shape or not sin.is_contiguous() or sin.device != dev:
+            raise ValueError("q_weight and k_weight must be contiguous float32 or bfloat16 tensors [D] on q's device")
+        weight_type = int(w.dtype is torch.bfloat16)
+        weights.append(w.data_ptr())
+    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        raise ValueError("q_weight and k_weight must have one type")
+    table = cos.shape
+    if len(table) != 2 or cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or sin.shape != table \
+            or not cos.is_contiguous() or not sin.is_contiguous() or cos.device != dev or sin.device != dev:
         raise ValueError("cos and sin must be contiguous float32 tensors [positions, rot_dim / 2] on q's device")
     pos_ptr, pos_type, pos_strides = None, 0, None
     if positions is not None:
         if positions.dtype not in (torch.int32, torch.int64) or positions.device != dev \
                 or positions.shape not in ((B, S), (S,)):
             raise ValueError("positions must be an int32 or int64 tensor [B, S] or [S] on q's device")
-        pos_ptr, pos_type = positions.data_ptr(), int(positions.dtype == torch.int64)
-        if positions.dim() == 1 or not positions.is_contiguous():
-            pos_strides = (ctypes.c_longlong * 2)(*((0, positions.stride(0)) if positions.dim() == 1 else positions.stride()))
-    lead = (q.data_ptr(), k.data_ptr(), None if q_weight is None else q_weight.data_ptr(),
-            None if k_weight is None else k_weight.data_ptr(), max(weight_type, 0), cos.data_ptr(), sin.data_ptr(),
-            pos_ptr, pos_type, pos_strides)
-    return lead, (B, S, Hq, Hkv, D, 2 * cos.shape[1], cos.shape[0])
+        pos_ptr, pos_type = positions.data_ptr(), int(positions.dtype is torch.int64)
+        if positions.dim() == 1:
+            pos_strides = (ctypes.c_longlong * 2)(0, positions.stride(0))
+        elif not positions.is_contiguous():
+            pos_strides = (ctypes.c_longlong * 2)(*positions.stride())
+    return (q.data_ptr(), k.data_ptr(), *weights, weight_type, cos.data_ptr(), sin.data_ptr(), pos_ptr, pos_type,
+            pos_strides), (B, S, Hq, kv_shape[2], D, 2 * table[1], table[0])
 
 
 def _strides3_or_none(t):
@@ -467,12 +481,10 @@ def _strides3_or_none(t):
 def attn_qk_norm_rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6,
                              interleaved: bool = False, stream=None) -> int:
     """Calls ``attn_qk_norm_rope`` on CUDA tensors and returns its raw status code."""
-    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, (("q_out", q_out), ("k_out", k_out)))
-    with torch.cuda.device(q.device):
-        if stream is None:
-            stream = torch.cuda.current_stream(q.device).cuda_stream
-        return load_library().attn_qk_norm_rope(*lead, q_out.data_ptr(), k_out.data_ptr(), *sizes, int(bool(interleaved)),
-                                                float(eps), *[_strides3_or_none(t) for t in (q, k, q_out, k_out)], stream)
+    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, ((q_out, k_out),))
+    return _on_device(q.device, load_library().attn_qk_norm_rope, *lead, q_out.data_ptr(), k_out.data_ptr(), *sizes,
+                      int(bool(interleaved)), float(eps), *[_strides3_or_none(t) for t in (q, k, q_out, k_out)],
+                      _raw_stream(q.device, stream))
 
 
 def attn_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6,
@@ -493,28 +505,24 @@ def attn_qk_norm_rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, 
                                  positions=None, eps: float = 1e-6, interleaved: bool = False, workspace=None,
                                  stream=None) -> int:
     """Calls ``attn_qk_norm_rope_bwd``; ``workspace`` is a contiguous cuda tensor (allocated here when None)."""
-    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions,
-                             (("dq_out", dq_out), ("dk_out", dk_out), ("dq", dq), ("dk", dk)))
+    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, ((dq_out, dk_out), (dq, dk)))
+    dev = q.device
     for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
-        if t is not None and (t.dtype != torch.float32 or t.shape != q.shape[3:] or not t.is_contiguous()
-                              or t.device != q.device):
+        if t is not None and (t.dtype is not torch.float32 or t.shape != q.shape[3:] or not t.is_contiguous()
+                              or t.device != dev):
             raise ValueError(f"{name} must be a contiguous float32 tensor [D] on q's device")
     lib = load_library()
     if workspace is None:
         if dq_weight is not None or dk_weight is not None:
-            workspace = torch.empty(lib.attn_qk_norm_rope_bwd_workspace_bytes(), dtype=torch.uint8, device=q.device)
-    elif not workspace.is_contiguous() or workspace.device != q.device:
+            workspace = q.new_empty(lib.attn_qk_norm_rope_bwd_workspace_bytes(), dtype=torch.uint8)
+    elif not workspace.is_contiguous() or workspace.device != dev:
         raise ValueError("workspace must be a contiguous tensor on q's device")
-    with torch.cuda.device(q.device):
-        if stream is None:
-            stream = torch.cuda.current_stream(q.device).cuda_stream
-        return lib.attn_qk_norm_rope_bwd(dq_out.data_ptr(), dk_out.data_ptr(), *lead, dq.data_ptr(), dk.data_ptr(),
-                                         None if dq_weight is None else dq_weight.data_ptr(),
-                                         None if dk_weight is None else dk_weight.data_ptr(), *sizes,
-                                         int(bool(interleaved)), float(eps),
-                                         *[_strides3_or_none(t) for t in (dq_out, dk_out, q, k, dq, dk)],
-                                         None if workspace is None else workspace.data_ptr(),
-                                         0 if workspace is None else workspace.numel() * workspace.element_size(), stream)
+    return _on_device(dev, lib.attn_qk_norm_rope_bwd, dq_out.data_ptr(), dk_out.data_ptr(), *lead, dq.data_ptr(),
+                      dk.data_ptr(), None if dq_weight is None else dq_weight.data_ptr(),
+                      None if dk_weight is None else dk_weight.data_ptr(), *sizes, int(bool(interleaved)), float(eps),
+                      *[_strides3_or_none(t) for t in (dq_out, dk_out, q, k, dq, dk)],
+                      None if workspace is None else workspace.data_ptr(),
+                      0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(dev, stream))
 
 
 def attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions=None,
@@ -595,6 +603,10 @@ def _ordered(grad):
     return grad
 
 
+def _new_like(t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float | None = None, dlse=None):
     """Gradients (dq, dk, dv) of ``attention_forward(q, k, v, causal, scale)`` from its results ``o``, ``lse`` and the
     gradient ``dout`` with respect to ``o`` (and ``dlse`` with respect to ``lse``).  Inputs may be views as in
@@ -603,7 +615,7 @@ def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1])
     dout = _ordered(dout)
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = _new_like(q), _new_like(k), _new_like(v)
     if all(t.is_contiguous() for t in (dout, q, k, v, o)):
         attn_bwd(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse)
     else:
@@ -614,7 +626,7 @@ def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float
 def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: float = 1e-6, interleaved: bool = False):
     """Convenience wrapper: the normed and rotated queries and keys as new contiguous tensors (see ``attn_qk_norm_rope``),
     ready for ``attention_forward``."""
-    q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    q_out, k_out = _new_like(q), _new_like(k)
     attn_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved)
     return q_out, k_out
 
@@ -623,9 +635,9 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, po
                           interleaved: bool = False):
     """Gradients (dq, dk, dq_weight, dk_weight) of ``qk_norm_rope``; a weight that is None has the gradient None."""
     dq_out, dk_out = _ordered(dq_out), _ordered(dk_out)
-    dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
-    dq_weight, dk_weight = (None if w is None else torch.empty(w.shape, dtype=torch.float32, device=w.device)
-                            for w in (q_weight, k_weight))
+    dq, dk = _new_like(q), _new_like(k)
+    dq_weight = None if q_weight is None else torch.empty_like(q_weight, dtype=torch.float32)
+    dk_weight = None if k_weight is None else torch.empty_like(k_weight, dtype=torch.float32)
     attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions, eps,
                           interleaved)
     return dq, dk, dq_weight, dk_weight

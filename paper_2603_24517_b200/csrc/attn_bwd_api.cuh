@@ -115,14 +115,16 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
   p.status = dev->status;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int padded = p.n_qt * attn::kTile;
-  const long long n_rows = static_cast<long long>(B) * Hq * padded;
-  long long blocks = (n_rows + attn::bwd::kPrepThreads / 16 - 1) / (attn::bwd::kPrepThreads / 16);
-  const long long cap = static_cast<long long>(dev->sm_count) * 8;
-  if (blocks > cap) blocks = cap;
-  attn::bwd::attn_bwd_prep_kernel<<<static_cast<int>(blocks), attn::bwd::kPrepThreads, 0, s>>>(
+  int heads_log2 = 0;  // heads of a block: up to 8, so that 256 rows are 32 positions or more
+  while (heads_log2 < 3 && (2 << heads_log2) <= Hq) ++heads_log2;
+  const int prep_rows = attn::bwd::kPrepThreads >> heads_log2;
+  const long long prep_blocks = static_cast<long long>(B) * ((padded + prep_rows - 1) / prep_rows) *
+                                ((Hq + (1 << heads_log2) - 1) >> heads_log2);
+  const int cap = dev->sm_count * 8;
+  attn::bwd::attn_bwd_prep_kernel<<<static_cast<int>(prep_blocks < cap ? prep_blocks : cap), attn::bwd::kPrepThreads, 0, s>>>(
       static_cast<const uint16_t*>(t.o), static_cast<const uint16_t*>(t.dout),
       attn::bwd::RowStrides{ts.o.b, ts.o.s, ts.o.h}, attn::bwd::RowStrides{ts.dout.b, ts.dout.s, ts.dout.h}, t.lse, t.dlse,
-      neg_lse2, neg_delta, Hq, Sq, padded, n_rows);
+      neg_lse2, neg_delta, Hq, Sq, padded, heads_log2, static_cast<int>(prep_blocks));
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
   const int grid = p.n_items;
   attn::bwd::attn_bwd_kernel<<<grid, attn::bwd::kBwdThreads, attn::bwd::kSmemBwdBytes, s>>>(tm_q, tm_k, tm_v, tm_do, tm_dq,

@@ -1029,8 +1029,9 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   }
 }
 
-// Row statistics of the backward pass: -LSE log2(e) and -delta = dLSE - sum_d dO O, one half warp per
-// (batch, row, head), rows padded to whole tiles.  HBM-bound: 512 bytes read per row.
+// Row statistics of the backward pass: -LSE log2(e) and -delta = dLSE - sum_d dO O, rows padded to whole tiles.
+// HBM-bound: 512 bytes read per row.  A block takes 256 rows, heads fastest as they lie in memory, half a warp a row
+// with four rows in flight; the sums pass through shared memory so that they are written along the sequence.
 constexpr int kPrepThreads = 256;
 struct RowStrides {
   long long b, s, h;  // elements
@@ -1044,35 +1045,55 @@ __device__ __forceinline__ float dot2_bf16(uint32_t a, uint32_t b, float acc) {
 __global__ void __launch_bounds__(kPrepThreads)
 attn_bwd_prep_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict__ dout, RowStrides so, RowStrides sdo,
                      const float* __restrict__ lse, const float* __restrict__ dlse, float* __restrict__ neg_lse2,
-                     float* __restrict__ neg_delta, int Hq, int Sq, int padded, long long n_rows) {
+                     float* __restrict__ neg_delta, int Hq, int Sq, int padded, int heads_log2, int n_blocks) {
+  __shared__ float sums[kPrepThreads];  // [sequence][head]
   const int sub = threadIdx.x & 15;
-  const long long step = static_cast<long long>(gridDim.x) * (kPrepThreads / 16);
-  for (long long r = static_cast<long long>(blockIdx.x) * (kPrepThreads / 16) + (threadIdx.x >> 4); r < n_rows; r += step) {
-    const int h = static_cast<int>(r % Hq);
-    const long long t = r / Hq;
-    const int s = static_cast<int>(t % padded);
-    const long long b = t / padded;
-    float acc = 0.f, l = -INFINITY, dl = 0.f;
-    if (s < Sq) {
-      const uint4 x = __ldg(reinterpret_cast<const uint4*>(o + b * so.b + s * so.s + h * so.h) + sub);
-      const uint4 y = __ldg(reinterpret_cast<const uint4*>(dout + b * sdo.b + s * sdo.s + h * sdo.h) + sub);
-      const long long at = (b * Hq + h) * Sq + s;
-      l = __ldg(lse + at);
-      if (dlse != nullptr) dl = __ldg(dlse + at);
-      acc = dot2_bf16(x.x, y.x, dot2_bf16(x.y, y.y, dot2_bf16(x.z, y.z, dot2_bf16(x.w, y.w, 0.f))));
-    }
+  const int heads = 1 << heads_log2, rows = kPrepThreads >> heads_log2;  // heads and sequence positions of a block
+  const int h_blocks = (Hq + heads - 1) >> heads_log2, s_blocks = (padded + rows - 1) / rows;
+  for (int blk = blockIdx.x; blk < n_blocks; blk += gridDim.x) {
+    const int hb = blk % h_blocks, t = blk / h_blocks;
+    const int sb = t % s_blocks;
+    const long long b = t / s_blocks;
+    const uint16_t* ob = o + b * so.b;
+    const uint16_t* db = dout + b * sdo.b;
 #pragma unroll
-    for (int m = 8; m > 0; m >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, m);
-    if (sub == 0) {
+    for (int i = 0; i < 16; i += 4) {
+      uint4 x[4], y[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int r = (i + u) * 16 + (threadIdx.x >> 4);
+        const int h = (hb << heads_log2) + (r & (heads - 1)), s = sb * rows + (r >> heads_log2);
+        x[u] = y[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (h < Hq && s < Sq) {
+          x[u] = __ldg(reinterpret_cast<const uint4*>(ob + s * so.s + h * so.h) + sub);
+          y[u] = __ldg(reinterpret_cast<const uint4*>(db + s * sdo.s + h * sdo.h) + sub);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float acc = dot2_bf16(x[u].x, y[u].x, dot2_bf16(x[u].y, y[u].y, dot2_bf16(x[u].z, y[u].z, dot2_bf16(x[u].w, y[u].w, 0.f))));
+#pragma unroll
+        for (int m = 8; m > 0; m >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, m);
+        if (sub == 0) sums[(i + u) * 16 + (threadIdx.x >> 4)] = acc;
+      }
+    }
+    __syncthreads();
+    const int h = (hb << heads_log2) + threadIdx.x / rows, s = sb * rows + threadIdx.x % rows;
+    if (h < Hq && s < padded) {
+      float l = -INFINITY, dl = 0.f;
+      if (s < Sq) {
+        const long long at = (b * Hq + h) * Sq + s;
+        l = __ldg(lse + at);
+        if (dlse != nullptr) dl = __ldg(dlse + at);
+      }
       const long long at = (b * Hq + h) * padded + s;
       const bool none = l == -INFINITY;  // the row sees no key, or does not exist: P = exp2(-inf) = 0
       neg_lse2[at] = none ? -INFINITY : -l * 1.4426950408889634f;
-      neg_delta[at] = none ? 0.f : dl - acc;
+      neg_delta[at] = none ? 0.f : dl - sums[(threadIdx.x % rows) * heads + threadIdx.x / rows];
     }
+    __syncthreads();
   }
 }
-
-#undef ATTN_F
 
 // Adds up the fp32 partial sums of split items in order and rounds once: one warp a row of 128, rows in the
 // order of the output [B][S][H]; blockIdx.y picks the output.  HBM-bound, and small: only problems with few tiles are

@@ -69,7 +69,9 @@ attn_status_t rope_params(const RopeArgs& a, const long long* const* in_strides,
   p->S = a.S;
   p->rot = a.rot_dim;
   p->eps = a.eps;
-  p->n_units = static_cast<long long>(a.B) * a.S * (p->units[0] + p->units[1]);
+  // the kernels count units in 32 bits (2^30 units are 2 TB of rows)
+  if (static_cast<long long>(a.B) * a.S > 0x3fffffffLL / (static_cast<long long>(p->units[0]) + p->units[1])) return ATTN_ERR_UNSUPPORTED;
+  p->n_units = a.B * a.S * (p->units[0] + p->units[1]);
   return ATTN_OK;
 }
 
@@ -86,8 +88,8 @@ attn_status_t rope_output(void* out, const long long* strides, const RopeParams&
 }
 
 int rope_grid(const RopeParams& p, int cap) {
-  const long long ctas = (p.n_units + attn::rope::kRopeWarps - 1) / attn::rope::kRopeWarps;
-  return static_cast<int>(ctas < cap ? ctas : cap);
+  const int ctas = (p.n_units + attn::rope::kRopeWarps - 1) / attn::rope::kRopeWarps;
+  return ctas < cap ? ctas : cap;
 }
 
 }  // namespace

@@ -47,7 +47,7 @@ struct RopeParams {
   int S, heads[2], units[2];  // units: ceil(heads / kUnitRows)
   int rot;
   float eps;
-  long long n_units;     // B * S * (units[0] + units[1])
+  int n_units;           // B * S * (units[0] + units[1])
   float* partials;       // gradient kernel: [gridDim.x][2][128], or null
 };
 
@@ -55,15 +55,16 @@ struct Unit {
   long long b;
   int s, t, h0;  // token, tensor (0 queries, 1 keys), first head
 };
-__device__ __forceinline__ Unit unit_of(const RopeParams& p, long long u) {
-  const int per = p.units[0] + p.units[1];
-  const long long token = u / per;
-  int k = static_cast<int>(u - token * per);
+// 32-bit division: a 64-bit one costs more instructions than the arithmetic of the unit's rows.
+__device__ __forceinline__ Unit unit_of(const RopeParams& p, uint32_t u) {
+  const uint32_t per = p.units[0] + p.units[1];
+  const uint32_t token = u / per, b = token / static_cast<uint32_t>(p.S);
+  const int k = static_cast<int>(u - token * per);
   Unit r;
   r.t = k >= p.units[0] ? 1 : 0;
   r.h0 = (r.t ? k - p.units[0] : k) * kUnitRows;
-  r.b = token / p.S;
-  r.s = static_cast<int>(token - r.b * p.S);
+  r.b = b;
+  r.s = static_cast<int>(token - b * p.S);
   return r;
 }
 
@@ -159,8 +160,8 @@ template <bool kInterleaved>
 __global__ void __launch_bounds__(kRopeThreads)
 qk_norm_rope_kernel(const __grid_constant__ RopeParams p) {
   const int lane = threadIdx.x & 31, sub = lane & 15, hw = lane >> 4;
-  const long long step = static_cast<long long>(gridDim.x) * kRopeWarps;
-  for (long long un = static_cast<long long>(blockIdx.x) * kRopeWarps + (threadIdx.x >> 5); un < p.n_units; un += step) {
+  const uint32_t step = gridDim.x * kRopeWarps;
+  for (uint32_t un = blockIdx.x * kRopeWarps + (threadIdx.x >> 5); un < static_cast<uint32_t>(p.n_units); un += step) {
     const Unit u = unit_of(p, un);
     const RopeStrides sx = p.sx[u.t], so = p.sout[u.t];
     // no restrict qualifiers and no non-coherent loads: y may be x itself (a lane's rows are read before written)
@@ -211,11 +212,11 @@ __global__ void __launch_bounds__(kRopeThreads)
 qk_norm_rope_bwd_kernel(const __grid_constant__ RopeParams p) {
   __shared__ float sums[kRopeWarps * 2][2][kRopeDim];
   const int lane = threadIdx.x & 31, sub = lane & 15, hw = lane >> 4;
-  const long long step = static_cast<long long>(gridDim.x) * kRopeWarps;
+  const uint32_t step = gridDim.x * kRopeWarps;
   float dw[2][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) dw[0][i] = dw[1][i] = 0.f;
-  for (long long un = static_cast<long long>(blockIdx.x) * kRopeWarps + (threadIdx.x >> 5); un < p.n_units; un += step) {
+  for (uint32_t un = blockIdx.x * kRopeWarps + (threadIdx.x >> 5); un < static_cast<uint32_t>(p.n_units); un += step) {
     const Unit u = unit_of(p, un);
     const RopeStrides sx = p.sx[u.t], sg = p.sdy[u.t], so = p.sout[u.t];
     const uint16_t* src = p.x[u.t] + u.b * sx.b + u.s * sx.s;
