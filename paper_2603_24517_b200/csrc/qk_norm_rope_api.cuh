@@ -71,7 +71,7 @@ attn_status_t rope_params(const RopeArgs& a, const long long* const* in_strides,
   p->eps = a.eps;
   // the kernels count units in 32 bits (2^30 units are 2 TB of rows)
   if (static_cast<long long>(a.B) * a.S > 0x3fffffffLL / (static_cast<long long>(p->units[0]) + p->units[1])) return ATTN_ERR_UNSUPPORTED;
-  p->n_units = a.B * a.S * (p->units[0] + p->units[1]);
+  for (int t = 0; t < 2; ++t) p->n_units[t] = static_cast<uint32_t>(a.B) * a.S * p->units[t];
   return ATTN_OK;
 }
 
@@ -88,7 +88,7 @@ attn_status_t rope_output(void* out, const long long* strides, const RopeParams&
 }
 
 int rope_grid(const RopeParams& p, int cap) {
-  const int ctas = (p.n_units + attn::rope::kRopeWarps - 1) / attn::rope::kRopeWarps;
+  const int ctas = static_cast<int>((p.n_units[0] + p.n_units[1] + attn::rope::kRopeWarps - 1) / attn::rope::kRopeWarps);
   return ctas < cap ? ctas : cap;
 }
 

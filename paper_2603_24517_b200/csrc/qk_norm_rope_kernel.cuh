@@ -7,11 +7,12 @@
 //
 //     dw = sum over rows of g x r,    dx = r (g w - x r^2 mean(g w x)).
 //
-// Elementwise with one 128-value reduction per row: bound by HBM (4 bytes a value forward, 6 backward).  Half a
-// warp owns a row, 16 bytes a lane, so a row is one 256-byte access and its sums are four shuffles; the partner
-// of a value sits in the same lane (adjacent pairs) or `rot / 16` lanes away (halves), where four shuffles of the
-// packed BF16 words fetch it.  A warp works on 8 rows of one token and one tensor at a time: four independent row
-// loads per lane are in flight, and the token's angles and the weights are read once for them.
+// Elementwise with one 128-value reduction per row: bound by HBM (4 bytes a value forward, 6 backward) as long as the
+// instructions stay few.  Half a warp owns a row, 16 bytes a lane, so a row is one 256-byte access and its sums are four
+// shuffles; the partner of a value sits in the same lane (adjacent pairs) or `rot / 16` lanes away (halves), where four
+// shuffles of the packed BF16 words fetch it.  A warp works on 8 rows of one token and one tensor at a time: four
+// independent row loads per lane are in flight and the token's angles are read once for them; it does all its query
+// units before its key units, so weights and weight sums stay in registers; the arithmetic is in packed fp32 pairs.
 #pragma once
 
 #include "attn_merge_kernel.cuh"
@@ -44,46 +45,51 @@ struct RopeParams {
   int positions_64;
   long long pos_b, pos_s;  // strides of positions
   long long n_positions;
-  int S, heads[2], units[2];  // units: ceil(heads / kUnitRows)
+  int S, heads[2], units[2];  // units: ceil(heads / kUnitRows), per token
   int rot;
   float eps;
-  int n_units;           // B * S * (units[0] + units[1])
+  uint32_t n_units[2];   // B * S * units
   float* partials;       // gradient kernel: [gridDim.x][2][128], or null
 };
 
 struct Unit {
   long long b;
-  int s, t, h0;  // token, tensor (0 queries, 1 keys), first head
+  int s, h0;  // token of the sequence, first head
 };
 // 32-bit division: a 64-bit one costs more instructions than the arithmetic of the unit's rows.
-__device__ __forceinline__ Unit unit_of(const RopeParams& p, uint32_t u) {
-  const uint32_t per = p.units[0] + p.units[1];
+__device__ __forceinline__ Unit unit_of(const RopeParams& p, int t, uint32_t u) {
+  const uint32_t per = p.units[t];
   const uint32_t token = u / per, b = token / static_cast<uint32_t>(p.S);
-  const int k = static_cast<int>(u - token * per);
   Unit r;
-  r.t = k >= p.units[0] ? 1 : 0;
-  r.h0 = (r.t ? k - p.units[0] : k) * kUnitRows;
+  r.h0 = static_cast<int>(u - token * per) * kUnitRows;
   r.b = b;
   r.s = static_cast<int>(token - b * p.S);
   return r;
 }
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
-  f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-  f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+// Eight values of a lane as four pairs.
+__device__ __forceinline__ void unpack8(const uint4& v, float2* f) {
+  f[0] = make_float2(bf16_lo(v.x), bf16_hi(v.x));
+  f[1] = make_float2(bf16_lo(v.y), bf16_hi(v.y));
+  f[2] = make_float2(bf16_lo(v.z), bf16_hi(v.z));
+  f[3] = make_float2(bf16_lo(v.w), bf16_hi(v.w));
 }
-__device__ __forceinline__ uint4 pack8(const float* f) {
-  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+__device__ __forceinline__ uint4 pack8(const float2* f) {
+  return make_uint4(pack_bf16x2(f[0].x, f[0].y), pack_bf16x2(f[1].x, f[1].y), pack_bf16x2(f[2].x, f[2].y),
+                    pack_bf16x2(f[3].x, f[3].y));
 }
-__device__ __forceinline__ void load8(const float* src, float* f) {
+__device__ __forceinline__ void load8(const float* src, float2* f) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(src)), b = __ldg(reinterpret_cast<const float4*>(src) + 1);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  f[0] = make_float2(a.x, a.y);
+  f[1] = make_float2(a.z, a.w);
+  f[2] = make_float2(b.x, b.y);
+  f[3] = make_float2(b.z, b.w);
 }
 // 8 weights starting at value `at` (a multiple of 8)
-__device__ __forceinline__ void load_weights(const RopeParams& p, int t, int at, float* f) {
+__device__ __forceinline__ void load_weights(const RopeParams& p, int t, int at, float2* f) {
   if (p.w[t] == nullptr) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = 1.f;
+    for (int i = 0; i < 4; ++i) f[i] = make_float2(1.f, 1.f);
   } else if (p.w_bf16) {
     unpack8(__ldg(reinterpret_cast<const uint4*>(p.w[t]) + at / 8), f);
   } else {
@@ -101,32 +107,35 @@ __device__ __forceinline__ uint4 shfl4(const uint4& v, int lane) {
 }
 
 // What a lane needs of the rotation: per value the cosine and the signed sine that goes with the pair's other value
-// (-sin for the first of a pair, +sin for the second), and in the halves layout the lane of the other value.
+// (-sin for the first of a pair, +sin for the second; cosine 1 and sine 0 behind the rotated values).
 struct Turn {
-  float c[8], s[8];
-  int lane;
-  bool inside;  // this lane's values are rotated
+  float2 c[4], s[4];
 };
-
-// `good` false: the position lies outside the tables; the token's rows become NaN, nothing is read out of bounds.
+// The lane that holds the other values of this lane's pairs (its own where they are in the lane or not rotated).
 template <bool kInterleaved>
-__device__ __forceinline__ void load_turn(const RopeParams& p, const Unit& u, int lane, Turn* tn, bool* good) {
+__device__ __forceinline__ int partner_lane(const RopeParams& p, int lane) {
   const int sub = lane & 15, half_lanes = p.rot >> 4;  // lanes that hold the first half of the rotated values
+  if (kInterleaved || sub >= 2 * half_lanes) return lane;
+  return sub < half_lanes ? lane + half_lanes : lane - half_lanes;
+}
+
+// False: the position lies outside the tables; the token's rows become NaN, nothing is read out of bounds.
+template <bool kInterleaved>
+__device__ __forceinline__ bool load_turn(const RopeParams& p, const Unit& u, int lane, Turn* tn) {
+  const int sub = lane & 15, half_lanes = p.rot >> 4;
   long long pos = u.s;
   if (p.positions != nullptr) {
     const long long at = u.b * p.pos_b + u.s * p.pos_s;
     pos = p.positions_64 ? __ldg(static_cast<const long long*>(p.positions) + at)
                          : static_cast<long long>(__ldg(static_cast<const int*>(p.positions) + at));
   }
-  *good = pos >= 0 && pos < p.n_positions;
-  tn->inside = sub < 2 * half_lanes;
-  tn->lane = lane;
+  const bool good = pos >= 0 && pos < p.n_positions;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    tn->c[i] = 1.f;
-    tn->s[i] = 0.f;
+  for (int i = 0; i < 4; ++i) {
+    tn->c[i] = make_float2(1.f, 1.f);
+    tn->s[i] = make_float2(0.f, 0.f);
   }
-  if (!tn->inside || !*good) return;
+  if (sub >= 2 * half_lanes || !good) return good;
   const long long row = pos * (p.rot >> 1);
   if (kInterleaved) {
     const float4 c = __ldg(reinterpret_cast<const float4*>(p.cos_tab + row) + sub);
@@ -134,19 +143,19 @@ __device__ __forceinline__ void load_turn(const RopeParams& p, const Unit& u, in
     const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      tn->c[2 * i] = tn->c[2 * i + 1] = cc[i];
-      tn->s[2 * i] = -ss[i];
-      tn->s[2 * i + 1] = ss[i];
+      tn->c[i] = make_float2(cc[i], cc[i]);
+      tn->s[i] = make_float2(-ss[i], ss[i]);
     }
   } else {
     const bool first = sub < half_lanes;
     const int at = (first ? sub : sub - half_lanes) * 8;
     load8(p.cos_tab + row + at, tn->c);
     load8(p.sin_tab + row + at, tn->s);
-    tn->lane = first ? lane + half_lanes : lane - half_lanes;
+    const float sign = first ? -1.f : 1.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) tn->s[i] = first ? -tn->s[i] : tn->s[i];
+    for (int i = 0; i < 4; ++i) tn->s[i] = mul2(tn->s[i], make_float2(sign, sign));
   }
+  return good;
 }
 
 // The other value of each of the lane's pairs, as packed words.
@@ -156,122 +165,146 @@ __device__ __forceinline__ uint4 partner(const uint4& v, int lane) {
   return shfl4(v, lane);
 }
 
-template <bool kInterleaved>
-__global__ void __launch_bounds__(kRopeThreads)
-qk_norm_rope_kernel(const __grid_constant__ RopeParams p) {
-  const int lane = threadIdx.x & 31, sub = lane & 15, hw = lane >> 4;
-  const uint32_t step = gridDim.x * kRopeWarps;
-  for (uint32_t un = blockIdx.x * kRopeWarps + (threadIdx.x >> 5); un < static_cast<uint32_t>(p.n_units); un += step) {
-    const Unit u = unit_of(p, un);
-    const RopeStrides sx = p.sx[u.t], so = p.sout[u.t];
+__device__ __forceinline__ float inv_rms(const float2* f, float eps) {
+  float2 a = mul2(f[0], f[0]), b = mul2(f[1], f[1]);
+  a = fma2(f[2], f[2], a);
+  b = fma2(f[3], f[3], b);
+  a = add2(a, b);
+  return rsqrtf(fmaf(sum16(a.x + a.y), 1.f / kRopeDim, eps));
+}
+
+// The warp's units `un`, un + step, ... of tensor t.  Returns the first number beyond them, minus n_units[t]: the warps'
+// numbering goes on through the other tensor's units.
+template <bool kInterleaved, int t>
+__device__ __forceinline__ uint32_t forward_units(const RopeParams& p, uint32_t un, uint32_t step, int lane) {
+  const int sub = lane & 15, hw = lane >> 4, other = partner_lane<kInterleaved>(p, lane);
+  const RopeStrides sx = p.sx[t], so = p.sout[t];
+  const int heads = p.heads[t];
+  float2 w[4], wp[4];
+  if (un < p.n_units[t]) {
+    load_weights(p, t, sub * 8, w);
+    load_weights(p, t, (other & 15) * 8, wp);
+    if (kInterleaved) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wp[i] = make_float2(w[i].y, w[i].x);
+    }
+  }
+  for (; un < p.n_units[t]; un += step) {
+    const Unit u = unit_of(p, t, un);
+    const int h0 = u.h0 + hw;
     // no restrict qualifiers and no non-coherent loads: y may be x itself (a lane's rows are read before written)
-    const uint16_t* src = p.x[u.t] + u.b * sx.b + u.s * sx.s;
+    const uint16_t* src = p.x[t] + u.b * sx.b + u.s * sx.s + h0 * sx.h + sub * 8;
+    uint16_t* dst = p.out[t] + u.b * so.b + u.s * so.s + h0 * so.h + sub * 8;
     uint4 x[kRowsPerLane];
 #pragma unroll
     for (int i = 0; i < kRowsPerLane; ++i) {
-      const int h = u.h0 + 2 * i + hw;
       x[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < p.heads[u.t]) x[i] = *(reinterpret_cast<const uint4*>(src + h * sx.h) + sub);
+      if (h0 + 2 * i < heads) x[i] = *reinterpret_cast<const uint4*>(src + 2 * i * sx.h);
     }
     Turn tn;
-    bool good;
-    load_turn<kInterleaved>(p, u, lane, &tn, &good);
-    float w[8], wp[8];
-    load_weights(p, u.t, sub * 8, w);
-    if (kInterleaved) {
+    const bool good = load_turn<kInterleaved>(p, u, lane, &tn);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) wp[i] = w[i ^ 1];
-    } else {
-      load_weights(p, u.t, (tn.lane & 15) * 8, wp);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {  // y = r (x * w c + x_partner * w_partner s)
-      w[i] *= tn.c[i];
-      wp[i] *= tn.s[i];
+    for (int i = 0; i < 4; ++i) {  // y = r (x * w c + x_partner * w_partner s)
+      tn.c[i] = mul2(tn.c[i], w[i]);
+      tn.s[i] = mul2(tn.s[i], wp[i]);
     }
 #pragma unroll
     for (int i = 0; i < kRowsPerLane; ++i) {
-      const int h = u.h0 + 2 * i + hw;
-      float f[8], g[8], ss = 0.f;
+      float2 f[4], g[4];
       unpack8(x[i], f);
-      unpack8(partner<kInterleaved>(x[i], tn.lane), g);
+      unpack8(partner<kInterleaved>(x[i], other), g);
+      const float r = good ? inv_rms(f, p.eps) : __int_as_float(0x7fffffff);
+      const float2 r2 = make_float2(r, r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
-      const float r = good ? rsqrtf(sum16(ss) * (1.f / kRopeDim) + p.eps) : __int_as_float(0x7fffffff);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = r * fmaf(f[e], w[e], tn.inside ? g[e] * wp[e] : 0.f);
-      if (h < p.heads[u.t])
-        *(reinterpret_cast<uint4*>(p.out[u.t] + u.b * so.b + u.s * so.s + h * so.h) + sub) = pack8(f);
+      for (int e = 0; e < 4; ++e) f[e] = mul2(fma2(f[e], tn.c[e], mul2(g[e], tn.s[e])), r2);
+      if (h0 + 2 * i < heads) *reinterpret_cast<uint4*>(dst + 2 * i * so.h) = pack8(f);
     }
   }
+  return un - p.n_units[t];
+}
+
+template <bool kInterleaved>
+__global__ void __launch_bounds__(kRopeThreads, 3)
+qk_norm_rope_kernel(const __grid_constant__ RopeParams p) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t step = gridDim.x * kRopeWarps;
+  const uint32_t un = blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
+  forward_units<kInterleaved, 1>(p, forward_units<kInterleaved, 0>(p, un, step, lane), step, lane);
+}
+
+// The same for the gradient; dw: the sums of g x r over the lane's values of all its rows.
+template <bool kInterleaved, int t>
+__device__ __forceinline__ uint32_t backward_units(const RopeParams& p, uint32_t un, uint32_t step, int lane, float2* dw) {
+  const int sub = lane & 15, hw = lane >> 4, other = partner_lane<kInterleaved>(p, lane);
+  const RopeStrides sx = p.sx[t], sg = p.sdy[t], so = p.sout[t];
+  const int heads = p.heads[t];
+  float2 w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) dw[i] = make_float2(0.f, 0.f);
+  if (un < p.n_units[t]) load_weights(p, t, sub * 8, w);
+  for (; un < p.n_units[t]; un += step) {
+    const Unit u = unit_of(p, t, un);
+    const int h0 = u.h0 + hw;
+    const uint16_t* src = p.x[t] + u.b * sx.b + u.s * sx.s + h0 * sx.h + sub * 8;
+    const uint16_t* grd = p.dy[t] + u.b * sg.b + u.s * sg.s + h0 * sg.h + sub * 8;
+    uint16_t* dst = p.out[t] + u.b * so.b + u.s * so.s + h0 * so.h + sub * 8;
+    uint4 x[kRowsPerLane], y[kRowsPerLane];
+#pragma unroll
+    for (int i = 0; i < kRowsPerLane; ++i) {
+      x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (h0 + 2 * i < heads) {
+        x[i] = *reinterpret_cast<const uint4*>(src + 2 * i * sx.h);
+        y[i] = *reinterpret_cast<const uint4*>(grd + 2 * i * sg.h);
+      }
+    }
+    Turn tn;
+    const bool good = load_turn<kInterleaved>(p, u, lane, &tn);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tn.s[i] = mul2(tn.s[i], make_float2(-1.f, -1.f));  // the transposed rotation
+#pragma unroll
+    for (int i = 0; i < kRowsPerLane; ++i) {
+      float2 f[4], g[4], q[4];
+      unpack8(x[i], f);
+      unpack8(y[i], g);
+      unpack8(partner<kInterleaved>(y[i], other), q);
+      const float r = good ? inv_rms(f, p.eps) : __int_as_float(0x7fffffff);
+      const float2 r2 = make_float2(r, r);
+      const bool row = h0 + 2 * i < heads;  // rows beyond the last head hold zeros and add nothing to dw
+      float2 gx = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        g[e] = fma2(g[e], tn.c[e], mul2(q[e], tn.s[e]));
+        q[e] = mul2(g[e], w[e]);
+        gx = fma2(q[e], f[e], gx);
+      }
+      const float k = -sum16(gx.x + gx.y) * (1.f / kRopeDim) * r * r;
+      const float2 k2 = make_float2(k, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        dw[e] = fma2(g[e], mul2(f[e], r2), dw[e]);
+        f[e] = mul2(fma2(f[e], k2, q[e]), r2);
+      }
+      if (row) *reinterpret_cast<uint4*>(dst + 2 * i * so.h) = pack8(f);
+    }
+  }
+  return un - p.n_units[t];
 }
 
 // dx, and per CTA the sums of g x r over its rows, added up in a fixed order.
 template <bool kInterleaved>
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, 2)
 qk_norm_rope_bwd_kernel(const __grid_constant__ RopeParams p) {
   __shared__ float sums[kRopeWarps * 2][2][kRopeDim];
   const int lane = threadIdx.x & 31, sub = lane & 15, hw = lane >> 4;
   const uint32_t step = gridDim.x * kRopeWarps;
-  float dw[2][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) dw[0][i] = dw[1][i] = 0.f;
-  for (uint32_t un = blockIdx.x * kRopeWarps + (threadIdx.x >> 5); un < static_cast<uint32_t>(p.n_units); un += step) {
-    const Unit u = unit_of(p, un);
-    const RopeStrides sx = p.sx[u.t], sg = p.sdy[u.t], so = p.sout[u.t];
-    const uint16_t* src = p.x[u.t] + u.b * sx.b + u.s * sx.s;
-    const uint16_t* grd = p.dy[u.t] + u.b * sg.b + u.s * sg.s;
-    uint4 x[kRowsPerLane], y[kRowsPerLane];
-#pragma unroll
-    for (int i = 0; i < kRowsPerLane; ++i) {
-      const int h = u.h0 + 2 * i + hw;
-      x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < p.heads[u.t]) {
-        x[i] = *(reinterpret_cast<const uint4*>(src + h * sx.h) + sub);
-        y[i] = *(reinterpret_cast<const uint4*>(grd + h * sg.h) + sub);
-      }
-    }
-    Turn tn;
-    bool good;
-    load_turn<kInterleaved>(p, u, lane, &tn, &good);
-    float w[8], acc[8];
-    load_weights(p, u.t, sub * 8, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-#pragma unroll
-    for (int i = 0; i < kRowsPerLane; ++i) {
-      const int h = u.h0 + 2 * i + hw;
-      float f[8], g[8], q[8], ss = 0.f, gx = 0.f;
-      unpack8(x[i], f);
-      unpack8(y[i], g);
-      unpack8(partner<kInterleaved>(y[i], tn.lane), q);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {  // the transposed rotation: the sines change sign
-        g[e] = fmaf(g[e], tn.c[e], tn.inside ? -(q[e] * tn.s[e]) : 0.f);
-        ss = fmaf(f[e], f[e], ss);
-        gx = fmaf(g[e] * w[e], f[e], gx);
-      }
-      const float r = good ? rsqrtf(sum16(ss) * (1.f / kRopeDim) + p.eps) : __int_as_float(0x7fffffff);
-      const float k = sum16(gx) * (1.f / kRopeDim) * r * r;
-      const bool row = h < p.heads[u.t];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (row) acc[e] = fmaf(g[e], f[e] * r, acc[e]);
-        f[e] = r * fmaf(-f[e], k, g[e] * w[e]);
-      }
-      if (row) *(reinterpret_cast<uint4*>(p.out[u.t] + u.b * so.b + u.s * so.s + h * so.h) + sub) = pack8(f);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      dw[0][e] += u.t == 0 ? acc[e] : 0.f;
-      dw[1][e] += u.t == 1 ? acc[e] : 0.f;
-    }
-  }
+  float2 dw[2][4];
+  const uint32_t un = backward_units<kInterleaved, 0>(p, blockIdx.x * kRopeWarps + (threadIdx.x >> 5), step, lane, dw[0]);
+  backward_units<kInterleaved, 1>(p, un, step, lane, dw[1]);
   if (p.partials == nullptr) return;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sums[(threadIdx.x >> 5) * 2 + hw][t][sub * 8 + e] = dw[t][e];
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<float2*>(&sums[(threadIdx.x >> 5) * 2 + hw][t][sub * 8 + e * 2]) = dw[t][e];
   }
   __syncthreads();
   const int t = threadIdx.x >> 7, c = threadIdx.x & 127;
