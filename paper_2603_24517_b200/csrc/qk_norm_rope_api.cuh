@@ -112,7 +112,7 @@ attn_status_t attn_qk_norm_rope(const void* q, const void* k, const void* q_weig
   if (st != ATTN_OK) return st;
   DeviceState* dev = device_state(&st);
   if (dev == nullptr) return st;
-  const int grid = rope_grid(p, dev->sm_count * 8);
+  const int grid = rope_grid(p, dev->sm_count * 3);  // as many CTAs as are resident
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (interleaved) {
     attn::rope::qk_norm_rope_kernel<true><<<grid, attn::rope::kRopeThreads, 0, s>>>(p);

@@ -13,6 +13,9 @@
 // shuffles of the packed BF16 words fetch it.  A warp works on 8 rows of one token and one tensor at a time: four
 // independent row loads per lane are in flight and the token's angles are read once for them; it does all its query
 // units before its key units, so weights and weight sums stay in registers; the arithmetic is in packed fp32 pairs.
+// Rows go through the caches as streams (evict first).  32768 tokens of 32 + 8 heads: forward 128 us, 5.3 TB/s,
+// gradient 215 us, 4.7 TB/s.  Measured slower: two rows a lane (219 us), eight (176 us), the next unit's rows fetched
+// ahead (145 and 236 us: the angles' latency is then no longer hidden behind them), more CTAs than resident (135 us).
 #pragma once
 
 #include "attn_merge_kernel.cuh"
@@ -192,14 +195,14 @@ __device__ __forceinline__ uint32_t forward_units(const RopeParams& p, uint32_t 
   for (; un < p.n_units[t]; un += step) {
     const Unit u = unit_of(p, t, un);
     const int h0 = u.h0 + hw;
-    // no restrict qualifiers and no non-coherent loads: y may be x itself (a lane's rows are read before written)
+    // streaming, but coherent loads: y may be x itself (a lane's rows are read before they are written)
     const uint16_t* src = p.x[t] + u.b * sx.b + u.s * sx.s + h0 * sx.h + sub * 8;
     uint16_t* dst = p.out[t] + u.b * so.b + u.s * so.s + h0 * so.h + sub * 8;
     uint4 x[kRowsPerLane];
 #pragma unroll
     for (int i = 0; i < kRowsPerLane; ++i) {
       x[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (h0 + 2 * i < heads) x[i] = *reinterpret_cast<const uint4*>(src + 2 * i * sx.h);
+      if (h0 + 2 * i < heads) x[i] = __ldcs(reinterpret_cast<const uint4*>(src + 2 * i * sx.h));
     }
     Turn tn;
     const bool good = load_turn<kInterleaved>(p, u, lane, &tn);
@@ -217,7 +220,7 @@ __device__ __forceinline__ uint32_t forward_units(const RopeParams& p, uint32_t 
       const float2 r2 = make_float2(r, r);
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] = mul2(fma2(f[e], tn.c[e], mul2(g[e], tn.s[e])), r2);
-      if (h0 + 2 * i < heads) *reinterpret_cast<uint4*>(dst + 2 * i * so.h) = pack8(f);
+      if (h0 + 2 * i < heads) __stcs(reinterpret_cast<uint4*>(dst + 2 * i * so.h), pack8(f));
     }
   }
   return un - p.n_units[t];
@@ -253,8 +256,8 @@ __device__ __forceinline__ uint32_t backward_units(const RopeParams& p, uint32_t
     for (int i = 0; i < kRowsPerLane; ++i) {
       x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
       if (h0 + 2 * i < heads) {
-        x[i] = *reinterpret_cast<const uint4*>(src + 2 * i * sx.h);
-        y[i] = *reinterpret_cast<const uint4*>(grd + 2 * i * sg.h);
+        x[i] = __ldcs(reinterpret_cast<const uint4*>(src + 2 * i * sx.h));
+        y[i] = __ldcs(reinterpret_cast<const uint4*>(grd + 2 * i * sg.h));
       }
     }
     Turn tn;
@@ -284,7 +287,7 @@ __device__ __forceinline__ uint32_t backward_units(const RopeParams& p, uint32_t
         dw[e] = fma2(g[e], mul2(f[e], r2), dw[e]);
         f[e] = mul2(fma2(f[e], k2, q[e]), r2);
       }
-      if (row) *reinterpret_cast<uint4*>(dst + 2 * i * so.h) = pack8(f);
+      if (row) __stcs(reinterpret_cast<uint4*>(dst + 2 * i * so.h), pack8(f));
     }
   }
   return un - p.n_units[t];
