@@ -374,7 +374,8 @@ attn_status_t attn_fwd_splitkv(const void* q, const void* k, const void* v, void
  * state is kept between calls: any number of calls may run at once, each with its own
  * workspace, and calls can be captured into a CUDA graph (after a first call on the device outside
  * capture); replays that may overlap need workspaces of their own.
- * Errors: those of attn_fwd; ATTN_ERR_TOO_LARGE if the workspace is too small.
+ * Errors: those of attn_fwd; ATTN_ERR_TOO_LARGE if the workspace is too small, ATTN_ERR_UNSUPPORTED
+ * also for an output (or the workspace) at the address of an input or of another output.
  */
 size_t attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal); /* 0: sizes attn_bwd refuses */
 attn_status_t attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -419,7 +420,8 @@ attn_status_t attn_bwd_strided(const void* dout, const void* q, const void* k, c
  * Asynchronous on `stream`, one launch, no state; any number of calls may run at once, and after a first call
  * on the device calls can be captured.  Overlaps other than the one named are not allowed.
  * Errors: ATTN_ERR_NULL, ATTN_ERR_SHAPE (a size or stride <= 0, S > n_positions without positions),
- * ATTN_ERR_UNSUPPORTED (D, rot_dim, eps, a type; an output at its input's address with other strides),
+ * ATTN_ERR_UNSUPPORTED (D, rot_dim, eps, a type; 2^30 or more groups of 8 heads of a token; an output at its
+ * input's address with other strides, or at the address of the other tensor's data),
  * ATTN_ERR_ALIGN, ATTN_ERR_CUDA, ATTN_ERR_ARCH.
  */
 attn_status_t attn_qk_norm_rope(const void* q, const void* k, const void* q_weight, const void* k_weight, int weight_type,

@@ -90,6 +90,17 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
     if (reinterpret_cast<uintptr_t>(a) & 15) return ATTN_ERR_ALIGN;
   }
   if (t.dlse != nullptr && (reinterpret_cast<uintptr_t>(t.dlse) & 3)) return ATTN_ERR_ALIGN;
+  // an output in the place of an input or of another output (slices of one buffer have addresses of their own)
+  const void* out[] = {t.dq, t.dk, t.dv, workspace};
+  const void* in[] = {t.dout, t.q, t.k, t.v, t.o, t.lse, t.dlse};
+  for (int i = 0; i < 4; ++i) {
+    for (const void* x : in) {
+      if (out[i] == x) return ATTN_ERR_UNSUPPORTED;
+    }
+    for (int j = 0; j < i; ++j) {
+      if (out[i] == out[j]) return ATTN_ERR_UNSUPPORTED;
+    }
+  }
   if (workspace_bytes < bwd_workspace_bytes(p)) return ATTN_ERR_TOO_LARGE;
   DeviceState* dev = device_state(&st);
   if (dev == nullptr) return st;

@@ -59,7 +59,7 @@ constexpr int kSmemFixed = 0;  // two resident tiles
 constexpr int kSmemRing = 2 * kTileBytes;
 constexpr int kSmemStat = kSmemRing + kRingSlots * kTileBytes;  // [kStatStages][2][128]: -LSE log2(e), -delta
 constexpr int kSmemBwdBars = kSmemStat + kStatStages * 2 * kStatBytes;
-constexpr int kBwdBars = 4 + 2 * kRingSlots + 2 * kStatStages + 2 + 1 + 1 + 2 + 4 + 2 + 2 + 2 + 4 + 2;
+constexpr int kBwdBars = 4 + 2 * kRingSlots + 2 * kStatStages + 2 + 1 + 1 + 2 + 4 + 2 + 1 + 2 + 4 + 2;
 constexpr int kItemInts = 12;
 constexpr int kSmemBwdClc = (kSmemBwdBars + kBwdBars * 8 + 15) / 16 * 16;  // [2] 16-byte answers of the launch queue
 constexpr int kSmemBwdItems = kSmemBwdClc + 32;                            // [2][kItemInts] mailbox of work items
@@ -87,7 +87,7 @@ struct BwdParams {
 enum : int {
   kRoleBwdLoad = 10 << 8, kRoleBwdMma = 11 << 8, kRoleBwdSoftmax = 12 << 8, kRoleBwdStore = 13 << 8, kRoleBwdMma2 = 14 << 8,
   kBarFixed = 1, kBarRingFull = 2, kBarRingEmpty = 3, kBarStat = 4, kBarStatEmpty = 5, kBarS = 6, kBarDp = 7,
-  kBarDpRead = 8, kBarP = 9, kBarDs = 10, kBarAcc = 11, kBarAccEmpty = 12, kBarStageReady = 13, kBarStage = 14, kBarItem = 15,
+  kBarDpRead = 8, kBarP = 9, kBarDs = 10, kBarAcc = 11, kBarAccEmpty = 12, kBarStageFree = 13, kBarStage = 14, kBarItem = 15,
   kBarItemEmpty = 16, kBarClc = 17, kBarFixedEmpty = 18
 };
 
@@ -107,7 +107,7 @@ struct BwdBarriers {
   uint64_t* ds_full;     // [4]  the same for dS; query items alternate two pairs, one for each score buffer
   uint64_t* acc_full;    // commits of both MMA warps: the accumulators are final
   uint64_t* acc_empty;   // softmax (all warps) -> MMA: they are in registers
-  uint64_t* stage_ready; // [2]  loader and store warp -> softmax: a slot of stream A / B is set aside for results
+  uint64_t* stage_free;  // store warp -> softmax: it has come to this item (keeps them from running further ahead)
   uint64_t* stage_full;  // [2]  softmax warps of a half tile -> store warp
   uint64_t* item_full;   // [2]  loader -> everybody else: the next item is in the mailbox
   uint64_t* item_empty;  // [2]
@@ -357,16 +357,13 @@ __device__ __forceinline__ bool load_item(const BwdParams& p, const BwdItem& it,
   mbar_arrive_expect_tx(clc_bar, 16);
   clc_request(clc_buf, clc_bar);
   if (staged(p, it)) {
-    // The slots behind the last tiles take the results.  The `full` barriers go through these positions too, so that
-    // they keep the phases of the `empty` ones.
+    // The slots behind the last tiles take the results: the `full` barriers of these positions tell the softmax warps.
     if (!mbar_wait(&bars.a_empty[ls.a.slot], ls.a.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
     mbar_arrive(&bars.a_full[ls.a.slot]);
-    mbar_arrive(&bars.stage_ready[0]);
     ls.a.next();
     if (it.keys) {
       if (!mbar_wait(&bars.b_empty[ls.b.slot], ls.b.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
       mbar_arrive(&bars.b_full[ls.b.slot]);
-      mbar_arrive(&bars.stage_ready[1]);
       ls.b.next();
     }
   }
@@ -413,12 +410,12 @@ __device__ __forceinline__ void role_store(const BwdParams& p, const BwdBarriers
     if (!staged(p, it)) continue;
     uint8_t* slot_a = smem + kSmemRing + (pos_a % kRingA) * kTileBytes;
     uint8_t* slot_b = smem + kSmemRing + (kRingA + pos_b % kRingB) * kTileBytes;
-    // ready for this item's results: keeps the softmax warps from running two items ahead of this warp
-    mbar_arrive(&bars.stage_ready[0]);
-    if (it.keys) mbar_arrive(&bars.stage_ready[1]);
+    mbar_arrive(bars.stage_free);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      if (!mbar_wait(&bars.stage_full[half], stores & 1, ctx, kRoleBwdStore | kBarStage)) return;
+      // this wait lasts as long as the item: every tile pair (1.5 us or so) adds to its limit
+      const WaitCtx whole{ctx.abort_flag, ctx.status, ctx.limit_ns + static_cast<uint64_t>(it.n) * 20000};
+      if (!mbar_wait(&bars.stage_full[half], stores & 1, whole, kRoleBwdStore | kBarStage)) return;
       if (it.keys) {  // half 0: dV in stream B's slot, half 1: dK in stream A's
         const CUtensorMap* tm = half == 0 ? tm_dv : tm_dk;
         uint8_t* src = half == 0 ? slot_b : slot_a;
@@ -838,10 +835,10 @@ __device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem&
 }
 
 // The results' way out.  Key items: half 0 takes dV, half 1 dK, 64 columns a thread; query items: 32 columns of dQ.
-// `staged_a`, `staged_b`: items that used a slot of stream A / B so far; pos_a, pos_b: ring positions of the slots.
+// pos_a, pos_b: ring positions of the slots set aside; `stored`: items that were staged so far.
 __device__ __forceinline__ bool write_results(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, uint8_t* smem,
                                               WaitCtx ctx, uint32_t tmem_row, int part, int row, int lane, int item,
-                                              uint32_t pos_a, uint32_t pos_b, uint32_t staged_a, uint32_t staged_b) {
+                                              uint32_t pos_a, uint32_t pos_b, uint32_t stored) {
   const int half = part / (kParts / 2);
   const int n32 = it.keys ? 2 : 1;  // 32-column pieces of this thread
   const int col0 = it.keys ? (part % (kParts / 2)) * 64 : part * 32;
@@ -880,8 +877,9 @@ __device__ __forceinline__ bool write_results(const BwdParams& p, const BwdItem&
   __syncwarp();
   if (lane == 0) mbar_arrive(bars.acc_empty);
   if (!out_bf16) return true;
-  ok = mbar_wait(&bars.stage_ready[0], staged_a & 1, ctx, kRoleBwdSoftmax | kBarStageReady) &&
-       (!it.keys || mbar_wait(&bars.stage_ready[1], staged_b & 1, ctx, kRoleBwdSoftmax | kBarStageReady));
+  ok = mbar_wait(bars.stage_free, stored & 1, ctx, kRoleBwdSoftmax | kBarStageFree) &&
+       mbar_wait(&bars.a_full[pos_a % kRingA], (pos_a / kRingA) & 1, ctx, kRoleBwdSoftmax | kBarRingFull) &&
+       (!it.keys || mbar_wait(&bars.b_full[pos_b % kRingB], (pos_b / kRingB) & 1, ctx, kRoleBwdSoftmax | kBarRingFull));
   if (!__all_sync(0xffffffffu, ok)) return false;
   uint8_t* slot_a = smem + kSmemRing + (pos_a % kRingA) * kTileBytes;
   uint8_t* slot_b = smem + kSmemRing + (kRingA + pos_b % kRingB) * kTileBytes;
@@ -899,7 +897,7 @@ __device__ __forceinline__ bool write_results(const BwdParams& p, const BwdItem&
 __device__ __forceinline__ void role_softmax(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem, const volatile int* box,
                                              WaitCtx ctx, uint32_t tmem, int part, int row, int lane) {
   const uint32_t tmem_row = tmem + (static_cast<uint32_t>(row & ~31) << 16);
-  uint32_t pos_a = 0, pos_b = 0, staged_a = 0, staged_b = 0;
+  uint32_t pos_a = 0, pos_b = 0, stored = 0;
   Phases ph;
   BwdItem it;
   for (int k = 0; next_item(bars, box, k, ctx, kRoleBwdSoftmax, true, lane == 0, it); ++k) {
@@ -910,14 +908,11 @@ __device__ __forceinline__ void role_softmax(const BwdParams& p, const BwdBarrie
     }
     pos_a += it.n;
     pos_b += it.n;
-    if (!ok || !write_results(p, it, bars, smem, ctx, tmem_row, part, row, lane, k, pos_a, pos_b, staged_a, staged_b)) return;
+    if (!ok || !write_results(p, it, bars, smem, ctx, tmem_row, part, row, lane, k, pos_a, pos_b, stored)) return;
     if (staged(p, it)) {
       ++pos_a;
-      ++staged_a;
-      if (it.keys) {
-        ++pos_b;
-        ++staged_b;
-      }
+      ++stored;
+      if (it.keys) ++pos_b;
     }
   }
 }
@@ -945,8 +940,8 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   bars.ds_full = bars.p_full + 2;
   bars.acc_full = bars.ds_full + 4;
   bars.acc_empty = bars.acc_full + 1;
-  bars.stage_ready = bars.acc_empty + 1;
-  bars.stage_full = bars.stage_ready + 2;
+  bars.stage_free = bars.acc_empty + 1;
+  bars.stage_full = bars.stage_free + 1;
   bars.item_full = bars.stage_full + 2;
   bars.item_empty = bars.item_full + 2;
   bars.clc_full = bars.item_empty + 2;
@@ -970,6 +965,7 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
     mbar_init(bars.dp_full, 1);
     mbar_init(bars.dp_read, kSoftmaxWarps);
+    mbar_init(bars.stage_free, 1);
     mbar_init(bars.acc_full, 2);
     mbar_init(bars.acc_empty, kSoftmaxWarps);
     for (int i = 0; i < 2; ++i) {
@@ -981,7 +977,6 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       mbar_init(&bars.p_full[i], kSoftmaxWarps);
       mbar_init(&bars.ds_full[i], kSoftmaxWarps);
       mbar_init(&bars.ds_full[2 + i], kSoftmaxWarps);
-      mbar_init(&bars.stage_ready[i], 2);
       mbar_init(&bars.stage_full[i], kSoftmaxWarps / 2);
       mbar_init(&bars.item_full[i], 1);
       mbar_init(&bars.item_empty[i], kItemConsumers);

@@ -82,6 +82,8 @@ attn_status_t rope_output(void* out, const long long* strides, const RopeParams&
   const attn_status_t st = rope_strides(strides, p.S, p.heads[t], &dst->sout[t]);
   if (st != ATTN_OK) return st;
   dst->out[t] = static_cast<uint16_t*>(out);
+  const int other = 1 - t;  // in the place of the other tensor's data
+  if (out == p.x[other] || out == p.dy[other] || out == dst->out[other]) return ATTN_ERR_UNSUPPORTED;
   if ((out == p.x[t] && !same_strides(dst->sout[t], p.sx[t])) || (out == p.dy[t] && !same_strides(dst->sout[t], p.sdy[t])))
     return ATTN_ERR_UNSUPPORTED;
   return ATTN_OK;

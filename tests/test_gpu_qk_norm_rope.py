@@ -81,3 +81,174 @@ def test_forward_and_backward_match_definition(B, S, Hq, Hkv, rot, inter, weight
         check_forward(y[i], x, w[i], cos, sin, pos, 1e-5, inter)
         check_backward(got[i], got[2 + i], dy, x, w[i], cos, sin, pos, 1e-5, inter)
         assert (got[2 + i] is None) == (w[i] is None)
+
+
+def _contiguous_run(q, k, dq, dk, w, cos, sin, pos, **named):
+    y = lib.qk_norm_rope(q.contiguous(), k.contiguous(), *w, cos, sin, positions=pos, **named)
+    g = lib.qk_norm_rope_backward(dq.contiguous(), dk.contiguous(), q.contiguous(), k.contiguous(), *w, cos, sin,
+                                  positions=pos, **named)
+    return y, g
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_strided_views_in_place_and_into_a_cache(inter):
+    B, S, Hq, Hkv = 2, 51, 6, 2
+    _, _, dq, dk, w, cos, sin, pos = make(B, S, Hq, Hkv, 64, 300, torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    qkv = torch.randn(B, S, Hq + 2 * Hkv, 128, generator=g, device="cuda").bfloat16()
+    q, k = qkv[:, :, :Hq], qkv[:, :, Hq:Hq + Hkv]
+    want, wantg = _contiguous_run(q, k, dq, dk, w, cos, sin, pos, interleaved=inter)
+    assert all(torch.equal(a, b) for a, b in zip(lib.qk_norm_rope(q, k, *w, cos, sin, positions=pos, interleaved=inter), want))
+    # the gradient, written over the incoming gradient
+    g1, g2 = dq.clone(), dk.clone()
+    dwq, dwk = torch.empty(128, device="cuda"), torch.empty(128, device="cuda")
+    lib.attn_qk_norm_rope_bwd(g1, g2, q, k, *w, cos, sin, g1, g2, dwq, dwk, positions=pos, interleaved=inter)
+    assert all(torch.equal(a, b) for a, b in zip((g1, g2, dwq, dwk), wantg))
+    # keys into the rows 10 .. 60 of a [B, H, rows, D] cache, the rest of which stays as it is
+    cache = torch.full((B, Hkv, 100, 128), 5.0, device="cuda", dtype=torch.bfloat16)
+    q_out = torch.empty(B, S, Hq, 128, device="cuda", dtype=torch.bfloat16)
+    lib.attn_qk_norm_rope(q, k, *w, cos, sin, q_out, cache.transpose(1, 2)[:, 10:10 + S], positions=pos, interleaved=inter)
+    assert torch.equal(cache.transpose(1, 2)[:, 10:10 + S], want[1])
+    assert bool((cache[:, :, :10] == 5.0).all()) and bool((cache[:, :, 10 + S:] == 5.0).all())
+    # in place, on the slices of the packed projection; the values (v) between them stay
+    v = qkv[:, :, Hq + Hkv:].clone()
+    lib.attn_qk_norm_rope(q, k, *w, cos, sin, q, k, positions=pos, interleaved=inter)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(qkv[:, :, Hq + Hkv:], v)
+
+
+def test_position_types_strides_and_shared_positions():
+    B, S = 3, 20
+    q, k, dq, dk, w, cos, sin, pos = make(B, S, 4, 2, 128, 500, torch.bfloat16)
+    want, wantg = _contiguous_run(q, k, dq, dk, w, cos, sin, pos)
+    wide = torch.zeros(B, 2 * S, device="cuda", dtype=torch.int64)
+    wide[:, ::2] = pos
+    for p in (pos.int(), wide[:, ::2], pos.t().contiguous().t()):
+        got, gotg = _contiguous_run(q, k, dq, dk, w, cos, sin, p)
+        assert all(torch.equal(a, b) for a, b in zip(got + gotg, want + wantg))
+    row = pos[0].contiguous()
+    want, wantg = _contiguous_run(q, k, dq, dk, w, cos, sin, row.expand(B, S).contiguous())
+    for p in (row, row.expand(B, S), row.int()):
+        got, gotg = _contiguous_run(q, k, dq, dk, w, cos, sin, p)
+        assert all(torch.equal(a, b) for a, b in zip(got + gotg, want + wantg))
+
+
+def test_positions_outside_the_tables_make_nan_rows():
+    q, k, dq, dk, w, cos, sin, pos = make(2, 9, 3, 2, 64, 50, torch.float32)
+    bad = pos.clone()
+    bad[0, 3], bad[1, 8], bad[1, 0] = 50, -1, 1 << 40
+    out = torch.zeros(2, 9, dtype=torch.bool, device="cuda")
+    out[0, 3] = out[1, 8] = out[1, 0] = True
+    y = lib.qk_norm_rope(q, k, *w, cos, sin, positions=bad)
+    good = lib.qk_norm_rope(q, k, *w, cos, sin, positions=pos)
+    g = lib.qk_norm_rope_backward(dq, dk, q, k, *w, cos, sin, positions=bad)
+    for a, b in zip(y, good):
+        assert bool(torch.isnan(a[out]).all()) and torch.equal(a[~out], b[~out])
+    assert bool(torch.isnan(g[0][out]).all()) and bool(torch.isfinite(g[0][~out]).all())
+    assert bool(torch.isnan(g[2]).all())
+
+
+def test_infinities_and_nan_stay_in_their_rows():
+    q, k, dq, dk, w, cos, sin, pos = make(1, 12, 3, 3, 128, 50, torch.float32)
+    want = lib.qk_norm_rope(q, k, *w, cos, sin, positions=pos)
+    q2 = q.clone()
+    q2[0, 5, 1, 7], q2[0, 2, 0, 100] = float("inf"), float("nan")
+    y = lib.qk_norm_rope(q2, k, *w, cos, sin, positions=pos)
+    keep = torch.ones(1, 12, 3, dtype=torch.bool, device="cuda")
+    keep[0, 5, 1] = keep[0, 2, 0] = False
+    assert torch.equal(y[0][keep], want[0][keep]) and torch.equal(y[1], want[1])
+    assert not bool(torch.isfinite(y[0][~keep]).all())
+
+
+def test_rows_of_zeros_and_of_large_and_small_values():
+    q, k, dq, dk, w, cos, sin, pos = make(1, 40, 4, 4, 128, 50, torch.float32)
+    q[:, 0] = 0
+    q[:, 1] *= 1e15
+    q[:, 2] *= 1e-3
+    y = lib.qk_norm_rope(q, k, *w, cos, sin, positions=pos)
+    g = lib.qk_norm_rope_backward(dq, dk, q, k, *w, cos, sin, positions=pos)
+    assert bool((y[0][:, 0] == 0).all())
+    check_forward(y[0], q, w[0], cos, sin, pos, 1e-6, False)
+    check_backward(g[0], g[2], dq, q, w[0], cos, sin, pos, 1e-6, False)
+
+
+def test_same_bits_on_any_stream_and_in_a_graph():
+    q, k, dq, dk, w, cos, sin, pos = make(4, 300, 8, 2, 128, 1000, torch.bfloat16)
+    want, wantg = _contiguous_run(q, k, dq, dk, w, cos, sin, pos)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = _contiguous_run(q, k, dq, dk, w, cos, sin, pos)
+    got2 = _contiguous_run(q, k, dq, dk, w, cos, sin, pos)
+    torch.cuda.synchronize()
+    for a, b in ((got, want), (got2, want)):
+        assert all(torch.equal(x, y) for x, y in zip(a[0] + a[1], want + wantg))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cap = _contiguous_run(q, k, dq, dk, w, cos, sin, pos)
+    q.copy_(q.flip(0))
+    pos.copy_(pos.flip(0))
+    want, wantg = _contiguous_run(q, k, dq, dk, w, cos, sin, pos)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(cap[0] + cap[1], want + wantg))
+
+
+def test_refusals():
+    q, k, dq, dk, w, cos, sin, pos = make(1, 8, 2, 2, 128, 16, torch.float32)
+    out = (torch.empty_like(q), torch.empty_like(k))
+    ok = lambda *a, **n: lib.attn_qk_norm_rope_status(*a, **n)  # noqa: E731
+    assert ok(q, k, *w, cos, sin, *out) == 0
+    assert ok(q, k, *w, cos, sin, *out, eps=0.0) == 3
+    assert ok(q, k, *w, cos[:, :4].contiguous(), sin[:, :4].contiguous(), *out) == 3        # rot_dim 8
+    assert ok(q, k, *w, cos[:7].contiguous(), sin[:7].contiguous(), *out) == 2              # 8 tokens, 7 positions
+    assert ok(q, k, *w, cos, sin, out[0], out[0]) == 3                                      # one output for both
+    assert ok(q, k, *w, cos, sin, k, out[1]) == 3                                           # queries over keys
+    turned = torch.as_strided(q, q.shape, (q.stride(0), 128, 8 * 128, 1))
+    assert ok(q, k, *w, cos, sin, turned, out[1]) == 3                                      # in place, other strides
+    for bad in (dict(positions=pos.float()), dict(positions=pos[:, :4])):
+        with pytest.raises(ValueError):
+            ok(q, k, *w, cos, sin, *out, **bad)
+    with pytest.raises(ValueError):
+        ok(q.float(), k, *w, cos, sin, *out)
+    with pytest.raises(ValueError):
+        ok(q, k, w[0], w[1].bfloat16(), cos, sin, *out)
+    with pytest.raises(ValueError):
+        ok(q, k[:, :, :, :64], *w, cos, sin, *out)
+    with pytest.raises(ValueError):
+        ok(q, k, *w, cos.double(), sin, *out)
+    torch.cuda.synchronize()
+
+
+def test_layer_step_with_attention():
+    """Projection slices -> norm and rotation -> attention -> its gradient -> the gradient of norm and rotation, queued
+    without a wait in between, in a graph too; every stage against its definition on what the stage before left."""
+    B, S, Hq, Hkv = 2, 270, 8, 2
+    g = torch.Generator(device="cuda").manual_seed(8)
+    qkv = torch.randn(B, S, Hq + 2 * Hkv, 128, generator=g, device="cuda").bfloat16()
+    dout = torch.randn(B, S, Hq, 128, generator=g, device="cuda").bfloat16()
+    _, _, _, _, w, cos, sin, _ = make(B, S, Hq, Hkv, 128, 400, torch.float32)
+    pos = torch.arange(S, device="cuda") + torch.tensor([[0], [100]], device="cuda")
+
+    def step():
+        q, k, v = qkv[:, :, :Hq], qkv[:, :, Hq:Hq + Hkv], qkv[:, :, Hq + Hkv:].contiguous()
+        qr, kr = lib.qk_norm_rope(q, k, *w, cos, sin, positions=pos)
+        o, lse = lib.attention_forward(qr, kr, v, causal=True)
+        dqr, dkr, dv = lib.attention_backward(dout, qr, kr, v, o, lse, causal=True)
+        dq, dk, dwq, dwk = lib.qk_norm_rope_backward(dqr, dkr, q, k, *w, cos, sin, positions=pos)
+        return q, k, v, qr, kr, o, lse, dqr, dkr, dv, dq, dk, dwq, dwk
+
+    from test_gpu_backward import SCALE, check
+    first = step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first[3:], captured[3:]))
+    q, k, v, qr, kr, o, lse, dqr, dkr, dv, dq, dk, dwq, dwk = first
+    for x, y, dy, dx, dw, wt in ((q, qr, dqr, dq, dwq, w[0]), (k, kr, dkr, dk, dwk, w[1])):
+        check_forward(y, x, wt, cos, sin, pos, 1e-6, False)
+        check_backward(dx, dw, dy, x, wt, cos, sin, pos, 1e-6, False)
+    check((dqr, dkr, dv), dout, qr, kr, v, o, lse, True, SCALE)
