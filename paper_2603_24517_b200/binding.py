@@ -367,13 +367,14 @@ def _on_device(dev, fn, *args):
         return fn(*args)
 
 
-def _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, strided):
+def _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, strided, made_here=False):
+    """``made_here``: dq, dk, dv are new contiguous tensors of the right kind."""
     tensors = (dout, q, k, v, o, dq, dk, dv)
     dev = q.device
     shape, kv_shape = q.shape, k.shape
     if len(shape) != 4 or len(kv_shape) != 4 or dev.type != "cuda":
         raise ValueError("q and k must be 4-D cuda tensors [B, S, H, D]")
-    for i, t in enumerate(tensors):
+    for i, t in enumerate(tensors[:5] if made_here else tensors):
         if t.dtype is not torch.bfloat16 or t.device != dev or t.shape != (kv_shape if i in (2, 3, 6, 7) else shape) \
                 or not (t.is_contiguous() or strided and t.stride(3) == 1):
             name = ("dout", "q", "k", "v", "o", "dq", "dk", "dv")[i]
@@ -481,7 +482,12 @@ def _strides3_or_none(t):
 def attn_qk_norm_rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6,
                              interleaved: bool = False, stream=None) -> int:
     """Calls ``attn_qk_norm_rope`` on CUDA tensors and returns its raw status code."""
-    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, ((q_out, k_out),))
+    return _rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved, stream,
+                        ((q_out, k_out),))
+
+
+def _rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved, stream, check):
+    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, check)
     return _on_device(q.device, load_library().attn_qk_norm_rope, *lead, q_out.data_ptr(), k_out.data_ptr(), *sizes,
                       int(bool(interleaved)), float(eps), *[_strides3_or_none(t) for t in (q, k, q_out, k_out)],
                       _raw_stream(q.device, stream))
@@ -505,9 +511,17 @@ def attn_qk_norm_rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, 
                                  positions=None, eps: float = 1e-6, interleaved: bool = False, workspace=None,
                                  stream=None) -> int:
     """Calls ``attn_qk_norm_rope_bwd``; ``workspace`` is a contiguous cuda tensor (allocated here when None)."""
-    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, ((dq_out, dk_out), (dq, dk)))
+    return _rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions, eps,
+                            interleaved, workspace, stream, False)
+
+
+def _rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions, eps,
+                     interleaved, workspace, stream, made_here):
+    """``made_here``: the outputs are new contiguous tensors of the right kind."""
+    lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions,
+                             ((dq_out, dk_out),) if made_here else ((dq_out, dk_out), (dq, dk)))
     dev = q.device
-    for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
+    for name, t in () if made_here else (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
         if t is not None and (t.dtype is not torch.float32 or t.shape != q.shape[3:] or not t.is_contiguous()
                               or t.device != dev):
             raise ValueError(f"{name} must be a contiguous float32 tensor [D] on q's device")
@@ -604,7 +618,7 @@ def _ordered(grad):
 
 
 def _new_like(t):
-    return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float | None = None, dlse=None):
@@ -616,10 +630,10 @@ def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float
         scale = 1.0 / math.sqrt(q.shape[-1])
     dout = _ordered(dout)
     dq, dk, dv = _new_like(q), _new_like(k), _new_like(v)
-    if all(t.is_contiguous() for t in (dout, q, k, v, o)):
-        attn_bwd(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse)
-    else:
-        attn_bwd_strided(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse)
+    strided = not (dout.is_contiguous() and q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous())
+    st = _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, None, None, strided, True)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_bwd_strided" if strided else "attn_bwd")
     return dq, dk, dv
 
 
@@ -627,7 +641,9 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: float 
     """Convenience wrapper: the normed and rotated queries and keys as new contiguous tensors (see ``attn_qk_norm_rope``),
     ready for ``attention_forward``."""
     q_out, k_out = _new_like(q), _new_like(k)
-    attn_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved)
+    st = _rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved, None, ())
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_qk_norm_rope")
     return q_out, k_out
 
 
@@ -638,6 +654,8 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, po
     dq, dk = _new_like(q), _new_like(k)
     dq_weight = None if q_weight is None else torch.empty_like(q_weight, dtype=torch.float32)
     dk_weight = None if k_weight is None else torch.empty_like(k_weight, dtype=torch.float32)
-    attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions, eps,
-                          interleaved)
+    st = _rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions, eps,
+                          interleaved, None, None, True)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_qk_norm_rope_bwd")
     return dq, dk, dq_weight, dk_weight
