@@ -20,6 +20,36 @@ size_t bwd_part_bytes(int splits, int B, int H, int tiles) {
   return splits > 1 ? static_cast<size_t>(splits) * B * H * tiles * attn::kTile * attn::kHeadDim * sizeof(float) : 0;
 }
 
+// Estimate of a launch, in SM clocks: the kind of item with the longer streams goes first, the other fills up behind it.
+// Measured on B200: a tile pair takes 2650 (key) or 2450 (query) clocks, the start and end of an item 3500, an fp32
+// partial result 8000 / 4000 more, and the join a launch and the reading of the partial sums.
+struct BwdCost {
+  double total, longest, average;
+  int queries_first;
+};
+BwdCost bwd_cost(const BwdParams& p, long long key_tiles, long long key_len, int ks, long long qry_tiles, long long qry_len, int qs,
+                 double seen) {
+  const double key_item = 3500 + (ks > 1 ? 8000 : 0), qry_item = 3500 + (qs > 1 ? 4000 : 0);
+  const double key_max = key_item + 2650.0 * key_len / ks, qry_max = qry_item + 2450.0 * qry_len / qs;
+  const double key_avg = key_item + 2650.0 * seen * key_len / ks, qry_avg = qry_item + 2450.0 * seen * qry_len / qs;
+  const double n_key = static_cast<double>(key_tiles) * ks, n_qry = static_cast<double>(qry_tiles) * qs;
+  BwdCost c;
+  c.queries_first = qry_max > key_max ? 1 : 0;
+  c.average = (n_key * key_avg + n_qry * qry_avg) / kPlanSms;
+  c.longest = std::fmax(key_max, qry_max);
+  const double n1 = c.queries_first ? n_qry : n_key, avg1 = c.queries_first ? qry_avg : key_avg;
+  const double max2 = std::fmin(key_max, qry_max), avg2 = c.queries_first ? key_avg : qry_avg;
+  const double first = n1 <= kPlanSms ? c.longest : std::ceil(n1 / kPlanSms) * avg1;  // the first kind by itself
+  const double second = std::floor(n1 / kPlanSms) * avg1 + max2;                      // the first free SM takes one of the second
+  const double tail = n_key + n_qry > kPlanSms ? 0.5 * avg2 : 0.0;
+  c.total = std::fmax(c.average + tail, std::fmax(first, second));
+  if (ks > 1 || qs > 1) {
+    const double parts = (ks > 1 ? 2 * n_key : 0) + (qs > 1 ? n_qry : 0);  // tiles of 64 KB
+    c.total += 7000 + parts * 65536 / 3500;
+  }
+  return c;
+}
+
 // Problem geometry and launch order (no device access).  False if the launch grid cannot hold the items.
 bool fill_bwd_plan(BwdParams* p, int B, int Hq, int Hkv, int Sq, int Sk, int causal) {
   std::memset(p, 0, sizeof(*p));
@@ -29,29 +59,38 @@ bool fill_bwd_plan(BwdParams* p, int B, int Hq, int Hkv, int Sq, int Sk, int cau
   p->off = Sk - Sq;
   p->n_qt = (Sq + attn::kTile - 1) / attn::kTile;
   p->n_kt = (Sk + attn::kTile - 1) / attn::kTile;
-  // Parts of an item's stream.  An item's cost is counted in products (a key tile pair has four, a query tile pair three);
-  // where the longest item exceeds a quarter of what an SM has to do on average, it is cut, so that no SM works on
-  // alone at the end, but not below 24 products: a part costs its partial sums and a third launch adds them up.
-  // (One head, 64 rows on 9000 keys, and the like; 512 rows on 65536 keys, 16 heads: 1.50 -> SPLIT_E.)
   const long long units = static_cast<long long>(B) * Hkv;
   const long long key_tiles = units * p->n_kt, qry_tiles = units * p->group * p->n_qt;
-  const long long key_cost = 4LL * p->group * p->n_qt, qry_cost = 3LL * p->n_kt;  // of the longest items
-  const double total = (static_cast<double>(key_tiles) * key_cost + static_cast<double>(qry_tiles) * qry_cost) *
-                       (causal && Sk >= Sq ? 1.0 - 0.5 * Sq / Sk : causal ? 0.5 * Sk / Sq : 1.0);
-  const double part = std::fmax(total / kPlanSms / 4, 24.0);
-  auto parts = [part](long long cost) {
-    const double n = std::ceil(static_cast<double>(cost) / part);
-    return n < 1 ? 1 : n > kMaxParts ? kMaxParts : static_cast<int>(n);
-  };
-  p->key_splits = parts(key_cost);
-  p->qry_splits = parts(qry_cost);
+  const long long key_len = static_cast<long long>(p->group) * p->n_qt, qry_len = p->n_kt;  // longest streams
+  const double seen = !causal ? 1.0 : Sk >= Sq ? 1.0 - 0.5 * Sq / Sk : 0.5 * Sk / Sq;       // share of visible tile pairs
+  const BwdCost one = bwd_cost(*p, key_tiles, key_len, 1, qry_tiles, qry_len, 1, seen);
+  p->key_splits = p->qry_splits = 1;
+  p->queries_first = one.queries_first;
+  // With many more items than SMs the order alone balances them; else the streams may be worth cutting.
+  const bool few = one.longest > 0.25 * one.average;
+  if (few) {
+    double best = one.total;
+    for (int ks = 1; ks <= kMaxParts; ks *= 2) {
+      for (int qs = 1; qs <= kMaxParts; qs *= 2) {
+        if ((ks > 1 && key_len < 2 * ks) || (qs > 1 && qry_len < 2 * qs)) continue;
+        const BwdCost c = bwd_cost(*p, key_tiles, key_len, ks, qry_tiles, qry_len, qs, seen);
+        if (c.total < best) {
+          best = c.total;
+          p->key_splits = ks;
+          p->qry_splits = qs;
+          p->queries_first = c.queries_first;
+        }
+      }
+    }
+  }
   const long long items = key_tiles * p->key_splits + qry_tiles * p->qry_splits;
   if (items > 0x3fffffffLL) return false;
   p->n_items = static_cast<int>(items);
-  // as many units in a run as keep their q, dout, k and v within 64 MB of L2
-  long long run = (64LL << 20) / (512LL * (static_cast<long long>(Sq) * p->group + Sk));
+  // as many units in a run as keep their q, dout, k and v within 64 MB of L2; all where the order has to balance the
+  // SMs (512 rows on 65536 keys, 16 heads: 1.17 -> 0.81 ms)
+  long long run = few ? units : (64LL << 20) / (512LL * (static_cast<long long>(Sq) * p->group + Sk));
   if (run < 1) run = 1;
-  if (run > 64) run = 64;
+  if (!few && run > 64) run = 64;
   if (run > units) run = units;
   // runs of nearly equal size, so that the last one is not a small remainder
   const int runs = static_cast<int>((units + run - 1) / run);

@@ -76,6 +76,7 @@ struct BwdParams {
   int key_splits, qry_splits;  // parts of a key / query item's stream
   int n_items;            // B * Hkv * (n_kt * key_splits + group * n_qt * qry_splits)
   int run, run_extra;     // launch order, see decode_item
+  int queries_first;      // in a run: 1: query items before key items
   float scale, scale_log2;
   const float* neg_lse2;  // [B * Hq][n_qt * 128], -LSE * log2(e); -inf in rows that see no key or do not exist
   const float* neg_delta; // same layout, -delta, 0 in those rows
@@ -161,7 +162,7 @@ struct BwdItem {
 
 // Launch order.  A unit is a (batch, KV head) with its query heads: n_kt key tiles and group * n_qt query tiles, each
 // in its number of parts.  Units are taken in runs of `run` (the first `run_extra` runs) or run - 1 units whose
-// tensors together fit L2; in a run come first all key items, then all query items.  Under the causal mask each kind
+// tensors together fit L2; in a run come first all items of the kind with the longer streams, then all of the other.  Under the causal mask each kind
 // goes rank by rank over the run's units, longest ranks (early keys, late rows) first, so that a run ends on
 // short items.  Without it items are alike and go unit by unit: neighbours then read the same stream at about the same
 // time, which the L2 answers with fewer requests (8 heads of 16384: 3 % over a mixed order).
@@ -183,7 +184,10 @@ __host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int 
     g = p.run - 1;
   }
   BwdItem it;
-  it.keys = rem < g * unit_keys ? 1 : 0;
+  const int run_keys = g * unit_keys, run_queries = g * (per_unit - unit_keys);
+  it.keys = (p.queries_first ? rem >= run_queries : rem < run_keys) ? 1 : 0;
+  if (p.queries_first && it.keys) rem -= run_queries;
+  if (!p.queries_first && !it.keys) rem -= run_keys;
   int splits;
   if (it.keys) {
     splits = p.key_splits;
@@ -200,7 +204,6 @@ __host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int 
     it.n = it.per_head * p.group;
   } else {
     splits = p.qry_splits;
-    rem -= g * unit_keys;
     const int wide = g * p.group, per_head = p.n_qt * splits;
     const int x = p.causal ? rem % wide : rem / per_head;  // which head of the run
     const int rank = p.causal ? rem / wide : rem - x * per_head;
@@ -692,11 +695,11 @@ __device__ __forceinline__ void store_part32(float* dst, const uint32_t* o, floa
 }
 
 // Both softmax roles: P = exp2(S * scale log2(e) - LSE log2(e)) on pairs of columns; of every eight pairs
-// kPolyPairs take the polynomial on the FMA pipe, the others the special-function unit.  Key items wait for P with the
-// tensor pipe idle behind them, so both units share the work; query items have the next scores ready and want the fewest
-// instructions (8 heads of 16384, each kind by itself, 1 / 2 / 4 of eight: key items 1545 / 1509 / 1489 us, query
-// items 1142 / 1191 / 1205 us).
-constexpr int kKeyPolyPairs = 4, kQryPolyPairs = 1;
+// kPolyPairs take the polynomial on the FMA pipe, the others the special-function unit.  Key items have the tensor pipe
+// waiting for P, so the two units share the work; query items have the next scores ready and want the fewest
+// instructions (8 heads of 16384, warm GPU, key / query pairs of eight: 0 / 0 3060 us, 1 / 1 2990, 2 / 1 2950, 4 / 1 2980,
+// 2 / 2 2960).
+constexpr int kKeyPolyPairs = 2, kQryPolyPairs = 1;
 #define ATTN_F(r, i) __uint_as_float((r)[(i)])
 
 // exp2 of kCols score columns in place, given per pair of columns the pair of -LSE log2(e).  Columns outside
