@@ -6,11 +6,8 @@ namespace {
 
 using attn::bwd::BwdParams;
 
-// Bytes of one row-statistics array: fp32 [B * Hq][ceil(Sq / 128) * 128].
-size_t bwd_stat_bytes(int B, int Hq, int Sq) {
-  const size_t padded = (static_cast<size_t>(Sq) + attn::kTile - 1) / attn::kTile * attn::kTile;
-  return static_cast<size_t>(B) * Hq * padded * sizeof(float);
-}
+// Bytes of one row-statistics array: fp32 [B * Hq][n_qt * 128].
+size_t bwd_stat_bytes(const BwdParams& p) { return static_cast<size_t>(p.B) * p.Hq * p.n_qt * attn::kTile * sizeof(float); }
 
 constexpr int kPlanSms = 148;  // the plan, and with it the workspace, does not depend on the device
 constexpr int kMaxParts = 32;
@@ -58,11 +55,25 @@ bool fill_bwd_plan(BwdParams* p, int B, int Hq, int Hkv, int Sq, int Sk, int cau
   p->causal = causal ? 1 : 0;
   p->off = Sk - Sq;
   p->n_qt = (Sq + attn::kTile - 1) / attn::kTile;
+  // Pack a group's heads into the rows of a tile where that saves an eighth of the query tiles or more (one row of 4
+  // heads for each of 8 key heads, 4 sequences of 32768 keys: 0.73 -> 0.40 ms).
+  const int group = p->group;
+  if (group >= 2 && group <= 16 && (group & (group - 1)) == 0 && static_cast<long long>(Sq) * group <= 0x3fffff00) {
+    const int packed = (Sq * group + attn::kTile - 1) / attn::kTile;
+    if (8LL * packed <= 7LL * group * p->n_qt) {
+      while ((1 << p->pack_log2) < group) ++p->pack_log2;
+      p->Hq = Hkv;
+      p->group = 1;
+      p->Sq = Sq = Sq * group;
+      p->n_qt = packed;
+    }
+  }
   p->n_kt = (Sk + attn::kTile - 1) / attn::kTile;
   const long long units = static_cast<long long>(B) * Hkv;
   const long long key_tiles = units * p->n_kt, qry_tiles = units * p->group * p->n_qt;
   const long long key_len = static_cast<long long>(p->group) * p->n_qt, qry_len = p->n_kt;  // longest streams
-  const double seen = !causal ? 1.0 : Sk >= Sq ? 1.0 - 0.5 * Sq / Sk : 0.5 * Sk / Sq;       // share of visible tile pairs
+  const double rows = Sq >> p->pack_log2;
+  const double seen = !causal ? 1.0 : Sk >= rows ? 1.0 - 0.5 * rows / Sk : 0.5 * Sk / rows;  // share of visible tile pairs
   const BwdCost one = bwd_cost(*p, key_tiles, key_len, 1, qry_tiles, qry_len, 1, seen);
   p->key_splits = p->qry_splits = 1;
   p->queries_first = one.queries_first;
@@ -102,7 +113,7 @@ bool fill_bwd_plan(BwdParams* p, int B, int Hq, int Hkv, int Sq, int Sk, int cau
 
 // Row statistics, then the partial sums of dq, dk and dv; every part is a multiple of 512 bytes.
 size_t bwd_workspace_bytes(const BwdParams& p) {
-  return 2 * bwd_stat_bytes(p.B, p.Hq, p.Sq) + bwd_part_bytes(p.qry_splits, p.B, p.Hq, p.n_qt) +
+  return 2 * bwd_stat_bytes(p) + bwd_part_bytes(p.qry_splits, p.B, p.Hq, p.n_qt) +
          2 * bwd_part_bytes(p.key_splits, p.B, p.Hkv, p.n_kt);
 }
 
@@ -145,17 +156,17 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
   if (dev == nullptr) return st;
 
   CUtensorMap tm_q, tm_k, tm_v, tm_do, tm_dq, tm_dk, tm_dv;
-  if (!make_tensor_map(&tm_q, t.q, B, Sq, Hq, ts.q) || !make_tensor_map(&tm_k, t.k, B, Sk, Hkv, ts.k) ||
-      !make_tensor_map(&tm_v, t.v, B, Sk, Hkv, ts.v) || !make_tensor_map(&tm_do, t.dout, B, Sq, Hq, ts.dout) ||
-      !make_tensor_map(&tm_dq, t.dq, B, Sq, Hq, ts.dq) || !make_tensor_map(&tm_dk, t.dk, B, Sk, Hkv, ts.dk) ||
+  if (!make_tensor_map(&tm_q, t.q, B, Sq, Hq, ts.q, p.pack_log2) || !make_tensor_map(&tm_k, t.k, B, Sk, Hkv, ts.k) ||
+      !make_tensor_map(&tm_v, t.v, B, Sk, Hkv, ts.v) || !make_tensor_map(&tm_do, t.dout, B, Sq, Hq, ts.dout, p.pack_log2) ||
+      !make_tensor_map(&tm_dq, t.dq, B, Sq, Hq, ts.dq, p.pack_log2) || !make_tensor_map(&tm_dk, t.dk, B, Sk, Hkv, ts.dk) ||
       !make_tensor_map(&tm_dv, t.dv, B, Sk, Hkv, ts.dv))
     return ATTN_ERR_CUDA;
 
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float* neg_lse2 = reinterpret_cast<float*>(ws);
-  float* neg_delta = reinterpret_cast<float*>(ws + bwd_stat_bytes(B, Hq, Sq));
-  const size_t dq_bytes = bwd_part_bytes(p.qry_splits, B, Hq, p.n_qt), dk_bytes = bwd_part_bytes(p.key_splits, B, Hkv, p.n_kt);
-  p.dq_part = reinterpret_cast<float*>(ws + 2 * bwd_stat_bytes(B, Hq, Sq));
+  float* neg_delta = reinterpret_cast<float*>(ws + bwd_stat_bytes(p));
+  const size_t dq_bytes = bwd_part_bytes(p.qry_splits, B, p.Hq, p.n_qt), dk_bytes = bwd_part_bytes(p.key_splits, B, Hkv, p.n_kt);
+  p.dq_part = reinterpret_cast<float*>(ws + 2 * bwd_stat_bytes(p));
   p.dk_part = p.dq_part + dq_bytes / sizeof(float);
   p.dv_part = p.dk_part + dk_bytes / sizeof(float);
   p.scale = scale;
@@ -164,7 +175,7 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
   p.neg_delta = neg_delta;
   p.status = dev->status;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int padded = p.n_qt * attn::kTile;
+  const int padded = (p.n_qt * attn::kTile) >> p.pack_log2;  // query rows of a head, to whole tiles
   int heads_log2 = 0;  // heads of a block: up to 8, so that 256 rows are 32 positions or more
   while (heads_log2 < 3 && (2 << heads_log2) <= Hq) ++heads_log2;
   const int prep_rows = attn::bwd::kPrepThreads >> heads_log2;
@@ -174,7 +185,7 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
   attn::bwd::attn_bwd_prep_kernel<<<static_cast<int>(prep_blocks < cap ? prep_blocks : cap), attn::bwd::kPrepThreads, 0, s>>>(
       static_cast<const uint16_t*>(t.o), static_cast<const uint16_t*>(t.dout),
       attn::bwd::RowStrides{ts.o.b, ts.o.s, ts.o.h}, attn::bwd::RowStrides{ts.dout.b, ts.dout.s, ts.dout.h}, t.lse, t.dlse,
-      neg_lse2, neg_delta, Hq, Sq, padded, heads_log2, static_cast<int>(prep_blocks));
+      neg_lse2, neg_delta, Hq, Sq, padded, p.pack_log2, heads_log2, static_cast<int>(prep_blocks));
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
   const int grid = p.n_items;
   attn::bwd::attn_bwd_kernel<<<grid, attn::bwd::kBwdThreads, attn::bwd::kSmemBwdBytes, s>>>(tm_q, tm_k, tm_v, tm_do, tm_dq,
@@ -184,7 +195,7 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
   attn::bwd::JoinParams jp = {};
   int n_out = 0;
   long long most = 0;
-  auto join = [&](const float* part, void* out, Strides3 st3, int splits, int H, int S, int tiles) {
+  auto join = [&](const float* part, void* out, Strides3 st3, int splits, int H, int S, int tiles, int pack_log2) {
     const long long padded_rows = static_cast<long long>(tiles) * attn::kTile;
     attn::bwd::JoinOut& j = jp.o[n_out++];
     j.part = part;
@@ -194,14 +205,15 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
     j.H = H;
     j.S = S;
     j.padded = tiles * attn::kTile;
+    j.pack_log2 = pack_log2;
     j.n_rows = static_cast<long long>(B) * H * S;
     j.part_stride = static_cast<long long>(B) * H * padded_rows * attn::kHeadDim;
     if (j.n_rows > most) most = j.n_rows;
   };
-  if (p.qry_splits > 1) join(p.dq_part, t.dq, ts.dq, p.qry_splits, Hq, Sq, p.n_qt);
+  if (p.qry_splits > 1) join(p.dq_part, t.dq, ts.dq, p.qry_splits, p.Hq, p.Sq, p.n_qt, p.pack_log2);
   if (p.key_splits > 1) {
-    join(p.dk_part, t.dk, ts.dk, p.key_splits, Hkv, Sk, p.n_kt);
-    join(p.dv_part, t.dv, ts.dv, p.key_splits, Hkv, Sk, p.n_kt);
+    join(p.dk_part, t.dk, ts.dk, p.key_splits, Hkv, Sk, p.n_kt, 0);
+    join(p.dv_part, t.dv, ts.dv, p.key_splits, Hkv, Sk, p.n_kt, 0);
   }
   long long join_blocks = (most + attn::bwd::kJoinThreads / 32 - 1) / (attn::bwd::kJoinThreads / 32);
   if (join_blocks > cap) join_blocks = cap;

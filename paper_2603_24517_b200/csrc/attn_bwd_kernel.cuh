@@ -67,11 +67,16 @@ constexpr int kSmemBwdMisc = kSmemBwdItems + 2 * kItemInts * 4;            // te
 constexpr int kSmemBwdBytes = kSmemBwdMisc + 8;
 static_assert(kSmemBwdBytes <= 232448, "shared memory budget of one CTA");
 
+// Packed query tiles (short query sequences of GQA groups): a tile's 128 rows hold 128 >> pack_log2 query rows of all
+// 1 << pack_log2 heads of a group, row r being query row r >> pack_log2 of head r % group.  To everything but the masks
+// and the addresses of query tiles that is a problem with Hq = Hkv and Sq << pack_log2 rows; Hq, group, Sq and
+// n_qt below describe it as such.
 struct BwdParams {
   int B, Hq, Hkv, Sq, Sk;
   int group;              // Hq / Hkv
+  int pack_log2;
   int causal;
-  int off;                // Sk - Sq: key j is visible to row i iff j <= i + off
+  int off;                // keys minus query rows: key j is visible to query row i (a tile's row >> pack_log2) iff j <= i + off
   int n_qt, n_kt;         // 128-row query tiles, 128-key tiles
   int key_splits, qry_splits;  // parts of a key / query item's stream
   int n_items;            // B * Hkv * (n_kt * key_splits + group * n_qt * qry_splits)
@@ -198,7 +203,7 @@ __host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int 
     it.b = unit / p.Hkv;
     it.h = unit - it.b * p.Hkv;
     it.row0 = kt * kTile;
-    const int first_row = p.causal && it.row0 > p.off ? it.row0 - p.off : 0;  // < Sq: the last row sees every key
+    const int first_row = p.causal && it.row0 > p.off ? (it.row0 - p.off) << p.pack_log2 : 0;  // < Sq: the last row sees all
     it.first = first_row / kTile;
     it.per_head = p.n_qt - it.first;
     it.n = it.per_head * p.group;
@@ -217,7 +222,7 @@ __host__ __device__ __forceinline__ BwdItem decode_item(const BwdParams& p, int 
     it.per_head = p.n_kt;
     if (p.causal) {
       const int row_end = it.row0 + kTile < p.Sq ? it.row0 + kTile : p.Sq;
-      const int last_key = row_end - 1 + p.off;
+      const int last_key = ((row_end - 1) >> p.pack_log2) + p.off;
       const int need = last_key < 0 ? 0 : last_key / kTile + 1;
       if (need < it.per_head) it.per_head = need;
     }
@@ -315,6 +320,8 @@ __device__ __forceinline__ bool load_item(const BwdParams& p, const BwdItem& it,
                                           void* clc_buf, uint64_t* clc_bar) {
   uint8_t* ring_a = smem + kSmemRing;
   uint8_t* ring_b = ring_a + kRingA * kTileBytes;
+  // query tiles are addressed by the first of their heads and their first query row
+  const int fixed_pack = it.keys ? 0 : p.pack_log2, stream_pack = it.keys ? p.pack_log2 : 0;
   const int head0 = it.keys ? it.h * p.group : it.h / p.group;
   int head = head0 + it.t0 / (it.per_head > 0 ? it.per_head : 1);
   int tile = it.first + it.t0 - (head - head0) * it.per_head;
@@ -324,17 +331,20 @@ __device__ __forceinline__ bool load_item(const BwdParams& p, const BwdItem& it,
       if (i == 0) {  // the resident tile of the product that comes first
         if (!mbar_wait(&bars.fixed_empty[x], (ls.fixed & 1) ^ 1, ctx, kRoleBwdLoad | kBarFixedEmpty)) return false;
         mbar_arrive_expect_tx(&bars.fixed_full[x], kTileBytes);
-        load_tile(smem + kSmemFixed + x * kTileBytes, x == 0 ? fixed_a : fixed_b, &bars.fixed_full[x], it.h, it.row0, it.b);
+        load_tile(smem + kSmemFixed + x * kTileBytes, x == 0 ? fixed_a : fixed_b, &bars.fixed_full[x], it.h << fixed_pack,
+                  it.row0 >> fixed_pack, it.b);
       }
       if (x == 0) {
         if (!mbar_wait(&bars.a_empty[ls.a.slot], ls.a.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
         mbar_arrive_expect_tx(&bars.a_full[ls.a.slot], kTileBytes);
-        load_tile(ring_a + ls.a.slot * kTileBytes, stream_a, &bars.a_full[ls.a.slot], head, tile * kTile, it.b);
+        load_tile(ring_a + ls.a.slot * kTileBytes, stream_a, &bars.a_full[ls.a.slot], head << stream_pack,
+                  (tile * kTile) >> stream_pack, it.b);
         ls.a.next();
       } else {
         if (!mbar_wait(&bars.b_empty[ls.b.slot], ls.b.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
         mbar_arrive_expect_tx(&bars.b_full[ls.b.slot], kTileBytes);
-        load_tile(ring_b + ls.b.slot * kTileBytes, stream_b, &bars.b_full[ls.b.slot], head, tile * kTile, it.b);
+        load_tile(ring_b + ls.b.slot * kTileBytes, stream_b, &bars.b_full[ls.b.slot], head << stream_pack,
+                  (tile * kTile) >> stream_pack, it.b);
         ls.b.next();
       }
     }
@@ -425,7 +435,7 @@ __device__ __forceinline__ void role_store(const BwdParams& p, const BwdBarriers
         tma_store_4d(tm, src, 0, it.h, it.row0, it.b);
         tma_store_4d(tm, src + kHalfBytes, 64, it.h, it.row0, it.b);
       } else {
-        tma_store_4d(tm_dq, slot_a + half * kHalfBytes, half * 64, it.h, it.row0, it.b);
+        tma_store_4d(tm_dq, slot_a + half * kHalfBytes, half * 64, it.h << p.pack_log2, it.row0 >> p.pack_log2, it.b);
       }
       tma_store_commit();
     }
@@ -761,8 +771,8 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
     tmem_ld_x16(t_s + 64, x[1]);
     tmem_wait_ld();
     // the key is visible to the queries of columns `seen_from` on
-    const int seen_from = it.row0 + row - p.off - tile * kTile - part * kCols;
-    const bool masked = p.causal && it.row0 + kTile - 1 > tile * kTile + p.off;  // the same for the whole CTA
+    const int seen_from = (max(0, it.row0 + row - p.off) << p.pack_log2) - tile * kTile - part * kCols;
+    const bool masked = p.causal && it.row0 + kTile - 1 > ((tile * kTile) >> p.pack_log2) + p.off;  // the same for the whole CTA
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       exp_row<kKeyPolyPairs>(x[h], c2, [&](int e) { return *reinterpret_cast<const float2*>(nl + h * 64 + e); }, masked,
@@ -799,8 +809,8 @@ __device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem&
   const size_t at = (static_cast<size_t>(it.b) * p.Hq + it.h) * p.n_qt * kTile + it.row0 + row;
   const float nl = __ldg(p.neg_lse2 + at), ndl = __ldg(p.neg_delta + at);
   const float2 nl2 = make_float2(nl, nl), ndl2 = make_float2(ndl, ndl);
-  const int row_limit = p.causal ? min(p.Sk, it.row0 + row + p.off + 1) : p.Sk;   // keys this row may see
-  const int tile_clear = p.causal ? min(p.Sk, it.row0 + p.off + 1) : p.Sk;        // keys every row of the tile sees
+  const int row_limit = p.causal ? min(p.Sk, ((it.row0 + row) >> p.pack_log2) + p.off + 1) : p.Sk;  // keys this row may see
+  const int tile_clear = p.causal ? min(p.Sk, (it.row0 >> p.pack_log2) + p.off + 1) : p.Sk;          // keys every row of the tile sees
   for (int j = 0; j < it.n; ++j) {
     const int x_buf = j & 1;
     bool ok = mbar_wait(&bars.s_full[x_buf], (ph.s >> x_buf) & 1, ctx, kRoleBwdSoftmax | kBarS);
@@ -1043,7 +1053,7 @@ __device__ __forceinline__ float dot2_bf16(uint32_t a, uint32_t b, float acc) {
 __global__ void __launch_bounds__(kPrepThreads)
 attn_bwd_prep_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict__ dout, RowStrides so, RowStrides sdo,
                      const float* __restrict__ lse, const float* __restrict__ dlse, float* __restrict__ neg_lse2,
-                     float* __restrict__ neg_delta, int Hq, int Sq, int padded, int heads_log2, int n_blocks) {
+                     float* __restrict__ neg_delta, int Hq, int Sq, int padded, int pack_log2, int heads_log2, int n_blocks) {
   __shared__ float sums[kPrepThreads];  // [sequence][head]
   const int sub = threadIdx.x & 15;
   const int heads = 1 << heads_log2, rows = kPrepThreads >> heads_log2;  // heads and sequence positions of a block
@@ -1076,6 +1086,7 @@ attn_bwd_prep_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict_
       }
     }
     __syncthreads();
+    // `padded`: positions of a head, to whole tiles
     const int h = (hb << heads_log2) + threadIdx.x / rows, s = sb * rows + threadIdx.x % rows;
     if (h < Hq && s < padded) {
       float l = -INFINITY, dl = 0.f;
@@ -1084,7 +1095,8 @@ attn_bwd_prep_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict_
         l = __ldg(lse + at);
         if (dlse != nullptr) dl = __ldg(dlse + at);
       }
-      const long long at = (b * Hq + h) * padded + s;
+      // [B][Hq][padded], or packed [B][Hkv][padded][group]
+      const long long at = ((((b * Hq + h) >> pack_log2) * padded + s) << pack_log2) + (h & ((1 << pack_log2) - 1));
       const bool none = l == -INFINITY;  // the row sees no key, or does not exist: P = exp2(-inf) = 0
       neg_lse2[at] = none ? -INFINITY : -l * 1.4426950408889634f;
       neg_delta[at] = none ? 0.f : dl - sums[(threadIdx.x % rows) * heads + threadIdx.x / rows];
@@ -1101,7 +1113,7 @@ struct JoinOut {
   const float* part;  // [splits][B][H][padded][128]
   uint16_t* out;
   RowStrides strides;
-  int splits, H, S, padded;
+  int splits, H, S, padded, pack_log2;
   long long n_rows, part_stride;
 };
 struct JoinParams {
@@ -1121,7 +1133,8 @@ __global__ void __launch_bounds__(kJoinThreads) attn_bwd_join_kernel(const __gri
       const float4 x = __ldg(reinterpret_cast<const float4*>(src + i * j.part_stride));
       v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
     }
-    *reinterpret_cast<uint2*>(j.out + b * j.strides.b + s * j.strides.s + h * j.strides.h + lane * 4) =
+    const long long head = (static_cast<long long>(h) << j.pack_log2) + (s & ((1 << j.pack_log2) - 1));
+    *reinterpret_cast<uint2*>(j.out + b * j.strides.b + (s >> j.pack_log2) * j.strides.s + head * j.strides.h + lane * 4) =
         make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
   }
 }

@@ -90,6 +90,33 @@ def test_split_streams_match_definition(B, Hq, Hkv, Sq, Sk, causal):
         assert bool((got[0][:, :Sq - Sk] == 0).all())
 
 
+# short query sequences of GQA groups: the group's heads share the rows of a query tile
+PACKED_SHAPES = [(1, 8, 1, 1, 1, False), (2, 8, 2, 1, 700, True), (1, 16, 1, 8, 300, True), (1, 16, 1, 9, 300, False),
+                 (1, 4, 2, 33, 129, True), (2, 6, 3, 65, 64, True), (1, 8, 1, 130, 130, True), (1, 32, 4, 5, 2500, True),
+                 (1, 16, 2, 40, 12, True), (1, 64, 4, 3, 20000, True), (1, 4, 1, 1000, 1000, True), (3, 8, 2, 300, 130, True)]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,Sq,Sk,causal", PACKED_SHAPES)
+def test_short_sequences_of_head_groups(B, Hq, Hkv, Sq, Sk, causal):
+    dout, q, k, v = make(B, Hq, Hkv, Sq, Sk)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    dlse = torch.randn(B, Hq, Sq, generator=g, device="cuda")
+    dead = max(0, Sq - Sk) if causal else 0
+    o, lse, got = grads(dout, q, k, v, causal, dlse=dlse)
+    dlse[:, :, :dead] = 0
+    check(got, dout, q, k, v, o, lse, causal, SCALE, dlse)
+    assert bool((got[0][:, :dead] == 0).all())
+    # the same on [B, H, S, D] buffers, into slices of larger ones
+    big = torch.full((B, Hq + 1, Sq + 3, 128), 7.0, device="cuda", dtype=torch.bfloat16)
+    view = lambda t: t.transpose(1, 2).contiguous().transpose(1, 2)  # noqa: E731
+    dq, dk, dv = big[:, :Hq, :Sq].transpose(1, 2), torch.empty_like(k), torch.empty_like(v)
+    o2, lse2 = lib.attention_forward(q, k, v, causal=causal, scale=SCALE)
+    lib.attn_bwd_strided(view(dout), view(q), view(k), view(v), view(o2), lse2, dq, dk, dv, causal, SCALE, dlse=dlse)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((dq, dk, dv), got))
+    assert bool((big[:, Hq] == 7.0).all()) and bool((big[:, :, Sq:] == 7.0).all())
+
+
 @pytest.mark.parametrize("causal", [False, True])
 def test_many_items_per_cta(causal):
     """More items than SMs, of both kinds: CTAs go from item to item, from one kind to the other and back."""
