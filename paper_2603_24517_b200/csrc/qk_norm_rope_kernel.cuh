@@ -14,8 +14,10 @@
 // independent row loads per lane are in flight and the token's angles are read once for them; it does all its query
 // units before its key units, so weights and weight sums stay in registers; the arithmetic is in packed fp32 pairs.
 // Rows go through the caches as streams (evict first).  32768 tokens of 32 + 8 heads: forward 128 us, 5.3 TB/s,
-// gradient 215 us, 4.7 TB/s.  Measured slower: two rows a lane (219 us), eight (176 us), the next unit's rows fetched
-// ahead (145 and 236 us: the angles' latency is then no longer hidden behind them), more CTAs than resident (135 us).
+// gradient 199 us, 5.1 TB/s (the same accesses without the arithmetic: 111 and 196 us).  Measured slower: two rows a
+// lane (219 us), eight (176 us), the next unit's rows fetched ahead into registers (145 and 236 us) or shared memory (175
+// and 224 us: a warp's own chain of sums is what takes the time, and both cost resident warps or instructions),
+// more CTAs than resident (135 us); in the forward pass, rows in pairs with shared sums (131 us).
 #pragma once
 
 #include "attn_merge_kernel.cuh"
@@ -104,6 +106,18 @@ __device__ __forceinline__ float sum16(float v) {  // over the half warp
   for (int m = 8; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
   return v;
 }
+// Four sums at once: the lanes first share out the values among themselves, so nine shuffles do what sixteen would, in a
+// chain hardly longer than one sum's.
+__device__ __forceinline__ void sum16x4(float* v, int lane) {
+  const bool b8 = lane & 8, b4 = lane & 4;
+  const float a0 = (b8 ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, b8 ? v[0] : v[2], 8);
+  const float a1 = (b8 ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, b8 ? v[1] : v[3], 8);
+  float c = (b4 ? a1 : a0) + __shfl_xor_sync(0xffffffffu, b4 ? a0 : a1, 4);
+  c += __shfl_xor_sync(0xffffffffu, c, 2);
+  c += __shfl_xor_sync(0xffffffffu, c, 1);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xffffffffu, c, (lane & 16) + (i >> 1) * 8 + (i & 1) * 4);
+}
 __device__ __forceinline__ uint4 shfl4(const uint4& v, int lane) {
   return make_uint4(__shfl_sync(0xffffffffu, v.x, lane), __shfl_sync(0xffffffffu, v.y, lane),
                     __shfl_sync(0xffffffffu, v.z, lane), __shfl_sync(0xffffffffu, v.w, lane));
@@ -168,12 +182,16 @@ __device__ __forceinline__ uint4 partner(const uint4& v, int lane) {
   return shfl4(v, lane);
 }
 
-__device__ __forceinline__ float inv_rms(const float2* f, float eps) {
+__device__ __forceinline__ float sum_squares(const float2* f) {  // of the lane's values
   float2 a = mul2(f[0], f[0]), b = mul2(f[1], f[1]);
   a = fma2(f[2], f[2], a);
   b = fma2(f[3], f[3], b);
   a = add2(a, b);
-  return rsqrtf(fmaf(sum16(a.x + a.y), 1.f / kRopeDim, eps));
+  return a.x + a.y;
+}
+// 1 / sqrt(mean + eps) of a row, NaN for a token whose position lies outside the tables
+__device__ __forceinline__ float inv_rms(float squares, float eps, bool good) {
+  return good ? rsqrtf(fmaf(squares, 1.f / kRopeDim, eps)) : __int_as_float(0x7fffffff);
 }
 
 // The warp's units `un`, un + step, ... of tensor t.  Returns the first number beyond them, minus n_units[t]: the warps'
@@ -216,7 +234,7 @@ __device__ __forceinline__ uint32_t forward_units(const RopeParams& p, uint32_t 
       float2 f[4], g[4];
       unpack8(x[i], f);
       unpack8(partner<kInterleaved>(x[i], other), g);
-      const float r = good ? inv_rms(f, p.eps) : __int_as_float(0x7fffffff);
+      const float r = inv_rms(sum16(sum_squares(f)), p.eps, good);
       const float2 r2 = make_float2(r, r);
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] = mul2(fma2(f[e], tn.c[e], mul2(g[e], tn.s[e])), r2);
@@ -265,29 +283,38 @@ __device__ __forceinline__ uint32_t backward_units(const RopeParams& p, uint32_t
 #pragma unroll
     for (int i = 0; i < 4; ++i) tn.s[i] = mul2(tn.s[i], make_float2(-1.f, -1.f));  // the transposed rotation
 #pragma unroll
-    for (int i = 0; i < kRowsPerLane; ++i) {
-      float2 f[4], g[4], q[4];
-      unpack8(x[i], f);
-      unpack8(y[i], g);
-      unpack8(partner<kInterleaved>(y[i], other), q);
-      const float r = good ? inv_rms(f, p.eps) : __int_as_float(0x7fffffff);
-      const float2 r2 = make_float2(r, r);
-      const bool row = h0 + 2 * i < heads;  // rows beyond the last head hold zeros and add nothing to dw
-      float2 gx = make_float2(0.f, 0.f);
+    for (int i = 0; i < kRowsPerLane; i += 2) {  // two rows at a time
+      float2 g[2][4];
+      float sums[4];  // squares, and g w x, of both rows
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        g[e] = fma2(g[e], tn.c[e], mul2(q[e], tn.s[e]));
-        q[e] = mul2(g[e], w[e]);
-        gx = fma2(q[e], f[e], gx);
-      }
-      const float k = -sum16(gx.x + gx.y) * (1.f / kRopeDim) * r * r;
-      const float2 k2 = make_float2(k, k);
+      for (int v = 0; v < 2; ++v) {
+        float2 f[4], q[4];
+        unpack8(x[i + v], f);
+        unpack8(y[i + v], g[v]);
+        unpack8(partner<kInterleaved>(y[i + v], other), q);
+        float2 gx = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        dw[e] = fma2(g[e], mul2(f[e], r2), dw[e]);
-        f[e] = mul2(fma2(f[e], k2, q[e]), r2);
+        for (int e = 0; e < 4; ++e) {
+          g[v][e] = fma2(g[v][e], tn.c[e], mul2(q[e], tn.s[e]));
+          gx = fma2(mul2(g[v][e], w[e]), f[e], gx);
+        }
+        sums[v] = sum_squares(f);
+        sums[2 + v] = gx.x + gx.y;
       }
-      if (row) __stcs(reinterpret_cast<uint4*>(dst + 2 * i * so.h), pack8(f));
+      sum16x4(sums, lane);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {  // rows beyond the last head hold zeros and add nothing to dw
+        float2 f[4];
+        unpack8(x[i + v], f);
+        const float r = inv_rms(sums[v], p.eps, good), k = -sums[2 + v] * (1.f / kRopeDim) * r * r;
+        const float2 r2 = make_float2(r, r), k2 = make_float2(k, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          dw[e] = fma2(g[v][e], mul2(f[e], r2), dw[e]);
+          f[e] = mul2(fma2(f[e], k2, mul2(g[v][e], w[e])), r2);
+        }
+        if (h0 + 2 * (i + v) < heads) __stcs(reinterpret_cast<uint4*>(dst + 2 * (i + v) * so.h), pack8(f));
+      }
     }
   }
   return un - p.n_units[t];
