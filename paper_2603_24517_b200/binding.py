@@ -359,6 +359,15 @@ def _raw_stream(dev, stream):
     return torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream
 
 
+def _new_workspace(like, n_bytes: int, stream):
+    """A workspace that is dropped when the call returns.  It belongs to torch's current stream; where the call goes to
+    another one, the allocator must not hand it out again before that stream is done with it."""
+    workspace = like.new_empty(n_bytes, dtype=torch.uint8)
+    if stream is not None:
+        workspace.record_stream(torch.cuda.ExternalStream(stream, device=like.device))
+    return workspace
+
+
 def _on_device(dev, fn, *args):
     """fn(*args) with ``dev`` current; switching devices costs more than a call that need not."""
     if torch.cuda.current_device() == dev.index:
@@ -393,7 +402,7 @@ def _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspac
     lib = load_library()
     causal = int(bool(causal))
     if workspace is None:
-        workspace = q.new_empty(max(lib.attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, causal), 16), dtype=torch.uint8)
+        workspace = _new_workspace(q, max(lib.attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, causal), 16), stream)
     elif not workspace.is_contiguous() or workspace.device != dev:
         raise ValueError("workspace must be a contiguous tensor on q's device")
     args = (dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
@@ -528,7 +537,7 @@ def _rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk,
     lib = load_library()
     if workspace is None:
         if dq_weight is not None or dk_weight is not None:
-            workspace = q.new_empty(lib.attn_qk_norm_rope_bwd_workspace_bytes(), dtype=torch.uint8)
+            workspace = _new_workspace(q, lib.attn_qk_norm_rope_bwd_workspace_bytes(), stream)
     elif not workspace.is_contiguous() or workspace.device != dev:
         raise ValueError("workspace must be a contiguous tensor on q's device")
     return _on_device(dev, lib.attn_qk_norm_rope_bwd, dq_out.data_ptr(), dk_out.data_ptr(), *lead, dq.data_ptr(),

@@ -284,3 +284,21 @@ def test_workspace_and_refusals():
     with pytest.raises(lib.AttnError):
         lib.attention_backward(dout, q, k, v, o, lse, scale=float("nan"))
     torch.cuda.synchronize()
+
+
+def test_explicit_stream_keeps_its_workspace():
+    """A call on a stream that is not torch's current one, with a workspace made in the call: memory that the current
+    stream allocates and overwrites meanwhile is not that workspace."""
+    dout, q, k, v = make(1, 4, 4, 300, 9000)
+    o, lse, want = grads(dout, q, k, v, False)
+    need = lib.attn_bwd_workspace_bytes(1, 4, 4, 300, 9000, 128, False)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [torch.empty_like(t) for t in (q, k, v)]
+        torch.cuda.synchronize()
+        lib.attn_bwd(dout, q, k, v, o, lse, *got, False, SCALE, stream=s.cuda_stream)
+        for _ in range(4):
+            torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
