@@ -751,6 +751,16 @@ __device__ __forceinline__ void hand_over(uint32_t taddr, const uint32_t* pk, ui
   if (lane == 0) mbar_arrive(bar);
 }
 
+// kCols row statistics, 16 bytes at a time (every thread of a warp reads the same ones).
+__device__ __forceinline__ void load_stats(const float* src, float2* f) {
+#pragma unroll
+  for (int i = 0; i < kCols / 4; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(src + 4 * i);
+    f[2 * i] = make_float2(v.x, v.y);
+    f[2 * i + 1] = make_float2(v.z, v.w);
+  }
+}
+
 // One softmax thread of a key item: row `row` of the tile (a key), columns part * kCols + [0, kCols) of each half.
 __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars,
                                             const uint8_t* smem, WaitCtx ctx, uint32_t tmem_row, int part, int row, int lane,
@@ -775,8 +785,9 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
     const bool masked = p.causal && it.row0 + kTile - 1 > ((tile * kTile) >> p.pack_log2) + p.off;  // the same for the whole CTA
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      exp_row<kKeyPolyPairs>(x[h], c2, [&](int e) { return *reinterpret_cast<const float2*>(nl + h * 64 + e); }, masked,
-                             seen_from - h * 64, kCols);
+      float2 st2[kCols / 2];
+      load_stats(nl + h * 64, st2);
+      exp_row<kKeyPolyPairs>(x[h], c2, [&](int e) { return st2[e / 2]; }, masked, seen_from - h * 64, kCols);
 #pragma unroll
       for (int e = 0; e < kCols / 2; ++e) pk[e] = pack_bf16x2(ATTN_F(x[h], 2 * e), ATTN_F(x[h], 2 * e + 1));
       hand_over(t_s + h * 64, pk, &bars.p_full[h], lane);
@@ -789,7 +800,9 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
     tmem_wait_ld();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {  // over this thread's own columns, which are in registers
-      ds_row(x[h], d[h], [&](int e) { return *reinterpret_cast<const float2*>(neg_delta + h * 64 + e); }, pk);
+      float2 st2[kCols / 2];
+      load_stats(neg_delta + h * 64, st2);
+      ds_row(x[h], d[h], [&](int e) { return st2[e / 2]; }, pk);
       hand_over(t_dp + h * 64, pk, &bars.ds_full[h], lane);
     }
     if (lane == 0) mbar_arrive(&bars.stat_empty[st]);
