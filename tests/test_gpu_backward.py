@@ -302,3 +302,25 @@ def test_explicit_stream_keeps_its_workspace():
             torch.full((need,), 255, dtype=torch.uint8, device="cuda")
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_offsets_beyond_32_bits():
+    """Batch entries 2^31 elements apart (4 GB), for every tensor: the same bits as on contiguous copies."""
+    B, S, Hq, Hkv = 2, 150, 2, 1
+    dout, q, k, v = make(B, Hq, Hkv, S, S, seed=5)
+    o, lse, want = grads(dout, q, k, v, True)
+    far = 1 << 31
+    buf = torch.empty(far + 16 * S * Hq * 128, device="cuda", dtype=torch.bfloat16)
+    at = 0
+
+    def view(t):
+        nonlocal at
+        out = buf.as_strided(t.shape, (far, *t.stride()[1:]), at)
+        at += t[0].numel()
+        return out.copy_(t)
+
+    ins = [view(t) for t in (dout, q, k, v, o)]
+    outs = [view(torch.zeros_like(t)) for t in (q, k, v)]
+    lib.attn_bwd_strided(*ins, lse, *outs, True, SCALE)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))

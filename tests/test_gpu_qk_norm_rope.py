@@ -194,6 +194,37 @@ def test_same_bits_on_any_stream_and_in_a_graph():
     assert all(torch.equal(x, y) for x, y in zip(cap[0] + cap[1], want + wantg))
 
 
+def test_offsets_beyond_32_bits():
+    """Rows, positions and table rows more than 2^31 elements into their tensors."""
+    B, S, Hq, Hkv = 2, 9, 3, 2
+    q, k, dq, dk, w, _, _, _ = make(B, S, Hq, Hkv, 128, 16, torch.float32)
+    far = 1 << 31
+    table = far // 64 + 100
+    cos, sin = torch.zeros(table, 64, device="cuda"), torch.zeros(table, 64, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(6)
+    angle = torch.randn(50, 64, generator=g, device="cuda")
+    cos[-50:], sin[-50:] = angle.cos(), angle.sin()
+    near = torch.randint(0, 50, (B, S), generator=g, device="cuda")
+    want, wantg = _contiguous_run(q, k, dq, dk, w, angle.cos().contiguous(), angle.sin().contiguous(), near)
+    buf = torch.empty(far + 64 * S * Hq * 128, device="cuda", dtype=torch.bfloat16)
+    at = 0
+
+    def view(t):
+        nonlocal at
+        out = buf.as_strided(t.shape, (far, *t.stride()[1:]), at)
+        at += t[0].numel()
+        return out.copy_(t)
+
+    qv, kv, dqv, dkv, q_out, k_out = (view(t) for t in (q, k, dq, dk, q, k))
+    pos = near + (table - 50)
+    lib.attn_qk_norm_rope(qv, kv, *w, cos, sin, q_out, k_out, positions=pos)
+    dwq, dwk = torch.empty(128, device="cuda"), torch.empty(128, device="cuda")
+    lib.attn_qk_norm_rope_bwd(dqv, dkv, qv, kv, *w, cos, sin, dqv, dkv, dwq, dwk, positions=pos)
+    torch.cuda.synchronize()
+    assert torch.equal(q_out, want[0]) and torch.equal(k_out, want[1])
+    assert all(torch.equal(a, b) for a, b in zip((dqv, dkv, dwq, dwk), wantg))
+
+
 def test_refusals():
     q, k, dq, dk, w, cos, sin, pos = make(1, 8, 2, 2, 128, 16, torch.float32)
     out = (torch.empty_like(q), torch.empty_like(k))

@@ -41,7 +41,8 @@ def test_backward_workspace_size(cdll):
     stats = lambda B, H, S: 2 * 4 * B * H * ((S + 127) // 128 * 128)  # noqa: E731
     assert size(8, 16, 16, 4096, 4096, 128, 1) == stats(8, 16, 4096)      # enough items: nothing is split
     assert size(1, 2, 2, 512, 512, 128, 0) == stats(1, 2, 512)            # too short to be worth it
-    assert size(1, 16, 16, 512, 65536, 128, 1) > stats(1, 16, 512)        # few query items, long streams
+    assert size(1, 16, 16, 512, 65536, 128, 1) == stats(1, 16, 512)       # few query items, but they go first
+    assert size(1, 1, 1, 64, 9000, 128, 1) > stats(1, 1, 64)              # one query item, a long stream
     assert size(1, 8, 8, 16384, 128, 128, 0) > stats(1, 8, 16384)         # few key items
     # never more than 32 parts of each output
     for a in ((1, 1, 1, 1, 1 << 20), (1, 1, 1, 1 << 20, 1), (1, 8, 1, 100000, 100000)):
