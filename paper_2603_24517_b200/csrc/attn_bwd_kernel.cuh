@@ -369,6 +369,11 @@ __device__ __forceinline__ bool load_item(const BwdParams& p, const BwdItem& it,
   fence_proxy_async_smem();  // the answer this one overwrites was read through the generic proxy
   mbar_arrive_expect_tx(clc_bar, 16);
   clc_request(clc_buf, clc_bar);
+  return true;
+}
+// The slots for the item's results.
+__device__ __forceinline__ bool load_stage_slots(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, WaitCtx ctx,
+                                                 LoaderState& ls) {
   if (staged(p, it)) {
     // The slots behind the last tiles take the results: the `full` barriers of these positions tell the softmax warps.
     if (!mbar_wait(&bars.a_empty[ls.a.slot], ls.a.par ^ 1, ctx, kRoleBwdLoad | kBarRingEmpty)) return false;
@@ -398,13 +403,14 @@ __device__ __forceinline__ void role_loader(const BwdParams& p, const BwdBarrier
                             : load_item(p, it, bars, smem, ctx, tm_q, tm_do, tm_k, tm_v, ls, answer, clc_bar);
     if (!ok || !mbar_wait(clc_bar, (k >> 1) & 1, ctx, kRoleBwdLoad | kBarClc)) return;
     const int w = clc_answer(answer);
+    // the divisions of the next item's index, before the wait for slots that this item's last products hold
+    const BwdItem coming = decode_item(p, w >= 0 ? w : 0);
+    if (!load_stage_slots(p, it, bars, ctx, ls)) return;
     const int n = k + 1;
     if (!mbar_wait(&bars.item_empty[n & 1], ((n >> 1) & 1) ^ 1, ctx, kRoleBwdLoad | kBarItemEmpty)) return;
     volatile int* slot = box + (n & 1) * kItemInts;
-    if (w >= 0) {
-      it = decode_item(p, w);
-      put_item(slot, it);
-    }
+    it = coming;
+    if (w >= 0) put_item(slot, it);
     slot[0] = w >= 0 ? 1 : 0;
     mbar_arrive(&bars.item_full[n & 1]);
     if (w < 0) return;
