@@ -31,6 +31,8 @@ EXPORTED_SYMBOLS = ("attn_fwd", "attn_fwd_strided", "attn_fwd_host", "attn_fwd_n
                     "attn_last_device_status")
 
 _lib = None
+_BF16 = torch.bfloat16
+_LL3 = ctypes.c_longlong * 3
 
 
 class AttnError(RuntimeError):
@@ -147,10 +149,9 @@ def _strides3(t):
     """Element strides of the (batch, sequence, head) axes of a [B, S, H, D] tensor as a C array.
     An axis of extent 1 is never stepped along, so it gets the stride a contiguous tensor would
     have (torch may report anything there)."""
-    _, S, H, D = t.shape
-    dense = (S * H * D, H * D, D)
-    vals = [dense[i] if t.shape[i] == 1 else t.stride(i) for i in range(3)]
-    return (ctypes.c_longlong * 3)(*vals)
+    B, S, H, D = t.shape
+    b, s, h, _ = t.stride()
+    return _LL3(S * H * D if B == 1 else b, H * D if S == 1 else s, D if H == 1 else h)
 
 
 def attn_fwd_strided_status(q, k, v, o, lse, causal: bool, scale: float, stream=None) -> int:
@@ -376,40 +377,50 @@ def _on_device(dev, fn, *args):
         return fn(*args)
 
 
-def _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, strided, made_here=False):
-    """``made_here``: dq, dk, dv are new contiguous tensors of the right kind."""
-    tensors = (dout, q, k, v, o, dq, dk, dv)
-    dev = q.device
-    shape, kv_shape = q.shape, k.shape
-    if len(shape) != 4 or len(kv_shape) != 4 or dev.type != "cuda":
-        raise ValueError("q and k must be 4-D cuda tensors [B, S, H, D]")
-    for i, t in enumerate(tensors[:5] if made_here else tensors):
-        if t.dtype is not torch.bfloat16 or t.device != dev or t.shape != (kv_shape if i in (2, 3, 6, 7) else shape) \
-                or not (t.is_contiguous() or strided and t.stride(3) == 1):
-            name = ("dout", "q", "k", "v", "o", "dq", "dk", "dv")[i]
+def _refuse_bwd(tensors, shape, kv_shape, strided):
+    """Names the tensor that is not what ``_bwd_status`` needs."""
+    dev = tensors[1].device
+    for name, t in zip(("dout", "q", "k", "v", "o", "dq", "dk", "dv"), tensors):
+        want = kv_shape if name in ("k", "v", "dk", "dv") else shape
+        if t.dtype is not _BF16 or t.device != dev or t.shape != want or not (t.stride(3) == 1 if strided else t.is_contiguous()):
             layout = "with a contiguous last axis" if strided else "that is contiguous"
             raise ValueError(f"{name} must be a bfloat16 tensor {layout}, of the shape [B, S, H, D] of "
-                             f"{'k' if i in (2, 3, 6, 7) else 'q'}, on q's device")
+                             f"{'k' if want is kv_shape else 'q'}, on q's device")
+
+
+def _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, workspace, stream, strided, made_here=False):
+    """``made_here``: dq, dk, dv are new contiguous tensors of the right kind."""
+    dev, shape, kv_shape = q.device, q.shape, k.shape
+    if len(shape) != 4 or len(kv_shape) != 4 or dev.type != "cuda" or kv_shape[0] != shape[0] or kv_shape[3] != shape[3]:
+        raise ValueError("q and k must be 4-D cuda tensors [B, S, H, D] of one batch size and head dimension")
+    # one expression for the usual call: these checks are a good part of its time
+    if not (q.dtype is _BF16 and k.dtype is _BF16 and v.dtype is _BF16 and o.dtype is _BF16 and dout.dtype is _BF16
+            and v.shape == kv_shape and o.shape == shape and dout.shape == shape
+            and k.device == dev and v.device == dev and o.device == dev and dout.device == dev):
+        _refuse_bwd((dout, q, k, v, o), shape, kv_shape, strided)
+    if not made_here:
+        _refuse_bwd((dout, q, k, v, o, dq, dk, dv), shape, kv_shape, strided)
+    elif strided and not (q.stride(3) == k.stride(3) == v.stride(3) == o.stride(3) == dout.stride(3) == 1):
+        _refuse_bwd((dout, q, k, v, o), shape, kv_shape, strided)
     B, Sq, Hq, D = shape
-    Bk, Sk, Hkv, Dk = kv_shape
-    if Bk != B or Dk != D:
-        raise ValueError("inconsistent q/k shapes")
-    for name, t in (("lse", lse), ("dlse", dlse)):
-        if t is None and name == "dlse":
-            continue
+    _, Sk, Hkv, _ = kv_shape
+    for name, t in (("lse", lse),) if dlse is None else (("lse", lse), ("dlse", dlse)):
         if t is None or t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != (B, Hq, Sq) or t.device != dev:
             raise ValueError(f"{name} must be a contiguous float32 tensor [B, Hq, Sq] on q's device")
     lib = load_library()
-    causal = int(bool(causal))
+    causal = 1 if causal else 0
     if workspace is None:
         workspace = _new_workspace(q, max(lib.attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, causal), 16), stream)
     elif not workspace.is_contiguous() or workspace.device != dev:
         raise ValueError("workspace must be a contiguous tensor on q's device")
     args = (dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
             None if dlse is None else dlse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Hq, Hkv, Sq, Sk, D)
-    tail = (causal, float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(dev, stream))
+    tail = (causal, float(scale), workspace.data_ptr(), workspace.nbytes, _raw_stream(dev, stream))
     if strided:
-        return _on_device(dev, lib.attn_bwd_strided, *args, *[_strides3(t) for t in tensors], *tail)
+        dense, kv_dense = _LL3(Sq * Hq * D, Hq * D, D), _LL3(Sk * Hkv * D, Hkv * D, D)
+        return _on_device(dev, lib.attn_bwd_strided, *args,
+                          *[(kv_dense if i in (2, 3, 6, 7) else dense) if t.is_contiguous() else _strides3(t)
+                            for i, t in enumerate((dout, q, k, v, o, dq, dk, dv))], *tail)
     return _on_device(dev, lib.attn_bwd, *args, *tail)
 
 
@@ -449,38 +460,37 @@ def _rope_args(q, k, q_weight, k_weight, cos, sin, positions, others):
     dev, shape, kv_shape = q.device, q.shape, k.shape
     if dev.type != "cuda" or len(shape) != 4 or len(kv_shape) != 4 or kv_shape[:2] != shape[:2] or kv_shape[3] != shape[3]:
         raise ValueError("q and k must be cuda tensors [B, S, Hq, D] and [B, S, Hkv, D]")
-    for pair in ((q, k), *others):
-        for t, want in zip(pair, (shape, kv_shape)):
-            if t.dtype is not torch.bfloat16 or t.shape != want or t.stride(3) != 1 or t.device != dev:
-                raise ValueError("queries, keys, their outputs and gradients must be bfloat16 tensors [B, S, H, D] of q's and "
-                                 "k's shapes with a contiguous last axis, all on q's device")
+    for x, y in ((q, k), *others):
+        if not (x.dtype is _BF16 and y.dtype is _BF16 and (x is q or x.shape == shape and y.shape == kv_shape)
+                and x.stride(3) == 1 and y.stride(3) == 1 and x.device == dev and y.device == dev):
+            raise ValueError("queries, keys, their outputs and gradients must be bfloat16 tensors [B, S, H, D] of q's and "
+                             "k's shapes with a contiguous last axis, all on q's device")
     B, S, Hq, D = shape
-    weight_type, weights = 0, []
+    weight_type = 0
     for w in (q_weight, k_weight):
         if w is None:
-            weights.append(None)
             continue
-        if w.dtype not in (torch.float32, torch.bfloat16) or w.shape != (D,) or not w.is_contiguous() or w.device != dev:
+        weight_type = 1 if w.dtype is _BF16 else 0
+        if not (weight_type or w.dtype is torch.float32) or w.shape != (D,) or not w.is_contiguous() or w.device != dev:
             raise ValueError("q_weight and k_weight must be contiguous float32 or bfloat16 tensors [D] on q's device")
-        weight_type = int(w.dtype is torch.bfloat16)
-        weights.append(w.data_ptr())
-    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
         raise ValueError("q_weight and k_weight must have one type")
     table = cos.shape
-    if len(table) != 2 or cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or sin.shape != table \
-            or not cos.is_contiguous() or not sin.is_contiguous() or cos.device != dev or sin.device != dev:
+    if not (len(table) == 2 and cos.dtype is torch.float32 and sin.dtype is torch.float32 and sin.shape == table
+            and cos.is_contiguous() and sin.is_contiguous() and cos.device == dev and sin.device == dev):
         raise ValueError("cos and sin must be contiguous float32 tensors [positions, rot_dim / 2] on q's device")
     pos_ptr, pos_type, pos_strides = None, 0, None
     if positions is not None:
-        if positions.dtype not in (torch.int32, torch.int64) or positions.device != dev \
-                or positions.shape not in ((B, S), (S,)):
+        pos_type = 1 if positions.dtype is torch.int64 else 0
+        if not (pos_type or positions.dtype is torch.int32) or positions.device != dev or positions.shape not in ((B, S), (S,)):
             raise ValueError("positions must be an int32 or int64 tensor [B, S] or [S] on q's device")
-        pos_ptr, pos_type = positions.data_ptr(), int(positions.dtype is torch.int64)
+        pos_ptr = positions.data_ptr()
         if positions.dim() == 1:
             pos_strides = (ctypes.c_longlong * 2)(0, positions.stride(0))
         elif not positions.is_contiguous():
             pos_strides = (ctypes.c_longlong * 2)(*positions.stride())
-    return (q.data_ptr(), k.data_ptr(), *weights, weight_type, cos.data_ptr(), sin.data_ptr(), pos_ptr, pos_type,
+    return (q.data_ptr(), k.data_ptr(), None if q_weight is None else q_weight.data_ptr(),
+            None if k_weight is None else k_weight.data_ptr(), weight_type, cos.data_ptr(), sin.data_ptr(), pos_ptr, pos_type,
             pos_strides), (B, S, Hq, kv_shape[2], D, 2 * table[1], table[0])
 
 
@@ -498,7 +508,8 @@ def attn_qk_norm_rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, p
 def _rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved, stream, check):
     lead, sizes = _rope_args(q, k, q_weight, k_weight, cos, sin, positions, check)
     return _on_device(q.device, load_library().attn_qk_norm_rope, *lead, q_out.data_ptr(), k_out.data_ptr(), *sizes,
-                      int(bool(interleaved)), float(eps), *[_strides3_or_none(t) for t in (q, k, q_out, k_out)],
+                      1 if interleaved else 0, float(eps), _strides3_or_none(q), _strides3_or_none(k),
+                      _strides3_or_none(q_out), _strides3_or_none(k_out),
                       _raw_stream(q.device, stream))
 
 
@@ -545,7 +556,7 @@ def _rope_bwd_status(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk,
                       None if dk_weight is None else dk_weight.data_ptr(), *sizes, int(bool(interleaved)), float(eps),
                       *[_strides3_or_none(t) for t in (dq_out, dk_out, q, k, dq, dk)],
                       None if workspace is None else workspace.data_ptr(),
-                      0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(dev, stream))
+                      0 if workspace is None else workspace.nbytes, _raw_stream(dev, stream))
 
 
 def attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions=None,
