@@ -365,7 +365,9 @@ def _new_workspace(like, n_bytes: int, stream):
     another one, the allocator must not hand it out again before that stream is done with it."""
     workspace = like.new_empty(n_bytes, dtype=torch.uint8)
     if stream is not None:
-        workspace.record_stream(torch.cuda.ExternalStream(stream, device=like.device))
+        # (an ExternalStream of 0 would be a stream out of torch's pool)
+        workspace.record_stream(torch.cuda.ExternalStream(stream, device=like.device) if stream
+                                else torch.cuda.default_stream(like.device))
     return workspace
 
 

@@ -88,6 +88,7 @@ def test_rotation_argument_errors(cdll):
     for bad in (dict(D=64), dict(rot=0), dict(rot=8), dict(rot=24), dict(rot=144), dict(eps=0.0), dict(eps=float("nan")),
                 dict(wt=2), dict(pt=-1), dict(B=1 << 30, S=8), dict(q_out=0x200), dict(k_out=0x100), dict(k_out=0x700)):
         assert _rope(cdll, **bad) == 3, bad
+    assert _rope(cdll, Hq=2 ** 31 - 1, Hkv=2 ** 31 - 8, S=8) == 3  # head counts at the end of their type
     for name, at in (("q", 0x108), ("wq", 0x304), ("cos", 0x508), ("q_out", 0x708), ("pos", 0x902)):
         assert _rope(cdll, **{name: at}) == 4, name
     assert _rope(cdll, pos=0x904, pt=1) == 4                       # 64-bit positions on a 4-byte address
@@ -128,3 +129,26 @@ def test_cpu_tensors_are_refused():
         lib.qk_norm_rope(q, q, None, None, table, table)
     with pytest.raises(ValueError):
         lib.qk_norm_rope_backward(q, q, q, q, None, None, table, table)
+
+
+def test_workspace_of_a_call_on_the_default_stream(monkeypatch):
+    """Stream 0, given as a number, is the default stream, not one out of a pool."""
+    from paper_2603_24517_b200 import binding
+    recorded, dev = [], torch.device("cuda", 0)
+
+    class Workspace:
+        def record_stream(self, stream):
+            recorded.append(stream)
+
+    class Like:
+        device = dev
+
+        def new_empty(self, n_bytes, dtype):
+            return Workspace()
+
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda stream, device: ("external", stream, device))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device: ("default", device))
+    binding._new_workspace(Like(), 64, 0)
+    binding._new_workspace(Like(), 64, 0x1230)
+    binding._new_workspace(Like(), 64, None)
+    assert recorded == [("default", dev), ("external", 0x1230, dev)]
