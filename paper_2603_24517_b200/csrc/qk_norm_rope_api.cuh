@@ -54,7 +54,7 @@ attn_status_t rope_params(const RopeArgs& a, const long long* const* in_strides,
   for (int t = 0; t < 2; ++t) {
     const attn_status_t st = rope_strides(in_strides[t], a.S, p->heads[t], &p->sx[t]);
     if (st != ATTN_OK) return st;
-    p->units[t] = (p->heads[t] + attn::rope::kUnitRows - 1) / attn::rope::kUnitRows;
+    p->units[t] = (p->heads[t] - 1) / attn::rope::kUnitRows + 1;
   }
   p->w[0] = a.q_weight;
   p->w[1] = a.k_weight;
