@@ -646,11 +646,14 @@ def _new_like(t):
 def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float | None = None, dlse=None):
     """Gradients (dq, dk, dv) of ``attention_forward(q, k, v, causal, scale)`` from its results ``o``, ``lse`` and the
     gradient ``dout`` with respect to ``o`` (and ``dlse`` with respect to ``lse``).  Inputs may be views as in
-    ``attn_fwd_strided``; a ``dout`` without an order of its own (the expanded gradient of a sum) is copied first.
+    ``attn_fwd_strided``; a ``dout`` without an order of its own (the expanded gradient of a sum), and a ``dlse`` that is
+    not contiguous, is copied first.
     The gradients are new contiguous tensors."""
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1])
     dout = _ordered(dout)
+    if dlse is not None and not dlse.is_contiguous():
+        dlse = dlse.contiguous()
     dq, dk, dv = _new_like(q), _new_like(k), _new_like(v)
     strided = not (dout.is_contiguous() and q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous())
     st = _bwd_status(dout, q, k, v, o, lse, dq, dk, dv, causal, scale, dlse, None, None, strided, True)

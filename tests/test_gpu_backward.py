@@ -221,6 +221,14 @@ def test_expanded_gradient_of_a_sum():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_expanded_gradient_of_a_sum_of_lse():
+    dout, q, k, v = make(1, 2, 2, 130, 130)
+    o, lse = lib.attention_forward(q, k, v)
+    got = lib.attention_backward(dout, q, k, v, o, lse, dlse=torch.ones((), device="cuda").expand(lse.shape))
+    want = lib.attention_backward(dout, q, k, v, o, lse, dlse=torch.ones_like(lse))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("shape", [(2, 4, 2, 500, 500, True), (1, 2, 2, 64, 9000, False)])
 def test_same_bits_every_time_on_any_stream(shape):
     B, Hq, Hkv, Sq, Sk, causal = shape
