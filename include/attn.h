@@ -371,7 +371,8 @@ attn_status_t attn_fwd_splitkv(const void* q, const void* k, const void* v, void
  * rows too (a weight of 0 times NaN is NaN); lse finite or -infinity.  dq, dk, dv and workspace must not
  * overlap each other or any input.  The options of attn_set_option concern the forward kernels only.
  * S, dP and the gradients accumulate in fp32 on the tensor cores and each output is rounded once;
- * P and dS are rounded to BF16 before the products that read them.
+ * P and dS are rounded to BF16 before the products that read them (kept as the sum of two BF16
+ * numbers where Sq or Sk is at most 64: in sums of few terms a rounding shows in full).
  * Every sum has a fixed order: the same call gives the same bits.  Asynchronous on `stream`, no
  * state is kept between calls: any number of calls may run at once, each with its own
  * workspace, and calls can be captured into a CUDA graph (after a first call on the device outside

@@ -129,7 +129,9 @@ DeviceState* device_state(attn_status_t* st) {
                            attn::pair::kSmemBytes2) != cudaSuccess ||
       cudaFuncSetAttribute(attn::w16::attn_fwd_w16_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::kSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           attn::bwd::kSmemBwdBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||
       cudaMalloc(&d.status, 2 * sizeof(int)) != cudaSuccess ||

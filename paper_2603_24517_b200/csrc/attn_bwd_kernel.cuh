@@ -36,6 +36,11 @@
 //
 // Transposed tiles in key items (rows are keys) let P^T and dS^T go back to tensor memory as the left
 // operand of the second products, so nothing is transposed through shared memory.
+//
+// Precision: every sum is fp32; P and dS are rounded to BF16 as operands, which adds to a result about as much as its own
+// rounding does: 0.0024 of it, where that one alone is 0.0017.  In sums of few terms the rounding of one weight shows in
+// full (up to 0.0037); for such problems (kFine) P and dS are handed over as the sum of two BF16 numbers, with a second
+// product each, and 0.0017 is left.
 #pragma once
 
 #include "attn_fwd_kernel.cuh"
@@ -264,7 +269,9 @@ __device__ __forceinline__ bool next_item(const BwdBarriers& bars, const volatil
 constexpr int kItemConsumers = kSoftmaxWarps + 3;  // softmax warps, MMA warps, store warp
 
 // D[128 x 128] (+)= A[tmem] B for one half (64) of the contraction rows.  A (BF16) was written over fp32 columns, by each
-// softmax thread over the first half of its own 16; B is MN-major (16 contraction rows are 2048 bytes).
+// softmax thread over the first half of its own 16 (kFine: and what that rounding left over the second half); B is
+// MN-major (16 contraction rows are 2048 bytes).
+template <bool kFine>
 __device__ __forceinline__ void issue_ts_half(bool leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t b_desc, int half,
                                               bool accumulate) {
   if (leader) {
@@ -272,6 +279,9 @@ __device__ __forceinline__ void issue_ts_half(bool leader, uint32_t tmem_d, uint
     for (int kk = 0; kk < 4; ++kk) {
       mma_ts(tmem_d, tmem_a + half * 64 + kk * kCols, desc_advance(b_desc, (half * 4 + kk) * 2048), kIdescPV,
              (accumulate || kk > 0) ? 1u : 0u);
+      if (kFine) {
+        mma_ts(tmem_d, tmem_a + half * 64 + kk * kCols + kCols / 2, desc_advance(b_desc, (half * 4 + kk) * 2048), kIdescPV, 1u);
+      }
     }
   }
 }
@@ -498,6 +508,7 @@ struct MmaItem {
 // there is nothing to issue.  Across items the same order holds between items of one kind; products into columns that
 // the item before used otherwise, and into its accumulators, wait until its results have left tensor memory
 // (acc_empty).
+template <bool kFine>
 __device__ __forceinline__ bool key_mma_1(const BwdItem& it, MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
   constexpr int kRole = kRoleBwdMma;
   const uint64_t k_desc = kmajor_desc(m.base + kSmemFixed);
@@ -521,7 +532,7 @@ __device__ __forceinline__ bool key_mma_1(const BwdItem& it, MmaItem& m, const B
     for (int h = 0; h < 2; ++h) {
       if (!mbar_wait_warp(&bars.p_full[h], ph.key & 1, ctx, kRole | kBarP)) return false;
       tc_fence_after_sync();
-      issue_ts_half(m.leader, m.tmem + kTmDv, m.tmem + kTmS, do_desc, h, i > 0 || h > 0);
+      issue_ts_half<kFine>(m.leader, m.tmem + kTmDv, m.tmem + kTmS, do_desc, h, i > 0 || h > 0);
     }
     if (next) {
       issue_qk(m.leader, m.tmem + kTmS, k_desc, q_desc);
@@ -539,6 +550,7 @@ __device__ __forceinline__ bool key_mma_1(const BwdItem& it, MmaItem& m, const B
   ph.s ^= it.n & 1;  // the other warp waits for dS
   return true;
 }
+template <bool kFine>
 __device__ __forceinline__ bool key_mma_2(const BwdItem& it, MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
   constexpr int kRole = kRoleBwdMma2;
   const uint64_t v_desc = kmajor_desc(m.base + kSmemFixed + kTileBytes);
@@ -563,7 +575,7 @@ __device__ __forceinline__ bool key_mma_2(const BwdItem& it, MmaItem& m, const B
     for (int h = 0; h < 2; ++h) {
       if (!mbar_wait_warp(&bars.ds_full[h], ph.s & 1, ctx, kRole | kBarDs)) return false;
       tc_fence_after_sync();
-      issue_ts_half(m.leader, m.tmem + kTmDk, m.tmem + kTmDp, q_desc, h, i > 0 || h > 0);
+      issue_ts_half<kFine>(m.leader, m.tmem + kTmDk, m.tmem + kTmDp, q_desc, h, i > 0 || h > 0);
     }
     if (next) {
       issue_qk(m.leader, m.tmem + kTmDp, v_desc, do_desc);
@@ -585,6 +597,7 @@ __device__ __forceinline__ bool key_mma_2(const BwdItem& it, MmaItem& m, const B
 // while tile j's are exponentiated: two score buffers, dS(j) goes over the scores of tile j, and S(j+2) into the same
 // columns is issued behind dS(j) K(j).
 // Second MMA warp: dP(j) = dO V(j)^T into one buffer, free as soon as the softmax warps have it in registers.
+template <bool kFine>
 __device__ __forceinline__ bool query_mma_1(const BwdItem& it, MmaItem& m, const BwdBarriers& bars, WaitCtx ctx, Phases& ph) {
   constexpr int kRole = kRoleBwdMma;
   const uint64_t q_desc = kmajor_desc(m.base + kSmemFixed);
@@ -603,7 +616,7 @@ __device__ __forceinline__ bool query_mma_1(const BwdItem& it, MmaItem& m, const
       for (int h = 0; h < 2; ++h) {
         if (!mbar_wait_warp(&bars.ds_full[2 * x + h], (ph.s >> x) & 1, ctx, kRole | kBarDs)) return false;
         tc_fence_after_sync();
-        issue_ts_half(m.leader, m.tmem + kTmDq, scores, kv_desc, h, j > 0 || h > 0);
+        issue_ts_half<kFine>(m.leader, m.tmem + kTmDq, scores, kv_desc, h, j > 0 || h > 0);
       }
       if (m.leader) mma_commit(&bars.a_empty[done.slot]);
       done.next();
@@ -652,7 +665,7 @@ __device__ __forceinline__ bool query_mma_2(const BwdItem& it, MmaItem& m, const
   return true;
 }
 
-template <bool kFirst>
+template <bool kFirst, bool kFine>
 __device__ __forceinline__ void role_mma(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem, const volatile int* box,
                                          WaitCtx ctx, uint32_t tmem, int lane) {
   constexpr int kRole = kFirst ? kRoleBwdMma : kRoleBwdMma2;
@@ -670,9 +683,9 @@ __device__ __forceinline__ void role_mma(const BwdParams& p, const BwdBarriers& 
     if (it.n > 0) {
       bool ok;
       if (kFirst) {
-        ok = it.keys ? key_mma_1(it, m, bars, ctx, ph) : query_mma_1(it, m, bars, ctx, ph);
+        ok = it.keys ? key_mma_1<kFine>(it, m, bars, ctx, ph) : query_mma_1<kFine>(it, m, bars, ctx, ph);
       } else {
-        ok = it.keys ? key_mma_2(it, m, bars, ctx, ph) : query_mma_2(it, m, bars, ctx, ph);
+        ok = it.keys ? key_mma_2<kFine>(it, m, bars, ctx, ph) : query_mma_2(it, m, bars, ctx, ph);
       }
       if (!ok) return;
       ++m.fixed;
@@ -738,19 +751,35 @@ __device__ __forceinline__ void exp_row(uint32_t* x, float2 c2, NegLse neg_lse, 
   }
 }
 
-// dS = P o (dP - delta) of kCols columns, as BF16 words, given per pair of columns the pair of -delta.
-template <typename NegDelta>
-__device__ __forceinline__ void ds_row(const uint32_t* x, const uint32_t* d, NegDelta neg_delta, uint32_t* pk) {
+// A thread's kCols columns of an operand as BF16 words; kFine: and then what their rounding left.
+template <bool kFine>
+struct Operand {
+  uint32_t word[kFine ? kCols : kCols / 2];
+  __device__ __forceinline__ void put(int e, float a, float b) {  // columns e, e + 1
+    const uint32_t w = pack_bf16x2(a, b);
+    word[e / 2] = w;
+    if constexpr (kFine) word[(kCols + e) / 2] = pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+  }
+};
+
+// dS = P o (dP - delta) of kCols columns, given per pair of columns the pair of -delta.
+template <bool kFine, typename NegDelta>
+__device__ __forceinline__ void ds_row(const uint32_t* x, const uint32_t* d, NegDelta neg_delta, Operand<kFine>& out) {
 #pragma unroll
   for (int e = 0; e < kCols; e += 2) {
     const float2 t = add2(make_float2(ATTN_F(d, e), ATTN_F(d, e + 1)), neg_delta(e));
     const float2 w = mul2(make_float2(ATTN_F(x, e), ATTN_F(x, e + 1)), t);
-    pk[e / 2] = pack_bf16x2(w.x, w.y);
+    out.put(e, w.x, w.y);
   }
 }
-// kCols / 2 words of a finished operand into tensor memory, and the word to the MMA warp that waits for it.
-__device__ __forceinline__ void hand_over(uint32_t taddr, const uint32_t* pk, uint64_t* bar, int lane) {
-  tmem_st_x8(taddr, pk);
+// A finished operand into tensor memory, and the word to the MMA warp that waits for it.
+template <bool kFine>
+__device__ __forceinline__ void hand_over(uint32_t taddr, const Operand<kFine>& op, uint64_t* bar, int lane) {
+  if constexpr (kFine) {
+    tmem_st_x16(taddr, op.word);
+  } else {
+    tmem_st_x8(taddr, op.word);
+  }
   tmem_wait_st();
   tc_fence_before_sync();
   __syncwarp();
@@ -768,6 +797,7 @@ __device__ __forceinline__ void load_stats(const float* src, float2* f) {
 }
 
 // One softmax thread of a key item: row `row` of the tile (a key), columns part * kCols + [0, kCols) of each half.
+template <bool kFine>
 __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars,
                                             const uint8_t* smem, WaitCtx ctx, uint32_t tmem_row, int part, int row, int lane,
                                             Phases& ph) {
@@ -782,7 +812,8 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
               mbar_wait(&bars.s_full[0], ph.s & 1, ctx, kRoleBwdSoftmax | kBarS);
     if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
-    uint32_t x[2][kCols], d[2][kCols], pk[kCols / 2];
+    uint32_t x[2][kCols], d[2][kCols];
+    Operand<kFine> op;
     tmem_ld_x16(t_s, x[0]);
     tmem_ld_x16(t_s + 64, x[1]);
     tmem_wait_ld();
@@ -795,8 +826,8 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
       load_stats(nl + h * 64, st2);
       exp_row<kKeyPolyPairs>(x[h], c2, [&](int e) { return st2[e / 2]; }, masked, seen_from - h * 64, kCols);
 #pragma unroll
-      for (int e = 0; e < kCols / 2; ++e) pk[e] = pack_bf16x2(ATTN_F(x[h], 2 * e), ATTN_F(x[h], 2 * e + 1));
-      hand_over(t_s + h * 64, pk, &bars.p_full[h], lane);
+      for (int e = 0; e < kCols; e += 2) op.put(e, ATTN_F(x[h], e), ATTN_F(x[h], e + 1));
+      hand_over<kFine>(t_s + h * 64, op, &bars.p_full[h], lane);
     }
     ok = mbar_wait(bars.dp_full, ph.dp & 1, ctx, kRoleBwdSoftmax | kBarDp);
     if (!__all_sync(0xffffffffu, ok)) return false;
@@ -808,8 +839,8 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
     for (int h = 0; h < 2; ++h) {  // over this thread's own columns, which are in registers
       float2 st2[kCols / 2];
       load_stats(neg_delta + h * 64, st2);
-      ds_row(x[h], d[h], [&](int e) { return st2[e / 2]; }, pk);
-      hand_over(t_dp + h * 64, pk, &bars.ds_full[h], lane);
+      ds_row<kFine>(x[h], d[h], [&](int e) { return st2[e / 2]; }, op);
+      hand_over<kFine>(t_dp + h * 64, op, &bars.ds_full[h], lane);
     }
     if (lane == 0) mbar_arrive(&bars.stat_empty[st]);
     ph.s ^= 1u;
@@ -821,6 +852,7 @@ __device__ __forceinline__ bool key_softmax(const BwdParams& p, const BwdItem& i
 }
 
 // The same for a query item: row `row` is a query, the columns are keys.
+template <bool kFine>
 __device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem& it, const BwdBarriers& bars, WaitCtx ctx,
                                               uint32_t tmem_row, int part, int row, int lane, Phases& ph) {
   const uint32_t t_dp = tmem_row + kTmQryDp + part * kCols;
@@ -836,7 +868,8 @@ __device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem&
     if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after_sync();
     const uint32_t t_s = tmem_row + kTmQryS + x_buf * kTile + part * kCols;
-    uint32_t x[2][kCols], d[2][kCols], pk[kCols / 2];
+    uint32_t x[2][kCols], d[2][kCols];
+    Operand<kFine> op;
     tmem_ld_x16(t_s, x[0]);
     tmem_ld_x16(t_s + 64, x[1]);
     tmem_wait_ld();
@@ -857,8 +890,8 @@ __device__ __forceinline__ bool query_softmax(const BwdParams& p, const BwdItem&
     if (lane == 0) mbar_arrive(bars.dp_read);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {  // over this thread's own scores, read above
-      ds_row(x[h], d[h], [&](int) { return ndl2; }, pk);
-      hand_over(t_s + h * 64, pk, &bars.ds_full[2 * x_buf + h], lane);
+      ds_row<kFine>(x[h], d[h], [&](int) { return ndl2; }, op);
+      hand_over<kFine>(t_s + h * 64, op, &bars.ds_full[2 * x_buf + h], lane);
     }
     ph.s ^= 1u << x_buf;
     ++ph.dp;
@@ -926,6 +959,7 @@ __device__ __forceinline__ bool write_results(const BwdParams& p, const BwdItem&
   return true;
 }
 
+template <bool kFine>
 __device__ __forceinline__ void role_softmax(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem, const volatile int* box,
                                              WaitCtx ctx, uint32_t tmem, int part, int row, int lane) {
   const uint32_t tmem_row = tmem + (static_cast<uint32_t>(row & ~31) << 16);
@@ -935,8 +969,8 @@ __device__ __forceinline__ void role_softmax(const BwdParams& p, const BwdBarrie
   for (int k = 0; next_item(bars, box, k, ctx, kRoleBwdSoftmax, true, lane == 0, it); ++k) {
     bool ok = true;
     if (it.n > 0) {
-      ok = it.keys ? key_softmax(p, it, bars, smem, ctx, tmem_row, part, row, lane, ph)
-                   : query_softmax(p, it, bars, ctx, tmem_row, part, row, lane, ph);
+      ok = it.keys ? key_softmax<kFine>(p, it, bars, smem, ctx, tmem_row, part, row, lane, ph)
+                   : query_softmax<kFine>(p, it, bars, ctx, tmem_row, part, row, lane, ph);
     }
     pos_a += it.n;
     pos_b += it.n;
@@ -949,6 +983,7 @@ __device__ __forceinline__ void role_softmax(const BwdParams& p, const BwdBarrie
   }
 }
 
+template <bool kFine>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
@@ -1028,13 +1063,13 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 
   if (warp < kSoftmaxWarps) {
     reg_alloc<kRegsSoftmax>();
-    role_softmax(p, bars, smem, box, ctx, tmem, warp >> 2, tid & 127, lane);
+    role_softmax<kFine>(p, bars, smem, box, ctx, tmem, warp >> 2, tid & 127, lane);
   } else {
     reg_dealloc<kRegsOther>();
     if (warp == kSoftmaxWarps) {
-      role_mma<true>(p, bars, smem, box, ctx, tmem, lane);
+      role_mma<true, kFine>(p, bars, smem, box, ctx, tmem, lane);
     } else if (warp == kSoftmaxWarps + 1) {
-      role_mma<false>(p, bars, smem, box, ctx, tmem, lane);
+      role_mma<false, kFine>(p, bars, smem, box, ctx, tmem, lane);
     } else if (lane != 0) {
       // the loader and the store warp are one thread each
     } else if (warp == kSoftmaxWarps + 2) {

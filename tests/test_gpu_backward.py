@@ -37,13 +37,13 @@ def make(B, Hq, Hkv, Sq, Sk, gain=1.0, seed=0):
     return dout, q, k, v
 
 
-def check(got, dout, q, k, v, o, lse, causal, scale, dlse=None):
+def check(got, dout, q, k, v, o, lse, causal, scale, dlse=None, operand=2.0 ** -8):
     want, sizes, noises = orc.attention_grads(dout, q, k, v, o, lse, causal, scale, dlse)
     terms = (k.shape[1], q.shape[1] * (q.shape[2] // k.shape[2]), q.shape[1] * (q.shape[2] // k.shape[2]))
     for name, a, b, size, noise, n in zip(("dq", "dk", "dv"), got, want, sizes, noises, terms):
         a = a.double()
         assert bool(torch.isfinite(a).all()), name
-        bound = (2.0 ** -8 + 5e-4 + n * 2.0 ** -23) * size + 130 * 2.0 ** -23 * noise + 2.0 ** -8 * b.abs() + 1e-30
+        bound = (operand + 5e-4 + n * 2.0 ** -23) * size + 130 * 2.0 ** -23 * noise + 2.0 ** -8 * b.abs() + 1e-30
         worst = float(((a - b).abs() / bound).max())
         assert worst <= 1.0, f"{name}: {worst} times the bound"
 
@@ -115,6 +115,21 @@ def test_short_sequences_of_head_groups(B, Hq, Hkv, Sq, Sk, causal):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((dq, dk, dv), got))
     assert bool((big[:, Hq] == 7.0).all()) and bool((big[:, :, Sq:] == 7.0).all())
+
+
+# at most 64 query rows or 64 keys: P and dS are the sum of two BF16 numbers (2^-9 of a term's rounding is rounded to
+# half a step again: 2^-16 of the term), so of the operands' roundings next to nothing is left
+SHORT_SHAPES = [(1, 1, 1, 1, 1, False), (1, 1, 1, 1, 9, True), (2, 1, 1, 2, 2, True), (1, 4, 2, 169, 3, True), (1, 1, 1, 9, 9, False),
+                (1, 8, 2, 1, 34, False), (2, 3, 3, 64, 1000, True), (2, 3, 1, 1000, 64, False), (1, 2, 2, 2000, 37, True),
+                (1, 3, 3, 2, 45152, False), (1, 32, 8, 1, 9000, True), (1, 1, 1, 3550, 3, True)]
+
+
+@pytest.mark.parametrize("gain", [1.0, 4.0])
+@pytest.mark.parametrize("B,Hq,Hkv,Sq,Sk,causal", SHORT_SHAPES)
+def test_short_sequences_round_results_only(B, Hq, Hkv, Sq, Sk, causal, gain):
+    dout, q, k, v = make(B, Hq, Hkv, Sq, Sk, gain=gain)
+    o, lse, got = grads(dout, q, k, v, causal)
+    check(got, dout, q, k, v, o, lse, causal, SCALE, operand=2.0 ** -16)
 
 
 @pytest.mark.parametrize("causal", [False, True])
