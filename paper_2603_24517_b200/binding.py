@@ -361,13 +361,17 @@ def _raw_stream(dev, stream):
 
 
 def _new_workspace(like, n_bytes: int, stream):
-    """A workspace that is dropped when the call returns.  It belongs to torch's current stream; where the call goes to
-    another one, the allocator must not hand it out again before that stream is done with it."""
-    workspace = like.new_empty(n_bytes, dtype=torch.uint8)
-    if stream is not None:
-        # (an ExternalStream of 0 would be a stream out of torch's pool)
-        workspace.record_stream(torch.cuda.ExternalStream(stream, device=like.device) if stream
-                                else torch.cuda.default_stream(like.device))
+    """A workspace that is dropped when the call returns, out of memory of the stream that the call goes to: memory of
+    torch's current stream may still be in use by what is queued there, and may be handed out again before ``stream`` is
+    done with it."""
+    if stream is None:
+        return like.new_empty(n_bytes, dtype=torch.uint8)
+    # (an ExternalStream of 0 would be a stream out of torch's pool)
+    target = torch.cuda.ExternalStream(stream, device=like.device) if stream else torch.cuda.default_stream(like.device)
+    with torch.cuda.stream(target):
+        workspace = like.new_empty(n_bytes, dtype=torch.uint8)
+    # torch's own allocator keeps memory by stream and has nothing to record here; one plugged into torch need not
+    workspace.record_stream(target)
     return workspace
 
 
