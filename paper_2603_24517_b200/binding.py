@@ -360,14 +360,22 @@ def _raw_stream(dev, stream):
     return torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream
 
 
+def _torch_stream(dev, stream):
+    """torch's stream for what the C ABI takes as one: a cudaStream_t as a number or a ``c_void_p``, or a ``torch.cuda.Stream``."""
+    handle = getattr(stream, "cuda_stream", stream)
+    if isinstance(handle, ctypes.c_void_p):
+        handle = handle.value or 0
+    # 0 and 1 (cudaStreamLegacy) both name the default stream; an ExternalStream of them would not
+    return torch.cuda.default_stream(dev) if handle in (0, 1) else torch.cuda.ExternalStream(handle, device=dev)
+
+
 def _new_workspace(like, n_bytes: int, stream):
     """A workspace that is dropped when the call returns, out of memory of the stream that the call goes to: memory of
     torch's current stream may still be in use by what is queued there, and may be handed out again before ``stream`` is
     done with it."""
     if stream is None:
         return like.new_empty(n_bytes, dtype=torch.uint8)
-    # (an ExternalStream of 0 would be a stream out of torch's pool)
-    target = torch.cuda.ExternalStream(stream, device=like.device) if stream else torch.cuda.default_stream(like.device)
+    target = _torch_stream(like.device, stream)
     with torch.cuda.stream(target):
         workspace = like.new_empty(n_bytes, dtype=torch.uint8)
     # torch's own allocator keeps memory by stream and has nothing to record here; one plugged into torch need not

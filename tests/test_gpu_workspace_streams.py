@@ -1,5 +1,6 @@
 """GPU tests of calls on a stream that is not torch's current one, with the workspace made inside the call: memory freed on
 the current stream, which a kernel queued there has still to read, is not that workspace."""
+import ctypes
 import math
 
 import pytest
@@ -59,3 +60,16 @@ def test_rotation_gradient():
     got = [torch.empty_like(t) for t in want]
     beside_a_late_reader(lib.attn_qk_norm_rope_bwd_workspace_bytes(), lambda s: lib.attn_qk_norm_rope_bwd(*args, *got, stream=s),
                          got, want)
+
+
+def test_stream_objects():
+    q, k, v, dout = normal(1, 65, 2, 128), normal(1, 300, 2, 128), normal(1, 300, 2, 128), normal(1, 65, 2, 128) * 0.5
+    o, lse = lib.attention_forward(q, k, v)
+    want = lib.attention_backward(dout, q, k, v, o, lse)
+    torch.cuda.synchronize()
+    for stream in (torch.cuda.Stream(), ctypes.c_void_p(torch.cuda.Stream().cuda_stream), 1, 2):
+        got = [torch.zeros_like(t) for t in (q, k, v)]
+        torch.cuda.synchronize()
+        lib.attn_bwd(dout, q, k, v, o, lse, *got, False, SCALE, stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

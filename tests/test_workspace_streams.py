@@ -44,3 +44,20 @@ def test_workspace_comes_from_the_stream_of_the_call(made):
     binding._new_workspace(like, 64, 0)
     binding._new_workspace(like, 64, None)
     assert seen == [("external", 0x1230, DEV), ("default", DEV), None]
+
+
+def test_every_form_of_a_stream(made):
+    """What ctypes passes on as a cudaStream_t, as the other entry points take it."""
+    import ctypes
+    like, seen = made
+
+    class Stream:
+        cuda_stream = 0x1230
+
+    for form in (Stream(), ctypes.c_void_p(0x1230), 2):   # 2: the calling thread's default stream
+        binding._new_workspace(like, 64, form)
+    assert seen == [("external", 0x1230, DEV)] * 2 + [("external", 2, DEV)]
+    del seen[:]
+    for form in (1, ctypes.c_void_p(0), ctypes.c_void_p(1)):
+        binding._new_workspace(like, 64, form)
+    assert seen == [("default", DEV)] * 3
