@@ -332,7 +332,7 @@ def attn_fwd_splitkv_status(q, k, v, o, lse, causal: bool, scale: float, n_split
     B, Hq, Hkv, Sq, Sk, D = _check_layout(q, k, v, o, lse, "cuda")
     need = attn_splitkv_workspace_bytes(B, Hq, Sq, D, n_splits) if 1 <= n_splits <= 64 else 0
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _new_workspace(q, need, stream)
     if stream is None:
         stream = torch.cuda.current_stream(q.device).cuda_stream
     with torch.cuda.device(q.device):

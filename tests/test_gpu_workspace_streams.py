@@ -73,3 +73,18 @@ def test_stream_objects():
         lib.attn_bwd(dout, q, k, v, o, lse, *got, False, SCALE, stream=stream)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_split_keys():
+    q, k, v = normal(1, 8, 2, 128), normal(1, 3000, 2, 128), normal(1, 3000, 2, 128)
+    want = [torch.empty_like(q), torch.empty(1, 2, 8, device="cuda")]
+    lib.attn_fwd_splitkv(q, k, v, *want, False, SCALE, 4)
+    got = [torch.empty_like(t) for t in want]
+    need = lib.attn_splitkv_workspace_bytes(1, 2, 8, 128, 4)
+    beside_a_late_reader(need, lambda s: lib.attn_fwd_splitkv(q, k, v, *got, False, SCALE, 4, stream=s), got, want)
+    s = torch.cuda.Stream()
+    got[0].zero_()
+    torch.cuda.synchronize()
+    lib.attn_fwd_splitkv(q, k, v, *got, False, SCALE, 4, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0])

@@ -61,3 +61,27 @@ def test_every_form_of_a_stream(made):
     for form in (1, ctypes.c_void_p(0), ctypes.c_void_p(1)):
         binding._new_workspace(like, 64, form)
     assert seen == [("default", DEV)] * 3
+
+
+def test_split_keys_make_their_workspace_there_too(monkeypatch):
+    made, calls = [], []
+
+    class Lib:
+        def attn_splitkv_workspace_bytes(self, *sizes):
+            return 4096
+
+        def attn_fwd_splitkv(self, *args):
+            calls.append(args)
+            return 0
+
+    q = torch.zeros(1, 2, 2, 128, dtype=torch.bfloat16)
+    monkeypatch.setattr(binding, "load_library", Lib)
+    monkeypatch.setattr(binding, "_check_layout", lambda *a: (1, 2, 2, 2, 2, 128))
+    monkeypatch.setattr(torch.cuda, "device", lambda dev: contextlib.nullcontext())
+    monkeypatch.setattr(binding, "_new_workspace",
+                        lambda like, n, stream: made.append((like is q, n, stream)) or torch.zeros(n, dtype=torch.uint8))
+    assert binding.attn_fwd_splitkv_status(q, q, q, q, None, False, 1.0, 2, stream=0x1230) == 0
+    assert made == [(True, 4096, 0x1230)] and calls[0][-2:] == (4096, 0x1230)
+    own = torch.zeros(4096, dtype=torch.uint8)
+    assert binding.attn_fwd_splitkv_status(q, q, q, q, None, False, 1.0, 2, workspace=own, stream=0x1230) == 0
+    assert len(made) == 1 and calls[1][-3] == own.data_ptr()
