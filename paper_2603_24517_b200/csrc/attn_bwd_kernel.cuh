@@ -147,13 +147,13 @@ __device__ __forceinline__ int clc_answer(const void* answer) {
       "{\n\t"
       ".reg .pred p;\n\t"
       ".reg .b128 r;\n\t"
-      "mov.u32 %1, 0;\n\t"
       "ld.shared.b128 r, [%2];\n\t"
+      "mov.u32 %1, 0;\n\t"
       "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t"
       "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t"
       "}\n"
-      : "=r"(got), "=r"(x)
+      : "=&r"(got), "=&r"(x)  // no output may share the address's register
       : "r"(smem_u32(answer))
       : "memory");
   return got != 0 ? static_cast<int>(x) : -1;
