@@ -427,24 +427,29 @@ __device__ __forceinline__ void role_loader(const BwdParams& p, const BwdBarrier
   }
 }
 
+// For a wait that lasts as long as an item of `n` tile pairs: each of them (1.5 us or so) adds to the limit.
+__device__ __forceinline__ WaitCtx whole_item(WaitCtx ctx, int n) {
+  return WaitCtx{ctx.abort_flag, ctx.status, ctx.limit_ns + static_cast<uint64_t>(n) * 20000};
+}
+
 // TMA stores of the staged results; hands the slots back to the loader once they have been read.
 __device__ __forceinline__ void role_store(const BwdParams& p, const BwdBarriers& bars, uint8_t* smem,
                                            const volatile int* box, WaitCtx ctx, const CUtensorMap* tm_dq,
                                            const CUtensorMap* tm_dk, const CUtensorMap* tm_dv) {
   uint32_t pos_a = 0, pos_b = 0, stores = 0;
   BwdItem it;
-  for (int k = 0; next_item(bars, box, k, ctx, kRoleBwdStore, false, true, it); ++k) {
+  int unstaged = 0;  // tile pairs of the item before, if this warp does nothing for it and waits until its tiles are loaded
+  for (int k = 0; next_item(bars, box, k, whole_item(ctx, unstaged), kRoleBwdStore, false, true, it); ++k) {
     pos_a += it.n;
     pos_b += it.n;
+    unstaged = staged(p, it) ? 0 : it.n;
     if (!staged(p, it)) continue;
     uint8_t* slot_a = smem + kSmemRing + (pos_a % kRingA) * kTileBytes;
     uint8_t* slot_b = smem + kSmemRing + (kRingA + pos_b % kRingB) * kTileBytes;
     mbar_arrive(bars.stage_free);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      // this wait lasts as long as the item: every tile pair (1.5 us or so) adds to its limit
-      const WaitCtx whole{ctx.abort_flag, ctx.status, ctx.limit_ns + static_cast<uint64_t>(it.n) * 20000};
-      if (!mbar_wait(&bars.stage_full[half], stores & 1, whole, kRoleBwdStore | kBarStage)) return;
+      if (!mbar_wait(&bars.stage_full[half], stores & 1, whole_item(ctx, it.n), kRoleBwdStore | kBarStage)) return;
       if (it.keys) {  // half 0: dV in stream B's slot, half 1: dK in stream A's
         const CUtensorMap* tm = half == 0 ? tm_dv : tm_dk;
         uint8_t* src = half == 0 ? slot_b : slot_a;

@@ -61,7 +61,10 @@ constexpr int kMailboxInts = 12;                     // work index + the decoded
 constexpr int kSmemBytes = kSmemMisc + 8 + 2 * kMailboxInts * 4;
 static_assert(kSmemBytes <= 232448, "shared memory budget of one CTA");
 
-constexpr uint64_t kWaitLimitNs = 2000000000ull;  // every in-kernel wait gives up after 2 s
+#ifndef ATTN_WAIT_LIMIT_NS
+#define ATTN_WAIT_LIMIT_NS 2000000000ull
+#endif
+constexpr uint64_t kWaitLimitNs = ATTN_WAIT_LIMIT_NS;  // every in-kernel wait gives up after 2 s (or what a build sets)
 
 struct FwdParams {
   int B, Hq, Hkv, Sq, Sk;
