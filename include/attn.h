@@ -386,6 +386,24 @@ attn_status_t attn_bwd(const void* dout, const void* q, const void* k, const voi
                        int causal, float scale, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * attn_bwd_plan / attn_bwd_plan_item -- host-only introspection of attn_bwd's launch, as attn_plan and
+ * attn_plan_item are for the forward pass.  No device is touched.
+ *
+ * attn_bwd_plan fills plan[0..8] = { n_items, q_heads, pack_log2, n_q_tiles, n_k_tiles, key_splits, query_splits,
+ * run, run_extra }.  Short query sequences of a head group may be packed: then q_heads = Hkv and the rows of a query
+ * tile are (query row, head of the group), heads fastest, 2^pack_log2 of them; else q_heads = Hq, pack_log2 = 0.
+ * Units (batch, KV head) are launched in runs: the first run_extra runs hold `run` of them, the others run - 1.
+ *
+ * attn_bwd_plan_item fills item[0..8] = { keys, b, head, row0, first, per_head, t0, n, split } for work item `w` in
+ * launch order: a 128-key tile from key row0 on (keys = 1; head is a KV head) or a 128-row query tile (keys = 0; head
+ * is one of q_heads), and the tiles that stream past it: t0 <= t < t0 + n, where t is tile first + t % per_head of
+ * the t / per_head-th head of the group (keys), or key tile t.  split: which of key_splits / query_splits parts.
+ * Both return ATTN_ERR_SHAPE / ATTN_ERR_UNSUPPORTED like attn_bwd, ATTN_ERR_SHAPE for w out of range.
+ */
+attn_status_t attn_bwd_plan(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal, int* plan);
+attn_status_t attn_bwd_plan_item(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal, int w, int* item);
+
+/*
  * attn_bwd_strided -- attn_bwd on strided views; the strides follow attn_fwd_strided's rules, for
  * every tensor (rows of dq, of dk and of dv must not overlap; lse and dlse are contiguous).
  */

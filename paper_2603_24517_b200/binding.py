@@ -23,7 +23,7 @@ STATUS_NAMES = {
     5: "ATTN_ERR_CUDA", 6: "ATTN_ERR_ARCH", 7: "ATTN_ERR_TIMEOUT", 8: "ATTN_ERR_TOO_LARGE",
 }
 EXPORTED_SYMBOLS = ("attn_fwd", "attn_fwd_strided", "attn_fwd_host", "attn_fwd_noalloc", "attn_merge", "attn_merge_n",
-                    "attn_fwd_splitkv", "attn_splitkv_workspace_bytes", "attn_bwd", "attn_bwd_strided", "attn_bwd_workspace_bytes",
+                    "attn_fwd_splitkv", "attn_splitkv_workspace_bytes", "attn_bwd", "attn_bwd_strided", "attn_bwd_workspace_bytes", "attn_bwd_plan", "attn_bwd_plan_item",
                     "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes",
                     "attn_release_host_staging", "attn_set_option",
                     "attn_get_option",
@@ -88,6 +88,10 @@ def load_library() -> ctypes.CDLL:
     lib.attn_bwd_strided.restype = ci
     lib.attn_bwd_workspace_bytes.argtypes = [ci] * 7
     lib.attn_bwd_workspace_bytes.restype = ctypes.c_size_t
+    lib.attn_bwd_plan.argtypes = [ci] * 7 + [ctypes.POINTER(ci)]
+    lib.attn_bwd_plan.restype = ci
+    lib.attn_bwd_plan_item.argtypes = [ci] * 8 + [ctypes.POINTER(ci)]
+    lib.attn_bwd_plan_item.restype = ci
     rope_in = [vp, vp, vp, vp, ci, vp, vp, vp, ci, ctypes.POINTER(ctypes.c_longlong)]
     lib.attn_qk_norm_rope.argtypes = rope_in + [vp, vp] + [ci] * 8 + [cf] + [ll3] * 4 + [vp]
     lib.attn_qk_norm_rope.restype = ci
@@ -353,6 +357,25 @@ def attn_fwd_splitkv(q, k, v, o, lse, causal: bool, scale: float, n_splits: int,
 
 def attn_bwd_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Sk: int, D: int, causal: bool) -> int:
     return int(load_library().attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, int(bool(causal))))
+
+
+def attn_bwd_plan(B, Hq, Hkv, Sq, Sk, D, causal) -> dict:
+    """Host-only: how ``attn_bwd`` cuts a problem into work items (see include/attn.h)."""
+    out = (ctypes.c_int * 9)()
+    st = load_library().attn_bwd_plan(B, Hq, Hkv, Sq, Sk, D, int(bool(causal)), out)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_bwd_plan")
+    keys = ("n_items", "q_heads", "pack_log2", "n_q_tiles", "n_k_tiles", "key_splits", "query_splits", "run", "run_extra")
+    return dict(zip(keys, list(out)))
+
+
+def attn_bwd_plan_item(B, Hq, Hkv, Sq, Sk, D, causal, w) -> dict:
+    """Host-only: work item ``w`` of ``attn_bwd`` in launch order (see include/attn.h)."""
+    out = (ctypes.c_int * 9)()
+    st = load_library().attn_bwd_plan_item(B, Hq, Hkv, Sq, Sk, D, int(bool(causal)), w, out)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_bwd_plan_item")
+    return dict(zip(("keys", "b", "head", "row0", "first", "per_head", "t0", "n", "split"), list(out)))
 
 
 def _raw_stream(dev, stream):

@@ -228,15 +228,43 @@ attn_status_t bwd_device(const BwdTensors& t, int B, int Hq, int Hkv, int Sq, in
   return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
 }
 
+// The plan for sizes alone, checked as a call checks them.
+attn_status_t bwd_plan_of(BwdParams* p, int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal) {
+  int dummy = 0;
+  const attn_status_t st = check_args(&dummy, &dummy, &dummy, &dummy, nullptr, B, Hq, Hkv, Sq, Sk, D, causal, 1.0f, false);
+  if (st != ATTN_OK) return st;
+  return fill_bwd_plan(p, B, Hq, Hkv, Sq, Sk, causal) ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal) {
-  int dummy = 0;
-  if (check_args(&dummy, &dummy, &dummy, &dummy, nullptr, B, Hq, Hkv, Sq, Sk, D, causal, 1.0f, false) != ATTN_OK) return 0;
   BwdParams p;
-  return fill_bwd_plan(&p, B, Hq, Hkv, Sq, Sk, causal) ? bwd_workspace_bytes(p) : 0;
+  return bwd_plan_of(&p, B, Hq, Hkv, Sq, Sk, D, causal) == ATTN_OK ? bwd_workspace_bytes(p) : 0;
+}
+
+attn_status_t attn_bwd_plan(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal, int* plan) {
+  if (plan == nullptr) return ATTN_ERR_NULL;
+  BwdParams p;
+  const attn_status_t st = bwd_plan_of(&p, B, Hq, Hkv, Sq, Sk, D, causal);
+  if (st != ATTN_OK) return st;
+  const int out[] = {p.n_items, p.Hq, p.pack_log2, p.n_qt, p.n_kt, p.key_splits, p.qry_splits, p.run, p.run_extra};
+  std::memcpy(plan, out, sizeof(out));
+  return ATTN_OK;
+}
+
+attn_status_t attn_bwd_plan_item(int B, int Hq, int Hkv, int Sq, int Sk, int D, int causal, int w, int* item) {
+  if (item == nullptr) return ATTN_ERR_NULL;
+  BwdParams p;
+  const attn_status_t st = bwd_plan_of(&p, B, Hq, Hkv, Sq, Sk, D, causal);
+  if (st != ATTN_OK) return st;
+  if (w < 0 || w >= p.n_items) return ATTN_ERR_SHAPE;
+  const attn::bwd::BwdItem it = attn::bwd::decode_item(p, w);
+  const int out[] = {it.keys, it.b, it.h, it.row0, it.first, it.per_head, it.t0, it.n, it.split};
+  std::memcpy(item, out, sizeof(out));
+  return ATTN_OK;
 }
 
 attn_status_t attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
