@@ -368,11 +368,12 @@ attn_status_t attn_fwd_splitkv(const void* q, const void* k, const void* v, void
  *
  * Rows that see no key (causal, Sq > Sk; their lse is -infinity) have dq = 0 and contribute nothing,
  * whatever their dlse.  q, k, v, o and dout must be finite everywhere, at masked places and in such
- * rows too (a weight of 0 times NaN is NaN); lse finite or -infinity.  dq, dk, dv and workspace must not
+ * rows too (a weight of 0 times NaN is NaN); lse finite, or -infinity in rows that see no key.  dq, dk, dv and workspace must not
  * overlap each other or any input.  The options of attn_set_option concern the forward kernels only.
  * S, dP and the gradients accumulate in fp32 on the tensor cores and each output is rounded once;
  * P and dS are rounded to BF16 before the products that read them (kept as the sum of two BF16
- * numbers where Sq or Sk is at most 64: in sums of few terms a rounding shows in full).
+ * numbers where Sq or Sk is at most 64: in sums of few terms a rounding shows in full; the short sums
+ * inside a longer call, of the first rows and the last keys under the causal mask, keep one).
  * Every sum has a fixed order: the same call gives the same bits.  Asynchronous on `stream`, no
  * state is kept between calls: any number of calls may run at once, each with its own
  * workspace, and calls can be captured into a CUDA graph (after a first call on the device outside
@@ -436,7 +437,9 @@ attn_status_t attn_bwd_strided(const void* dout, const void* q, const void* k, c
  *   D           must be 128;  rot_dim  a multiple of 16 from 16 to 128;  eps  finite and > 0
  *   *_strides   as in attn_fwd_strided; NULL: contiguous.  An output may be a slice of a key cache
  *
- * A position outside the tables reads nothing there: that token's outputs are NaN.  Each row is
+ * q and k have one sequence length S and are both required.
+ * A position outside the tables reads nothing there: that token's outputs are NaN.  Rows whose sum of squares
+ * overflows fp32 (values of about 1e18) come out as zeros or NaN.  Each row is
  * computed by itself: infinities and NaN stay in their row.  Pointers 16-byte aligned (positions: their size).
  * Asynchronous on `stream`, one launch, no state; any number of calls may run at once, and after a first call
  * on the device calls can be captured.  Overlaps other than the one named are not allowed.

@@ -657,7 +657,8 @@ def attn_last_device_status():
 
 
 def attention_forward(q, k, v, causal: bool = False, scale: float | None = None, return_lse: bool = True):
-    """Convenience wrapper: allocates o (and lse) with torch and calls ``attn_fwd``."""
+    """Convenience wrapper: allocates o (and lse) with torch and calls ``attn_fwd``.  Not part of autograd's graph: its
+    gradients are ``attention_backward``'s."""
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1])
     o = torch.empty_like(q)
@@ -682,7 +683,7 @@ def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float
     """Gradients (dq, dk, dv) of ``attention_forward(q, k, v, causal, scale)`` from its results ``o``, ``lse`` and the
     gradient ``dout`` with respect to ``o`` (and ``dlse`` with respect to ``lse``).  Inputs may be views as in
     ``attn_fwd_strided``; a ``dout`` without an order of its own (the expanded gradient of a sum), and a ``dlse`` that is
-    not contiguous, is copied first.
+    not contiguous, is copied first; ``lse`` is contiguous, as the forward pass leaves it.
     The gradients are new contiguous tensors."""
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1])
@@ -699,7 +700,7 @@ def attention_backward(dout, q, k, v, o, lse, causal: bool = False, scale: float
 
 def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: float = 1e-6, interleaved: bool = False):
     """Convenience wrapper: the normed and rotated queries and keys as new contiguous tensors (see ``attn_qk_norm_rope``),
-    ready for ``attention_forward``."""
+    ready for ``attention_forward``.  Not part of autograd's graph (``qk_norm_rope_backward``)."""
     q_out, k_out = _new_like(q), _new_like(k)
     st = _rope_status(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, eps, interleaved, None, ())
     if st != ATTN_OK:

@@ -118,9 +118,10 @@ size_t bwd_workspace_bytes(const BwdParams& p) {
 }
 
 // Whether the gradients are sums of so few terms that P and dS are kept as two BF16 numbers (see attn_bwd_kernel.cuh).
-// With one, results with at most 64 rows or keys were up to 2.3 times as far off as a rounding of their own leaves them,
-// with more up to 1.57 times; with two 1.00 times, in 7 to 15 % more time (16 sequences of 64 rows, 32 heads: 48 -> 55 us;
-// one row, 32 heads on 8, 4 sequences of 32768 keys: 382 -> 415 us).
+// With one, results with at most 64 rows or keys were up to 2.3 times as far off as a rounding of their own leaves them;
+// with two 1.00 times, in 7 to 15 % more time (16 sequences of 64 rows, 32 heads: 48 -> 55 us;
+// one row, 32 heads on 8, 4 sequences of 32768 keys: 382 -> 415 us).  The rule is one for whole calls: short sums inside a
+// longer call (first rows and last keys under the causal mask) keep one number, and a long dq of one row gets two.
 constexpr int kFineRows = 64;
 bool fine_bwd(int Sq, int Sk) { return Sq <= kFineRows || Sk <= kFineRows; }
 

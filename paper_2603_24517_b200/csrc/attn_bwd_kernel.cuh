@@ -1156,7 +1156,9 @@ attn_bwd_prep_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict_
       }
       // [B][Hq][padded], or packed [B][Hkv][padded][group]
       const long long at = ((((b * Hq + h) >> pack_log2) * padded + s) << pack_log2) + (h & ((1 << pack_log2) - 1));
-      const bool none = l == -INFINITY;  // the row sees no key, or does not exist: P = exp2(-inf) = 0
+      // The row sees no key, or does not exist.  Its P is not always an exact 0 (the polynomial stops at 2^-126): rows that
+      // see no key vanish by the mask, rows that do not exist by their dO, which TMA fills with zeros, and delta 0.
+      const bool none = l == -INFINITY;
       neg_lse2[at] = none ? -INFINITY : -l * 1.4426950408889634f;
       neg_delta[at] = none ? 0.f : dl - sums[(threadIdx.x % rows) * heads + threadIdx.x / rows];
     }

@@ -13,8 +13,9 @@
 // shuffles of the packed BF16 words fetch it.  A warp works on 8 rows of one token and one tensor at a time: four
 // independent row loads per lane are in flight and the token's angles are read once for them; it does all its query
 // units before its key units, so weights and weight sums stay in registers; the arithmetic is in packed fp32 pairs.
-// Rows go through the caches as streams (evict first).  32768 tokens of 32 + 8 heads: forward 128 us, 5.3 TB/s,
-// gradient 199 us, 5.1 TB/s (the same accesses without the arithmetic: 111 and 196 us).  Measured slower: two rows a
+// Rows go through the caches as streams (evict first).  32768 tokens of 32 + 8 heads: forward 130 us, 5.2 TB/s,
+// gradient 203 us, 5.0 TB/s, as replayed launches (calls on a busy GPU 136 and 215 us; a timing copy with the same accesses
+// and no arithmetic 111 and 196 us, so the gradient is held by its access plan).  Measured slower: two rows a
 // lane (219 us), eight (176 us), the next unit's rows fetched ahead into registers (145 and 236 us) or shared memory (175
 // and 224 us: a warp's own chain of sums is what takes the time, and both cost resident warps or instructions),
 // more CTAs than resident (135 us); in the forward pass, rows in pairs with shared sums (131 us).
