@@ -481,6 +481,95 @@ attn_status_t attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, cons
                                     size_t workspace_bytes, void* stream);
 
 /*
+ * attn_kv_cache_t -- a paged key/value cache in 8 bits and the sequences of one call that live in it.  (The paper times
+ * attention over BF16 keys and values that a call brings along; a server keeps them between calls.)
+ *
+ *   k, v          codes [n_pages, page_size, Hkv, D], 8 bits each; strides {page, slot, head} in bytes, the head dimension
+ *                 contiguous.  Strides are positive multiples of 16, those of slot and head at least 128
+ *   k_scale, v_scale  FP32 [n_pages, Hkv]: a code c of a page and head stands for c * scale; finite, >= 0
+ *   block_table   int32 [B, max_blocks], rows table_stride elements apart: position p of sequence b is slot
+ *                 p % page_size of page block_table[b][p / page_size]
+ *   seq_lens      int32 [B]: tokens of each sequence, those of this call included
+ *   starts        NULL: every sequence has S rows in this call's tensors, [B, S, H, D].  Else int32 [B + 1], ascending: the
+ *                 tensors are packed, [S, H, D] with S rows in all, and rows starts[b] .. starts[b + 1] - 1 are sequence b's
+ *   type          ATTN_KV_E4M3 or ATTN_KV_INT8;  page_size 16, 32, 64 or 128;  D 128
+ *
+ * The n rows of a sequence are its last n positions, seq_lens - n .. seq_lens - 1, in all three calls below.  Pages may be
+ * shared by sequences; a page that a call writes must belong to one of them.  block_table, seq_lens and starts are read on the
+ * device.  A page number outside the cache, a block beyond max_blocks, rows outside [0, S) are read and written nowhere (below: what
+ * comes out); a sequence without rows takes no part, and packed rows that belong to no sequence are left as they were.
+ * The struct itself is read during the call only.
+ */
+typedef enum { ATTN_KV_E4M3 = 0, ATTN_KV_INT8 = 1 } attn_kv_type_t;
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  const int* block_table;
+  const int* seq_lens;
+  const int* starts;
+  long long k_strides[3];
+  long long v_strides[3];
+  long long table_stride;
+  int type;
+  int n_pages, page_size, Hkv, D;
+  int B, max_blocks;
+} attn_kv_cache_t;
+
+/*
+ * attn_kv_append -- quantises the keys and values of new tokens into their pages.  With A the largest finite magnitude of the
+ * new values of a page and head:
+ *
+ *     E4M3: s = the smallest power of two with A <= 448 s;   INT8: s = A / 127;   s = 0 where A = 0, else at least 2^-100
+ *     s = max(s, the page's scale) if the page holds earlier tokens of the sequence
+ *     code = x / s rounded to nearest even, and where s grew, the codes of the page's earlier slots = round(code s_old / s)
+ *
+ * A page whose slot 0 is written starts afresh: its old scale and codes do not count.  Infinities saturate; NaN becomes the
+ * E4M3 NaN, or 0 in INT8.  Appending E4M3 to pages filled elsewhere needs their scales to be powers of two.
+ *   k, v       BF16 [B, S, Hkv, D], or [S, Hkv, D] with starts (read); strides {batch, sequence, head} in elements as in
+ *              attn_fwd_strided (the batch stride is not used with starts); NULL: contiguous
+ * Rows at positions < 0 (seq_lens < n) or without a page are dropped.  The same call on the same cache gives the same bits, once
+ * more or again.  Asynchronous on `stream`, one launch, no state; any number of calls may run at once on pages of their own.
+ * Errors: ATTN_ERR_NULL, ATTN_ERR_SHAPE, ATTN_ERR_UNSUPPORTED (D, page_size, type, sizes beyond 2^30; tensors at one
+ * address), ATTN_ERR_ALIGN, ATTN_ERR_CUDA, ATTN_ERR_ARCH.
+ */
+attn_status_t attn_kv_append(const attn_kv_cache_t* cache, const void* k, const void* v, int S, const long long* k_strides,
+                             const long long* v_strides, void* stream);
+
+/*
+ * attn_kv_read -- the last tokens of each sequence back in BF16: code * scale, rounded once (written; shapes and strides as in
+ * attn_kv_append).  Rows at positions < 0 are zeros, rows without a page NaN.  Otherwise as attn_kv_append.
+ */
+attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S, const long long* k_strides,
+                           const long long* v_strides, void* stream);
+
+/*
+ * attn_fwd_cached -- attention of each sequence's rows over its tokens in the cache, as attn_fwd computes it over
+ * contiguous BF16 keys and values; append the rows' own keys and values first.
+ *
+ *   q          BF16 [B, S, Hq, D], or [S, Hq, D] with starts (read); Hq % Hkv == 0
+ *   o          BF16 like q (written); must not overlap q or the cache
+ *   lse        FP32 [B, Hq, S], or [Hq, S] with starts; may be NULL (written)
+ *   max_new    at least 1: about how many rows the longest sequence has; chooses the kernel, not the result's meaning
+ *   causal     non-zero: a row at position p sees the keys 0 .. p; 0: all of its sequence's keys
+ *   scale, strides  as in attn_fwd_strided (NULL: contiguous)
+ *   workspace  device memory, 16-byte aligned, attn_fwd_cached_workspace_bytes() bytes; contents undefined
+ *
+ * A row that sees no key has o = 0 and lse = -infinity.  A row that sees a key whose page does not exist has o and lse NaN.
+ * Slots behind a sequence's last token may hold anything; the codes and scales of its tokens, and q, must be finite.
+ * Scores and sums accumulate in fp32; queries and codes enter the products exactly (but query values 2^22 times smaller than
+ * the row's largest), weights with 11 bits; o is rounded once.  Values whose V scale is 2^-20 of the largest V scale of the
+ * sequence, or less, lose bits.  Sums have a fixed order: the same call gives the same bits on the same kind of GPU.
+ * Asynchronous on `stream`, no state; calls that may overlap, replays of one captured call too, need workspaces of their own.
+ * Errors: as attn_kv_append, ATTN_ERR_SHAPE also for head counts and max_new, ATTN_ERR_TOO_LARGE for a small workspace.
+ */
+size_t attn_fwd_cached_workspace_bytes(void);
+attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
+                              int causal, float scale, const long long* q_strides, const long long* o_strides, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
  * attn_selftest_wait_timeout -- exercises the bounded waits every kernel of this library uses
  * between its warp roles (the paper's kernels hand work between MMA, softmax, correction and
  * load warps "with barrier-based signaling", Section 2.2; here every such wait has a time limit).

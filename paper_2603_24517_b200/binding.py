@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -25,6 +26,7 @@ STATUS_NAMES = {
 EXPORTED_SYMBOLS = ("attn_fwd", "attn_fwd_strided", "attn_fwd_host", "attn_fwd_noalloc", "attn_merge", "attn_merge_n",
                     "attn_fwd_splitkv", "attn_splitkv_workspace_bytes", "attn_bwd", "attn_bwd_strided", "attn_bwd_workspace_bytes", "attn_bwd_plan", "attn_bwd_plan_item",
                     "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes",
+                    "attn_kv_append", "attn_kv_read", "attn_fwd_cached", "attn_fwd_cached_workspace_bytes",
                     "attn_release_host_staging", "attn_set_option",
                     "attn_get_option",
                     "attn_plan", "attn_plan_item", "attn_plan_item_pair", "attn_last_launch_clock", "attn_launch_clocks", "attn_selftest_wait_timeout", "attn_status_str", "attn_version",
@@ -33,6 +35,18 @@ EXPORTED_SYMBOLS = ("attn_fwd", "attn_fwd_strided", "attn_fwd_host", "attn_fwd_n
 _lib = None
 _BF16 = torch.bfloat16
 _LL3 = ctypes.c_longlong * 3
+
+
+_KV_TYPES = {torch.float8_e4m3fn: 0, torch.int8: 1}
+
+
+class _KvCacheStruct(ctypes.Structure):
+    """``attn_kv_cache_t`` of include/attn.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("k_strides", _LL3), ("v_strides", _LL3), ("table_stride", ctypes.c_longlong), ("type", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int),
+                ("B", ctypes.c_int), ("max_blocks", ctypes.c_int)]
 
 
 class AttnError(RuntimeError):
@@ -99,6 +113,15 @@ def load_library() -> ctypes.CDLL:
     lib.attn_qk_norm_rope_bwd.restype = ci
     lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = []
     lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
+    cache = ctypes.POINTER(_KvCacheStruct)
+    lib.attn_kv_append.argtypes = [cache, vp, vp, ci, ll3, ll3, vp]
+    lib.attn_kv_append.restype = ci
+    lib.attn_kv_read.argtypes = [cache, vp, vp, ci, ll3, ll3, vp]
+    lib.attn_kv_read.restype = ci
+    lib.attn_fwd_cached.argtypes = [cache, vp, vp, vp, ci, ci, ci, ci, cf, ll3, ll3, vp, ctypes.c_size_t, vp]
+    lib.attn_fwd_cached.restype = ci
+    lib.attn_fwd_cached_workspace_bytes.argtypes = []
+    lib.attn_fwd_cached_workspace_bytes.restype = ctypes.c_size_t
     lib.attn_selftest_wait_timeout.argtypes = [ci, vp]
     lib.attn_selftest_wait_timeout.restype = ci
     lib.attn_status_str.argtypes = [ci]
@@ -606,6 +629,146 @@ def attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq
         raise AttnError(st, "attn_qk_norm_rope_bwd")
 
 
+class KVCache(NamedTuple):
+    """A paged key/value cache in 8 bits: codes [pages, page_size, Hkv, D] (torch.float8_e4m3fn or torch.int8, any order of
+    the first three axes in memory) and a float32 scale [pages, Hkv] for each page and head (see ``attn_kv_cache_t``)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def new_kv_cache(n_pages: int, page_size: int, n_kv_heads: int, dtype=torch.float8_e4m3fn, device="cuda", head_dim: int = 128) -> KVCache:
+    """An empty cache whose pages lie head by head in memory ([page, head, slot, D])."""
+    if dtype not in _KV_TYPES:
+        raise ValueError("a cache is torch.float8_e4m3fn or torch.int8")
+    k, v = (torch.zeros(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype, device=device).transpose(1, 2) for _ in range(2))
+    k_scale, v_scale = (torch.zeros(n_pages, n_kv_heads, dtype=torch.float32, device=device) for _ in range(2))
+    return KVCache(k, v, k_scale, v_scale)
+
+
+def _page_strides(t):
+    """Byte strides of the (page, slot, head) axes of a [pages, page_size, Hkv, D] tensor of 8-bit codes as a C array."""
+    n, page, heads, D = t.shape
+    a, b, c, _ = t.stride()
+    return _LL3(page * heads * D if n == 1 else a, b, D if heads == 1 else c)
+
+
+def _kv_cache_struct(cache, block_table, seq_lens, starts):
+    k, v, k_scale, v_scale = cache
+    dev, kind, shape = k.device, k.dtype, k.shape
+    if dev.type != "cuda" or kind not in _KV_TYPES or len(shape) != 4 or v.shape != shape or v.dtype is not kind \
+            or v.device != dev or k.stride(3) != 1 or v.stride(3) != 1:
+        raise ValueError("a cache's k and v must be cuda tensors [pages, page_size, Hkv, D] of one shape, float8_e4m3fn or int8, "
+                         "with a contiguous last axis")
+    scales = (shape[0], shape[2])
+    if not (k_scale.dtype is torch.float32 and v_scale.dtype is torch.float32 and k_scale.shape == scales and v_scale.shape == scales
+            and k_scale.is_contiguous() and v_scale.is_contiguous() and k_scale.device == dev and v_scale.device == dev):
+        raise ValueError("a cache's scales must be contiguous float32 tensors [pages, Hkv] on its device")
+    if block_table.dtype is not torch.int32 or block_table.dim() != 2 or block_table.device != dev \
+            or (block_table.stride(1) != 1 and block_table.shape[1] > 1):
+        raise ValueError("block_table must be an int32 tensor [B, blocks] on the cache's device with a contiguous last axis")
+    B, blocks = block_table.shape
+    if seq_lens.dtype is not torch.int32 or seq_lens.shape != (B,) or not seq_lens.is_contiguous() or seq_lens.device != dev:
+        raise ValueError("seq_lens must be a contiguous int32 tensor [B] on the cache's device")
+    if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (B + 1,) or not starts.is_contiguous()
+                               or starts.device != dev):
+        raise ValueError("starts must be a contiguous int32 tensor [B + 1] on the cache's device")
+    return _KvCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
+                          seq_lens.data_ptr(), None if starts is None else starts.data_ptr(), _page_strides(k), _page_strides(v),
+                          block_table.stride(0) if B > 1 else blocks, _KV_TYPES[kind], shape[0], shape[1], shape[2], shape[3], B, blocks)
+
+
+def _cached_rows(c, starts, heads, dev, *named):
+    """Checks tensors of the call's rows, [B, S, heads, D] or [S, heads, D] with ``starts``; their S."""
+    shape = named[0][1].shape
+    if len(shape) != (4 if starts is None else 3) or shape[-1] != c.D or (starts is None and shape[0] != c.B) \
+            or (heads is not None and shape[-2] != heads):
+        raise ValueError(f"{named[0][0]} must be [B, S, heads, D], or [rows, heads, D] with starts, of the cache's D, and keys "
+                         "and values of its heads")
+    for name, t in named:
+        if t.dtype is not _BF16 or t.shape != shape or t.device != dev or t.stride(-1) != 1:
+            raise ValueError(f"{name} must be a bfloat16 tensor {list(shape)} with a contiguous last axis on the cache's device")
+    return shape[-3]
+
+
+def _row_strides(t):
+    """None for a contiguous tensor, else the C array of its (batch, sequence, head) strides; 3-D tensors have no batch axis."""
+    if t.is_contiguous():
+        return None
+    return _strides3(t if t.dim() == 4 else t[None])
+
+
+def _kv_rows_status(name, cache, k, v, block_table, seq_lens, starts, stream):
+    c = _kv_cache_struct(cache, block_table, seq_lens, starts)
+    dev = cache.k.device
+    S = _cached_rows(c, starts, c.Hkv, dev, ("k", k), ("v", v))
+    return _on_device(dev, getattr(load_library(), name), ctypes.byref(c), k.data_ptr(), v.data_ptr(), S, _row_strides(k), _row_strides(v),
+                      _raw_stream(dev, stream))
+
+
+def attn_kv_append_status(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> int:
+    """Calls ``attn_kv_append`` on CUDA tensors and returns its raw status code."""
+    return _kv_rows_status("attn_kv_append", cache, k, v, block_table, seq_lens, starts, stream)
+
+
+def attn_kv_append(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> None:
+    """``attn_kv_append`` of the C ABI: the keys and values k, v [B,S,Hkv,D] (or [rows,Hkv,D] with ``starts`` int32 [B+1]) of
+    new tokens, quantised into the pages of ``cache`` that ``block_table`` int32 [B,blocks] names; ``seq_lens`` int32 [B] counts
+    the new tokens in."""
+    st = attn_kv_append_status(cache, k, v, block_table, seq_lens, starts, stream)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_kv_append")
+
+
+def attn_kv_read_status(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> int:
+    """Calls ``attn_kv_read`` on CUDA tensors and returns its raw status code."""
+    return _kv_rows_status("attn_kv_read", cache, k, v, block_table, seq_lens, starts, stream)
+
+
+def attn_kv_read(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> None:
+    """``attn_kv_read`` of the C ABI: the last tokens of each sequence back into k, v (written; shapes as in ``attn_kv_append``)."""
+    st = attn_kv_read_status(cache, k, v, block_table, seq_lens, starts, stream)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_kv_read")
+
+
+def attn_fwd_cached_workspace_bytes() -> int:
+    return int(load_library().attn_fwd_cached_workspace_bytes())
+
+
+def attn_fwd_cached_status(q, cache, o, lse, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale=None,
+                           workspace=None, stream=None) -> int:
+    """Calls ``attn_fwd_cached`` on CUDA tensors and returns its raw status code.  ``workspace`` is a contiguous cuda tensor
+    (allocated here when None)."""
+    c = _kv_cache_struct(cache, block_table, seq_lens, starts)
+    dev = cache.k.device
+    S = _cached_rows(c, starts, None, dev, ("q", q), ("o", o))
+    Hq = q.shape[-2]
+    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.device != dev
+                            or lse.shape != ((c.B, Hq, S) if starts is None else (Hq, S))):
+        raise ValueError("lse must be a contiguous float32 tensor [B, Hq, S], or [Hq, rows] with starts, on the cache's device")
+    lib = load_library()
+    if workspace is None:
+        workspace = _new_workspace(q, lib.attn_fwd_cached_workspace_bytes(), stream)
+    elif not workspace.is_contiguous() or workspace.device != dev:
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    return _on_device(dev, lib.attn_fwd_cached, ctypes.byref(c), q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), Hq, S,
+                      S if max_new is None else int(max_new), 1 if causal else 0,
+                      float(scale) if scale is not None else 1.0 / math.sqrt(c.D), _row_strides(q), _row_strides(o),
+                      workspace.data_ptr(), workspace.nbytes, _raw_stream(dev, stream))
+
+
+def attn_fwd_cached(q, cache, o, lse, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale=None, workspace=None,
+                    stream=None) -> None:
+    """``attn_fwd_cached`` of the C ABI: attention of the rows q [B,S,Hq,D] (or [rows,Hq,D] with ``starts``), the last ones of
+    their sequences, over the cache -> o, lse [B,Hq,S] or [Hq,rows] (lse may be None).  ``max_new``: rows of the longest sequence
+    (a hint; None: all rows of a packed batch)."""
+    st = attn_fwd_cached_status(q, cache, o, lse, block_table, seq_lens, starts, max_new, causal, scale, workspace, stream)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_fwd_cached")
+
+
 def attn_selftest_wait_timeout(limit_ms: int, device=0, stream=None) -> None:
     """Launches the bounded-wait self-test (see include/attn.h); read the outcome with
     ``attn_last_device_status``."""
@@ -720,3 +883,33 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, po
     if st != ATTN_OK:
         raise AttnError(st, "attn_qk_norm_rope_bwd")
     return dq, dk, dq_weight, dk_weight
+
+
+def kv_cache_append(cache, k, v, block_table, seq_lens, starts=None) -> None:
+    """Puts new tokens' keys and values into a paged 8-bit cache (see ``attn_kv_append``)."""
+    attn_kv_append(cache, k, v, block_table, seq_lens, starts)
+
+
+def kv_cache_read(cache, block_table, seq_lens, starts=None, n: int | None = None):
+    """The last tokens of each sequence as new BF16 tensors (k, v): ``n`` of each sequence, [B, n, Hkv, D], or with ``starts`` the
+    ``n`` rows that it ends with, [n, Hkv, D] (rows behind its last one are undefined).  See ``attn_kv_read``."""
+    if n is None or n <= 0:
+        raise ValueError("n, the number of rows, must be given and positive")
+    heads, D = cache.k.shape[2:]
+    shape = (n, heads, D) if starts is not None else (block_table.shape[0], n, heads, D)
+    k, v = (torch.empty(shape, dtype=_BF16, device=cache.k.device) for _ in range(2))
+    attn_kv_read(cache, k, v, block_table, seq_lens, starts)
+    return k, v
+
+
+def attention_cached(q, cache, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale: float | None = None,
+                     return_lse: bool = True):
+    """Convenience wrapper: allocates o (and lse) with torch and calls ``attn_fwd_cached``.  q holds the queries of the last
+    tokens of each sequence, whose keys and values are in the cache already (``kv_cache_append``)."""
+    o = _new_like(q)
+    lse = None
+    if return_lse:
+        shape = (q.shape[1], q.shape[0]) if starts is not None else (q.shape[0], q.shape[2], q.shape[1])
+        lse = torch.empty(shape, dtype=torch.float32, device=q.device)
+    attn_fwd_cached(q, cache, o, lse, block_table, seq_lens, starts, max_new, causal, scale)
+    return (o, lse) if return_lse else o

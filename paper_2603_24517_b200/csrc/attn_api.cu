@@ -1,6 +1,6 @@
 // Host side of the C ABI declared in include/attn.h: argument checks, TMA descriptors,
 // persistent-grid set-up and the launch of attn_fwd_kernel.  The backward pass and the norm with
-// rotation have their entry points in attn_bwd_api.cuh and qk_norm_rope_api.cuh, included at the end.
+// rotation have their entry points in attn_bwd_api.cuh and qk_norm_rope_api.cuh, the paged cache in kv_cache_api.cuh, included at the end.
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -15,6 +15,7 @@
 #include "attn_merge_kernel.cuh"
 #include "attn_bwd_kernel.cuh"
 #include "qk_norm_rope_kernel.cuh"
+#include "attn_cached_kernel.cuh"
 
 namespace {
 
@@ -133,6 +134,10 @@ DeviceState* device_state(attn_status_t* st) {
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           attn::kv::kDecSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           attn::kv::kDecSmemBytes) != cudaSuccess ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||
       cudaMalloc(&d.status, 2 * sizeof(int)) != cudaSuccess ||
       cudaMemset(d.status, 0, 2 * sizeof(int)) != cudaSuccess ||
@@ -960,3 +965,4 @@ attn_status_t attn_last_device_status(int* code, int* detail) {
 
 #include "attn_bwd_api.cuh"
 #include "qk_norm_rope_api.cuh"
+#include "kv_cache_api.cuh"

@@ -1,0 +1,184 @@
+// Host side of attn_kv_append, attn_kv_read and attn_fwd_cached.  Included by attn_api.cu.
+#pragma once
+
+namespace {
+
+using attn::kv::CachedParams;
+using attn::kv::CacheView;
+using attn::kv::RowStrides;
+
+// Checks what all three share and fills the kernels' view of the cache.  `S`: rows a sequence, or rows in all with starts.
+attn_status_t cache_view(const attn_kv_cache_t* c, int S, CacheView* v) {
+  if (c == nullptr || c->k == nullptr || c->v == nullptr || c->k_scale == nullptr || c->v_scale == nullptr ||
+      c->block_table == nullptr || c->seq_lens == nullptr)
+    return ATTN_ERR_NULL;
+  if (c->B <= 0 || c->Hkv <= 0 || c->D <= 0 || c->n_pages <= 0 || c->page_size <= 0 || c->max_blocks <= 0 || S <= 0)
+    return ATTN_ERR_SHAPE;
+  if (c->D != attn::kv::kKvDim) return ATTN_ERR_UNSUPPORTED;
+  int page_log2 = 4;
+  while (page_log2 < 7 && (1 << page_log2) != c->page_size) ++page_log2;
+  if ((1 << page_log2) != c->page_size) return ATTN_ERR_UNSUPPORTED;
+  if (c->type != ATTN_KV_E4M3 && c->type != ATTN_KV_INT8) return ATTN_ERR_UNSUPPORTED;
+  // 32-bit positions and units
+  if (static_cast<long long>(c->max_blocks) * c->page_size > (1ll << 30) || c->Hkv > 32767) return ATTN_ERR_UNSUPPORTED;
+  if (S > (1 << 30) / (c->starts != nullptr ? 1 : c->B) || c->B > (1 << 24)) return ATTN_ERR_UNSUPPORTED;
+  if (misaligned(c->k, 15) || misaligned(c->v, 15) || misaligned(c->k_scale, 3) || misaligned(c->v_scale, 3) ||
+      misaligned(c->block_table, 3) || misaligned(c->seq_lens, 3) || misaligned(c->starts, 3))
+    return ATTN_ERR_ALIGN;
+  const long long* strides[2] = {c->k_strides, c->v_strides};
+  for (int t = 0; t < 2; ++t) {
+    for (int i = 0; i < 3; ++i) {
+      if (strides[t][i] <= 0) return ATTN_ERR_SHAPE;
+      if (strides[t][i] % 16 != 0) return ATTN_ERR_ALIGN;
+      if (strides[t][i] >= (1ll << 39)) return ATTN_ERR_UNSUPPORTED;
+    }
+    if (strides[t][1] < attn::kv::kKvDim || strides[t][2] < attn::kv::kKvDim) return ATTN_ERR_SHAPE;
+    v->sp[t] = strides[t][0];
+    v->ss[t] = strides[t][1];
+    v->sh[t] = strides[t][2];
+  }
+  if (c->table_stride < 0) return ATTN_ERR_SHAPE;
+  v->codes[0] = static_cast<uint8_t*>(c->k);
+  v->codes[1] = static_cast<uint8_t*>(c->v);
+  v->scales[0] = c->k_scale;
+  v->scales[1] = c->v_scale;
+  v->table = c->block_table;
+  v->table_stride = c->table_stride;
+  v->lens = c->seq_lens;
+  v->starts = c->starts;
+  v->B = c->B;
+  v->S = S;
+  v->Hkv = c->Hkv;
+  v->n_pages = c->n_pages;
+  v->page_log2 = page_log2;
+  v->max_blocks = c->max_blocks;
+  v->type = c->type;
+  return ATTN_OK;
+}
+
+// Strides of rows [B, S, H, D], or [S, H, D] of a packed batch (the first one is then not used).
+attn_status_t row_strides(const long long* s, bool packed, int S, int H, RowStrides* out) {
+  if (s == nullptr) {
+    const Strides3 c = contiguous_strides(S, H);
+    *out = RowStrides{c.b, c.s, c.h};
+    return ATTN_OK;
+  }
+  const long long checked[3] = {packed ? 128 : s[0], s[1], s[2]};
+  const attn_status_t st = check_strides(checked);
+  if (st == ATTN_OK) *out = RowStrides{checked[0], checked[1], checked[2]};
+  return st;
+}
+
+// What attn_kv_append and attn_kv_read share: arguments and the launch by pages.
+struct PageLaunch {
+  CacheView c;
+  RowStrides ks, vs;
+  dim3 grid;
+  int threads;
+};
+attn_status_t page_launch(const attn_kv_cache_t* cache, const void* k, const void* v, int S, const long long* k_strides,
+                          const long long* v_strides, PageLaunch* l) {
+  if (k == nullptr || v == nullptr) return ATTN_ERR_NULL;
+  attn_status_t st = cache_view(cache, S, &l->c);
+  if (st != ATTN_OK) return st;
+  if (misaligned(k, 15) || misaligned(v, 15)) return ATTN_ERR_ALIGN;
+  st = row_strides(k_strides, cache->starts != nullptr, S, cache->Hkv, &l->ks);
+  if (st == ATTN_OK) st = row_strides(v_strides, cache->starts != nullptr, S, cache->Hkv, &l->vs);
+  if (st != ATTN_OK) return st;
+  const long long units = attn::kv::unit_count(cache->starts != nullptr, l->c.B, S, l->c.page_log2);
+  if (units > 0x7fffffffLL) return ATTN_ERR_UNSUPPORTED;
+  l->grid = dim3(static_cast<unsigned>(units), 2u * l->c.Hkv);
+  l->threads = (cache->page_size / attn::kv::kSlotsPerWarp) * 32;
+  return ATTN_OK;
+}
+
+// A part of a tile for every CTA that may end in one or begin in one.
+size_t cached_parts(int ctas, int rows) { return 2ull * ctas * rows; }
+size_t cached_workspace(int ctas, int rows) {
+  return cached_parts(ctas, rows) * (attn::kv::kKvDim + 2) * sizeof(float) + static_cast<size_t>(ctas) * sizeof(int4);
+}
+constexpr int kWorkspaceCtas = 160;  // CTAs of a launch at most: one an SM
+
+}  // namespace
+
+extern "C" {
+
+attn_status_t attn_kv_append(const attn_kv_cache_t* cache, const void* k, const void* v, int S, const long long* k_strides,
+                             const long long* v_strides, void* stream) {
+  PageLaunch l;
+  attn_status_t st = page_launch(cache, k, v, S, k_strides, v_strides, &l);
+  if (st != ATTN_OK) return st;
+  if (k == cache->k || k == cache->v || v == cache->k || v == cache->v || cache->k == cache->v || cache->k_scale == cache->v_scale)
+    return ATTN_ERR_UNSUPPORTED;
+  if (device_state(&st) == nullptr) return st;
+  const uint16_t *kp = static_cast<const uint16_t*>(k), *vp = static_cast<const uint16_t*>(v);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (l.c.type == ATTN_KV_E4M3) {
+    attn::kv::kv_append_kernel<attn::kv::kE4m3><<<l.grid, l.threads, 0, s>>>(l.c, kp, vp, l.ks, l.vs);
+  } else {
+    attn::kv::kv_append_kernel<attn::kv::kInt8><<<l.grid, l.threads, 0, s>>>(l.c, kp, vp, l.ks, l.vs);
+  }
+  return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
+
+attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S, const long long* k_strides,
+                           const long long* v_strides, void* stream) {
+  PageLaunch l;
+  attn_status_t st = page_launch(cache, k, v, S, k_strides, v_strides, &l);
+  if (st != ATTN_OK) return st;
+  if (k == v || k == cache->k || k == cache->v || v == cache->k || v == cache->v) return ATTN_ERR_UNSUPPORTED;
+  if (device_state(&st) == nullptr) return st;
+  uint16_t *kp = static_cast<uint16_t*>(k), *vp = static_cast<uint16_t*>(v);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (l.c.type == ATTN_KV_E4M3) {
+    attn::kv::kv_read_kernel<attn::kv::kE4m3><<<l.grid, l.threads, 0, s>>>(l.c, kp, vp, l.ks, l.vs);
+  } else {
+    attn::kv::kv_read_kernel<attn::kv::kInt8><<<l.grid, l.threads, 0, s>>>(l.c, kp, vp, l.ks, l.vs);
+  }
+  return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
+
+size_t attn_fwd_cached_workspace_bytes(void) { return cached_workspace(kWorkspaceCtas, attn::kv::kDecRows); }
+
+attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
+                              int causal, float scale, const long long* q_strides, const long long* o_strides, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  if (q == nullptr || o == nullptr || workspace == nullptr) return ATTN_ERR_NULL;
+  CachedParams p;
+  std::memset(&p, 0, sizeof(p));
+  attn_status_t st = cache_view(cache, S, &p.c);
+  if (st != ATTN_OK) return st;
+  if (Hq <= 0 || Hq % cache->Hkv != 0 || max_new <= 0) return ATTN_ERR_SHAPE;
+  if (!std::isfinite(scale) || !(scale > 0.f)) return ATTN_ERR_UNSUPPORTED;
+  if (static_cast<long long>(S) * (Hq / cache->Hkv) > (1ll << 30)) return ATTN_ERR_UNSUPPORTED;
+  if (misaligned(q, 15) || misaligned(o, 15) || misaligned(lse, 3) || misaligned(workspace, 15)) return ATTN_ERR_ALIGN;
+  st = row_strides(q_strides, cache->starts != nullptr, S, Hq, &p.sq);
+  if (st == ATTN_OK) st = row_strides(o_strides, cache->starts != nullptr, S, Hq, &p.so);
+  if (st != ATTN_OK) return st;
+  if (o == q || o == cache->k || o == cache->v || workspace == q || workspace == o || workspace == cache->k || workspace == cache->v)
+    return ATTN_ERR_UNSUPPORTED;
+  if (workspace_bytes < attn_fwd_cached_workspace_bytes()) return ATTN_ERR_TOO_LARGE;
+  DeviceState* dev = device_state(&st);
+  if (dev == nullptr) return st;
+  p.q = static_cast<const uint16_t*>(q);
+  p.o = static_cast<uint16_t*>(o);
+  p.lse = lse;
+  p.Hq = Hq;
+  p.group = Hq / cache->Hkv;
+  p.causal = causal ? 1 : 0;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.ctas = dev->sm_count < kWorkspaceCtas ? dev->sm_count : kWorkspaceCtas;
+  p.parts = static_cast<float*>(workspace);
+  p.pieces = reinterpret_cast<int4*>(p.parts + cached_parts(p.ctas, attn::kv::kDecRows) * (attn::kv::kKvDim + 2));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (p.c.type == ATTN_KV_E4M3) {
+    attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3><<<p.ctas, attn::kv::kDecThreads, attn::kv::kDecSmemBytes, s>>>(p);
+  } else {
+    attn::kv::attn_cached_decode_kernel<attn::kv::kInt8><<<p.ctas, attn::kv::kDecThreads, attn::kv::kDecSmemBytes, s>>>(p);
+  }
+  if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
+  attn::kv::attn_cached_join_kernel<attn::kv::kDecRows><<<dim3(p.ctas, attn::kv::kDecRows), 256, 0, s>>>(p);
+  return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
+
+}  // extern "C"
