@@ -526,7 +526,7 @@ typedef struct {
  *     code = x / s rounded to nearest even, and where s grew, the codes of the page's earlier slots = round(code s_old / s)
  *
  * A page whose slot 0 is written starts afresh: its old scale and codes do not count.  Infinities saturate; NaN becomes the
- * E4M3 NaN, or 0 in INT8.  Appending E4M3 to pages filled elsewhere needs their scales to be powers of two.
+ * E4M3 NaN, or 0 in INT8.  (A value within 2^-4 of 2^128 may round to that, and is read back as infinity.)  Appending E4M3 to pages filled elsewhere needs their scales to be powers of two.
  *   k, v       BF16 [B, S, Hkv, D], or [S, Hkv, D] with starts (read); strides {batch, sequence, head} in elements as in
  *              attn_fwd_strided (the batch stride is not used with starts); NULL: contiguous
  * Rows at positions < 0 (seq_lens < n) or without a page are dropped.  The same call on the same cache gives the same bits, once
