@@ -554,7 +554,7 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
  *   max_new    at least 1: about how many rows the longest sequence has; chooses the kernel, not the result's meaning
  *   causal     non-zero: a row at position p sees the keys 0 .. p; 0: all of its sequence's keys
  *   scale, strides  as in attn_fwd_strided (NULL: contiguous)
- *   workspace  device memory, 16-byte aligned, attn_fwd_cached_workspace_bytes() bytes; contents undefined
+ *   workspace  device memory, 16-byte aligned, attn_fwd_cached_workspace_bytes(Hq, Hkv, max_new) bytes; contents undefined
  *
  * A row that sees no key has o = 0 and lse = -infinity.  A row that sees a key whose page does not exist has o and lse NaN.
  * Slots behind a sequence's last token may hold anything; the codes and scales of its tokens, and q, must be finite.
@@ -564,7 +564,7 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
  * Asynchronous on `stream`, no state; calls that may overlap, replays of one captured call too, need workspaces of their own.
  * Errors: as attn_kv_append, ATTN_ERR_SHAPE also for head counts and max_new, ATTN_ERR_TOO_LARGE for a small workspace.
  */
-size_t attn_fwd_cached_workspace_bytes(void);
+size_t attn_fwd_cached_workspace_bytes(int Hq, int Hkv, int max_new); /* 0: arguments attn_fwd_cached refuses */
 attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
                               int causal, float scale, const long long* q_strides, const long long* o_strides, void* workspace,
                               size_t workspace_bytes, void* stream);

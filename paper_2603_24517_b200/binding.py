@@ -120,7 +120,7 @@ def load_library() -> ctypes.CDLL:
     lib.attn_kv_read.restype = ci
     lib.attn_fwd_cached.argtypes = [cache, vp, vp, vp, ci, ci, ci, ci, cf, ll3, ll3, vp, ctypes.c_size_t, vp]
     lib.attn_fwd_cached.restype = ci
-    lib.attn_fwd_cached_workspace_bytes.argtypes = []
+    lib.attn_fwd_cached_workspace_bytes.argtypes = [ci, ci, ci]
     lib.attn_fwd_cached_workspace_bytes.restype = ctypes.c_size_t
     lib.attn_selftest_wait_timeout.argtypes = [ci, vp]
     lib.attn_selftest_wait_timeout.restype = ci
@@ -733,8 +733,8 @@ def attn_kv_read(cache, k, v, block_table, seq_lens, starts=None, stream=None) -
         raise AttnError(st, "attn_kv_read")
 
 
-def attn_fwd_cached_workspace_bytes() -> int:
-    return int(load_library().attn_fwd_cached_workspace_bytes())
+def attn_fwd_cached_workspace_bytes(Hq: int, Hkv: int, max_new: int) -> int:
+    return int(load_library().attn_fwd_cached_workspace_bytes(Hq, Hkv, max_new))
 
 
 def attn_fwd_cached_status(q, cache, o, lse, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale=None,
@@ -748,13 +748,14 @@ def attn_fwd_cached_status(q, cache, o, lse, block_table, seq_lens, starts=None,
     if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.device != dev
                             or lse.shape != ((c.B, Hq, S) if starts is None else (Hq, S))):
         raise ValueError("lse must be a contiguous float32 tensor [B, Hq, S], or [Hq, rows] with starts, on the cache's device")
+    max_new = S if max_new is None else int(max_new)
     lib = load_library()
     if workspace is None:
-        workspace = _new_workspace(q, lib.attn_fwd_cached_workspace_bytes(), stream)
+        workspace = _new_workspace(q, max(lib.attn_fwd_cached_workspace_bytes(Hq, c.Hkv, max_new), 16), stream)
     elif not workspace.is_contiguous() or workspace.device != dev:
         raise ValueError("workspace must be a contiguous tensor on the cache's device")
     return _on_device(dev, lib.attn_fwd_cached, ctypes.byref(c), q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), Hq, S,
-                      S if max_new is None else int(max_new), 1 if causal else 0,
+                      max_new, 1 if causal else 0,
                       float(scale) if scale is not None else 1.0 / math.sqrt(c.D), _row_strides(q), _row_strides(o),
                       workspace.data_ptr(), workspace.nbytes, _raw_stream(dev, stream))
 

@@ -16,6 +16,7 @@
 #include "attn_bwd_kernel.cuh"
 #include "qk_norm_rope_kernel.cuh"
 #include "attn_cached_kernel.cuh"
+#include "attn_cached_tile_kernel.cuh"
 
 namespace {
 
@@ -138,6 +139,10 @@ DeviceState* device_state(attn_status_t* st) {
                            attn::kv::kDecSmemBytes) != cudaSuccess ||
       cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::kv::kDecSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           attn::kv::kTSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           attn::kv::kTSmemBytes) != cudaSuccess ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||
       cudaMalloc(&d.status, 2 * sizeof(int)) != cudaSuccess ||
       cudaMemset(d.status, 0, 2 * sizeof(int)) != cudaSuccess ||

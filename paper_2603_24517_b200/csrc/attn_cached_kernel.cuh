@@ -45,6 +45,8 @@ struct CachedParams {
   float* parts;           // [2 ctas][rows][kKvDim], then [2 ctas][rows][2] (reference maximum in log2 units, sum)
   int4* pieces;           // [ctas]: {sequence, head, tile, last CTA with a part} of the tile the CTA began and did not end
   int ctas;
+  int min_steps;          // a piece has at least about so many
+  int* status;            // bounded waits that ran out, see WaitCtx
 };
 
 // One sequence of the line of work.
@@ -130,7 +132,7 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   long long total = 0;
   for (int w = 0; w < warps; ++w) total += scratch[w];
   line.total = total;
-  line.ctas = min(static_cast<long long>(p.ctas), total);
+  line.ctas = min(static_cast<long long>(p.ctas), (total + p.min_steps - 1) / p.min_steps);
   if (blockIdx.x >= line.ctas) return false;
   line.begin = total * blockIdx.x / line.ctas;
   line.end = total * (blockIdx.x + 1) / line.ctas;
@@ -537,58 +539,77 @@ __global__ void __launch_bounds__(kDecThreads, 1) attn_cached_decode_kernel(cons
 }
 
 // Joins the parts of a tile that several CTAs worked on: sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, parts in order.
-// Grid: (ctas, rows); a block joins one row of the tile that CTA blockIdx.x began and did not end.
+// Grid: (ctas, ROWS / 8); a block joins 8 rows of the tile that CTA blockIdx.x began and did not end, a warp a row.  Where a tile
+// is spread over many CTAs the block takes the rows one after another and its warps share the parts.
+constexpr int kJoinRows = 8;
+constexpr int kJoinMany = 12;
+
+struct JoinRow {
+  float top, sum;
+};
+// The joint maximum and sum of a row, in every lane: the lanes' terms and then the lanes in a fixed order.
+template <class Slot>
+__device__ __forceinline__ JoinRow join_stats(const float2* stats, const Slot& slot, int n, int lane) {
+  JoinRow j{-INFINITY, 0.f};
+  for (int i = lane; i < n; i += 32) j.top = fmaxf(j.top, stats[slot(i)].x);
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) j.top = fmaxf(j.top, __shfl_xor_sync(0xffffffffu, j.top, k));
+  for (int i = lane; i < n; i += 32) {
+    const float2 ml = stats[slot(i)];
+    j.sum += ml.x == -INFINITY ? ml.y : ml.y * ex2_approx(ml.x - j.top);
+  }
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) j.sum += __shfl_xor_sync(0xffffffffu, j.sum, k);
+  return j;
+}
+
 template <int ROWS>
 __global__ void __launch_bounds__(256) attn_cached_join_kernel(const CachedParams p) {
   __shared__ float4 sums[8][32];
   const int4 piece = p.pieces[blockIdx.x];
   if (piece.w < 0) return;
   const SeqWork s = seq_work(p.c, piece.x);
-  const int r = blockIdx.y;
-  const TilePlace w = tile_place(p, s, piece.y, static_cast<long long>(piece.z) * ROWS + r);
-  if (!w.real) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int first = blockIdx.x, n = piece.w - first + 1;
   const float2* stats = reinterpret_cast<const float2*>(p.parts + 2ll * p.ctas * ROWS * kKvDim);
-  auto slot = [&](int i) { return (2ll * (first + i) + (i == 0 ? 1 : 0)) * ROWS + r; };
-  float top = -INFINITY;
-  for (int i = lane; i < n; i += 32) top = fmaxf(top, stats[slot(i)].x);
-#pragma unroll
-  for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-  float sum = 0.f;  // every warp: the whole sum, a lane's terms and then the lanes in a fixed order
-  for (int i = lane; i < n; i += 32) {
-    const float2 ml = stats[slot(i)];
-    sum += ml.x == -INFINITY ? ml.y : ml.y * ex2_approx(ml.x - top);
-  }
-#pragma unroll
-  for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const bool many = n > kJoinMany;
+  for (int k = many ? 0 : warp; k < kJoinRows; k += many ? 1 : kJoinRows) {
+    const int r = blockIdx.y * kJoinRows + k;
+    const TilePlace w = tile_place(p, s, piece.y, static_cast<long long>(piece.z) * ROWS + r);
+    if (!w.real) break;  // rows are in order: none behind it is
+    auto slot = [&](int i) { return (2ll * (first + i) + (i == 0 ? 1 : 0)) * ROWS + r; };
+    const JoinRow j = join_stats(stats, slot, n, lane);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int i = warp; i < n; i += 8) {
-    const float m = stats[slot(i)].x;
-    const float4 x = reinterpret_cast<const float4*>(p.parts + slot(i) * kKvDim)[lane];
-    const float f = m == -INFINITY ? 0.f : ex2_approx(m - top);
-    o.x += x.x * f;
-    o.y += x.y * f;
-    o.z += x.z * f;
-    o.w += x.w * f;
-  }
-  sums[warp][lane] = o;
-  __syncthreads();
-  if (warp != 0) return;
+    for (int i = many ? warp : 0; i < n; i += many ? 8 : 1) {
+      const float m = stats[slot(i)].x;
+      const float4 x = reinterpret_cast<const float4*>(p.parts + slot(i) * kKvDim)[lane];
+      const float f = m == -INFINITY ? 0.f : ex2_approx(m - j.top);
+      o.x += x.x * f;
+      o.y += x.y * f;
+      o.z += x.z * f;
+      o.w += x.w * f;
+    }
+    if (many) {
+      __syncthreads();  // the row before has been read
+      sums[warp][lane] = o;
+      __syncthreads();
+      if (warp != 0) continue;
 #pragma unroll
-  for (int k = 1; k < 8; ++k) {
-    const float4 x = sums[k][lane];
-    o.x += x.x;
-    o.y += x.y;
-    o.z += x.z;
-    o.w += x.w;
+      for (int i = 1; i < 8; ++i) {
+        const float4 x = sums[i][lane];
+        o.x += x.x;
+        o.y += x.y;
+        o.z += x.z;
+        o.w += x.w;
+      }
+    }
+    const float inv = j.sum > 0.f ? 1.f / j.sum : j.sum == 0.f ? 0.f : j.sum;
+    const uint2 y = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    *reinterpret_cast<uint2*>(p.o + row_offset(p, p.so, piece.x, s, w) + lane * 4) = y;
+    if (lane == 0 && p.lse != nullptr)
+      p.lse[lse_index(p, piece.x, s, w)] = j.sum == 0.f ? -INFINITY : (j.top - kWeightShift + log2f(j.sum)) * kLn2;
   }
-  const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-  const uint2 y = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-  *reinterpret_cast<uint2*>(p.o + row_offset(p, p.so, piece.x, s, w) + lane * 4) = y;
-  if (lane == 0 && p.lse != nullptr)
-    p.lse[lse_index(p, piece.x, s, w)] = sum == 0.f ? -INFINITY : (top - kWeightShift + log2f(sum)) * kLn2;
 }
 
 }  // namespace kv

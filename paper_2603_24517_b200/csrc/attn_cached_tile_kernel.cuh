@@ -1,0 +1,636 @@
+// Attention of new tokens over a paged 8-bit cache, for many query rows a key head (prompts, chunks): tensor cores.
+//
+// The scheme of the forward kernel: a CTA holds two 128-row query tiles ("stages") against one stream of 128-key tiles, S and
+// O in tensor memory, one softmax thread a row.  A query tile's rows are (token, head of the group), heads fastest, so a key
+// head is read once for its group.  What differs:
+//
+//   warps 0-7    softmax; each thread also brings its row of Q into shared memory, as f16 scaled by a power of two of the row
+//   warps 8-11   O / l -> BF16 -> memory, or an fp32 part where the tile's keys are spread over CTAs
+//   warp  12     tcgen05.mma, f16 operands
+//   warps 13-15  converters: codes by 16-byte asynchronous copies (any page size, order and length; what lies behind the last
+//                token is zeros) into 32 KB of staging, from there exactly to f16 in the swizzled ring of K / V tiles.  A lane
+//                converts what it has copied itself, so the staging needs no barrier; a piece is requested again for the
+//                next step as soon as it is converted.  They sit on the sub-partitions that the MMA warp does not share
+//
+// Scales: 16 keys ("a granule") lie in one page.  K's scale multiplies the row's factor granule by granule, V's enters the
+// exponent as log2 of its ratio to the largest V scale so far, and is taken out of the row sum again granule by granule, so
+// both products run on bare codes.  When the largest V scale grows, O is rescaled as for a grown row maximum.
+//
+// Work: the line of (sequence, key head, tile pair, 128 keys) steps cut into equal pieces, as in the decoding kernel; every
+// role walks its CTA's piece by itself.  Bound by the softmax / tensor pipe chain of the forward kernel.
+#pragma once
+
+#include "attn_cached_kernel.cuh"
+
+namespace attn {
+namespace kv {
+
+constexpr int kTileRows = 256;  // rows of a work item: two stages
+constexpr int kConvWarps = 3;
+
+constexpr int kTSmemQ = 0;
+constexpr int kTSmemKv = 2 * kTileBytes;
+constexpr int kTSmemRaw = kTSmemKv + kKvSlots * kTileBytes;      // codes of one K and one V tile
+constexpr int kTSmemStats = kTSmemRaw + 2 * kTile * kKvDim;      // float [2 stages][2][128]
+constexpr int kMetaSteps = 4;
+constexpr int kMetaFloats = 32;
+constexpr int kTSmemMeta = kTSmemStats + 2 * 2 * kTile * 4;
+constexpr int kTSmemBars = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
+constexpr int kTNumBars = 2 + 2 * kKvSlots + 2 * 7 + kMetaSteps;
+constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
+constexpr int kTSmemBytes = kTSmemMisc + 16;
+static_assert(kTSmemBytes <= 232448, "shared memory budget of one CTA");
+static_assert(kHeadDim == kKvDim && kTile == kStepKeys, "one head dimension, one tile");
+
+// What the converters tell the softmax warps about a step.
+enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaGrow = 25, kMetaBad = 26 };
+constexpr float kMinRatioLog2 = -60.f;  // V scales below 2^-60 of the largest count as that: nothing in f16
+
+struct TileBarriers {
+  uint64_t* q_full;    // [2] softmax (4 warps): the stage's Q is in shared memory -> MMA
+  uint64_t* kv_full;   // [kKvSlots] converters (3 warps) -> MMA
+  uint64_t* kv_empty;  // [kKvSlots] MMA commit -> converters
+  uint64_t* s_full;    // [2] MMA commit -> softmax
+  uint64_t* p_half;    // [2] softmax (4 warps): the first 64 keys of P -> MMA
+  uint64_t* p_full;    // [2] softmax (4 warps) -> MMA
+  uint64_t* o_full;    // [2] MMA commit (last P V) -> epilogue
+  uint64_t* o_empty;   // [2] epilogue (4 warps) -> MMA
+  uint64_t* l_full;    // [2] softmax (128 threads) -> epilogue
+  uint64_t* l_empty;   // [2] epilogue (128 threads) -> softmax
+  uint64_t* meta_full; // [kMetaSteps] first converter warp -> softmax
+};
+enum : int { kRoleConvert = 6 << 8, kBarMeta = 20 };
+
+constexpr uint32_t make_idesc_f16(uint32_t b_mn_major) {  // as make_idesc_bf16, both operand formats 0
+  return (1u << 4) | (b_mn_major << 16) | ((kTile >> 3) << 17) | ((kTile >> 4) << 24);
+}
+constexpr uint32_t kIdescQKf16 = make_idesc_f16(0);
+constexpr uint32_t kIdescPVf16 = make_idesc_f16(1);
+
+// One tile pair, or the CTA's piece of it.
+struct Item {
+  int t_first, n;   // steps
+  bool two;         // the second stage has rows
+  bool whole;       // all of the tile's steps
+};
+__device__ __forceinline__ Item item_of(const CachedParams& p, const Line& line, const Cursor<kTileRows>& c, long long at) {
+  Item it;
+  it.t_first = c.t;
+  it.n = static_cast<int>(min(static_cast<long long>(c.steps - c.t), line.end - at));
+  it.two = static_cast<long long>(c.tile) * kTileRows + kTile < static_cast<long long>(c.s.n) * p.group;
+  it.whole = c.t == 0 && it.n == c.steps;
+  return it;
+}
+
+// ---- converters ------------------------------------------------------------------------------------------------------
+struct StepPlace {  // where a step's codes are; `page` is that of granule (lane & 7): -1 does not exist, -2 behind the last token
+  int page, h, key0, keys;
+  bool first;       // of its item in this CTA
+};
+
+template <int TYPE>
+__device__ __forceinline__ void role_convert(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
+                                             const Line& line, Cursor<kTileRows> ahead, int cw, int lane) {
+  const CacheView& c = p.c;
+  const int slot_mask = (1 << c.page_log2) - 1;
+  long long left = line.end - line.begin;  // steps whose pages have not been looked up yet
+  bool first = true;
+  auto look_up = [&]() {
+    StepPlace f;
+    f.keys = 0;  // no step: nothing is copied
+    f.page = -2;
+    f.h = f.key0 = 0;
+    f.first = false;
+    if (left > 0) {
+      --left;
+      f.h = ahead.h;
+      f.key0 = ahead.t * kStepKeys;
+      f.keys = ahead.s.keys;
+      f.first = first || ahead.t == 0;
+      first = false;
+      const int key = f.key0 + (lane & 7) * 16;
+      if (key < f.keys) f.page = page_of(c, ahead.b, key >> c.page_log2);
+      if (++ahead.t >= ahead.steps && left > 0) ahead.next_tile(p);
+    }
+    return f;
+  };
+  auto scale_of = [&](const StepPlace& f) {  // lanes 0-7: K's of granule lane, 8-15: V's of granule lane - 8
+    return lane < 16 && f.page >= 0 ? __ldg(c.scales[lane >> 3] + static_cast<long long>(f.page) * c.Hkv + f.h) : 0.f;
+  };
+  const int sub = lane >> 2;  // row of a group of 8
+  // the lane's two 16-byte pieces (units lane & 3 and 4 + lane & 3) of row 8 rg + sub
+  auto request = [&](const StepPlace& f, int kv, int rg) {
+    const int page = __shfl_sync(0xffffffffu, f.page, rg >> 1);
+    const int key = f.key0 + rg * 8 + sub;
+    const bool take = page >= 0 && key < f.keys;
+    const uint8_t* src = c.codes[kv];
+    if (take) src += page * c.sp[kv] + f.h * c.sh[kv] + (key & slot_mask) * c.ss[kv] + (lane & 3) * 16;
+    const uint32_t dst = smem_u32(smem) + kTSmemRaw + kv * kTile * kKvDim + rg * 1024 + lane * 16;
+    cp_async16(dst, src, take);
+    cp_async16(dst + 512, take ? src + 64 : src, take);
+  };
+
+  StepPlace now = look_up(), next = look_up();
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    for (int rg = (cw + kv) % kConvWarps; rg < 16; rg += kConvWarps) request(now, kv, rg);
+    cp_async_commit();
+  }
+  float scale_now = scale_of(now);
+  float vref = 0.f;
+  uint32_t kv_cnt = 0;
+  const long long steps = line.end - line.begin;
+  for (long long i = 0; i < steps; ++i) {
+    const StepPlace after = look_up();
+    const float scale_next = scale_of(next);
+    if (cw == 0) {
+      if (now.first) vref = 0.f;
+      float top = lane >= 8 && lane < 16 ? scale_now : 0.f;
+#pragma unroll
+      for (int m = 4; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+      top = __shfl_sync(0xffffffffu, top, 8);
+      const float ref = fmaxf(fmaxf(vref, top), 1e-30f);
+      float* meta = reinterpret_cast<float*>(smem + kTSmemMeta) + (i % kMetaSteps) * kMetaFloats;
+      const unsigned bad = __ballot_sync(0xffffffffu, lane < 8 && now.page == -1);
+      if (lane < 8) {
+        meta[kMetaK + lane] = scale_now;
+      } else if (lane < 16) {
+        const float ratio = now.page >= 0 ? fmaxf(lg2_approx(__fdividef(scale_now, ref)), kMinRatioLog2) : 0.f;
+        meta[kMetaV + lane - 8] = ratio;
+        meta[kMetaInv + lane - 8] = ex2_approx(-ratio);
+      } else if (lane == 16) {
+        meta[kMetaVref] = ref;
+        meta[kMetaGrow] = vref == ref ? 1.f : __fdividef(vref, ref);
+        reinterpret_cast<int*>(meta)[kMetaBad] = bad != 0 ? (__ffs(bad) - 1) * 16 : kStepKeys;
+      }
+      vref = ref;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars.meta_full[i % kMetaSteps]);
+    }
+#pragma unroll 1
+    for (int kv = 0; kv < 2; ++kv) {
+      const uint32_t slot = kv_cnt % kKvSlots;
+      const bool ok = mbar_wait_warp(&bars.kv_empty[slot], ((kv_cnt / kKvSlots) & 1) ^ 1, ctx, kRoleConvert | kBarKvEmpty);
+      if (!ok) {
+        cp_async_wait<0>();
+        return;
+      }
+      ++kv_cnt;
+      cp_async_wait<1>();
+      uint8_t* tile = smem + kTSmemKv + slot * kTileBytes;
+#pragma unroll 2
+      for (int rg = (cw + kv) % kConvWarps; rg < 16; rg += kConvWarps) {
+        const uint8_t* raw = smem + kTSmemRaw + kv * kTile * kKvDim + rg * 1024 + lane * 16;
+        uint8_t* row = tile + (rg * 8 + sub) * 128;
+        const int ch = (lane & 3) * 2;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint4 w = *reinterpret_cast<const uint4*>(raw + half * 512);
+          uint4 lo, hi;
+          codes_to_f16<TYPE>(w.x, lo.x, lo.y);
+          codes_to_f16<TYPE>(w.y, lo.z, lo.w);
+          codes_to_f16<TYPE>(w.z, hi.x, hi.y);
+          codes_to_f16<TYPE>(w.w, hi.z, hi.w);
+          *reinterpret_cast<uint4*>(row + half * kHalfBytes + ((ch ^ sub) << 4)) = lo;
+          *reinterpret_cast<uint4*>(row + half * kHalfBytes + (((ch + 1) ^ sub) << 4)) = hi;
+        }
+        request(next, kv, rg);  // the piece has been read: its conversion is done
+      }
+      cp_async_commit();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars.kv_full[slot]);
+    }
+    now = next;
+    next = after;
+    scale_now = scale_next;
+  }
+  cp_async_wait<0>();
+}
+
+// ---- MMA --------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void issue_qk_f16(bool leader, uint32_t tmem_s, uint64_t q_desc, uint64_t k_desc) {
+  if (leader) {
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const uint32_t off = (kk >> 2) * kHalfBytes + (kk & 3) * 32;
+      mma_ss(tmem_s, desc_advance(q_desc, off), desc_advance(k_desc, off), kIdescQKf16, kk > 0);
+    }
+  }
+}
+__device__ __forceinline__ void issue_pv_f16(bool leader, uint32_t tmem_o, uint32_t tmem_p, uint64_t v_desc, bool accumulate,
+                                             int kk_begin, int kk_end) {
+  if (leader) {
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      if (kk >= kk_begin && kk < kk_end) {
+        mma_ts(tmem_o, tmem_p + kk * 8, desc_advance(v_desc, kk * 2048), kIdescPVf16, (accumulate || kk > 0) ? 1u : 0u);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void role_tile_mma(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
+                                              const Line& line, Cursor<kTileRows> cur, uint32_t tmem) {
+  const bool leader = elect_one();
+  const uint32_t base = smem_u32(smem);
+  const uint64_t q_desc[2] = {kmajor_desc(base + kTSmemQ), kmajor_desc(base + kTSmemQ + kTileBytes)};
+  uint32_t kv_cnt = 0;
+  uint32_t q_cnt[2] = {0, 0};
+  uint32_t sp_cnt[2] = {0, 0};
+  for (long long at = line.begin; at < line.end;) {
+    const Item it = item_of(p, line, cur, at);
+    {
+      const uint32_t slot = kv_cnt % kKvSlots, par = (kv_cnt / kKvSlots) & 1;
+      if (!mbar_wait_warp(&bars.kv_full[slot], par, ctx, kRoleMma | kBarKvFull)) return;
+      const uint64_t k_desc = kmajor_desc(base + kTSmemKv + slot * kTileBytes);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (s == 0 || it.two) {
+          if (!mbar_wait_warp(&bars.q_full[s], q_cnt[s] & 1, ctx, kRoleMma | kBarQFull)) return;
+          tc_fence_after_sync();
+          issue_qk_f16(leader, tmem + s * kTile, q_desc[s], k_desc);
+          if (leader) mma_commit(&bars.s_full[s]);
+        }
+      }
+      if (leader) mma_commit(&bars.kv_empty[slot]);
+      ++kv_cnt;
+    }
+    for (int j = 0; j < it.n; ++j) {
+      const uint32_t vslot = kv_cnt % kKvSlots, vpar = (kv_cnt / kKvSlots) & 1;
+      ++kv_cnt;
+      const bool has_next = j + 1 < it.n;
+      uint32_t kslot = 0, kpar = 0;
+      if (has_next) {
+        kslot = kv_cnt % kKvSlots;
+        kpar = (kv_cnt / kKvSlots) & 1;
+        ++kv_cnt;
+      }
+      if (!mbar_wait_warp(&bars.kv_full[vslot], vpar, ctx, kRoleMma | kBarKvFull)) return;
+      bool k_ready = false;
+      const uint64_t v_desc = vtile_desc(base + kTSmemKv + vslot * kTileBytes);
+      const uint64_t k_desc = kmajor_desc(base + kTSmemKv + kslot * kTileBytes);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (s == 0 || it.two) {
+          if (j == 0) {  // the previous item's O must have left tensor memory
+            if (!mbar_wait_warp(&bars.o_empty[s], (q_cnt[s] & 1) ^ 1, ctx, kRoleMma | kBarOEmpty)) return;
+          }
+          if (!mbar_wait_warp(&bars.p_half[s], sp_cnt[s] & 1, ctx, kRoleMma | kBarPHalf)) return;
+          tc_fence_after_sync();
+          issue_pv_f16(leader, tmem + 2 * kTile + s * kTile, tmem + s * kTile, v_desc, j > 0, 0, 4);
+          if (!mbar_wait_warp(&bars.p_full[s], sp_cnt[s] & 1, ctx, kRoleMma | kBarPFull)) return;
+          ++sp_cnt[s];
+          tc_fence_after_sync();
+          issue_pv_f16(leader, tmem + 2 * kTile + s * kTile, tmem + s * kTile, v_desc, j > 0, 4, 8);
+          if (leader && !has_next) mma_commit(&bars.o_full[s]);
+          if (has_next) {
+            if (!k_ready) {
+              if (!mbar_wait_warp(&bars.kv_full[kslot], kpar, ctx, kRoleMma | kBarKvFull)) return;
+              tc_fence_after_sync();
+              k_ready = true;
+            }
+            issue_qk_f16(leader, tmem + s * kTile, q_desc[s], k_desc);
+            if (leader) mma_commit(&bars.s_full[s]);
+          }
+        }
+      }
+      if (leader) {
+        mma_commit(&bars.kv_empty[vslot]);
+        if (has_next) mma_commit(&bars.kv_empty[kslot]);
+      }
+    }
+    ++q_cnt[0];
+    if (it.two) ++q_cnt[1];
+    at += it.n;
+    if (at < line.end) cur.next_tile(p);
+  }
+}
+
+// ---- softmax: one thread owns one row of stage `s` ------------------------------------------------------------------------
+__device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
+                                                  const Line& line, Cursor<kTileRows> cur, uint32_t tmem, int s, int row, int lane) {
+  const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
+  const uint32_t t_s = tmem + lane_sel + s * kTile;
+  const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
+  float* stats = reinterpret_cast<float*>(smem + kTSmemStats) + s * 2 * kTile;
+  uint32_t s_cnt = 0, l_cnt = 0, step = 0;
+  for (long long at = line.begin; at < line.end;) {
+    const Item it = item_of(p, line, cur, at);
+    if (s == 0 || it.two) {
+      // Q: the stage's last product that reads it has completed (its scores have been taken)
+      const long long r0 = static_cast<long long>(cur.tile) * kTileRows + s * kTile;
+      const TilePlace w = tile_place(p, cur.s, cur.h, r0 + row);
+      int limit = cur.s.keys;  // keys the row sees; rows that are not real see all
+      float factor;
+      {
+        uint4 x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = make_uint4(0, 0, 0, 0);
+        if (w.real) {
+          limit = visible(cur.s, w.token, p.causal);
+          const uint4* src = reinterpret_cast<const uint4*>(p.q + row_offset(p, p.sq, cur.b, cur.s, w));
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = __ldg(src + i);
+        }
+        float largest = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = unpack_bf16x2(words[k]);
+            largest = max3(largest, fabsf(f.x), fabsf(f.y));
+          }
+        }
+        const float up = row_factor(largest);
+        factor = p.scale_log2 / up;
+        uint8_t* dst = smem + kTSmemQ + s * kTileBytes + row * 128;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          uint32_t y[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = unpack_bf16x2(words[k]);
+            y[k] = pack_f16x2(f.x * up, f.y * up);
+          }
+          *reinterpret_cast<uint4*>(dst + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.q_full[s]);
+      }
+      // keys that all rows of the stage see: steps up to there need no mask
+      const int clear = visible(cur.s, min(static_cast<int>(r0 / p.group), cur.s.n - 1), p.causal);
+      float m_used = -INFINITY;  // reference maximum, log2 units
+      float l = 0.f, vref = 0.f;
+      for (int j = 0; j < it.n; ++j) {
+        const uint32_t q = (step + j) % kMetaSteps;
+        bool ok = mbar_wait(&bars.meta_full[q], ((step + j) / kMetaSteps) & 1, ctx, kRoleSoftmax | kBarMeta);
+        const float* meta = reinterpret_cast<const float*>(smem + kTSmemMeta) + q * kMetaFloats;
+        ok = ok && mbar_wait(&bars.s_full[s], s_cnt & 1, ctx, kRoleSoftmax | kBarSFull);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return;
+        ++s_cnt;
+        tc_fence_after_sync();
+        uint32_t xr[kTile];
+        tmem_ld_x32(t_s + 0, xr + 0);
+        tmem_ld_x32(t_s + 32, xr + 32);
+        tmem_ld_x32(t_s + 64, xr + 64);
+        tmem_ld_x32(t_s + 96, xr + 96);
+        float cg[8];
+#pragma unroll
+        for (int g = 0; g < 8; ++g) cg[g] = fmaxf(meta[kMetaK + g] * factor, 1e-37f);  // not 0: -inf stays -inf
+        tmem_wait_ld();
+#define X(i) __uint_as_float(xr[(i)])
+        const int key0 = (it.t_first + j) * kStepKeys;
+        if (key0 + kStepKeys > clear) {  // warp-uniform
+          const int vis = limit - key0;
+#pragma unroll
+          for (int i = 0; i < kTile; ++i) {
+            if (i >= vis) xr[i] = 0xff800000u;
+          }
+        }
+        float m_blk = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          const int i = g * 16;
+          const float a = max3(X(i), X(i + 1), X(i + 2)), b = max3(X(i + 3), X(i + 4), X(i + 5));
+          const float c = max3(X(i + 6), X(i + 7), X(i + 8)), d = max3(X(i + 9), X(i + 10), X(i + 11));
+          const float e = max3(X(i + 12), X(i + 13), X(i + 14));
+          m_blk = fmaxf(m_blk, fmaxf(max3(a, b, X(i + 15)), max3(c, d, e)) * cg[g]);
+        }
+        vref = meta[kMetaVref];
+        if (j == 0) {
+          m_used = m_blk == -INFINITY ? 0.f : m_blk;
+        } else {
+          const float m_new = fmaxf(m_used, m_blk);
+          const float v_grow = meta[kMetaGrow];
+          if (__any_sync(0xffffffffu, m_new - m_used > kWeightLag || v_grow != 1.f)) {
+            // P V of the step before has completed (S of this one was issued after it): O is quiescent
+            const float alpha = ex2_approx(m_used - m_new);
+            m_used = m_new;
+            l *= alpha;
+            const float f = alpha * v_grow;
+#pragma unroll
+            for (int cc = 0; cc < 8; ++cc) {
+              uint32_t o[16];
+              tmem_ld_x16(t_o + cc * 16, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st_x16(t_o + cc * 16, o);
+            }
+          }
+        }
+        const float neg_m = kWeightShift - m_used;
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int g = cc * 2 + h;
+            const float add = neg_m + meta[kMetaV + g];
+            const float inv = meta[kMetaInv + g];
+            const float2 c2 = make_float2(cg[g], cg[g]), a2 = make_float2(add, add);
+            float2 part;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int i = g * 16 + k * 2;
+              const float2 x = fma2(make_float2(X(i), X(i + 1)), c2, a2);
+              const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+              part = k == 0 ? e : add2(part, e);
+              pk[h * 8 + k] = pack_f16x2(e.x, e.y);
+            }
+            sum = fma2(part, make_float2(inv, inv), sum);
+          }
+          tmem_st_x16(t_s + cc * 16, pk);
+          if (cc == 1) {
+            tmem_wait_st();
+            tc_fence_before_sync();
+            if (lane == 0) mbar_arrive(&bars.p_half[s]);
+          }
+        }
+#undef X
+        l += sum.x + sum.y;
+        const int bad = reinterpret_cast<const int*>(meta)[kMetaBad];
+        if (bad < kStepKeys && key0 + bad < limit) l = __int_as_float(0x7fffffff);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        if (lane == 0) mbar_arrive(&bars.p_full[s]);
+      }
+      bool ok = mbar_wait(&bars.l_empty[s], (l_cnt & 1) ^ 1, ctx, kRoleSoftmax | kBarLEmpty);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      // a row that has seen no key here has the sum 0 by definition, and no maximum
+      const bool seen = limit > it.t_first * kStepKeys;
+      stats[row] = seen ? l : 0.f;
+      stats[kTile + row] = seen ? m_used : -INFINITY;
+      if (row == 0) reinterpret_cast<float*>(smem + kTSmemMisc)[2 + s] = vref;
+      mbar_arrive(&bars.l_full[s]);
+      ++l_cnt;
+    }
+    step += it.n;
+    at += it.n;
+    if (at < line.end) cur.next_tile(p);
+  }
+}
+
+// ---- results ----------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
+                                                   const Line& line, Cursor<kTileRows> cur, uint32_t tmem, int row, int lane) {
+  const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
+  uint32_t cnt[2] = {0, 0};
+  for (long long at = line.begin; at < line.end;) {
+    const Item it = item_of(p, line, cur, at);
+#pragma unroll 1
+    for (int s = 0; s < 2; ++s) {
+      if (s == 1 && !it.two) continue;
+      const float* stats = reinterpret_cast<const float*>(smem + kTSmemStats) + s * 2 * kTile;
+      bool ok = mbar_wait(&bars.l_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarLFull);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      float l = stats[row];
+      const float m = stats[kTile + row];
+      const float vref = reinterpret_cast<const float*>(smem + kTSmemMisc)[2 + s];
+      mbar_arrive(&bars.l_empty[s]);
+      ok = mbar_wait(&bars.o_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarOFull);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      ++cnt[s];
+      tc_fence_after_sync();
+      const int r = s * kTile + row;
+      const TilePlace w = tile_place(p, cur.s, cur.h, static_cast<long long>(cur.tile) * kTileRows + r);
+      // keys beyond the table's reach
+      if (w.real && cur.s.len > cur.s.keys && (!p.causal || cur.s.len - cur.s.n + w.token >= cur.s.keys)) l = __int_as_float(0x7fffffff);
+      const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
+      const long long slot = 2ll * blockIdx.x + (it.t_first == 0 ? 1 : 0);
+      const float f = it.whole ? (l == 0.f ? 0.f : __fdividef(vref, l)) : vref;
+      uint16_t* out = p.o + row_offset(p, p.so, cur.b, cur.s, w);
+      float* part = p.parts + (slot * kTileRows + r) * kKvDim;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) {
+        uint32_t o[32];
+        tmem_ld_x32(t_o + cc * 32, o);
+        tmem_wait_ld();
+        if (w.real && it.whole) {
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) {
+            uint4 val;
+            val.x = pack_bf16x2(__uint_as_float(o[ch * 8 + 0]) * f, __uint_as_float(o[ch * 8 + 1]) * f);
+            val.y = pack_bf16x2(__uint_as_float(o[ch * 8 + 2]) * f, __uint_as_float(o[ch * 8 + 3]) * f);
+            val.z = pack_bf16x2(__uint_as_float(o[ch * 8 + 4]) * f, __uint_as_float(o[ch * 8 + 5]) * f);
+            val.w = pack_bf16x2(__uint_as_float(o[ch * 8 + 6]) * f, __uint_as_float(o[ch * 8 + 7]) * f);
+            *reinterpret_cast<uint4*>(out + cc * 32 + ch * 8) = val;
+          }
+        } else if (w.real) {
+#pragma unroll
+          for (int ch = 0; ch < 8; ++ch) {
+            *reinterpret_cast<float4*>(part + cc * 32 + ch * 4) =
+                make_float4(__uint_as_float(o[ch * 4]) * f, __uint_as_float(o[ch * 4 + 1]) * f,
+                            __uint_as_float(o[ch * 4 + 2]) * f, __uint_as_float(o[ch * 4 + 3]) * f);
+          }
+        }
+        __syncwarp();
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars.o_empty[s]);
+      if (it.whole) {
+        if (w.real && p.lse != nullptr)
+          p.lse[lse_index(p, cur.b, cur.s, w)] = l == 0.f ? -INFINITY : (m - kWeightShift + lg2_approx(l)) * kLn2;
+      } else {
+        reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kTileRows * kKvDim)[slot * kTileRows + r] = make_float2(m, l);
+        if (r == 0 && it.t_first == 0) {
+          p.pieces[blockIdx.x] = make_int4(cur.b, cur.h, cur.tile, static_cast<int>(line.owner(at + cur.steps - 1)));
+        }
+      }
+    }
+    at += it.n;
+    if (at < line.end) cur.next_tile(p);
+  }
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const CachedParams p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bar_mem = reinterpret_cast<uint64_t*>(smem + kTSmemBars);
+  TileBarriers bars;
+  bars.q_full = bar_mem;
+  bars.kv_full = bars.q_full + 2;
+  bars.kv_empty = bars.kv_full + kKvSlots;
+  bars.s_full = bars.kv_empty + kKvSlots;
+  bars.p_half = bars.s_full + 2;
+  bars.p_full = bars.p_half + 2;
+  bars.o_full = bars.p_full + 2;
+  bars.o_empty = bars.o_full + 2;
+  bars.l_full = bars.o_empty + 2;
+  bars.l_empty = bars.l_full + 2;
+  bars.meta_full = bars.l_empty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kTSmemMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kTSmemMisc + 4);
+  const WaitCtx ctx{abort_flag, p.status, kWaitLimitNs};
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) p.pieces[blockIdx.x] = make_int4(0, 0, 0, -1);
+  if ((smem_u32(smem) & 1023u) != 0) {  // the swizzled tiles need a 1024-byte aligned base
+    if (tid == 0 && atomicCAS(p.status, 0, kBadSmemAlign) == 0) p.status[1] = static_cast<int>(blockIdx.x);
+    return;
+  }
+  Line line;
+  Cursor<kTileRows> cur;
+  if (!find_piece<kTileRows>(p, line, cur, reinterpret_cast<long long*>(smem))) return;
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.q_full[i], 4);
+      mbar_init(&bars.s_full[i], 1);
+      mbar_init(&bars.p_half[i], 4);
+      mbar_init(&bars.p_full[i], 4);
+      mbar_init(&bars.o_full[i], 1);
+      mbar_init(&bars.o_empty[i], 4);
+      mbar_init(&bars.l_full[i], kTile);
+      mbar_init(&bars.l_empty[i], kTile);
+    }
+    for (int i = 0; i < kKvSlots; ++i) {
+      mbar_init(&bars.kv_full[i], kConvWarps);
+      mbar_init(&bars.kv_empty[i], 1);
+    }
+    for (int i = 0; i < kMetaSteps; ++i) mbar_init(&bars.meta_full[i], 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 12) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp < 8) {
+    reg_alloc<ATTN_REGS_SOFTMAX>();
+    role_tile_softmax(p, bars, smem, ctx, line, cur, tmem, warp >> 2, tid & 127, lane);
+  } else if (warp < 12) {
+    reg_dealloc<ATTN_REGS_EPILOGUE>();
+    role_tile_epilogue(p, bars, smem, ctx, line, cur, tmem, tid & 127, lane);
+  } else {
+    reg_dealloc<ATTN_REGS_OTHER>();
+    if (warp == 12) {
+      role_tile_mma(p, bars, smem, ctx, line, cur, tmem);
+    } else {
+      role_convert<TYPE>(p, bars, smem, ctx, line, cur, warp - 13, lane);
+    }
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+}  // namespace kv
+}  // namespace attn

@@ -99,6 +99,10 @@ size_t cached_workspace(int ctas, int rows) {
 }
 constexpr int kWorkspaceCtas = 160;  // CTAs of a launch at most: one an SM
 
+// Rows (token, head of a group) of the longest sequence from which on the tensor-memory kernel is taken.
+constexpr int kManyRows = 17;
+bool many_rows(int Hq, int Hkv, int max_new) { return static_cast<long long>(Hq / Hkv) * max_new >= kManyRows; }
+
 }  // namespace
 
 extern "C" {
@@ -138,7 +142,10 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
   return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
 }
 
-size_t attn_fwd_cached_workspace_bytes(void) { return cached_workspace(kWorkspaceCtas, attn::kv::kDecRows); }
+size_t attn_fwd_cached_workspace_bytes(int Hq, int Hkv, int max_new) {
+  if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_new <= 0) return 0;
+  return cached_workspace(kWorkspaceCtas, many_rows(Hq, Hkv, max_new) ? attn::kv::kTileRows : attn::kv::kDecRows);
+}
 
 attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
                               int causal, float scale, const long long* q_strides, const long long* o_strides, void* workspace,
@@ -157,7 +164,7 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   if (st != ATTN_OK) return st;
   if (o == q || o == cache->k || o == cache->v || workspace == q || workspace == o || workspace == cache->k || workspace == cache->v)
     return ATTN_ERR_UNSUPPORTED;
-  if (workspace_bytes < attn_fwd_cached_workspace_bytes()) return ATTN_ERR_TOO_LARGE;
+  if (workspace_bytes < attn_fwd_cached_workspace_bytes(Hq, cache->Hkv, max_new)) return ATTN_ERR_TOO_LARGE;
   DeviceState* dev = device_state(&st);
   if (dev == nullptr) return st;
   p.q = static_cast<const uint16_t*>(q);
@@ -168,16 +175,33 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   p.causal = causal ? 1 : 0;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.ctas = dev->sm_count < kWorkspaceCtas ? dev->sm_count : kWorkspaceCtas;
+  const bool many = many_rows(Hq, cache->Hkv, max_new);
+  p.min_steps = many ? 4 : 1;
+  p.status = dev->status;
   p.parts = static_cast<float*>(workspace);
-  p.pieces = reinterpret_cast<int4*>(p.parts + cached_parts(p.ctas, attn::kv::kDecRows) * (attn::kv::kKvDim + 2));
+  p.pieces = reinterpret_cast<int4*>(
+      p.parts + cached_parts(p.ctas, many ? attn::kv::kTileRows : attn::kv::kDecRows) * (attn::kv::kKvDim + 2));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (p.c.type == ATTN_KV_E4M3) {
+  const bool e4m3 = p.c.type == ATTN_KV_E4M3;
+  if (many) {
+    if (e4m3) {
+      attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(p);
+    } else {
+      attn::kv::attn_cached_tile_kernel<attn::kv::kInt8><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(p);
+    }
+  } else if (e4m3) {
     attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3><<<p.ctas, attn::kv::kDecThreads, attn::kv::kDecSmemBytes, s>>>(p);
   } else {
     attn::kv::attn_cached_decode_kernel<attn::kv::kInt8><<<p.ctas, attn::kv::kDecThreads, attn::kv::kDecSmemBytes, s>>>(p);
   }
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-  attn::kv::attn_cached_join_kernel<attn::kv::kDecRows><<<dim3(p.ctas, attn::kv::kDecRows), 256, 0, s>>>(p);
+  if (many) {
+    attn::kv::attn_cached_join_kernel<attn::kv::kTileRows>
+        <<<dim3(p.ctas, attn::kv::kTileRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
+  } else {
+    attn::kv::attn_cached_join_kernel<attn::kv::kDecRows>
+        <<<dim3(p.ctas, attn::kv::kDecRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
+  }
   return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
 }
 

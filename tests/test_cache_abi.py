@@ -90,7 +90,7 @@ def test_attention_argument_errors(cdll):
         assert _attend(cdll, scale=scale) == 3
     assert _attend(cdll, qs=(0, 512, 128)) == 2 and _attend(cdll, os=(2560, 512, 130)) == 4
     assert _attend(cdll, o=0x7000) == 3 and _attend(cdll, ws=0x7000) == 3 and _attend(cdll, o=0x2000) == 3
-    assert _attend(cdll, ws_bytes=cdll.attn_fwd_cached_workspace_bytes() - 1) == 8
+    assert _attend(cdll, ws_bytes=cdll.attn_fwd_cached_workspace_bytes(4, 2, 5) - 1) == 8
 
 
 def test_binding_refusals():
