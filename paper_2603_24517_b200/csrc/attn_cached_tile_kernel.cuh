@@ -7,10 +7,8 @@
 //   warps 0-7    softmax; each thread also brings its row of Q into shared memory, as f16 scaled by a power of two of the row
 //   warps 8-11   O / l -> BF16 -> memory, or an fp32 part where the tile's keys are spread over CTAs
 //   warp  12     tcgen05.mma, f16 operands
-//   warps 13-15  converters: codes by 16-byte asynchronous copies (any page size, order and length; what lies behind the last
-//                token is zeros) into 32 KB of staging, from there exactly to f16 in the swizzled ring of K / V tiles.  A lane
-//                converts what it has copied itself, so the staging needs no barrier; a piece is requested again for the
-//                next step as soon as it is converted.  They sit on the sub-partitions that the MMA warp does not share
+//   warp  13     fetch: page numbers and scales, codes by TMA, a page a copy (any page size and strides), into 32 KB of staging
+//   warps 14-15  converters: codes exactly to f16 in the swizzled ring of K / V tiles, zeros behind the last token
 //
 // Scales: 16 keys ("a granule") lie in one page.  K's scale multiplies the row's factor granule by granule, V's enters the
 // exponent as log2 of its ratio to the largest V scale so far, and is taken out of the row sum again granule by granule, so
@@ -26,7 +24,10 @@ namespace attn {
 namespace kv {
 
 constexpr int kTileRows = 256;  // rows of a work item: two stages
-constexpr int kConvWarps = 3;
+constexpr int kConvWarps = 2;
+// registers of a thread after the split of the CTA's 64K: 8 softmax, 4 epilogue, 4 other warps
+constexpr int kTRegsSoftmax = 192, kTRegsEpilogue = 64, kTRegsOther = 64;
+static_assert(8 * kTRegsSoftmax + 4 * kTRegsEpilogue + 4 * kTRegsOther <= 2048, "register split");
 
 constexpr int kTSmemQ = 0;
 constexpr int kTSmemKv = 2 * kTileBytes;
@@ -36,19 +37,21 @@ constexpr int kMetaSteps = 4;
 constexpr int kMetaFloats = 32;
 constexpr int kTSmemMeta = kTSmemStats + 2 * 2 * kTile * 4;
 constexpr int kTSmemBars = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
-constexpr int kTNumBars = 2 + 2 * kKvSlots + 2 * 7 + kMetaSteps;
+constexpr int kTNumBars = 2 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 4;
 constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
 constexpr int kTSmemBytes = kTSmemMisc + 16;
 static_assert(kTSmemBytes <= 232448, "shared memory budget of one CTA");
 static_assert(kHeadDim == kKvDim && kTile == kStepKeys, "one head dimension, one tile");
 
 // What the converters tell the softmax warps about a step.
-enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaGrow = 25, kMetaBad = 26 };
+enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaGrow = 25, kMetaBad = 26, kMetaValid = 27 };
 constexpr float kMinRatioLog2 = -60.f;  // V scales below 2^-60 of the largest count as that: nothing in f16
 
 struct TileBarriers {
   uint64_t* q_full;    // [2] softmax (4 warps): the stage's Q is in shared memory -> MMA
-  uint64_t* kv_full;   // [kKvSlots] converters (3 warps) -> MMA
+  uint64_t* raw_full;  // [2] TMA: the codes of the keys, of the values -> converters
+  uint64_t* raw_empty; // [2] converters (2 warps) -> fetching warp
+  uint64_t* kv_full;   // [kKvSlots] converters (2 warps) -> MMA
   uint64_t* kv_empty;  // [kKvSlots] MMA commit -> converters
   uint64_t* s_full;    // [2] MMA commit -> softmax
   uint64_t* p_half;    // [2] softmax (4 warps): the first 64 keys of P -> MMA
@@ -57,7 +60,7 @@ struct TileBarriers {
   uint64_t* o_empty;   // [2] epilogue (4 warps) -> MMA
   uint64_t* l_full;    // [2] softmax (128 threads) -> epilogue
   uint64_t* l_empty;   // [2] epilogue (128 threads) -> softmax
-  uint64_t* meta_full; // [kMetaSteps] first converter warp -> softmax
+  uint64_t* meta_full; // [kMetaSteps] fetching warp -> softmax
 };
 enum : int { kRoleConvert = 6 << 8, kBarMeta = 20 };
 
@@ -82,22 +85,22 @@ __device__ __forceinline__ Item item_of(const CachedParams& p, const Line& line,
   return it;
 }
 
-// ---- converters ------------------------------------------------------------------------------------------------------
+// ---- the pages' codes -------------------------------------------------------------------------------------------------
 struct StepPlace {  // where a step's codes are; `page` is that of granule (lane & 7): -1 does not exist, -2 behind the last token
   int page, h, key0, keys;
   bool first;       // of its item in this CTA
 };
 
-template <int TYPE>
-__device__ __forceinline__ void role_convert(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
-                                             const Line& line, Cursor<kTileRows> ahead, int cw, int lane) {
+// Looks pages up two steps ahead and their scales one, requests the codes page by page and writes what the softmax warps need.
+__device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
+                                           const Line& line, Cursor<kTileRows> ahead, int lane, const CUtensorMap* tm_k,
+                                           const CUtensorMap* tm_v) {
   const CacheView& c = p.c;
-  const int slot_mask = (1 << c.page_log2) - 1;
   long long left = line.end - line.begin;  // steps whose pages have not been looked up yet
   bool first = true;
   auto look_up = [&]() {
     StepPlace f;
-    f.keys = 0;  // no step: nothing is copied
+    f.keys = 0;
     f.page = -2;
     f.h = f.key0 = 0;
     f.first = false;
@@ -117,95 +120,101 @@ __device__ __forceinline__ void role_convert(const CachedParams& p, const TileBa
   auto scale_of = [&](const StepPlace& f) {  // lanes 0-7: K's of granule lane, 8-15: V's of granule lane - 8
     return lane < 16 && f.page >= 0 ? __ldg(c.scales[lane >> 3] + static_cast<long long>(f.page) * c.Hkv + f.h) : 0.f;
   };
-  const int sub = lane >> 2;  // row of a group of 8
-  // the lane's two 16-byte pieces (units lane & 3 and 4 + lane & 3) of row 8 rg + sub
-  auto request = [&](const StepPlace& f, int kv, int rg) {
-    const int page = __shfl_sync(0xffffffffu, f.page, rg >> 1);
-    const int key = f.key0 + rg * 8 + sub;
-    const bool take = page >= 0 && key < f.keys;
-    const uint8_t* src = c.codes[kv];
-    if (take) src += page * c.sp[kv] + f.h * c.sh[kv] + (key & slot_mask) * c.ss[kv] + (lane & 3) * 16;
-    const uint32_t dst = smem_u32(smem) + kTSmemRaw + kv * kTile * kKvDim + rg * 1024 + lane * 16;
-    cp_async16(dst, src, take);
-    cp_async16(dst + 512, take ? src + 64 : src, take);
-  };
-
   StepPlace now = look_up(), next = look_up();
-#pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    for (int rg = (cw + kv) % kConvWarps; rg < 16; rg += kConvWarps) request(now, kv, rg);
-    cp_async_commit();
-  }
   float scale_now = scale_of(now);
   float vref = 0.f;
-  uint32_t kv_cnt = 0;
-  const long long steps = line.end - line.begin;
-  for (long long i = 0; i < steps; ++i) {
+  const bool asks = lane < 8 && ((lane * 16) & ((1 << c.page_log2) - 1)) == 0;  // one lane a page
+  const uint32_t steps = static_cast<uint32_t>(line.end - line.begin);
+  for (uint32_t i = 0; i < steps; ++i) {
     const StepPlace after = look_up();
     const float scale_next = scale_of(next);
-    if (cw == 0) {
-      if (now.first) vref = 0.f;
-      float top = lane >= 8 && lane < 16 ? scale_now : 0.f;
+    float top = lane >= 8 && lane < 16 ? scale_now : 0.f;
 #pragma unroll
-      for (int m = 4; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-      top = __shfl_sync(0xffffffffu, top, 8);
-      const float ref = fmaxf(fmaxf(vref, top), 1e-30f);
-      float* meta = reinterpret_cast<float*>(smem + kTSmemMeta) + (i % kMetaSteps) * kMetaFloats;
-      const unsigned bad = __ballot_sync(0xffffffffu, lane < 8 && now.page == -1);
-      if (lane < 8) {
-        meta[kMetaK + lane] = scale_now;
-      } else if (lane < 16) {
-        const float ratio = now.page >= 0 ? fmaxf(lg2_approx(__fdividef(scale_now, ref)), kMinRatioLog2) : 0.f;
-        meta[kMetaV + lane - 8] = ratio;
-        meta[kMetaInv + lane - 8] = ex2_approx(-ratio);
-      } else if (lane == 16) {
-        meta[kMetaVref] = ref;
-        meta[kMetaGrow] = vref == ref ? 1.f : __fdividef(vref, ref);
-        reinterpret_cast<int*>(meta)[kMetaBad] = bad != 0 ? (__ffs(bad) - 1) * 16 : kStepKeys;
+    for (int m = 4; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    top = __shfl_sync(0xffffffffu, top, 8);
+    if (now.first) vref = 0.f;
+    const float ref = fmaxf(fmaxf(vref, top), 1e-30f);
+    const unsigned bad = __ballot_sync(0xffffffffu, lane < 8 && now.page == -1);
+    float* meta = reinterpret_cast<float*>(smem + kTSmemMeta) + (i % kMetaSteps) * kMetaFloats;
+#pragma unroll 1
+    for (int kv = 0; kv < 2; ++kv) {
+      // the step's entry may be written once the codes of the keys of the step before have been converted: that needed the
+      // slot of the keys two steps before that, so the scores of i - 3 are complete and the weights of i - 4 were taken
+      const bool ok = mbar_wait_warp(&bars.raw_empty[kv], (i & 1) ^ 1, ctx, kRoleLoad | kBarKvEmpty);
+      if (!ok) return;
+      if (kv == 0) {
+        if (lane < 8) {
+          meta[kMetaK + lane] = scale_now;
+        } else if (lane < 16) {
+          const float ratio = now.page >= 0 ? fmaxf(lg2_approx(__fdividef(scale_now, ref)), kMinRatioLog2) : 0.f;
+          meta[kMetaV + lane - 8] = ratio;
+          meta[kMetaInv + lane - 8] = ex2_approx(-ratio);
+        } else if (lane == 16) {
+          meta[kMetaVref] = ref;
+          meta[kMetaGrow] = vref == ref ? 1.f : __fdividef(vref, ref);
+          reinterpret_cast<int*>(meta)[kMetaBad] = bad != 0 ? (__ffs(bad) - 1) * 16 : kStepKeys;
+          reinterpret_cast<int*>(meta)[kMetaValid] = now.keys - now.key0;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.meta_full[i % kMetaSteps]);
       }
-      vref = ref;
+      if (lane == 0) mbar_arrive_expect_tx(&bars.raw_full[kv], kTile * kKvDim);
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars.meta_full[i % kMetaSteps]);
+      if (asks)  // a page that is not there lies behind the last one: zeros
+        tma_load_4d(smem + kTSmemRaw + kv * kTile * kKvDim + lane * 16 * kKvDim, kv == 0 ? tm_k : tm_v, &bars.raw_full[kv], 0, 0,
+                    now.h, now.page >= 0 ? now.page : c.n_pages);
+      __syncwarp();
     }
+    vref = ref;
+    now = next;
+    next = after;
+    scale_now = scale_next;
+  }
+}
+
+// Codes to f16.  A lane takes 16 codes of one of 8 rows at a time, odd rows the other half of the head dimension than even
+// ones, so neither its reads nor its writes meet another lane's bank.
+template <int TYPE>
+__device__ __forceinline__ void role_convert(const TileBarriers& bars, uint8_t* smem, WaitCtx ctx, uint32_t steps, int cw, int lane) {
+  const int sub = lane >> 2, ch = (lane & 3) * 2;
+  uint32_t kv_cnt = 0;
+  for (uint32_t i = 0; i < steps; ++i) {
 #pragma unroll 1
     for (int kv = 0; kv < 2; ++kv) {
       const uint32_t slot = kv_cnt % kKvSlots;
-      const bool ok = mbar_wait_warp(&bars.kv_empty[slot], ((kv_cnt / kKvSlots) & 1) ^ 1, ctx, kRoleConvert | kBarKvEmpty);
-      if (!ok) {
-        cp_async_wait<0>();
-        return;
-      }
+      bool ok = mbar_wait(&bars.raw_full[kv], i & 1, ctx, kRoleConvert | kBarKvFull);
+      ok = ok && mbar_wait(&bars.kv_empty[slot], ((kv_cnt / kKvSlots) & 1) ^ 1, ctx, kRoleConvert | kBarKvEmpty);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
       ++kv_cnt;
-      cp_async_wait<1>();
-      uint8_t* tile = smem + kTSmemKv + slot * kTileBytes;
-#pragma unroll 2
-      for (int rg = (cw + kv) % kConvWarps; rg < 16; rg += kConvWarps) {
-        const uint8_t* raw = smem + kTSmemRaw + kv * kTile * kKvDim + rg * 1024 + lane * 16;
-        uint8_t* row = tile + (rg * 8 + sub) * 128;
-        const int ch = (lane & 3) * 2;
+      const int valid = reinterpret_cast<const int*>(smem + kTSmemMeta)[(i % kMetaSteps) * kMetaFloats + kMetaValid];
+      const uint8_t* raw = smem + kTSmemRaw + kv * kTile * kKvDim + sub * kKvDim + (lane & 3) * 16;
+      uint8_t* tile = smem + kTSmemKv + slot * kTileBytes + sub * 128;
+#pragma unroll 4
+      for (int rg = cw; rg < 16; rg += kConvWarps) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint4 w = *reinterpret_cast<const uint4*>(raw + half * 512);
+        for (int k = 0; k < 2; ++k) {
+          const int half = k ^ (sub & 1);
+          uint4 w = *reinterpret_cast<const uint4*>(raw + rg * 8 * kKvDim + half * 64);
+          if (valid < kTile && rg * 8 + sub >= valid) w = make_uint4(0, 0, 0, 0);  // behind the last token: zeros
           uint4 lo, hi;
           codes_to_f16<TYPE>(w.x, lo.x, lo.y);
           codes_to_f16<TYPE>(w.y, lo.z, lo.w);
           codes_to_f16<TYPE>(w.z, hi.x, hi.y);
           codes_to_f16<TYPE>(w.w, hi.z, hi.w);
-          *reinterpret_cast<uint4*>(row + half * kHalfBytes + ((ch ^ sub) << 4)) = lo;
-          *reinterpret_cast<uint4*>(row + half * kHalfBytes + (((ch + 1) ^ sub) << 4)) = hi;
+          uint8_t* row = tile + rg * 8 * 128 + half * kHalfBytes;
+          *reinterpret_cast<uint4*>(row + ((ch ^ sub) << 4)) = lo;
+          *reinterpret_cast<uint4*>(row + (((ch + 1) ^ sub) << 4)) = hi;
         }
-        request(next, kv, rg);  // the piece has been read: its conversion is done
       }
-      cp_async_commit();
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars.kv_full[slot]);
+      if (lane == 0) {
+        mbar_arrive(&bars.raw_empty[kv]);
+        mbar_arrive(&bars.kv_full[slot]);
+      }
     }
-    now = next;
-    next = after;
-    scale_now = scale_next;
   }
-  cp_async_wait<0>();
 }
 
 // ---- MMA --------------------------------------------------------------------------------------------------------------
@@ -554,12 +563,15 @@ __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const 
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const CachedParams p) {
+__global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __grid_constant__ CUtensorMap tm_k,
+                                                                     const __grid_constant__ CUtensorMap tm_v, const CachedParams p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bar_mem = reinterpret_cast<uint64_t*>(smem + kTSmemBars);
   TileBarriers bars;
   bars.q_full = bar_mem;
-  bars.kv_full = bars.q_full + 2;
+  bars.raw_full = bars.q_full + 2;
+  bars.raw_empty = bars.raw_full + 2;
+  bars.kv_full = bars.raw_empty + 2;
   bars.kv_empty = bars.kv_full + kKvSlots;
   bars.s_full = bars.kv_empty + kKvSlots;
   bars.p_half = bars.s_full + 2;
@@ -585,6 +597,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const Cac
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.q_full[i], 4);
+      mbar_init(&bars.raw_full[i], 1);
+      mbar_init(&bars.raw_empty[i], kConvWarps);
       mbar_init(&bars.s_full[i], 1);
       mbar_init(&bars.p_half[i], 4);
       mbar_init(&bars.p_full[i], 4);
@@ -611,17 +625,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const Cac
   const uint32_t tmem = *tmem_slot;
 
   if (warp < 8) {
-    reg_alloc<ATTN_REGS_SOFTMAX>();
+    reg_alloc<kTRegsSoftmax>();
     role_tile_softmax(p, bars, smem, ctx, line, cur, tmem, warp >> 2, tid & 127, lane);
   } else if (warp < 12) {
-    reg_dealloc<ATTN_REGS_EPILOGUE>();
+    reg_dealloc<kTRegsEpilogue>();
     role_tile_epilogue(p, bars, smem, ctx, line, cur, tmem, tid & 127, lane);
   } else {
-    reg_dealloc<ATTN_REGS_OTHER>();
+    reg_dealloc<kTRegsOther>();
     if (warp == 12) {
       role_tile_mma(p, bars, smem, ctx, line, cur, tmem);
+    } else if (warp == 13) {
+      role_fetch(p, bars, smem, ctx, line, cur, lane, &tm_k, &tm_v);
+      if (*abort_flag) {  // let loads in flight land before the CTA's shared memory is released
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 1000000ull) {
+        }
+      }
     } else {
-      role_convert<TYPE>(p, bars, smem, ctx, line, cur, warp - 13, lane);
+      role_convert<TYPE>(bars, smem, ctx, static_cast<uint32_t>(line.end - line.begin), warp - 14, lane);
     }
   }
   tc_fence_before_sync();

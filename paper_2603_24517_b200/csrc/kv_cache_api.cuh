@@ -92,6 +92,19 @@ attn_status_t page_launch(const attn_kv_cache_t* cache, const void* k, const voi
   return ATTN_OK;
 }
 
+// The codes [n_pages, Hkv, page, D] as a 4-D tensor; a box is one page of one head.  A page number of n_pages reads zeros.
+bool make_page_map(CUtensorMap* tm, const attn_kv_cache_t* c, int t) {
+  const long long* st = t == 0 ? c->k_strides : c->v_strides;
+  const cuuint64_t dims[4] = {attn::kv::kKvDim, static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->Hkv),
+                              static_cast<cuuint64_t>(c->n_pages)};
+  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(st[1]), static_cast<cuuint64_t>(st[2]), static_cast<cuuint64_t>(st[0])};
+  const cuuint32_t box[4] = {attn::kv::kKvDim, static_cast<cuuint32_t>(c->page_size), 1, 1};
+  const cuuint32_t elem_strides[4] = {1, 1, 1, 1};
+  return g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, t == 0 ? c->k : c->v, dims, strides, box, elem_strides,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // A part of a tile for every CTA that may end in one or begin in one.
 size_t cached_parts(int ctas, int rows) { return 2ull * ctas * rows; }
 size_t cached_workspace(int ctas, int rows) {
@@ -184,10 +197,12 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool e4m3 = p.c.type == ATTN_KV_E4M3;
   if (many) {
+    CUtensorMap tm_k, tm_v;
+    if (!make_page_map(&tm_k, cache, 0) || !make_page_map(&tm_v, cache, 1)) return ATTN_ERR_CUDA;
     if (e4m3) {
-      attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(p);
+      attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
     } else {
-      attn::kv::attn_cached_tile_kernel<attn::kv::kInt8><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(p);
+      attn::kv::attn_cached_tile_kernel<attn::kv::kInt8><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
     }
   } else if (e4m3) {
     attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3><<<p.ctas, attn::kv::kDecThreads, attn::kv::kDecSmemBytes, s>>>(p);
