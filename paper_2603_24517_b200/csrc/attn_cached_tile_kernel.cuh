@@ -34,10 +34,13 @@ constexpr int kTSmemKv = 2 * kTileBytes;
 constexpr int kTSmemRaw = kTSmemKv + kKvSlots * kTileBytes;      // codes of one K and one V tile
 constexpr int kTSmemStats = kTSmemRaw + 2 * kTile * kKvDim;      // float [2 stages][2][128]
 constexpr int kMetaSteps = 4;
-constexpr int kMetaFloats = 32;
+constexpr int kMetaFloats = 28;
+constexpr int kItemSlots = 4;      // items published ahead: the fetching warp looks two steps ahead, which may be two items
+constexpr int kItemInts = 12;
 constexpr int kTSmemMeta = kTSmemStats + 2 * 2 * kTile * 4;
-constexpr int kTSmemBars = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
-constexpr int kTNumBars = 2 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 4;
+constexpr int kTSmemItems = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
+constexpr int kTSmemBars = kTSmemItems + kItemSlots * kItemInts * 4;
+constexpr int kTNumBars = 2 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemSlots;
 constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
 constexpr int kTSmemBytes = kTSmemMisc + 16;
 static_assert(kTSmemBytes <= 232448, "shared memory budget of one CTA");
@@ -61,6 +64,8 @@ struct TileBarriers {
   uint64_t* l_full;    // [2] softmax (128 threads) -> epilogue
   uint64_t* l_empty;   // [2] epilogue (128 threads) -> softmax
   uint64_t* meta_full; // [kMetaSteps] fetching warp -> softmax
+  uint64_t* item_full;  // [kItemSlots] fetching warp -> MMA, softmax, epilogue
+  uint64_t* item_empty; // [kItemSlots] those 13 warps -> fetching warp
 };
 enum : int { kRoleConvert = 6 << 8, kBarMeta = 20 };
 
@@ -70,19 +75,49 @@ constexpr uint32_t make_idesc_f16(uint32_t b_mn_major) {  // as make_idesc_bf16,
 constexpr uint32_t kIdescQKf16 = make_idesc_f16(0);
 constexpr uint32_t kIdescPVf16 = make_idesc_f16(1);
 
-// One tile pair, or the CTA's piece of it.
+// One tile pair, or the CTA's piece of it, as the fetching warp publishes it: the roles keep no place on the line of work
+// themselves (the softmax warps have no registers for it).
 struct Item {
-  int t_first, n;   // steps
+  int n;            // steps; 0: no more items
+  int t_first;      // the first of them
   bool two;         // the second stage has rows
   bool whole;       // all of the tile's steps
+  int b, h, tile;
+  SeqWork s;
+  int last;         // the last CTA with a part of the tile
 };
-__device__ __forceinline__ Item item_of(const CachedParams& p, const Line& line, const Cursor<kTileRows>& c, long long at) {
-  Item it;
-  it.t_first = c.t;
-  it.n = static_cast<int>(min(static_cast<long long>(c.steps - c.t), line.end - at));
-  it.two = static_cast<long long>(c.tile) * kTileRows + kTile < static_cast<long long>(c.s.n) * p.group;
-  it.whole = c.t == 0 && it.n == c.steps;
-  return it;
+__device__ __forceinline__ void publish_item(int* box, const CachedParams& p, const Line& line, const Cursor<kTileRows>& c, long long at) {
+  const int n = static_cast<int>(min(static_cast<long long>(c.steps - c.t), line.end - at));
+  const bool two = static_cast<long long>(c.tile) * kTileRows + kTile < static_cast<long long>(c.s.n) * p.group;
+  box[0] = n;
+  box[1] = c.t;
+  box[2] = (two ? 1 : 0) | (c.t == 0 && n == c.steps ? 2 : 0);
+  box[3] = c.b;
+  box[4] = c.h;
+  box[5] = c.tile;
+  box[6] = c.s.row0;
+  box[7] = c.s.n;
+  box[8] = c.s.len;
+  box[9] = c.s.keys;
+  box[10] = static_cast<int>(line.owner(at - c.t + c.steps - 1));
+}
+// The k-th item of this CTA for a whole warp of a consuming role; false when a wait ran out.
+__device__ __forceinline__ bool take_item(const TileBarriers& bars, const uint8_t* smem, uint32_t k, WaitCtx ctx, int role, int lane, Item& it) {
+  const uint32_t slot = k % kItemSlots;
+  if (!mbar_wait_warp(&bars.item_full[slot], (k / kItemSlots) & 1, ctx, role | kBarSchedFull)) return false;
+  const int* box = reinterpret_cast<const int*>(smem + kTSmemItems) + slot * kItemInts;
+  it.n = box[0];
+  it.t_first = box[1];
+  it.two = (box[2] & 1) != 0;
+  it.whole = (box[2] & 2) != 0;
+  it.b = box[3];
+  it.h = box[4];
+  it.tile = box[5];
+  it.s = SeqWork{box[6], box[7], box[8], box[9]};
+  it.last = box[10];
+  __syncwarp();
+  if (lane == 0) mbar_arrive(&bars.item_empty[slot]);
+  return true;
 }
 
 // ---- the pages' codes -------------------------------------------------------------------------------------------------
@@ -97,14 +132,35 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
                                            const CUtensorMap* tm_v) {
   const CacheView& c = p.c;
   long long left = line.end - line.begin;  // steps whose pages have not been looked up yet
-  bool first = true;
+  bool first = true, ended = false, ok = true;
+  uint32_t items = 0;
+  auto publish = [&](bool some) {
+    const uint32_t slot = items % kItemSlots;
+    ok = ok && mbar_wait_warp(&bars.item_empty[slot], ((items / kItemSlots) & 1) ^ 1, ctx, kRoleLoad | kBarSchedEmpty);
+    ++items;
+    if (!ok) return;
+    if (lane == 0) {
+      int* box = reinterpret_cast<int*>(smem + kTSmemItems) + slot * kItemInts;
+      if (some) {
+        publish_item(box, p, line, ahead, line.end - left);
+      } else {
+        box[0] = 0;
+      }
+      mbar_arrive(&bars.item_full[slot]);
+    }
+    __syncwarp();
+  };
   auto look_up = [&]() {
     StepPlace f;
     f.keys = 0;
     f.page = -2;
     f.h = f.key0 = 0;
     f.first = false;
-    if (left > 0) {
+    if (left <= 0) {
+      if (!ended) publish(false);
+      ended = true;
+    } else {
+      if (first || ahead.t == 0) publish(true);
       --left;
       f.h = ahead.h;
       f.key0 = ahead.t * kStepKeys;
@@ -127,6 +183,7 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
   const uint32_t steps = static_cast<uint32_t>(line.end - line.begin);
   for (uint32_t i = 0; i < steps; ++i) {
     const StepPlace after = look_up();
+    if (!ok) return;
     const float scale_next = scale_of(next);
     float top = lane >= 8 && lane < 16 ? scale_now : 0.f;
 #pragma unroll
@@ -140,8 +197,7 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
     for (int kv = 0; kv < 2; ++kv) {
       // the step's entry may be written once the codes of the keys of the step before have been converted: that needed the
       // slot of the keys two steps before that, so the scores of i - 3 are complete and the weights of i - 4 were taken
-      const bool ok = mbar_wait_warp(&bars.raw_empty[kv], (i & 1) ^ 1, ctx, kRoleLoad | kBarKvEmpty);
-      if (!ok) return;
+      if (!mbar_wait_warp(&bars.raw_empty[kv], (i & 1) ^ 1, ctx, kRoleLoad | kBarKvEmpty)) return;
       if (kv == 0) {
         if (lane < 8) {
           meta[kMetaK + lane] = scale_now;
@@ -239,16 +295,16 @@ __device__ __forceinline__ void issue_pv_f16(bool leader, uint32_t tmem_o, uint3
   }
 }
 
-__device__ __forceinline__ void role_tile_mma(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
-                                              const Line& line, Cursor<kTileRows> cur, uint32_t tmem) {
+__device__ __forceinline__ void role_tile_mma(const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,                                              uint32_t tmem, int lane) {
   const bool leader = elect_one();
   const uint32_t base = smem_u32(smem);
   const uint64_t q_desc[2] = {kmajor_desc(base + kTSmemQ), kmajor_desc(base + kTSmemQ + kTileBytes)};
   uint32_t kv_cnt = 0;
   uint32_t q_cnt[2] = {0, 0};
   uint32_t sp_cnt[2] = {0, 0};
-  for (long long at = line.begin; at < line.end;) {
-    const Item it = item_of(p, line, cur, at);
+  for (uint32_t k = 0;; ++k) {
+    Item it;
+    if (!take_item(bars, smem, k, ctx, kRoleMma, lane, it) || it.n == 0) return;
     {
       const uint32_t slot = kv_cnt % kKvSlots, par = (kv_cnt / kKvSlots) & 1;
       if (!mbar_wait_warp(&bars.kv_full[slot], par, ctx, kRoleMma | kBarKvFull)) return;
@@ -311,34 +367,42 @@ __device__ __forceinline__ void role_tile_mma(const CachedParams& p, const TileB
     }
     ++q_cnt[0];
     if (it.two) ++q_cnt[1];
-    at += it.n;
-    if (at < line.end) cur.next_tile(p);
   }
 }
 
 // ---- softmax: one thread owns one row of stage `s` ------------------------------------------------------------------------
 __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
-                                                  const Line& line, Cursor<kTileRows> cur, uint32_t tmem, int s, int row, int lane) {
+                                                  uint32_t tmem, int s, int row, int lane) {
   const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
   const uint32_t t_s = tmem + lane_sel + s * kTile;
   const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
   float* stats = reinterpret_cast<float*>(smem + kTSmemStats) + s * 2 * kTile;
   uint32_t s_cnt = 0, l_cnt = 0, step = 0;
-  for (long long at = line.begin; at < line.end;) {
-    const Item it = item_of(p, line, cur, at);
-    if (s == 0 || it.two) {
-      // Q: the stage's last product that reads it has completed (its scores have been taken)
-      const long long r0 = static_cast<long long>(cur.tile) * kTileRows + s * kTile;
-      const TilePlace w = tile_place(p, cur.s, cur.h, r0 + row);
-      int limit = cur.s.keys;  // keys the row sees; rows that are not real see all
-      float factor;
-      {
+  for (uint32_t k = 0;; ++k) {
+    int n, key0;  // steps left, first key of the step
+    int limit;    // keys the row sees; rows that are not real see all
+    int clear;    // keys that all rows of the stage see: steps up to there need no mask
+    float factor;
+    bool used;
+    bool seen;    // the row sees a key here
+    {
+      Item it;
+      if (!take_item(bars, smem, k, ctx, kRoleSoftmax, lane, it) || it.n == 0) return;
+      n = it.n;
+      used = s == 0 || it.two;
+      if (used) {
+        // Q: the stage's last product that reads it has completed (its scores have been taken)
+        const long long r0 = static_cast<long long>(it.tile) * kTileRows + s * kTile;
+        const TilePlace w = tile_place(p, it.s, it.h, r0 + row);
+        limit = w.real ? visible(it.s, w.token, p.causal) : it.s.keys;
+        clear = visible(it.s, min(static_cast<int>(r0 / p.group), it.s.n - 1), p.causal);
+        key0 = it.t_first * kStepKeys;
+        seen = limit > key0;
         uint4 x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = make_uint4(0, 0, 0, 0);
         if (w.real) {
-          limit = visible(cur.s, w.token, p.causal);
-          const uint4* src = reinterpret_cast<const uint4*>(p.q + row_offset(p, p.sq, cur.b, cur.s, w));
+          const uint4* src = reinterpret_cast<const uint4*>(p.q + row_offset(p, p.sq, it.b, it.s, w));
 #pragma unroll
           for (int i = 0; i < 16; ++i) x[i] = __ldg(src + i);
         }
@@ -347,8 +411,8 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         for (int i = 0; i < 16; ++i) {
           const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 f = unpack_bf16x2(words[k]);
+          for (int m = 0; m < 4; ++m) {
+            const float2 f = unpack_bf16x2(words[m]);
             largest = max3(largest, fabsf(f.x), fabsf(f.y));
           }
         }
@@ -360,9 +424,9 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
           const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
           uint32_t y[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 f = unpack_bf16x2(words[k]);
-            y[k] = pack_f16x2(f.x * up, f.y * up);
+          for (int m = 0; m < 4; ++m) {
+            const float2 f = unpack_bf16x2(words[m]);
+            y[m] = pack_f16x2(f.x * up, f.y * up);
           }
           *reinterpret_cast<uint4*>(dst + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
         }
@@ -370,13 +434,13 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.q_full[s]);
       }
-      // keys that all rows of the stage see: steps up to there need no mask
-      const int clear = visible(cur.s, min(static_cast<int>(r0 / p.group), cur.s.n - 1), p.causal);
+    }
+    if (used) {
       float m_used = -INFINITY;  // reference maximum, log2 units
-      float l = 0.f, vref = 0.f;
-      for (int j = 0; j < it.n; ++j) {
-        const uint32_t q = (step + j) % kMetaSteps;
-        bool ok = mbar_wait(&bars.meta_full[q], ((step + j) / kMetaSteps) & 1, ctx, kRoleSoftmax | kBarMeta);
+      float l = 0.f;
+      for (int j = 0; j < n; ++j, ++step, key0 += kStepKeys) {
+        const uint32_t q = step % kMetaSteps;
+        bool ok = mbar_wait(&bars.meta_full[q], (step / kMetaSteps) & 1, ctx, kRoleSoftmax | kBarMeta);
         const float* meta = reinterpret_cast<const float*>(smem + kTSmemMeta) + q * kMetaFloats;
         ok = ok && mbar_wait(&bars.s_full[s], s_cnt & 1, ctx, kRoleSoftmax | kBarSFull);
         ok = __all_sync(0xffffffffu, ok);
@@ -393,7 +457,6 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         for (int g = 0; g < 8; ++g) cg[g] = fmaxf(meta[kMetaK + g] * factor, 1e-37f);  // not 0: -inf stays -inf
         tmem_wait_ld();
 #define X(i) __uint_as_float(xr[(i)])
-        const int key0 = (it.t_first + j) * kStepKeys;
         if (key0 + kStepKeys > clear) {  // warp-uniform
           const int vis = limit - key0;
 #pragma unroll
@@ -410,7 +473,6 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
           const float e = max3(X(i + 12), X(i + 13), X(i + 14));
           m_blk = fmaxf(m_blk, fmaxf(max3(a, b, X(i + 15)), max3(c, d, e)) * cg[g]);
         }
-        vref = meta[kMetaVref];
         if (j == 0) {
           m_used = m_blk == -INFINITY ? 0.f : m_blk;
         } else {
@@ -474,26 +536,28 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
       // a row that has seen no key here has the sum 0 by definition, and no maximum
-      const bool seen = limit > it.t_first * kStepKeys;
       stats[row] = seen ? l : 0.f;
       stats[kTile + row] = seen ? m_used : -INFINITY;
-      if (row == 0) reinterpret_cast<float*>(smem + kTSmemMisc)[2 + s] = vref;
+      if (row == 0) {  // the last step's entry: the next one that takes its place needs scores of the next item
+        reinterpret_cast<float*>(smem + kTSmemMisc)[2 + s] =
+            reinterpret_cast<const float*>(smem + kTSmemMeta)[(step - 1) % kMetaSteps * kMetaFloats + kMetaVref];
+      }
       mbar_arrive(&bars.l_full[s]);
       ++l_cnt;
+    } else {
+      step += n;
     }
-    step += it.n;
-    at += it.n;
-    if (at < line.end) cur.next_tile(p);
   }
 }
 
 // ---- results ----------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
-                                                   const Line& line, Cursor<kTileRows> cur, uint32_t tmem, int row, int lane) {
+                                                   uint32_t tmem, int row, int lane) {
   const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
   uint32_t cnt[2] = {0, 0};
-  for (long long at = line.begin; at < line.end;) {
-    const Item it = item_of(p, line, cur, at);
+  for (uint32_t k = 0;; ++k) {
+    Item it;
+    if (!take_item(bars, smem, k, ctx, kRoleEpilogue, lane, it) || it.n == 0) return;
 #pragma unroll 1
     for (int s = 0; s < 2; ++s) {
       if (s == 1 && !it.two) continue;
@@ -511,13 +575,13 @@ __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const 
       ++cnt[s];
       tc_fence_after_sync();
       const int r = s * kTile + row;
-      const TilePlace w = tile_place(p, cur.s, cur.h, static_cast<long long>(cur.tile) * kTileRows + r);
+      const TilePlace w = tile_place(p, it.s, it.h, static_cast<long long>(it.tile) * kTileRows + r);
       // keys beyond the table's reach
-      if (w.real && cur.s.len > cur.s.keys && (!p.causal || cur.s.len - cur.s.n + w.token >= cur.s.keys)) l = __int_as_float(0x7fffffff);
+      if (w.real && it.s.len > it.s.keys && (!p.causal || it.s.len - it.s.n + w.token >= it.s.keys)) l = __int_as_float(0x7fffffff);
       const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
       const long long slot = 2ll * blockIdx.x + (it.t_first == 0 ? 1 : 0);
       const float f = it.whole ? (l == 0.f ? 0.f : __fdividef(vref, l)) : vref;
-      uint16_t* out = p.o + row_offset(p, p.so, cur.b, cur.s, w);
+      uint16_t* out = p.o + row_offset(p, p.so, it.b, it.s, w);
       float* part = p.parts + (slot * kTileRows + r) * kKvDim;
 #pragma unroll
       for (int cc = 0; cc < 4; ++cc) {
@@ -549,16 +613,14 @@ __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const 
       if (lane == 0) mbar_arrive(&bars.o_empty[s]);
       if (it.whole) {
         if (w.real && p.lse != nullptr)
-          p.lse[lse_index(p, cur.b, cur.s, w)] = l == 0.f ? -INFINITY : (m - kWeightShift + lg2_approx(l)) * kLn2;
+          p.lse[lse_index(p, it.b, it.s, w)] = l == 0.f ? -INFINITY : (m - kWeightShift + lg2_approx(l)) * kLn2;
       } else {
         reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kTileRows * kKvDim)[slot * kTileRows + r] = make_float2(m, l);
         if (r == 0 && it.t_first == 0) {
-          p.pieces[blockIdx.x] = make_int4(cur.b, cur.h, cur.tile, static_cast<int>(line.owner(at + cur.steps - 1)));
+          p.pieces[blockIdx.x] = make_int4(it.b, it.h, it.tile, it.last);
         }
       }
     }
-    at += it.n;
-    if (at < line.end) cur.next_tile(p);
   }
 }
 
@@ -581,6 +643,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   bars.l_full = bars.o_empty + 2;
   bars.l_empty = bars.l_full + 2;
   bars.meta_full = bars.l_empty + 2;
+  bars.item_full = bars.meta_full + kMetaSteps;
+  bars.item_empty = bars.item_full + kItemSlots;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kTSmemMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kTSmemMisc + 4);
   const WaitCtx ctx{abort_flag, p.status, kWaitLimitNs};
@@ -612,6 +676,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
       mbar_init(&bars.kv_empty[i], 1);
     }
     for (int i = 0; i < kMetaSteps; ++i) mbar_init(&bars.meta_full[i], 1);
+    for (int i = 0; i < kItemSlots; ++i) {
+      mbar_init(&bars.item_full[i], 1);
+      mbar_init(&bars.item_empty[i], kSchedConsumers);
+    }
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -626,14 +694,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
 
   if (warp < 8) {
     reg_alloc<kTRegsSoftmax>();
-    role_tile_softmax(p, bars, smem, ctx, line, cur, tmem, warp >> 2, tid & 127, lane);
+    role_tile_softmax(p, bars, smem, ctx, tmem, warp >> 2, tid & 127, lane);
   } else if (warp < 12) {
     reg_dealloc<kTRegsEpilogue>();
-    role_tile_epilogue(p, bars, smem, ctx, line, cur, tmem, tid & 127, lane);
+    role_tile_epilogue(p, bars, smem, ctx, tmem, tid & 127, lane);
   } else {
     reg_dealloc<kTRegsOther>();
     if (warp == 12) {
-      role_tile_mma(p, bars, smem, ctx, line, cur, tmem);
+      role_tile_mma(bars, smem, ctx, tmem, lane);
     } else if (warp == 13) {
       role_fetch(p, bars, smem, ctx, line, cur, lane, &tm_k, &tm_v);
       if (*abort_flag) {  // let loads in flight land before the CTA's shared memory is released
