@@ -87,6 +87,14 @@ int resident_pairs(int sm_count) {
   return n > 0 ? n : 1;
 }
 
+template <int NB>
+bool prepare_decode() {
+  return cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::Dec<NB>::kSmem) == cudaSuccess &&
+         cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kInt8, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::Dec<NB>::kSmem) == cudaSuccess;
+}
+
 // Per-device one-time set-up: architecture check, kernel attribute, scheduler counters and
 // status word.  Returns the state or nullptr (with *st set).
 DeviceState* device_state(attn_status_t* st) {
@@ -135,10 +143,7 @@ DeviceState* device_state(attn_status_t* st) {
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           attn::kv::kDecSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           attn::kv::kDecSmemBytes) != cudaSuccess ||
+      !prepare_decode<1>() || !prepare_decode<2>() || !prepare_decode<4>() ||
       cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::kv::kTSmemBytes) != cudaSuccess ||
       cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize,

@@ -2,18 +2,22 @@
 //
 //     s_ij = scale k_scale(page of j) q_i . c^K_j,    o_i = sum_j softmax_j(s_ij) v_scale(page of j) c^V_j
 //
-// Bound by HBM: 256 bytes a cached token and key head, read once for all query heads of the group.  A query tile is 16 rows
-// (token, head of the group), heads fastest.  All work is a line of (sequence, key head, query tile, 128 keys) steps, cut into
-// equal contiguous pieces, one a CTA, whatever the lengths are; the cut is computed on the device from the lengths.  A CTA
-// that holds a whole tile's keys writes its result, the others leave fp32 parts, which a second kernel joins in order.
+// Bound by HBM: 256 bytes a cached token and key head, read once for all query heads of the group.  A query tile is 8, 16 or 32
+// rows (token, head of the group), heads fastest.  All work is a line of (sequence, key head, query tile, 128 keys) steps, cut
+// into equal contiguous pieces, one a CTA, whatever the lengths are; the cut is computed on the device from the lengths.  A
+// CTA that holds a whole tile's keys writes its result, the others leave fp32 parts, which a second kernel joins in order.
 //
-// In a CTA each of 8 warps owns 16 keys of a step and works alone until its piece of a tile ends: its own ring of four 4 KB
-// stages filled by 16-byte asynchronous copies three steps ahead, its own running maximum, sum and 16 x 128 accumulator.
-// 16 keys lie in one page, so the scales are one factor a warp and step.  Keys go from shared memory to the operands of
-// mma.m16n8k16 (f16) without a transpose: the products' inner index may be in any order, so a lane takes 16 consecutive head
-// dimensions of its key (K) or of four keys (V), and the queries are loaded in the same order.  Codes are exact in f16;
-// queries are scaled by a power of two of their row, weights are held as 2^6 exp(s - m) with a maximum that may lag by a
-// factor of 2^8, so f16 keeps 11 bits of both; V's scale enters as its ratio to the largest one met so far.
+// In a CTA each of 8 warps owns 16 keys of a step and works alone until its piece of a tile ends: its own ring of 4 KB stages
+// filled by TMA, its own running maximum, sum and accumulator.  16 keys lie in one page, so the scales are one factor a warp
+// and step.  The products are S^T = K Q^T and O^T = V^T P^T by mma.m16n8k16 (f16): the keys, then the head dimension fill the 16
+// rows of the left operand, so 8 query rows leave nothing idle (with the queries on the left, 16 rows were computed for any
+// group).  Codes go from shared memory to the left operand without a transpose: the inner index of a product may be in
+// any order, so a lane takes 16 consecutive head dimensions of its keys (K) or of four keys (V) and the queries are loaded in the
+// same order; the weights change sides by movmatrix.  Which key and which 16 dimensions a lane takes is chosen (`spread`) so that
+// the reads of a 128-byte-swizzled stage meet no bank twice.
+// Codes are exact in f16; queries are scaled by a power of two of their row, weights are held as 2^6 exp(s - m) with a maximum
+// that may lag by a factor of 2^8 (so it is reduced over the lanes only when one of them meets a larger score), which leaves
+// f16 its 11 bits of both; V's scale enters as its ratio to the largest one met so far.
 #pragma once
 
 #include "attn_fwd_kernel.cuh"
@@ -24,15 +28,23 @@ namespace kv {
 
 constexpr int kDecWarps = 8;
 constexpr int kDecThreads = kDecWarps * 32;
-constexpr int kDecRows = 16;
-constexpr int kDecStages = 4;
 constexpr int kStepKeys = 128;                         // keys a CTA takes in one step: 16 a warp
 constexpr int kWarpStageBytes = 2 * 16 * kKvDim;       // K then V
-constexpr int kDecRingBytes = kDecWarps * kDecStages * kWarpStageBytes;  // 128 KB
-constexpr int kDecMergeBytes = kDecWarps * kDecRows * kKvDim * 4;        // 64 KB
-constexpr int kDecSmemBytes = kDecRingBytes + kDecMergeBytes + kDecWarps * kDecStages * 16 + kDecWarps * kDecRows * 8;
 constexpr float kWeightShift = 6.f;   // weights are held as 2^kWeightShift exp(s - m)
 constexpr float kWeightLag = 8.f;     // log2 units the reference maximum may lag
+
+// Query tiles of 8 NB rows.  8 rows: two CTAs an SM, so that one's start and end run beside the other's steps.
+template <int NB>
+struct Dec {
+  static constexpr int kRows = 8 * NB;
+  static constexpr int kCtasPerSm = NB == 1 ? 2 : 1;
+  static constexpr int kStages = NB == 1 ? 2 : NB == 2 ? 4 : 2;
+  static constexpr int kRing = kDecWarps * kStages * kWarpStageBytes;
+  static constexpr int kMerge = kDecWarps * kRows * kKvDim * 4;
+  static constexpr int kStats = kDecWarps * kRows * 8;
+  static constexpr int kBars = kDecWarps * kStages * 8;
+  static constexpr int kSmem = kRing + kMerge + kStats + kBars + 16 + 1024;  // 1024: the ring starts at a multiple of it
+};
 
 struct CachedParams {
   CacheView c;
@@ -187,19 +199,6 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   return true;
 }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool take) {
-  const int bytes = take ? 16 : 0;  // 0: zeros are written, nothing is read
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool take) {
-  const int bytes = take ? 4 : 0;
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -237,79 +236,102 @@ __device__ __forceinline__ long long lse_index(const CachedParams& p, int b, con
                                : static_cast<long long>(w.head) * p.c.S + s.row0 + w.token;
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(kDecThreads, 1) attn_cached_decode_kernel(const CachedParams p) {
-  extern __shared__ __align__(128) uint8_t smem[];
-  uint8_t* merge = smem + kDecRingBytes;
-  float2* scale_ring = reinterpret_cast<float2*>(merge + kDecMergeBytes);          // [warp][stage]{k, v}, 16 bytes apart
-  float2* row_stats = reinterpret_cast<float2*>(merge + kDecMergeBytes + kDecWarps * kDecStages * 16);  // [warp][row]{m, l}
+// Transpose of an 8 x 8 matrix of 16-bit numbers that lies over the warp, two a lane.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// 0..7 in an order in which neighbours 2 i, 2 i + 1 lie four apart.
+__device__ __forceinline__ int spread(int g) { return (g & 1) << 2 | g >> 1; }
+
+template <int TYPE, int NB>
+__global__ void __launch_bounds__(kDecThreads, Dec<NB>::kCtasPerSm)
+attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const CachedParams p) {
+  using D = Dec<NB>;
+  constexpr int kRows = D::kRows;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);  // the swizzle goes by the address
+  uint8_t* merge = smem + D::kRing;
+  float2* row_stats = reinterpret_cast<float2*>(merge + D::kMerge);  // [warp][row]{m, l}
+  uint64_t* bars = reinterpret_cast<uint64_t*>(merge + D::kMerge + D::kStats);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(merge + D::kMerge + D::kStats + D::kBars);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
+  const WaitCtx ctx{abort_flag, p.status, kWaitLimitNs};
 
   Line line;
-  Cursor<kDecRows> now;
-  const bool works = find_piece<kDecRows>(p, line, now, reinterpret_cast<long long*>(merge));
-  __syncthreads();  // the scratch is the merge buffer
-  if (threadIdx.x == 0) p.pieces[blockIdx.x] = make_int4(0, 0, 0, -1);
+  Cursor<kRows> now;
+  const bool works = find_piece<kRows>(p, line, now, reinterpret_cast<long long*>(merge));
+  if (threadIdx.x == 0) {
+    p.pieces[blockIdx.x] = make_int4(0, 0, 0, -1);
+    for (int i = 0; i < kDecWarps * D::kStages; ++i) mbar_init(&bars[i], 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  __syncthreads();  // also: the scratch of find_piece is the merge buffer
   if (!works) return;
-  Cursor<kDecRows> ahead = now;          // what is requested next
-  long long left_ahead = line.end - line.begin;
 
-  const uint32_t ring = smem_u32(smem) + warp * kDecStages * kWarpStageBytes;
-  const uint32_t scales = smem_u32(scale_ring) + warp * kDecStages * 16;
-  volatile int* bad_ring = reinterpret_cast<volatile int*>(scale_ring) + warp * kDecStages * 4 + 2;
-  int put = 0;
-  // requests 16 keys of the step `ahead` stands at and moves on
-  auto request = [&]() {
+  Cursor<kRows> ahead = now;  // the step whose codes are requested next
+  long long left_ahead = line.end - line.begin;
+  uint8_t* ring = smem + warp * D::kStages * kWarpStageBytes;
+  uint64_t* full = bars + warp * D::kStages;
+  const int slot_mask = (1 << p.c.page_log2) - 1;
+  // page of this warp's keys in the step `ahead` stands at: -1 does not exist, -2 no key there
+  auto look_up = [&]() {
+    const int key = ahead.t * kStepKeys + warp * 16;
+    return left_ahead > 0 && key < ahead.s.keys ? page_of(p.c, ahead.b, key >> p.c.page_log2) : -2;
+  };
+  int page = look_up(), put = 0;
+  float2 scales[D::kStages];  // of the requested steps, the oldest first; keys of a page that does not exist: -1
+  // requests the 16 keys of that step and moves on to the next
+  auto request = [&](float2& scale) {
+    scale = make_float2(0.f, 0.f);
+    if (page != -2) {
+      if (lane == 0) {
+        uint8_t* dst = ring + put * kWarpStageBytes;
+        const int at = page >= 0 ? page : p.c.n_pages;  // behind the last page: zeros
+        const int slot = (ahead.t * kStepKeys + warp * 16) & slot_mask;
+        mbar_arrive_expect_tx(&full[put], kWarpStageBytes);
+        tma_load_4d(dst, &tm_k, &full[put], 0, slot, ahead.h, at);
+        tma_load_4d(dst + 16 * kKvDim, &tm_v, &full[put], 0, slot, ahead.h, at);
+      }
+      if (page >= 0) {
+        const long long at = static_cast<long long>(page) * p.c.Hkv + ahead.h;
+        scale = make_float2(__ldg(p.c.scales[0] + at), __ldg(p.c.scales[1] + at));
+      } else {
+        scale.x = -1.f;
+      }
+    }
+    put = put + 1 == D::kStages ? 0 : put + 1;
     if (left_ahead > 0) {
       --left_ahead;
-      const int key0 = ahead.t * kStepKeys + warp * 16;
-      const bool any = key0 < ahead.s.keys;
-      const int page = any ? page_of(p.c, ahead.b, key0 >> p.c.page_log2) : -1;
-      const int slot0 = key0 & ((1 << p.c.page_log2) - 1);
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const uint8_t* base = p.c.codes[kv] + max(page, 0) * p.c.sp[kv] + ahead.h * p.c.sh[kv] + slot0 * p.c.ss[kv];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * i + (lane >> 3), u = lane & 7;
-          const int swz = kv == 0 ? u ^ ((r & 1) << 2) : u ^ (r & 6);
-          const bool take = page >= 0 && key0 + r < ahead.s.keys;
-          cp_async16(ring + put * kWarpStageBytes + kv * 16 * kKvDim + r * kKvDim + swz * 16,
-                     take ? base + r * p.c.ss[kv] + u * 16 : p.c.codes[kv], take);
-        }
-      }
-      if (lane < 2) {
-        cp_async4(scales + put * 16 + lane * 4,
-                  p.c.scales[lane] + (page >= 0 ? static_cast<long long>(page) * p.c.Hkv + ahead.h : 0ll), page >= 0);
-      }
-      if (lane == 2) bad_ring[put * 4] = any && page < 0;
-      if (++ahead.t >= ahead.steps) ahead.next_tile(p);
+      if (++ahead.t >= ahead.steps && left_ahead > 0) ahead.next_tile(p);
+      page = look_up();
     }
-    cp_async_commit();
-    put = put + 1 == kDecStages ? 0 : put + 1;
   };
-  for (int i = 0; i < kDecStages - 1; ++i) request();
+#pragma unroll
+  for (int i = 0; i < D::kStages; ++i) request(scales[i]);
 
   int get = 0;
+  uint32_t phase = 0;  // a bit a stage
   long long at = line.begin;
   while (at < line.end) {
     // ---- one tile, or this CTA's piece of it ----
     const int t_first = now.t;
     const int n_steps = static_cast<int>(min(static_cast<long long>(now.steps - now.t), line.end - at));
-    const long long tile_begin = at - now.t;
-    // queries, in the order that a lane's K bytes have: step i of the product takes d = 64 (i / 4) + 16 t4 + 4 (i % 4) + 0..3
-    uint32_t qf[8][4];
-    float factor[2];
-    int limit[2];  // keys the row sees
+    const long long tile_begin = at - now.t, row_first = static_cast<long long>(now.tile) * kRows;
+    // queries (right operand): lane (g, t4) has row g; step i of the product takes d = 64 (i / 4) + 16 t4 + 4 (i % 4) + 0..3, the
+    // order that a lane's codes of K have.  Scores: lane (g, t4) has rows 2 t4, 2 t4 + 1 of keys spread(g), 8 + spread(g)
+    uint32_t qf[NB][8][2];
+    float factor[NB][2];
+    int limit[NB][2];  // keys the row sees
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      const TilePlace w = tile_place(p, now.s, now.h, static_cast<long long>(now.tile) * kDecRows + g + 8 * rr);
+    for (int nb = 0; nb < NB; ++nb) {
+      const TilePlace w = tile_place(p, now.s, now.h, row_first + 8 * nb + g);
       uint32_t raw[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) raw[i] = 0;
-      limit[rr] = 0;
       if (w.real) {
-        limit[rr] = visible(now.s, w.token, p.causal);
         const uint16_t* row = p.q + row_offset(p, p.sq, now.b, now.s, w) + t4 * 16;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -324,218 +346,241 @@ __global__ void __launch_bounds__(kDecThreads, 1) attn_cached_decode_kernel(cons
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float2 f = unpack_bf16x2(raw[i]);
-        largest = fmaxf(largest, fmaxf(fabsf(f.x), fabsf(f.y)));
+        largest = max3(largest, fabsf(f.x), fabsf(f.y));
       }
       largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
       largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 2));
       const float up = row_factor(largest);
-      factor[rr] = p.scale_log2 / up;
+      const float down = p.scale_log2 / up;
+      const int sees = w.real ? visible(now.s, w.token, p.causal) : 0;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {  // row 2 t4 + e is with the lanes of g = 2 t4 + e
+        factor[nb][e] = __shfl_sync(0xffffffffu, down, 8 * t4 + 4 * e);
+        limit[nb][e] = __shfl_sync(0xffffffffu, sees, 8 * t4 + 4 * e);
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {  // word i: d = 64 (i / 8) + 16 t4 + 2 (i % 8)
         const float2 f = unpack_bf16x2(raw[i]);
-        qf[i >> 1][(i & 1) * 2 + rr] = pack_f16x2(f.x * up, f.y * up);
+        qf[nb][i >> 1][i & 1] = pack_f16x2(f.x * up, f.y * up);
       }
     }
-    float acc[16][4];
+    // keys that all rows see: steps up to there need no mask
+    const int clear = visible(now.s, min(static_cast<int>(row_first / p.group), now.s.n - 1), p.causal);
+    float acc[NB][8][4];  // d = 16 spread(g) + 2 mt (values 0, 1) and + 1 (2, 3); rows 2 t4 (0, 2) and 2 t4 + 1 (1, 3)
+    float m[NB][2], l[NB][2], vref = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, vref = 0.f;
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) acc[nb][mt][0] = acc[nb][mt][1] = acc[nb][mt][2] = acc[nb][mt][3] = 0.f;
+      m[nb][0] = m[nb][1] = -INFINITY;
+      l[nb][0] = l[nb][1] = 0.f;
+    }
 
+#pragma unroll 1
     for (int step = 0; step < n_steps; ++step) {
-      request();
-      cp_async_wait<kDecStages - 1>();
-      __syncwarp();
       const int key0 = (t_first + step) * kStepKeys + warp * 16;
-      if (key0 < now.s.keys) {
-        const uint8_t* stage = smem + warp * kDecStages * kWarpStageBytes + get * kWarpStageBytes;
-        const float* sc = reinterpret_cast<const float*>(scale_ring) + (warp * kDecStages + get) * 4;
-        const float k_scale = sc[0], v_scale = sc[1];
-        const bool bad = bad_ring[get * 4] != 0;
-        float s[2][4];
+      float k_scale = scales[0].x;
+      const float v_scale = scales[0].y;
+      if (key0 < now.s.keys) {  // else nothing was requested
+        // a wait that runs out leaves the codes as they are: the status word says that the results are void
+        mbar_wait_warp(&full[get], phase >> get & 1, ctx, kRoleLoad | kBarKvFull);
+        phase ^= 1u << get;
+        const uint8_t* stage = ring + get * kWarpStageBytes;
+        const bool bad = k_scale < 0.f;
+        if (bad) k_scale = 0.f;
+        float s[NB][4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-          const int r = 8 * j + g;
+        for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
+        const int kr = spread(g);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const uint4 w = *reinterpret_cast<const uint4*>(stage + r * kKvDim + ((half * 4 + t4) ^ ((r & 1) << 2)) * 16);
-            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        for (int half = 0; half < 2; ++half) {
+          const uint8_t* src = stage + kr * kKvDim + (((half * 4 + t4) ^ kr) << 4);
+          const uint4 w0 = *reinterpret_cast<const uint4*>(src), w1 = *reinterpret_cast<const uint4*>(src + 8 * kKvDim);
+          const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t b0, b1;
-              codes_to_f16<TYPE>(words[i], b0, b1);
-              mma_f16(s[j], qf[half * 4 + i], b0, b1);
-            }
+          for (int i = 0; i < 4; ++i) {
+            uint32_t a[4];
+            codes_to_f16<TYPE>(x0[i], a[0], a[2]);
+            codes_to_f16<TYPE>(x1[i], a[1], a[3]);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_f16(s[nb], a, qf[nb][half * 4 + i][0], qf[nb][half * 4 + i][1]);
           }
         }
-        // columns 2 t4 + e of n-tile j are keys key0 + 8 j + 2 t4 + e; rows g (values 0, 1) and g + 8 (2, 3)
-        float top[2];
+        bool grow = false;
 #pragma unroll
-        for (int rr = 0; rr < 2; ++rr) {
-          const float f = factor[rr] * k_scale;
+        for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
+          for (int e = 0; e < 2; ++e) {
+            const float f = factor[nb][e] * k_scale;
+            s[nb][e] *= f;
+            s[nb][2 + e] *= f;
+            if (key0 + 16 > clear) {  // warp-uniform
+              if (key0 + kr >= limit[nb][e]) s[nb][e] = -INFINITY;
+              if (key0 + 8 + kr >= limit[nb][e]) s[nb][2 + e] = -INFINITY;
+              if (bad && key0 < limit[nb][e]) l[nb][e] = __int_as_float(0x7fffffff);
+            } else if (bad) {
+              l[nb][e] = __int_as_float(0x7fffffff);
+            }
+            grow = grow || fmaxf(s[nb][e], s[nb][2 + e]) > m[nb][e] + kWeightLag;
+          }
+        }
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            float a[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float x = s[j][2 * rr + e] * f;
-              s[j][2 * rr + e] = key0 + 8 * j + 2 * t4 + e < limit[rr] ? x : -INFINITY;
+              float top = fmaxf(s[nb][e], s[nb][2 + e]);
+#pragma unroll
+              for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+              const float to = fmaxf(m[nb][e], top);
+              a[e] = m[nb][e] == -INFINITY ? 0.f : ex2_approx(m[nb][e] - to);
+              m[nb][e] = to;
+              l[nb][e] *= a[e];
             }
-          }
-          top[rr] = fmaxf(fmaxf(s[0][2 * rr], s[0][2 * rr + 1]), fmaxf(s[1][2 * rr], s[1][2 * rr + 1]));
-          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xffffffffu, top[rr], 1));
-          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xffffffffu, top[rr], 2));
-        }
-        if (__any_sync(0xffffffffu, top[0] > m[0] + kWeightLag || top[1] > m[1] + kWeightLag)) {
-          float a[2];
 #pragma unroll
-          for (int rr = 0; rr < 2; ++rr) {
-            const float to = fmaxf(m[rr], top[rr]);
-            a[rr] = m[rr] == -INFINITY ? 0.f : ex2_approx(m[rr] - to);
-            m[rr] = to;
-            l[rr] *= a[rr];
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            acc[i][0] *= a[0];
-            acc[i][1] *= a[0];
-            acc[i][2] *= a[1];
-            acc[i][3] *= a[1];
+            for (int mt = 0; mt < 8; ++mt) {
+              acc[nb][mt][0] *= a[0];
+              acc[nb][mt][1] *= a[1];
+              acc[nb][mt][2] *= a[0];
+              acc[nb][mt][3] *= a[1];
+            }
           }
         }
         if (v_scale > vref) {
           const float a = __fdividef(vref, v_scale);
           vref = v_scale;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][e] *= a;
+            for (int mt = 0; mt < 8; ++mt) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[nb][mt][e] *= a;
+            }
           }
         }
         const float ratio = vref > 0.f ? __fdividef(v_scale, vref) : 0.f;
-        uint32_t pf[4];
+        uint32_t pf[NB][2];
 #pragma unroll
-        for (int rr = 0; rr < 2; ++rr) {
-          const float ref = m[rr] == -INFINITY ? 0.f : m[rr] - kWeightShift;
+        for (int nb = 0; nb < NB; ++nb) {
+          float x[4];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float x = ex2_approx(s[j][2 * rr] - ref), y = ex2_approx(s[j][2 * rr + 1] - ref);
-            l[rr] += x + y;
-            pf[2 * j + rr] = pack_f16x2(x * ratio, y * ratio);
+          for (int e = 0; e < 2; ++e) {
+            const float ref = m[nb][e] == -INFINITY ? 0.f : m[nb][e] - kWeightShift;
+            x[e] = ex2_approx(s[nb][e] - ref);
+            x[2 + e] = ex2_approx(s[nb][2 + e] - ref);
+            l[nb][e] += x[e] + x[2 + e];
           }
-          if (bad && key0 < limit[rr]) l[rr] = __int_as_float(0x7fffffff);
+          pf[nb][0] = transpose8x8(pack_f16x2(x[0] * ratio, x[1] * ratio));
+          pf[nb][1] = transpose8x8(pack_f16x2(x[2] * ratio, x[3] * ratio));
         }
-        // V: lane (g, t4) takes d = 16 g .. 16 g + 15 of keys 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9; n-tile i is d = 16 g + i
-        const uint8_t* v = stage + 16 * kKvDim;
+        // V^T: inner indices 2 t4, 2 t4 + 1 are keys t4, t4 + 4, and 8 more those + 8; a lane takes d = 16 spread(g) .. + 15 of them
         uint4 w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int r = 2 * t4 + (i & 1) + 8 * (i >> 1);
-          w[i] = *reinterpret_cast<const uint4*>(v + r * kKvDim + (g ^ (r & 6)) * 16);
+          const int r = t4 + 4 * i;
+          w[i] = *reinterpret_cast<const uint4*>(stage + (16 + r) * kKvDim + ((kr ^ (r & 7)) << 4));
+          if (key0 + 16 > now.s.keys && key0 + r >= now.s.keys) w[i] = make_uint4(0, 0, 0, 0);  // behind the last token: anything
         }
 #pragma unroll
         for (int word = 0; word < 4; ++word) {
-          uint32_t x[4], b0[4], b1[4];
+          uint32_t x[4], a[4], b[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] = word == 0 ? w[i].x : word == 1 ? w[i].y : word == 2 ? w[i].z : w[i].w;
-          codes_to_f16<TYPE>(__byte_perm(x[0], x[1], 0x5140), b0[0], b0[1]);
-          codes_to_f16<TYPE>(__byte_perm(x[0], x[1], 0x7362), b0[2], b0[3]);
-          codes_to_f16<TYPE>(__byte_perm(x[2], x[3], 0x5140), b1[0], b1[1]);
-          codes_to_f16<TYPE>(__byte_perm(x[2], x[3], 0x7362), b1[2], b1[3]);
+          codes_to_f16<TYPE>(__byte_perm(x[0], x[1], 0x5140), a[0], a[1]);
+          codes_to_f16<TYPE>(__byte_perm(x[2], x[3], 0x5140), a[2], a[3]);
+          codes_to_f16<TYPE>(__byte_perm(x[0], x[1], 0x7362), b[0], b[1]);
+          codes_to_f16<TYPE>(__byte_perm(x[2], x[3], 0x7362), b[2], b[3]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mma_f16(acc[word * 4 + i], pf, b0[i], b1[i]);
+          for (int nb = 0; nb < NB; ++nb) {
+            mma_f16(acc[nb][2 * word], a, pf[nb][0], pf[nb][1]);
+            mma_f16(acc[nb][2 * word + 1], b, pf[nb][0], pf[nb][1]);
+          }
         }
       }
       __syncwarp();
-      get = get + 1 == kDecStages ? 0 : get + 1;
+      get = get + 1 == D::kStages ? 0 : get + 1;
+#pragma unroll
+      for (int i = 0; i + 1 < D::kStages; ++i) scales[i] = scales[i + 1];
+      request(scales[D::kStages - 1]);
     }
 
     // ---- the eight warps' parts of the tile ----
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      l[rr] += __shfl_xor_sync(0xffffffffu, l[rr], 1);
-      l[rr] += __shfl_xor_sync(0xffffffffu, l[rr], 2);
-      if (t4 == 0) row_stats[warp * kDecRows + g + 8 * rr] = make_float2(m[rr], l[rr]);
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], x);
+        if (g == 0) row_stats[warp * kRows + 8 * nb + 2 * t4 + e] = make_float2(m[nb][e], l[nb][e]);
+      }
     }
     __syncthreads();
-    float a[2];
+    const int swz = t4 | (g & 1) << 2;
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      float to = -INFINITY;
+    for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) to = fmaxf(to, row_stats[w * kDecRows + g + 8 * rr].x);
-      a[rr] = m[rr] == -INFINITY ? 0.f : ex2_approx(m[rr] - to) * vref;
-    }
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * nb + 2 * t4 + e;
+        float to = -INFINITY;
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      const int r = g + 8 * rr;
-      float4* row = reinterpret_cast<float4*>(merge) + (warp * kDecRows + r) * (kKvDim / 4);
-      const int swz = t4 | (r & 1) << 2;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {  // column 2 t4 + e of n-tile i is d = 16 (2 t4 + e) + i
+        for (int w = 0; w < kDecWarps; ++w) to = fmaxf(to, row_stats[w * kRows + r].x);
+        const float a = m[nb][e] == -INFINITY ? 0.f : ex2_approx(m[nb][e] - to) * vref;
+        float4* row = reinterpret_cast<float4*>(merge) + (warp * kRows + r) * (kKvDim / 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          row[(8 * t4 + 4 * e + i) ^ swz] = make_float4(acc[4 * i][2 * rr + e] * a[rr], acc[4 * i + 1][2 * rr + e] * a[rr],
-                                                        acc[4 * i + 2][2 * rr + e] * a[rr], acc[4 * i + 3][2 * rr + e] * a[rr]);
+          row[(4 * spread(g) + i) ^ swz] = make_float4(acc[nb][2 * i][e] * a, acc[nb][2 * i][2 + e] * a, acc[nb][2 * i + 1][e] * a,
+                                                       acc[nb][2 * i + 1][2 + e] * a);
         }
       }
     }
     __syncthreads();
-    {
-      const int r = threadIdx.x >> 4, c8 = threadIdx.x & 15;  // row, eight columns
+#pragma unroll 1
+    for (int nb = 0; nb < NB; ++nb) {  // a warp a row, four columns a lane
+      const int r = 8 * nb + warp;
+      const TilePlace w = tile_place(p, now.s, now.h, row_first + r);
+      if (!w.real) break;
       float to = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) to = fmaxf(to, row_stats[w * kDecRows + r].x);
+      for (int i = 0; i < kDecWarps; ++i) to = fmaxf(to, row_stats[i * kRows + r].x);
       float sum = 0.f;
-      float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) {
-        const float2 ml = row_stats[w * kDecRows + r];
+      for (int i = 0; i < kDecWarps; ++i) {
+        const float2 ml = row_stats[i * kRows + r];
         sum += ml.x == -INFINITY ? ml.y : ml.y * ex2_approx(ml.x - to);
-        const float4* row = reinterpret_cast<const float4*>(merge) + (w * kDecRows + r) * (kKvDim / 4);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int u = 2 * c8 + i;
-          const float4 x = row[u ^ (u >> 3 | (r & 1) << 2)];
-          o[4 * i] += x.x;
-          o[4 * i + 1] += x.y;
-          o[4 * i + 2] += x.z;
-          o[4 * i + 3] += x.w;
-        }
+        const float4 x = reinterpret_cast<const float4*>(merge)[(i * kRows + r) * (kKvDim / 4) + (lane ^ ((r >> 1 & 3) | (lane >> 4) << 2))];
+        o.x += x.x;
+        o.y += x.y;
+        o.z += x.z;
+        o.w += x.w;
       }
-      const TilePlace w = tile_place(p, now.s, now.h, static_cast<long long>(now.tile) * kDecRows + r);
       // a row that sees keys beyond the table's reach is NaN, as one that needs a page that does not exist
-      if (w.real && now.s.len > now.s.keys && (!p.causal || now.s.len - now.s.n + w.token >= now.s.keys)) sum = __int_as_float(0x7fffffff);
+      if (now.s.len > now.s.keys && (!p.causal || now.s.len - now.s.n + w.token >= now.s.keys)) sum = __int_as_float(0x7fffffff);
       if (t_first == 0 && n_steps == now.steps) {
-        if (w.real) {
-          const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;  // 0: a row that sees no key
-          uint4 x;
-          x.x = pack_bf16x2(o[0] * inv, o[1] * inv);
-          x.y = pack_bf16x2(o[2] * inv, o[3] * inv);
-          x.z = pack_bf16x2(o[4] * inv, o[5] * inv);
-          x.w = pack_bf16x2(o[6] * inv, o[7] * inv);
-          *reinterpret_cast<uint4*>(p.o + row_offset(p, p.so, now.b, now.s, w) + c8 * 8) = x;
-          if (c8 == 0 && p.lse != nullptr) {
-            p.lse[lse_index(p, now.b, now.s, w)] = sum == 0.f ? -INFINITY : (to - kWeightShift + log2f(sum)) * kLn2;
-          }
-        }
+        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;  // 0: a row that sees no key
+        *reinterpret_cast<uint2*>(p.o + row_offset(p, p.so, now.b, now.s, w) + lane * 4) =
+            make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+        if (lane == 0 && p.lse != nullptr)
+          p.lse[lse_index(p, now.b, now.s, w)] = sum == 0.f ? -INFINITY : (to - kWeightShift + log2f(sum)) * kLn2;
       } else {  // slot 2 i: a tile begun by an earlier CTA; 2 i + 1: one begun here
         const long long slot = 2ll * blockIdx.x + (t_first == 0 ? 1 : 0);
-        float4* part = reinterpret_cast<float4*>(p.parts + (slot * kDecRows + r) * kKvDim) + 2 * c8;
-        part[0] = make_float4(o[0], o[1], o[2], o[3]);
-        part[1] = make_float4(o[4], o[5], o[6], o[7]);
-        if (c8 == 0) {
-          reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kDecRows * kKvDim)[slot * kDecRows + r] = make_float2(to, sum);
-        }
-        if (threadIdx.x == 0 && t_first == 0) {
-          p.pieces[blockIdx.x] = make_int4(now.b, now.h, now.tile, static_cast<int>(line.owner(tile_begin + now.steps - 1)));
-        }
+        reinterpret_cast<float4*>(p.parts + (slot * kRows + r) * kKvDim)[lane] = o;
+        if (lane == 0)
+          reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kRows * kKvDim)[slot * kRows + r] = make_float2(to, sum);
       }
     }
+    if (threadIdx.x == 0 && t_first == 0 && n_steps != now.steps)
+      p.pieces[blockIdx.x] = make_int4(now.b, now.h, now.tile, static_cast<int>(line.owner(tile_begin + now.steps - 1)));
     __syncthreads();
     at += n_steps;
     if (at < line.end) now.next_tile(p);
   }
-  cp_async_wait<0>();
+  if (*abort_flag && lane == 0) {  // let loads in flight land before the CTA's shared memory is released
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 1000000ull) {
+    }
+  }
 }
 
 // Joins the parts of a tile that several CTAs worked on: sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, parts in order.

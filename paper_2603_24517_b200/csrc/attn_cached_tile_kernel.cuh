@@ -44,6 +44,7 @@ constexpr int kTNumBars = 2 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemS
 constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
 constexpr int kTSmemBytes = kTSmemMisc + 16;
 static_assert(kTSmemBytes <= 232448, "shared memory budget of one CTA");
+static_assert(kTSmemBars % 8 == 0 && kTSmemMeta % 16 == 0 && kTSmemStats % 16 == 0 && kTSmemMisc % 8 == 0, "alignment");
 static_assert(kHeadDim == kKvDim && kTile == kStepKeys, "one head dimension, one tile");
 
 // What the converters tell the softmax warps about a step.

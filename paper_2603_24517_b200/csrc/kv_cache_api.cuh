@@ -92,16 +92,16 @@ attn_status_t page_launch(const attn_kv_cache_t* cache, const void* k, const voi
   return ATTN_OK;
 }
 
-// The codes [n_pages, Hkv, page, D] as a 4-D tensor; a box is one page of one head.  A page number of n_pages reads zeros.
-bool make_page_map(CUtensorMap* tm, const attn_kv_cache_t* c, int t) {
+// The codes [n_pages, Hkv, page, D] as a 4-D tensor; a box is `rows` slots of one head.  A page number of n_pages reads zeros.
+bool make_page_map(CUtensorMap* tm, const attn_kv_cache_t* c, int t, int rows, CUtensorMapSwizzle swizzle) {
   const long long* st = t == 0 ? c->k_strides : c->v_strides;
   const cuuint64_t dims[4] = {attn::kv::kKvDim, static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->Hkv),
                               static_cast<cuuint64_t>(c->n_pages)};
   const cuuint64_t strides[3] = {static_cast<cuuint64_t>(st[1]), static_cast<cuuint64_t>(st[2]), static_cast<cuuint64_t>(st[0])};
-  const cuuint32_t box[4] = {attn::kv::kKvDim, static_cast<cuuint32_t>(c->page_size), 1, 1};
+  const cuuint32_t box[4] = {attn::kv::kKvDim, static_cast<cuuint32_t>(rows), 1, 1};
   const cuuint32_t elem_strides[4] = {1, 1, 1, 1};
   return g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, t == 0 ? c->k : c->v, dims, strides, box, elem_strides,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -110,11 +110,27 @@ size_t cached_parts(int ctas, int rows) { return 2ull * ctas * rows; }
 size_t cached_workspace(int ctas, int rows) {
   return cached_parts(ctas, rows) * (attn::kv::kKvDim + 2) * sizeof(float) + static_cast<size_t>(ctas) * sizeof(int4);
 }
-constexpr int kWorkspaceCtas = 160;  // CTAs of a launch at most: one an SM
+constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 
-// Rows (token, head of a group) of the longest sequence from which on the tensor-memory kernel is taken.
-constexpr int kManyRows = 17;
-bool many_rows(int Hq, int Hkv, int max_new) { return static_cast<long long>(Hq / Hkv) * max_new >= kManyRows; }
+// Rows of a query tile for the longest sequence's (token, head of a group) rows: the smallest tile that holds them.
+int tile_rows(int Hq, int Hkv, int max_new) {
+  const long long rows = static_cast<long long>(Hq / Hkv) * max_new;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : attn::kv::kTileRows;
+}
+int cached_ctas(int sms, int rows) { return rows == 8 ? sms * attn::kv::Dec<1>::kCtasPerSm : sms; }
+
+template <int NB>
+attn_status_t launch_decode(const CachedParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
+  using D = attn::kv::Dec<NB>;
+  if (p.c.type == ATTN_KV_E4M3) {
+    attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3, NB><<<p.ctas, attn::kv::kDecThreads, D::kSmem, s>>>(tm_k, tm_v, p);
+  } else {
+    attn::kv::attn_cached_decode_kernel<attn::kv::kInt8, NB><<<p.ctas, attn::kv::kDecThreads, D::kSmem, s>>>(tm_k, tm_v, p);
+  }
+  if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
+  attn::kv::attn_cached_join_kernel<D::kRows><<<dim3(p.ctas, D::kRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
+  return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
 
 }  // namespace
 
@@ -157,7 +173,8 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
 
 size_t attn_fwd_cached_workspace_bytes(int Hq, int Hkv, int max_new) {
   if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_new <= 0) return 0;
-  return cached_workspace(kWorkspaceCtas, many_rows(Hq, Hkv, max_new) ? attn::kv::kTileRows : attn::kv::kDecRows);
+  const int rows = tile_rows(Hq, Hkv, max_new);
+  return cached_workspace(cached_ctas(kWorkspaceSms, rows), rows);
 }
 
 attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
@@ -187,36 +204,29 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   p.group = Hq / cache->Hkv;
   p.causal = causal ? 1 : 0;
   p.scale_log2 = scale * 1.4426950408889634f;
-  p.ctas = dev->sm_count < kWorkspaceCtas ? dev->sm_count : kWorkspaceCtas;
-  const bool many = many_rows(Hq, cache->Hkv, max_new);
-  p.min_steps = many ? 4 : 1;
+  const int rows = tile_rows(Hq, cache->Hkv, max_new);
+  p.ctas = cached_ctas(dev->sm_count < kWorkspaceSms ? dev->sm_count : kWorkspaceSms, rows);
+  p.min_steps = rows == attn::kv::kTileRows ? 4 : 1;
   p.status = dev->status;
   p.parts = static_cast<float*>(workspace);
-  p.pieces = reinterpret_cast<int4*>(
-      p.parts + cached_parts(p.ctas, many ? attn::kv::kTileRows : attn::kv::kDecRows) * (attn::kv::kKvDim + 2));
+  p.pieces = reinterpret_cast<int4*>(p.parts + cached_parts(p.ctas, rows) * (attn::kv::kKvDim + 2));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool e4m3 = p.c.type == ATTN_KV_E4M3;
-  if (many) {
-    CUtensorMap tm_k, tm_v;
-    if (!make_page_map(&tm_k, cache, 0) || !make_page_map(&tm_v, cache, 1)) return ATTN_ERR_CUDA;
-    if (e4m3) {
-      attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
-    } else {
-      attn::kv::attn_cached_tile_kernel<attn::kv::kInt8><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
-    }
-  } else if (e4m3) {
-    attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3><<<p.ctas, attn::kv::kDecThreads, attn::kv::kDecSmemBytes, s>>>(p);
+  CUtensorMap tm_k, tm_v;
+  const bool many = rows == attn::kv::kTileRows;
+  const int box = many ? cache->page_size : 16;
+  const CUtensorMapSwizzle swizzle = many ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+  if (!make_page_map(&tm_k, cache, 0, box, swizzle) || !make_page_map(&tm_v, cache, 1, box, swizzle)) return ATTN_ERR_CUDA;
+  if (rows == 8) return launch_decode<1>(p, tm_k, tm_v, s);
+  if (rows == 16) return launch_decode<2>(p, tm_k, tm_v, s);
+  if (rows == 32) return launch_decode<4>(p, tm_k, tm_v, s);
+  if (p.c.type == ATTN_KV_E4M3) {
+    attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
   } else {
-    attn::kv::attn_cached_decode_kernel<attn::kv::kInt8><<<p.ctas, attn::kv::kDecThreads, attn::kv::kDecSmemBytes, s>>>(p);
+    attn::kv::attn_cached_tile_kernel<attn::kv::kInt8><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
   }
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-  if (many) {
-    attn::kv::attn_cached_join_kernel<attn::kv::kTileRows>
-        <<<dim3(p.ctas, attn::kv::kTileRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
-  } else {
-    attn::kv::attn_cached_join_kernel<attn::kv::kDecRows>
-        <<<dim3(p.ctas, attn::kv::kDecRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
-  }
+  attn::kv::attn_cached_join_kernel<attn::kv::kTileRows>
+      <<<dim3(p.ctas, attn::kv::kTileRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
   return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
 }
 
