@@ -55,7 +55,8 @@ struct CachedParams {
   int Hq, group, causal;
   float scale_log2;       // scale * log2(e)
   float* parts;           // [2 ctas][rows][kKvDim], then [2 ctas][rows][2] (reference maximum in log2 units, sum)
-  int4* pieces;           // [ctas]: {sequence, head, tile, last CTA with a part} of the tile the CTA began and did not end
+  int4* pieces;           // [ctas][2]: {sequence, head, tile, last CTA with a part or -1}, {first row, rows of the sequence} of the
+                          // tile that the CTA began and did not end
   int ctas;
   int min_steps;          // a piece has at least about so many
   int* status;            // bounded waits that ran out, see WaitCtx
@@ -131,50 +132,45 @@ struct Line {
   __device__ __forceinline__ long long owner(long long step) const { return ((step + 1) * ctas - 1) / total; }
 };
 
-// Cuts the line and finds where this CTA's piece begins.  All threads call; `scratch` holds 2 * (threads / 32) + 8 long longs.
+// Cuts the line and finds where this CTA's piece begins.  All threads call; `scratch` holds 3 * (threads / 32) + 2 long longs.
+// A thread's sequences are neighbours, so their sums are scanned once and only the thread that holds the place looks closer.
 template <int ROWS>
 __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cursor<ROWS>& at, long long* scratch) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int per = (p.c.B + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
+  const int b0 = static_cast<int>(threadIdx.x) * per, b1 = min(b0 + per, p.c.B);
   long long mine = 0;
-  for (int b = threadIdx.x; b < p.c.B; b += blockDim.x) mine += head_steps<ROWS>(p, seq_work(p.c, b)) * p.c.Hkv;
+  for (int b = b0; b < b1; ++b) mine += head_steps<ROWS>(p, seq_work(p.c, b)) * p.c.Hkv;
+  long long upto = mine;
 #pragma unroll
-  for (int m = 16; m > 0; m >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, m);
-  if (lane == 0) scratch[warp] = mine;
+  for (int m = 1; m < 32; m <<= 1) {
+    const long long other = __shfl_up_sync(0xffffffffu, upto, m);
+    if (lane >= m) upto += other;
+  }
+  if (lane == 31) scratch[warp] = upto;
   __syncthreads();
-  long long total = 0;
-  for (int w = 0; w < warps; ++w) total += scratch[w];
+  long long total = 0, before = 0;
+  for (int w = 0; w < warps; ++w) {
+    if (w == warp) before = total;
+    total += scratch[w];
+  }
   line.total = total;
   line.ctas = min(static_cast<long long>(p.ctas), (total + p.min_steps - 1) / p.min_steps);
   if (blockIdx.x >= line.ctas) return false;
   line.begin = total * blockIdx.x / line.ctas;
   line.end = total * (blockIdx.x + 1) / line.ctas;
-  // the sequence that holds step line.begin: a scan over the sequences, a block of them at a time
   long long* found = scratch + warps;  // sequence, its first step
-  long long before = 0;
-  for (int b0 = 0; b0 < p.c.B; b0 += blockDim.x) {
-    __syncthreads();
-    const int b = b0 + threadIdx.x;
-    const long long cost = b < p.c.B ? head_steps<ROWS>(p, seq_work(p.c, b)) * p.c.Hkv : 0;
-    long long upto = cost;
-#pragma unroll
-    for (int m = 1; m < 32; m <<= 1) {
-      const long long other = __shfl_up_sync(0xffffffffu, upto, m);
-      if (lane >= m) upto += other;
+  long long from = before + upto - mine;
+  if (line.begin >= from && line.begin < from + mine) {
+    for (int b = b0; b < b1; ++b) {
+      const long long cost = head_steps<ROWS>(p, seq_work(p.c, b)) * p.c.Hkv;
+      if (line.begin < from + cost) {
+        found[0] = b;
+        found[1] = from;
+        break;
+      }
+      from += cost;
     }
-    if (lane == 31) scratch[warp] = upto;
-    __syncthreads();
-    long long base = before, block = 0;
-    for (int w = 0; w < warps; ++w) {
-      if (w < warp) base += scratch[w];
-      block += scratch[w];
-    }
-    const long long from = base + upto - cost;
-    if (cost > 0 && line.begin >= from && line.begin < from + cost) {
-      found[0] = b;
-      found[1] = from;
-    }
-    before += block;
-    if (before > line.begin) break;
   }
   __syncthreads();
   at.b = static_cast<int>(found[0]);
@@ -198,6 +194,9 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   at.t = static_cast<int>(left);
   return true;
 }
+// The launch behind this one may start to take its place on the SMs; it waits for this one's results itself.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -263,12 +262,13 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
   Cursor<kRows> now;
   const bool works = find_piece<kRows>(p, line, now, reinterpret_cast<long long*>(merge));
   if (threadIdx.x == 0) {
-    p.pieces[blockIdx.x] = make_int4(0, 0, 0, -1);
+    p.pieces[2 * blockIdx.x] = make_int4(0, 0, 0, -1);
     for (int i = 0; i < kDecWarps * D::kStages; ++i) mbar_init(&bars[i], 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
   __syncthreads();  // also: the scratch of find_piece is the merge buffer
+  let_next_start();
   if (!works) return;
 
   Cursor<kRows> ahead = now;  // the step whose codes are requested next
@@ -570,8 +570,10 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
           reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kRows * kKvDim)[slot * kRows + r] = make_float2(to, sum);
       }
     }
-    if (threadIdx.x == 0 && t_first == 0 && n_steps != now.steps)
-      p.pieces[blockIdx.x] = make_int4(now.b, now.h, now.tile, static_cast<int>(line.owner(tile_begin + now.steps - 1)));
+    if (threadIdx.x == 0 && t_first == 0 && n_steps != now.steps) {
+      p.pieces[2 * blockIdx.x] = make_int4(now.b, now.h, now.tile, static_cast<int>(line.owner(tile_begin + now.steps - 1)));
+      p.pieces[2 * blockIdx.x + 1] = make_int4(now.s.row0, now.s.n, 0, 0);
+    }
     __syncthreads();
     at += n_steps;
     if (at < line.end) now.next_tile(p);
@@ -584,76 +586,95 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
 }
 
 // Joins the parts of a tile that several CTAs worked on: sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, parts in order.
-// Grid: (ctas, ROWS / 8); a block joins 8 rows of the tile that CTA blockIdx.x began and did not end, a warp a row.  Where a tile
-// is spread over many CTAs the block takes the rows one after another and its warps share the parts.
-constexpr int kJoinRows = 8;
+//
+// A row is 512 bytes of every part.  Where a tile has few parts a warp takes kJoinRows rows at once, so that their loads are in
+// flight together; where it has many, the eight warps of a block share the parts of one row.  Block (i, y) looks at the tile that
+// CTA i began and did not end; ROWS / 8 blocks a tile.  The launch starts while the kernel before it ends.
+constexpr int kJoinRows = 4;
 constexpr int kJoinMany = 12;
 
-struct JoinRow {
-  float top, sum;
+struct JoinSum {
+  float m, l;
+  float4 o;
 };
-// The joint maximum and sum of a row, in every lane: the lanes' terms and then the lanes in a fixed order.
-template <class Slot>
-__device__ __forceinline__ JoinRow join_stats(const float2* stats, const Slot& slot, int n, int lane) {
-  JoinRow j{-INFINITY, 0.f};
-  for (int i = lane; i < n; i += 32) j.top = fmaxf(j.top, stats[slot(i)].x);
-#pragma unroll
-  for (int k = 16; k > 0; k >>= 1) j.top = fmaxf(j.top, __shfl_xor_sync(0xffffffffu, j.top, k));
-  for (int i = lane; i < n; i += 32) {
-    const float2 ml = stats[slot(i)];
-    j.sum += ml.x == -INFINITY ? ml.y : ml.y * ex2_approx(ml.x - j.top);
-  }
-#pragma unroll
-  for (int k = 16; k > 0; k >>= 1) j.sum += __shfl_xor_sync(0xffffffffu, j.sum, k);
-  return j;
+__device__ __forceinline__ void join_part(JoinSum& j, const float2 ml, const float4 x) {
+  const float to = fmaxf(j.m, ml.x);
+  const float a = j.m == -INFINITY ? 0.f : ex2_approx(j.m - to), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - to);
+  // a part that has seen no key has the sum 0, or NaN where a page was missing
+  j.l = j.l * (j.m == -INFINITY ? 1.f : a) + ml.y * (ml.x == -INFINITY ? 1.f : f);
+  j.m = to;
+  j.o.x = j.o.x * a + x.x * f;
+  j.o.y = j.o.y * a + x.y * f;
+  j.o.z = j.o.z * a + x.z * f;
+  j.o.w = j.o.w * a + x.w * f;
+}
+__device__ __forceinline__ void join_write(const CachedParams& p, const JoinSum& j, int b, const SeqWork& s, const TilePlace& w, int lane) {
+  const float inv = j.l > 0.f ? 1.f / j.l : j.l == 0.f ? 0.f : j.l;
+  *reinterpret_cast<uint2*>(p.o + row_offset(p, p.so, b, s, w) + lane * 4) =
+      make_uint2(pack_bf16x2(j.o.x * inv, j.o.y * inv), pack_bf16x2(j.o.z * inv, j.o.w * inv));
+  if (lane == 0 && p.lse != nullptr)
+    p.lse[lse_index(p, b, s, w)] = j.l == 0.f ? -INFINITY : (j.m - kWeightShift + log2f(j.l)) * kLn2;
 }
 
 template <int ROWS>
 __global__ void __launch_bounds__(256) attn_cached_join_kernel(const CachedParams p) {
   __shared__ float4 sums[8][32];
-  const int4 piece = p.pieces[blockIdx.x];
+  __shared__ float2 stat[8];
+  wait_for_launch_before();
+  const int4 piece = p.pieces[2 * blockIdx.x], rows = p.pieces[2 * blockIdx.x + 1];
   if (piece.w < 0) return;
-  const SeqWork s = seq_work(p.c, piece.x);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int first = blockIdx.x, n = piece.w - first + 1;
+  SeqWork s;
+  s.row0 = rows.x;
+  s.n = rows.y;
   const float2* stats = reinterpret_cast<const float2*>(p.parts + 2ll * p.ctas * ROWS * kKvDim);
-  const bool many = n > kJoinMany;
-  for (int k = many ? 0 : warp; k < kJoinRows; k += many ? 1 : kJoinRows) {
-    const int r = blockIdx.y * kJoinRows + k;
-    const TilePlace w = tile_place(p, s, piece.y, static_cast<long long>(piece.z) * ROWS + r);
-    if (!w.real) break;  // rows are in order: none behind it is
-    auto slot = [&](int i) { return (2ll * (first + i) + (i == 0 ? 1 : 0)) * ROWS + r; };
-    const JoinRow j = join_stats(stats, slot, n, lane);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = many ? warp : 0; i < n; i += many ? 8 : 1) {
-      const float m = stats[slot(i)].x;
-      const float4 x = reinterpret_cast<const float4*>(p.parts + slot(i) * kKvDim)[lane];
-      const float f = m == -INFINITY ? 0.f : ex2_approx(m - j.top);
-      o.x += x.x * f;
-      o.y += x.y * f;
-      o.z += x.z * f;
-      o.w += x.w * f;
-    }
-    if (many) {
-      __syncthreads();  // the row before has been read
-      sums[warp][lane] = o;
-      __syncthreads();
-      if (warp != 0) continue;
+  const float4* parts = reinterpret_cast<const float4*>(p.parts);
+  const long long tile_row = static_cast<long long>(piece.z) * ROWS;
+  if (n <= kJoinMany) {
+    for (int r0 = (blockIdx.y * 8 + warp) * kJoinRows; r0 < ROWS; r0 += static_cast<int>(gridDim.y) * 8 * kJoinRows) {
+      if (!tile_place(p, s, piece.y, tile_row + r0).real) return;  // rows are in order: none behind it is
+      JoinSum j[kJoinRows];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) {
-        const float4 x = sums[i][lane];
-        o.x += x.x;
-        o.y += x.y;
-        o.z += x.z;
-        o.w += x.w;
+      for (int k = 0; k < kJoinRows; ++k) j[k] = JoinSum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 2
+      for (int i = 0; i < n; ++i) {
+        const long long at = (2ll * (first + i) + (i == 0 ? 1 : 0)) * ROWS + r0;
+        float2 ml[kJoinRows];
+        float4 x[kJoinRows];
+#pragma unroll
+        for (int k = 0; k < kJoinRows; ++k) {
+          ml[k] = stats[at + k];
+          x[k] = parts[(at + k) * (kKvDim / 4) + lane];
+        }
+#pragma unroll
+        for (int k = 0; k < kJoinRows; ++k) join_part(j[k], ml[k], x[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kJoinRows; ++k) {
+        const TilePlace w = tile_place(p, s, piece.y, tile_row + r0 + k);
+        if (w.real) join_write(p, j[k], piece.x, s, w, lane);
       }
     }
-    const float inv = j.sum > 0.f ? 1.f / j.sum : j.sum == 0.f ? 0.f : j.sum;
-    const uint2 y = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-    *reinterpret_cast<uint2*>(p.o + row_offset(p, p.so, piece.x, s, w) + lane * 4) = y;
-    if (lane == 0 && p.lse != nullptr)
-      p.lse[lse_index(p, piece.x, s, w)] = j.sum == 0.f ? -INFINITY : (j.top - kWeightShift + log2f(j.sum)) * kLn2;
+    return;
+  }
+  for (int r = blockIdx.y; r < ROWS; r += gridDim.y) {
+    const TilePlace w = tile_place(p, s, piece.y, tile_row + r);
+    if (!w.real) return;
+    JoinSum j{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 4
+    for (int i = warp; i < n; i += 8) {
+      const long long at = (2ll * (first + i) + (i == 0 ? 1 : 0)) * ROWS + r;
+      join_part(j, stats[at], parts[at * (kKvDim / 4) + lane]);
+    }
+    __syncthreads();  // the row before has been read
+    sums[warp][lane] = j.o;
+    if (lane == 0) stat[warp] = make_float2(j.m, j.l);
+    __syncthreads();
+    if (warp != 0) continue;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) join_part(j, stat[i], sums[i][lane]);
+    join_write(p, j, piece.x, s, w, lane);
   }
 }
 

@@ -618,7 +618,8 @@ __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const 
       } else {
         reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kTileRows * kKvDim)[slot * kTileRows + r] = make_float2(m, l);
         if (r == 0 && it.t_first == 0) {
-          p.pieces[blockIdx.x] = make_int4(it.b, it.h, it.tile, it.last);
+          p.pieces[2 * blockIdx.x] = make_int4(it.b, it.h, it.tile, it.last);
+          p.pieces[2 * blockIdx.x + 1] = make_int4(it.s.row0, it.s.n, 0, 0);
         }
       }
     }
@@ -651,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   const WaitCtx ctx{abort_flag, p.status, kWaitLimitNs};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-  if (tid == 0) p.pieces[blockIdx.x] = make_int4(0, 0, 0, -1);
+  if (tid == 0) p.pieces[2 * blockIdx.x] = make_int4(0, 0, 0, -1);
   if ((smem_u32(smem) & 1023u) != 0) {  // the swizzled tiles need a 1024-byte aligned base
     if (tid == 0 && atomicCAS(p.status, 0, kBadSmemAlign) == 0) p.status[1] = static_cast<int>(blockIdx.x);
     return;
@@ -692,6 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  let_next_start();
 
   if (warp < 8) {
     reg_alloc<kTRegsSoftmax>();

@@ -108,7 +108,7 @@ bool make_page_map(CUtensorMap* tm, const attn_kv_cache_t* c, int t, int rows, C
 // A part of a tile for every CTA that may end in one or begin in one.
 size_t cached_parts(int ctas, int rows) { return 2ull * ctas * rows; }
 size_t cached_workspace(int ctas, int rows) {
-  return cached_parts(ctas, rows) * (attn::kv::kKvDim + 2) * sizeof(float) + static_cast<size_t>(ctas) * sizeof(int4);
+  return cached_parts(ctas, rows) * (attn::kv::kKvDim + 2) * sizeof(float) + static_cast<size_t>(ctas) * 2 * sizeof(int4);
 }
 constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 
@@ -119,6 +119,21 @@ int tile_rows(int Hq, int Hkv, int max_new) {
 }
 int cached_ctas(int sms, int rows) { return rows == 8 ? sms * attn::kv::Dec<1>::kCtasPerSm : sms; }
 
+// The join as a launch that may begin before the one in front of it has ended (it waits for that one's results on the device).
+template <int ROWS>
+attn_status_t launch_join(const CachedParams& p, int blocks, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.ctas, blocks);
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attn::kv::attn_cached_join_kernel<ROWS>, p) == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
+
 template <int NB>
 attn_status_t launch_decode(const CachedParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
   using D = attn::kv::Dec<NB>;
@@ -128,8 +143,7 @@ attn_status_t launch_decode(const CachedParams& p, const CUtensorMap& tm_k, cons
     attn::kv::attn_cached_decode_kernel<attn::kv::kInt8, NB><<<p.ctas, attn::kv::kDecThreads, D::kSmem, s>>>(tm_k, tm_v, p);
   }
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-  attn::kv::attn_cached_join_kernel<D::kRows><<<dim3(p.ctas, D::kRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
-  return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+  return launch_join<D::kRows>(p, D::kRows, s);
 }
 
 }  // namespace
@@ -225,9 +239,7 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
     attn::kv::attn_cached_tile_kernel<attn::kv::kInt8><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
   }
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-  attn::kv::attn_cached_join_kernel<attn::kv::kTileRows>
-      <<<dim3(p.ctas, attn::kv::kTileRows / attn::kv::kJoinRows), 256, 0, s>>>(p);
-  return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+  return launch_join<attn::kv::kTileRows>(p, attn::kv::kTileRows / (8 * attn::kv::kJoinRows), s);
 }
 
 }  // extern "C"
