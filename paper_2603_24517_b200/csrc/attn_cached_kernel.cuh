@@ -58,7 +58,7 @@ struct CachedParams {
   int4* pieces;           // [ctas][2]: {sequence, head, tile, last CTA with a part or -1}, {first row, rows of the sequence} of the
                           // tile that the CTA began and did not end
   int ctas;
-  int min_steps;          // a piece has at least about so many
+  int wide_o;             // rows of o begin at multiples of 32 bytes
   int* status;            // bounded waits that ran out, see WaitCtx
 };
 
@@ -94,7 +94,7 @@ struct Cursor {
   }
   __device__ __forceinline__ void enter_sequence(const CachedParams& p) {
     s = seq_work(p.c, b);
-    tiles = static_cast<int>((static_cast<long long>(s.n) * p.group + ROWS - 1) / ROWS);
+    tiles = (s.n * p.group + ROWS - 1) / ROWS;
   }
   __device__ __forceinline__ void next_tile(const CachedParams& p) {  // of the head, then the next head, the next sequence
     t = 0;
@@ -115,8 +115,7 @@ struct Cursor {
 // Steps of one head of a sequence.
 template <int ROWS>
 __device__ __forceinline__ long long head_steps(const CachedParams& p, const SeqWork& s) {
-  const long long rows = static_cast<long long>(s.n) * p.group;
-  const int tiles = static_cast<int>((rows + ROWS - 1) / ROWS);
+  const int tiles = (s.n * p.group + ROWS - 1) / ROWS;
   if (tiles == 0) return 0;
   if (!p.causal) return static_cast<long long>(tiles) * steps_of(s, s.n - 1, 0);
   long long sum = 0;
@@ -155,10 +154,16 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
     total += scratch[w];
   }
   line.total = total;
-  line.ctas = min(static_cast<long long>(p.ctas), (total + p.min_steps - 1) / p.min_steps);
+  line.ctas = min(static_cast<long long>(p.ctas), total);
   if (blockIdx.x >= line.ctas) return false;
-  line.begin = total * blockIdx.x / line.ctas;
-  line.end = total * (blockIdx.x + 1) / line.ctas;
+  if (total < 1 << 20) {  // at most 2^11 CTAs: 32-bit divisions
+    const uint32_t t = static_cast<uint32_t>(total), c = static_cast<uint32_t>(line.ctas);
+    line.begin = t * blockIdx.x / c;
+    line.end = t * (blockIdx.x + 1) / c;
+  } else {
+    line.begin = total * blockIdx.x / line.ctas;
+    line.end = total * (blockIdx.x + 1) / line.ctas;
+  }
   long long* found = scratch + warps;  // sequence, its first step
   long long from = before + upto - mine;
   if (line.begin >= from && line.begin < from + mine) {
@@ -177,7 +182,7 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   long long left = line.begin - found[1];
   at.enter_sequence(p);
   const long long per_head = head_steps<ROWS>(p, at.s);
-  at.h = static_cast<int>(left / per_head);
+  at.h = total < 1 << 20 ? static_cast<int>(static_cast<uint32_t>(left) / static_cast<uint32_t>(per_head)) : static_cast<int>(left / per_head);
   left -= at.h * per_head;
   at.tile = 0;
   at.enter_tile(p);
@@ -198,6 +203,11 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool take) {
+  const int bytes = take ? 16 : 0;  // 0: zeros are written, nothing is read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -220,10 +230,10 @@ struct TilePlace {
   int token, head;  // row's token of the sequence, query head
   bool real;
 };
-__device__ __forceinline__ TilePlace tile_place(const CachedParams& p, const SeqWork& s, int h, long long r) {
+__device__ __forceinline__ TilePlace tile_place(const CachedParams& p, const SeqWork& s, int h, int r) {
   TilePlace w;
-  w.token = static_cast<int>(r / p.group);
-  w.head = h * p.group + static_cast<int>(r - static_cast<long long>(w.token) * p.group);
+  w.token = r / p.group;  // rows are below 2^30
+  w.head = h * p.group + (r - w.token * p.group);
   w.real = w.token < s.n;
   return w;
 }
@@ -319,7 +329,8 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
     // ---- one tile, or this CTA's piece of it ----
     const int t_first = now.t;
     const int n_steps = static_cast<int>(min(static_cast<long long>(now.steps - now.t), line.end - at));
-    const long long tile_begin = at - now.t, row_first = static_cast<long long>(now.tile) * kRows;
+    const long long tile_begin = at - now.t;
+    const int row_first = now.tile * kRows;
     // queries (right operand): lane (g, t4) has row g; step i of the product takes d = 64 (i / 4) + 16 t4 + 4 (i % 4) + 0..3, the
     // order that a lane's codes of K have.  Scores: lane (g, t4) has rows 2 t4, 2 t4 + 1 of keys spread(g), 8 + spread(g)
     uint32_t qf[NB][8][2];
@@ -365,7 +376,7 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
       }
     }
     // keys that all rows see: steps up to there need no mask
-    const int clear = visible(now.s, min(static_cast<int>(row_first / p.group), now.s.n - 1), p.causal);
+    const int clear = visible(now.s, min(row_first / p.group, now.s.n - 1), p.causal);
     float acc[NB][8][4];  // d = 16 spread(g) + 2 mt (values 0, 1) and + 1 (2, 3); rows 2 t4 (0, 2) and 2 t4 + 1 (1, 3)
     float m[NB][2], l[NB][2], vref = 0.f;
 #pragma unroll
@@ -630,7 +641,7 @@ __global__ void __launch_bounds__(256) attn_cached_join_kernel(const CachedParam
   s.n = rows.y;
   const float2* stats = reinterpret_cast<const float2*>(p.parts + 2ll * p.ctas * ROWS * kKvDim);
   const float4* parts = reinterpret_cast<const float4*>(p.parts);
-  const long long tile_row = static_cast<long long>(piece.z) * ROWS;
+  const int tile_row = piece.z * ROWS;
   if (n <= kJoinMany) {
     for (int r0 = (blockIdx.y * 8 + warp) * kJoinRows; r0 < ROWS; r0 += static_cast<int>(gridDim.y) * 8 * kJoinRows) {
       if (!tile_place(p, s, piece.y, tile_row + r0).real) return;  // rows are in order: none behind it is

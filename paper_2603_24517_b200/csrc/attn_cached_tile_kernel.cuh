@@ -89,7 +89,7 @@ struct Item {
 };
 __device__ __forceinline__ void publish_item(int* box, const CachedParams& p, const Line& line, const Cursor<kTileRows>& c, long long at) {
   const int n = static_cast<int>(min(static_cast<long long>(c.steps - c.t), line.end - at));
-  const bool two = static_cast<long long>(c.tile) * kTileRows + kTile < static_cast<long long>(c.s.n) * p.group;
+  const bool two = c.tile * kTileRows + kTile < c.s.n * p.group;
   box[0] = n;
   box[1] = c.t;
   box[2] = (two ? 1 : 0) | (c.t == 0 && n == c.steps ? 2 : 0);
@@ -393,44 +393,49 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
       used = s == 0 || it.two;
       if (used) {
         // Q: the stage's last product that reads it has completed (its scores have been taken)
-        const long long r0 = static_cast<long long>(it.tile) * kTileRows + s * kTile;
+        const int r0 = it.tile * kTileRows + s * kTile;
         const TilePlace w = tile_place(p, it.s, it.h, r0 + row);
         limit = w.real ? visible(it.s, w.token, p.causal) : it.s.keys;
-        clear = visible(it.s, min(static_cast<int>(r0 / p.group), it.s.n - 1), p.causal);
+        clear = visible(it.s, min(r0 / p.group, it.s.n - 1), p.causal);
         key0 = it.t_first * kStepKeys;
         seen = limit > key0;
-        uint4 x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = make_uint4(0, 0, 0, 0);
-        if (w.real) {
-          const uint4* src = reinterpret_cast<const uint4*>(p.q + row_offset(p, p.sq, it.b, it.s, w));
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = __ldg(src + i);
-        }
-        float largest = 0.f;
+        // half a warp brings a row, 16 bytes a lane, as it is, and then turns what it has brought into f16 in place
+        const long long mine = w.real ? row_offset(p, p.sq, it.b, it.s, w) : -1;
+        uint8_t* dst = smem + kTSmemQ + s * kTileBytes + ((lane & 15) >> 3) * kHalfBytes + ((row & ~31) + (lane >> 4)) * 128;
+        const uint32_t dst32 = smem_u32(dst);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          const long long from = __shfl_sync(0xffffffffu, mine, 2 * i + (lane >> 4));
+          const uint32_t at = i * 256 + (((lane & 7) ^ ((2 * i + (lane >> 4)) & 7)) << 4);
+          cp_async16(dst32 + at, p.q + (from >= 0 ? from : 0) + (lane & 15) * 8, from >= 0);
+        }
+        cp_async_wait_all();
+        float my_up = 1.f;
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+          uint4* at = reinterpret_cast<uint4*>(dst + i * 256 + (((lane & 7) ^ ((2 * i + (lane >> 4)) & 7)) << 4));
+          const uint4 x = *at;
+          const uint32_t words[4] = {x.x, x.y, x.z, x.w};
+          float largest = 0.f;
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const float2 f = unpack_bf16x2(words[m]);
             largest = max3(largest, fabsf(f.x), fabsf(f.y));
           }
-        }
-        const float up = row_factor(largest);
-        factor = p.scale_log2 / up;
-        uint8_t* dst = smem + kTSmemQ + s * kTileBytes + row * 128;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          for (int m = 8; m > 0; m >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, m));
+          const float up = row_factor(largest);
           uint32_t y[4];
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const float2 f = unpack_bf16x2(words[m]);
             y[m] = pack_f16x2(f.x * up, f.y * up);
           }
-          *reinterpret_cast<uint4*>(dst + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *at = make_uint4(y[0], y[1], y[2], y[3]);
+          const float ups = __shfl_sync(0xffffffffu, up, (lane & 1) << 4);
+          if (lane >> 1 == i) my_up = ups;
         }
+        factor = p.scale_log2 / my_up;
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.q_full[s]);
@@ -551,6 +556,16 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
   }
 }
 
+// A thread writes rows of its own, so every store of a warp meets 32 lines: the fewer and wider the stores, the better.
+__device__ __forceinline__ void store_32_bytes(void* at, const uint32_t* v, bool aligned) {
+  if (aligned) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), ATTN_W4(v, 0), ATTN_W4(v, 4) : "memory");
+  } else {
+    reinterpret_cast<uint4*>(at)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(at)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
+
 // ---- results ----------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
                                                    uint32_t tmem, int row, int lane) {
@@ -576,7 +591,7 @@ __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const 
       ++cnt[s];
       tc_fence_after_sync();
       const int r = s * kTile + row;
-      const TilePlace w = tile_place(p, it.s, it.h, static_cast<long long>(it.tile) * kTileRows + r);
+      const TilePlace w = tile_place(p, it.s, it.h, it.tile * kTileRows + r);
       // keys beyond the table's reach
       if (w.real && it.s.len > it.s.keys && (!p.causal || it.s.len - it.s.n + w.token >= it.s.keys)) l = __int_as_float(0x7fffffff);
       const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
@@ -591,21 +606,18 @@ __device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const 
         tmem_wait_ld();
         if (w.real && it.whole) {
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            uint4 val;
-            val.x = pack_bf16x2(__uint_as_float(o[ch * 8 + 0]) * f, __uint_as_float(o[ch * 8 + 1]) * f);
-            val.y = pack_bf16x2(__uint_as_float(o[ch * 8 + 2]) * f, __uint_as_float(o[ch * 8 + 3]) * f);
-            val.z = pack_bf16x2(__uint_as_float(o[ch * 8 + 4]) * f, __uint_as_float(o[ch * 8 + 5]) * f);
-            val.w = pack_bf16x2(__uint_as_float(o[ch * 8 + 6]) * f, __uint_as_float(o[ch * 8 + 7]) * f);
-            *reinterpret_cast<uint4*>(out + cc * 32 + ch * 8) = val;
+          for (int ch = 0; ch < 2; ++ch) {
+            uint32_t val[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              val[i] = pack_bf16x2(__uint_as_float(o[ch * 16 + 2 * i]) * f, __uint_as_float(o[ch * 16 + 2 * i + 1]) * f);
+            store_32_bytes(out + cc * 32 + ch * 16, val, p.wide_o);
           }
         } else if (w.real) {
 #pragma unroll
-          for (int ch = 0; ch < 8; ++ch) {
-            *reinterpret_cast<float4*>(part + cc * 32 + ch * 4) =
-                make_float4(__uint_as_float(o[ch * 4]) * f, __uint_as_float(o[ch * 4 + 1]) * f,
-                            __uint_as_float(o[ch * 4 + 2]) * f, __uint_as_float(o[ch * 4 + 3]) * f);
-          }
+          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) store_32_bytes(part + cc * 32 + ch * 8, o + ch * 8, true);
         }
         __syncwarp();
       }

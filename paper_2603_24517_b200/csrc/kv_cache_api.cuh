@@ -108,7 +108,7 @@ bool make_page_map(CUtensorMap* tm, const attn_kv_cache_t* c, int t, int rows, C
 // A part of a tile for every CTA that may end in one or begin in one.
 size_t cached_parts(int ctas, int rows) { return 2ull * ctas * rows; }
 size_t cached_workspace(int ctas, int rows) {
-  return cached_parts(ctas, rows) * (attn::kv::kKvDim + 2) * sizeof(float) + static_cast<size_t>(ctas) * 2 * sizeof(int4);
+  return cached_parts(ctas, rows) * (attn::kv::kKvDim + 2) * sizeof(float) + static_cast<size_t>(ctas) * 2 * sizeof(int4) + 32;
 }
 constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 
@@ -220,9 +220,9 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   p.scale_log2 = scale * 1.4426950408889634f;
   const int rows = tile_rows(Hq, cache->Hkv, max_new);
   p.ctas = cached_ctas(dev->sm_count < kWorkspaceSms ? dev->sm_count : kWorkspaceSms, rows);
-  p.min_steps = rows == attn::kv::kTileRows ? 4 : 1;
+  p.wide_o = !misaligned(o, 31) && p.so.b % 16 == 0 && p.so.s % 16 == 0 && p.so.h % 16 == 0;
   p.status = dev->status;
-  p.parts = static_cast<float*>(workspace);
+  p.parts = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(workspace) + 31) & ~static_cast<uintptr_t>(31));
   p.pieces = reinterpret_cast<int4*>(p.parts + cached_parts(p.ctas, rows) * (attn::kv::kKvDim + 2));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   CUtensorMap tm_k, tm_v;
