@@ -24,10 +24,10 @@ namespace attn {
 namespace kv {
 
 constexpr int kTileRows = 256;  // rows of a work item: two stages
-constexpr int kConvWarps = 2;
-// registers of a thread after the split of the CTA's 64K: 8 softmax, 4 epilogue, 4 other warps
-constexpr int kTRegsSoftmax = 192, kTRegsEpilogue = 64, kTRegsOther = 64;
-static_assert(8 * kTRegsSoftmax + 4 * kTRegsEpilogue + 4 * kTRegsOther <= 2048, "register split");
+constexpr int kConvWarps = 6;
+// registers of a thread after the split of the CTA's 64K: 8 softmax, 8 other warps
+constexpr int kTRegsSoftmax = 192, kTRegsOther = 64;
+static_assert(8 * kTRegsSoftmax + 8 * kTRegsOther <= 2048, "register split");
 
 constexpr int kTSmemQ = 0;
 constexpr int kTSmemKv = 2 * kTileBytes;
@@ -35,11 +35,11 @@ constexpr int kTSmemRaw = kTSmemKv + kKvSlots * kTileBytes;      // codes of one
 constexpr int kTSmemStats = kTSmemRaw + 2 * kTile * kKvDim;      // float [2 stages][2][128]
 constexpr int kMetaSteps = 4;
 constexpr int kMetaFloats = 28;
-constexpr int kItemSlots = 4;      // items published ahead: the fetching warp looks two steps ahead, which may be two items
-constexpr int kItemInts = 12;
+constexpr int kItemSlots = 5;      // the fetching warp looks two steps (items) ahead of the codes it requests, results follow one behind
+constexpr int kItemInts = 11;
 constexpr int kTSmemMeta = kTSmemStats + 2 * 2 * kTile * 4;
 constexpr int kTSmemItems = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
-constexpr int kTSmemBars = kTSmemItems + kItemSlots * kItemInts * 4;
+constexpr int kTSmemBars = (kTSmemItems + kItemSlots * kItemInts * 4 + 7) / 8 * 8;
 constexpr int kTNumBars = 2 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemSlots;
 constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
 constexpr int kTSmemBytes = kTSmemMisc + 16;
@@ -102,11 +102,15 @@ __device__ __forceinline__ void publish_item(int* box, const CachedParams& p, co
   box[9] = c.s.keys;
   box[10] = static_cast<int>(line.owner(at - c.t + c.steps - 1));
 }
-// The k-th item of this CTA for a whole warp of a consuming role; false when a wait ran out.
-__device__ __forceinline__ bool take_item(const TileBarriers& bars, const uint8_t* smem, uint32_t k, WaitCtx ctx, int role, int lane, Item& it) {
-  const uint32_t slot = k % kItemSlots;
-  if (!mbar_wait_warp(&bars.item_full[slot], (k / kItemSlots) & 1, ctx, role | kBarSchedFull)) return false;
-  const int* box = reinterpret_cast<const int*>(smem + kTSmemItems) + slot * kItemInts;
+__device__ __forceinline__ const int* item_box(const uint8_t* smem, uint32_t k) {
+  return reinterpret_cast<const int*>(smem + kTSmemItems) + (k % kItemSlots) * kItemInts;
+}
+// The k-th item of this CTA, once a whole warp of a consuming role has waited for it.
+__device__ __forceinline__ bool wait_item(const TileBarriers& bars, uint32_t k, WaitCtx ctx, int role) {
+  return mbar_wait_warp(&bars.item_full[k % kItemSlots], (k / kItemSlots) & 1, ctx, role | kBarSchedFull);
+}
+__device__ __forceinline__ void read_item(const uint8_t* smem, uint32_t k, Item& it) {
+  const int* box = item_box(smem, k);
   it.n = box[0];
   it.t_first = box[1];
   it.two = (box[2] & 1) != 0;
@@ -116,8 +120,15 @@ __device__ __forceinline__ bool take_item(const TileBarriers& bars, const uint8_
   it.tile = box[5];
   it.s = SeqWork{box[6], box[7], box[8], box[9]};
   it.last = box[10];
+}
+__device__ __forceinline__ void drop_item(const TileBarriers& bars, uint32_t k, int lane) {
   __syncwarp();
-  if (lane == 0) mbar_arrive(&bars.item_empty[slot]);
+  if (lane == 0) mbar_arrive(&bars.item_empty[k % kItemSlots]);
+}
+__device__ __forceinline__ bool take_item(const TileBarriers& bars, const uint8_t* smem, uint32_t k, WaitCtx ctx, int role, int lane, Item& it) {
+  if (!wait_item(bars, k, ctx, role)) return false;
+  read_item(smem, k, it);
+  drop_item(bars, k, lane);
   return true;
 }
 
@@ -229,49 +240,46 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
   }
 }
 
-// Codes to f16.  A lane takes 16 codes of one of 8 rows at a time, odd rows the other half of the head dimension than even
-// ones, so neither its reads nor its writes meet another lane's bank.
+// The codes of step i (keys, then values) to f16: converter warp cw's rows of the tiles.  A lane takes 16 codes of one of 8 rows at
+// a time, odd rows the other half of the head dimension than even ones, so neither its reads nor its writes meet another
+// lane's bank.
 template <int TYPE>
-__device__ __forceinline__ void role_convert(const TileBarriers& bars, uint8_t* smem, WaitCtx ctx, uint32_t steps, int cw, int lane) {
+__device__ __forceinline__ bool convert_step(const TileBarriers& bars, uint8_t* smem, WaitCtx ctx, uint32_t i, int cw, int lane) {
   const int sub = lane >> 2, ch = (lane & 3) * 2;
-  uint32_t kv_cnt = 0;
-  for (uint32_t i = 0; i < steps; ++i) {
 #pragma unroll 1
-    for (int kv = 0; kv < 2; ++kv) {
-      const uint32_t slot = kv_cnt % kKvSlots;
-      bool ok = mbar_wait(&bars.raw_full[kv], i & 1, ctx, kRoleConvert | kBarKvFull);
-      ok = ok && mbar_wait(&bars.kv_empty[slot], ((kv_cnt / kKvSlots) & 1) ^ 1, ctx, kRoleConvert | kBarKvEmpty);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
-      ++kv_cnt;
-      const int valid = reinterpret_cast<const int*>(smem + kTSmemMeta)[(i % kMetaSteps) * kMetaFloats + kMetaValid];
-      const uint8_t* raw = smem + kTSmemRaw + kv * kTile * kKvDim + sub * kKvDim + (lane & 3) * 16;
-      uint8_t* tile = smem + kTSmemKv + slot * kTileBytes + sub * 128;
-#pragma unroll 4
-      for (int rg = cw; rg < 16; rg += kConvWarps) {
+  for (int kv = 0; kv < 2; ++kv) {
+    const uint32_t kv_cnt = 2 * i + kv, slot = kv_cnt % kKvSlots;
+    bool ok = mbar_wait(&bars.raw_full[kv], i & 1, ctx, kRoleConvert | kBarKvFull);
+    ok = ok && mbar_wait(&bars.kv_empty[slot], ((kv_cnt / kKvSlots) & 1) ^ 1, ctx, kRoleConvert | kBarKvEmpty);
+    if (!__all_sync(0xffffffffu, ok)) return false;
+    const int valid = reinterpret_cast<const int*>(smem + kTSmemMeta)[(i % kMetaSteps) * kMetaFloats + kMetaValid];
+    const uint8_t* raw = smem + kTSmemRaw + kv * kTile * kKvDim + sub * kKvDim + (lane & 3) * 16;
+    uint8_t* tile = smem + kTSmemKv + slot * kTileBytes + sub * 128;
+#pragma unroll 1
+    for (int rg = cw; rg < 16; rg += kConvWarps) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int half = k ^ (sub & 1);
-          uint4 w = *reinterpret_cast<const uint4*>(raw + rg * 8 * kKvDim + half * 64);
-          if (valid < kTile && rg * 8 + sub >= valid) w = make_uint4(0, 0, 0, 0);  // behind the last token: zeros
-          uint4 lo, hi;
-          codes_to_f16<TYPE>(w.x, lo.x, lo.y);
-          codes_to_f16<TYPE>(w.y, lo.z, lo.w);
-          codes_to_f16<TYPE>(w.z, hi.x, hi.y);
-          codes_to_f16<TYPE>(w.w, hi.z, hi.w);
-          uint8_t* row = tile + rg * 8 * 128 + half * kHalfBytes;
-          *reinterpret_cast<uint4*>(row + ((ch ^ sub) << 4)) = lo;
-          *reinterpret_cast<uint4*>(row + (((ch + 1) ^ sub) << 4)) = hi;
-        }
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&bars.raw_empty[kv]);
-        mbar_arrive(&bars.kv_full[slot]);
+      for (int k = 0; k < 2; ++k) {
+        const int half = k ^ (sub & 1);
+        uint4 w = *reinterpret_cast<const uint4*>(raw + rg * 8 * kKvDim + half * 64);
+        if (valid < kTile && rg * 8 + sub >= valid) w = make_uint4(0, 0, 0, 0);  // behind the last token: zeros
+        uint4 lo, hi;
+        codes_to_f16<TYPE>(w.x, lo.x, lo.y);
+        codes_to_f16<TYPE>(w.y, lo.z, lo.w);
+        codes_to_f16<TYPE>(w.z, hi.x, hi.y);
+        codes_to_f16<TYPE>(w.w, hi.z, hi.w);
+        uint8_t* row = tile + rg * 8 * 128 + half * kHalfBytes;
+        *reinterpret_cast<uint4*>(row + ((ch ^ sub) << 4)) = lo;
+        *reinterpret_cast<uint4*>(row + (((ch + 1) ^ sub) << 4)) = hi;
       }
     }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(&bars.raw_empty[kv]);
+      mbar_arrive(&bars.kv_full[slot]);
+    }
   }
+  return true;
 }
 
 // ---- MMA --------------------------------------------------------------------------------------------------------------
@@ -567,74 +575,92 @@ __device__ __forceinline__ void store_32_bytes(void* at, const uint32_t* v, bool
 }
 
 // ---- results ----------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void role_tile_epilogue(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
-                                                   uint32_t tmem, int row, int lane) {
+__device__ __forceinline__ bool write_item(const CachedParams& p, const TileBarriers& bars, const uint8_t* smem, WaitCtx ctx, uint32_t tmem,
+                                           uint32_t k, uint32_t* cnt, int row, int lane) {
   const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
-  uint32_t cnt[2] = {0, 0};
-  for (uint32_t k = 0;; ++k) {
-    Item it;
-    if (!take_item(bars, smem, k, ctx, kRoleEpilogue, lane, it) || it.n == 0) return;
+  Item it;
+  read_item(smem, k, it);
 #pragma unroll 1
-    for (int s = 0; s < 2; ++s) {
-      if (s == 1 && !it.two) continue;
-      const float* stats = reinterpret_cast<const float*>(smem + kTSmemStats) + s * 2 * kTile;
-      bool ok = mbar_wait(&bars.l_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarLFull);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
-      float l = stats[row];
-      const float m = stats[kTile + row];
-      const float vref = reinterpret_cast<const float*>(smem + kTSmemMisc)[2 + s];
-      mbar_arrive(&bars.l_empty[s]);
-      ok = mbar_wait(&bars.o_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarOFull);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
-      ++cnt[s];
-      tc_fence_after_sync();
-      const int r = s * kTile + row;
-      const TilePlace w = tile_place(p, it.s, it.h, it.tile * kTileRows + r);
-      // keys beyond the table's reach
-      if (w.real && it.s.len > it.s.keys && (!p.causal || it.s.len - it.s.n + w.token >= it.s.keys)) l = __int_as_float(0x7fffffff);
-      const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
-      const long long slot = 2ll * blockIdx.x + (it.t_first == 0 ? 1 : 0);
-      const float f = it.whole ? (l == 0.f ? 0.f : __fdividef(vref, l)) : vref;
-      uint16_t* out = p.o + row_offset(p, p.so, it.b, it.s, w);
-      float* part = p.parts + (slot * kTileRows + r) * kKvDim;
+  for (int s = 0; s < 2; ++s) {
+    if (s == 1 && !it.two) continue;
+    const float* stats = reinterpret_cast<const float*>(smem + kTSmemStats) + s * 2 * kTile;
+    bool ok = mbar_wait(&bars.l_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarLFull);
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return false;
+    float l = stats[row];
+    const float m = stats[kTile + row];
+    const float vref = reinterpret_cast<const float*>(smem + kTSmemMisc)[2 + s];
+    mbar_arrive(&bars.l_empty[s]);
+    ok = mbar_wait(&bars.o_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarOFull);
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return false;
+    ++cnt[s];
+    tc_fence_after_sync();
+    const int r = s * kTile + row;
+    const TilePlace w = tile_place(p, it.s, it.h, it.tile * kTileRows + r);
+    // keys beyond the table's reach
+    if (w.real && it.s.len > it.s.keys && (!p.causal || it.s.len - it.s.n + w.token >= it.s.keys)) l = __int_as_float(0x7fffffff);
+    const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
+    const long long slot = 2ll * blockIdx.x + (it.t_first == 0 ? 1 : 0);
+    const float f = it.whole ? (l == 0.f ? 0.f : __fdividef(vref, l)) : vref;
+    uint16_t* out = p.o + row_offset(p, p.so, it.b, it.s, w);
+    float* part = p.parts + (slot * kTileRows + r) * kKvDim;
 #pragma unroll
-      for (int cc = 0; cc < 4; ++cc) {
-        uint32_t o[32];
-        tmem_ld_x32(t_o + cc * 32, o);
-        tmem_wait_ld();
-        if (w.real && it.whole) {
+    for (int cc = 0; cc < 4; ++cc) {
+      uint32_t o[32];
+      tmem_ld_x32(t_o + cc * 32, o);
+      tmem_wait_ld();
+      if (w.real && it.whole) {
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            uint32_t val[8];
+        for (int ch = 0; ch < 2; ++ch) {
+          uint32_t val[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              val[i] = pack_bf16x2(__uint_as_float(o[ch * 16 + 2 * i]) * f, __uint_as_float(o[ch * 16 + 2 * i + 1]) * f);
-            store_32_bytes(out + cc * 32 + ch * 16, val, p.wide_o);
-          }
-        } else if (w.real) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-#pragma unroll
-          for (int ch = 0; ch < 4; ++ch) store_32_bytes(part + cc * 32 + ch * 8, o + ch * 8, true);
+          for (int i = 0; i < 8; ++i)
+            val[i] = pack_bf16x2(__uint_as_float(o[ch * 16 + 2 * i]) * f, __uint_as_float(o[ch * 16 + 2 * i + 1]) * f);
+          store_32_bytes(out + cc * 32 + ch * 16, val, p.wide_o);
         }
-        __syncwarp();
+      } else if (w.real) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) store_32_bytes(part + cc * 32 + ch * 8, o + ch * 8, true);
       }
-      tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars.o_empty[s]);
-      if (it.whole) {
-        if (w.real && p.lse != nullptr)
-          p.lse[lse_index(p, it.b, it.s, w)] = l == 0.f ? -INFINITY : (m - kWeightShift + lg2_approx(l)) * kLn2;
-      } else {
-        reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kTileRows * kKvDim)[slot * kTileRows + r] = make_float2(m, l);
-        if (r == 0 && it.t_first == 0) {
-          p.pieces[2 * blockIdx.x] = make_int4(it.b, it.h, it.tile, it.last);
-          p.pieces[2 * blockIdx.x + 1] = make_int4(it.s.row0, it.s.n, 0, 0);
-        }
+    }
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&bars.o_empty[s]);
+    if (it.whole) {
+      if (w.real && p.lse != nullptr)
+        p.lse[lse_index(p, it.b, it.s, w)] = l == 0.f ? -INFINITY : (m - kWeightShift + lg2_approx(l)) * kLn2;
+    } else {
+      reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kTileRows * kKvDim)[slot * kTileRows + r] = make_float2(m, l);
+      if (r == 0 && it.t_first == 0) {
+        p.pieces[2 * blockIdx.x] = make_int4(it.b, it.h, it.tile, it.last);
+        p.pieces[2 * blockIdx.x + 1] = make_int4(it.s.row0, it.s.n, 0, 0);
       }
     }
+  }
+  drop_item(bars, k, lane);
+  return true;
+}
+
+// Converter warps.  Those that `write` write an item's results one step into the next one, when its last product is long done;
+// the two steps of tiles that lie converted by then keep the tensor pipe busy meanwhile.
+template <int TYPE>
+__device__ __forceinline__ void role_convert(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx, uint32_t tmem,
+                                             int cw, bool writes, int row, int lane) {
+  uint32_t cnt[2] = {0, 0};
+  uint32_t step = 0;
+  for (uint32_t k = 0;; ++k) {
+    if (!wait_item(bars, k, ctx, kRoleEpilogue)) return;
+    const int n = item_box(smem, k)[0];
+    if (!writes) drop_item(bars, k, lane);
+    for (int j = 0; j < max(n, 1); ++j, ++step) {
+      if (n > 0 && !convert_step<TYPE>(bars, smem, ctx, step, cw, lane)) return;
+      if (writes && j == 0 && k > 0 && !write_item(p, bars, smem, ctx, tmem, k - 1, cnt, row, lane)) return;
+    }
+    if (n == 0) return;
   }
 }
 
@@ -692,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
     for (int i = 0; i < kMetaSteps; ++i) mbar_init(&bars.meta_full[i], 1);
     for (int i = 0; i < kItemSlots; ++i) {
       mbar_init(&bars.item_full[i], 1);
-      mbar_init(&bars.item_empty[i], kSchedConsumers);
+      mbar_init(&bars.item_empty[i], kSchedConsumers + 2);
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -710,9 +736,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   if (warp < 8) {
     reg_alloc<kTRegsSoftmax>();
     role_tile_softmax(p, bars, smem, ctx, tmem, warp >> 2, tid & 127, lane);
-  } else if (warp < 12) {
-    reg_dealloc<kTRegsEpilogue>();
-    role_tile_epilogue(p, bars, smem, ctx, tmem, tid & 127, lane);
   } else {
     reg_dealloc<kTRegsOther>();
     if (warp == 12) {
@@ -725,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
         }
       }
     } else {
-      role_convert<TYPE>(bars, smem, ctx, static_cast<uint32_t>(line.end - line.begin), warp - 14, lane);
+      role_convert<TYPE>(p, bars, smem, ctx, tmem, warp < 12 ? warp - 8 : warp - 10, warp < 12, tid & 127, lane);
     }
   }
   tc_fence_before_sync();
