@@ -95,6 +95,12 @@ bool prepare_decode() {
                               attn::kv::Dec<NB>::kSmem) == cudaSuccess;
 }
 
+template <int TYPE, int GRAN>
+bool prepare_tile() {
+  return cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<TYPE, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::kTSmemBytes) == cudaSuccess;
+}
+
 // Per-device one-time set-up: architecture check, kernel attribute, scheduler counters and
 // status word.  Returns the state or nullptr (with *st set).
 DeviceState* device_state(attn_status_t* st) {
@@ -144,10 +150,8 @@ DeviceState* device_state(attn_status_t* st) {
       cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       !prepare_decode<1>() || !prepare_decode<2>() || !prepare_decode<4>() ||
-      cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           attn::kv::kTSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           attn::kv::kTSmemBytes) != cudaSuccess ||
+      !prepare_tile<attn::kv::kE4m3, 16>() || !prepare_tile<attn::kv::kE4m3, 64>() ||
+      !prepare_tile<attn::kv::kInt8, 16>() || !prepare_tile<attn::kv::kInt8, 64>() ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||
       cudaMalloc(&d.status, 2 * sizeof(int)) != cudaSuccess ||
       cudaMemset(d.status, 0, 2 * sizeof(int)) != cudaSuccess ||

@@ -10,7 +10,7 @@
 //   warp  13     fetch: page numbers and scales, codes by TMA, a page a copy (any page size and strides), into 32 KB of staging
 //   warps 14-15  converters: codes exactly to f16 in the swizzled ring of K / V tiles, zeros behind the last token
 //
-// Scales: 16 keys ("a granule") lie in one page.  K's scale multiplies the row's factor granule by granule, V's enters the
+// Scales: 16 keys lie in one page, 64 where pages have 64 slots or more (GRAN, "a granule").  K's scale multiplies the row's factor granule by granule, V's enters the
 // exponent as log2 of its ratio to the largest V scale so far, and is taken out of the row sum again granule by granule, so
 // both products run on bare codes.  When the largest V scale grows, O is rescaled as for a grown row maximum.
 //
@@ -380,6 +380,7 @@ __device__ __forceinline__ void role_tile_mma(const TileBarriers& bars, uint8_t*
 }
 
 // ---- softmax: one thread owns one row of stage `s` ------------------------------------------------------------------------
+template <int GRAN>
 __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
                                                   uint32_t tmem, int s, int row, int lane) {
   const uint32_t lane_sel = static_cast<uint32_t>(row & ~31) << 16;
@@ -456,6 +457,9 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         const uint32_t q = step % kMetaSteps;
         bool ok = mbar_wait(&bars.meta_full[q], (step / kMetaSteps) & 1, ctx, kRoleSoftmax | kBarMeta);
         const float* meta = reinterpret_cast<const float*>(smem + kTSmemMeta) + q * kMetaFloats;
+        float cg[kTile / GRAN];
+#pragma unroll
+        for (int g = 0; g < kTile / GRAN; ++g) cg[g] = fmaxf(meta[kMetaK + g * (GRAN / 16)] * factor, 1e-37f);  // not 0: -inf stays -inf
         ok = ok && mbar_wait(&bars.s_full[s], s_cnt & 1, ctx, kRoleSoftmax | kBarSFull);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) return;
@@ -466,9 +470,6 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         tmem_ld_x32(t_s + 32, xr + 32);
         tmem_ld_x32(t_s + 64, xr + 64);
         tmem_ld_x32(t_s + 96, xr + 96);
-        float cg[8];
-#pragma unroll
-        for (int g = 0; g < 8; ++g) cg[g] = fmaxf(meta[kMetaK + g] * factor, 1e-37f);  // not 0: -inf stays -inf
         tmem_wait_ld();
 #define X(i) __uint_as_float(xr[(i)])
         if (key0 + kStepKeys > clear) {  // warp-uniform
@@ -480,12 +481,17 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         }
         float m_blk = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          const int i = g * 16;
-          const float a = max3(X(i), X(i + 1), X(i + 2)), b = max3(X(i + 3), X(i + 4), X(i + 5));
-          const float c = max3(X(i + 6), X(i + 7), X(i + 8)), d = max3(X(i + 9), X(i + 10), X(i + 11));
-          const float e = max3(X(i + 12), X(i + 13), X(i + 14));
-          m_blk = fmaxf(m_blk, fmaxf(max3(a, b, X(i + 15)), max3(c, d, e)) * cg[g]);
+        for (int g = 0; g < kTile / GRAN; ++g) {
+          float top[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int i = g * GRAN + c * (GRAN / 4);
+            top[c] = max3(X(i), X(i + 1), X(i + 2));
+#pragma unroll
+            for (int k = 3; k + 1 < GRAN / 4; k += 2) top[c] = max3(top[c], X(i + k), X(i + k + 1));
+            top[c] = fmaxf(top[c], X(i + GRAN / 4 - 1));
+          }
+          m_blk = fmaxf(m_blk, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * cg[g]);
         }
         if (j == 0) {
           m_used = m_blk == -INFINITY ? 0.f : m_blk;
@@ -510,26 +516,28 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
           }
         }
         const float neg_m = kWeightShift - m_used;
-        float2 sum = make_float2(0.f, 0.f);
+        float2 sum = make_float2(0.f, 0.f), part = make_float2(0.f, 0.f);
 #pragma unroll
         for (int cc = 0; cc < 4; ++cc) {
           uint32_t pk[16];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int g = cc * 2 + h;
-            const float add = neg_m + meta[kMetaV + g];
-            const float inv = meta[kMetaInv + g];
+          for (int h = 0; h < 2; ++h) {  // 16 keys
+            const int g = (cc * 2 + h) * 16 / GRAN;
+            const float add = neg_m + meta[kMetaV + g * (GRAN / 16)];
             const float2 c2 = make_float2(cg[g], cg[g]), a2 = make_float2(add, add);
-            float2 part;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              const int i = g * 16 + k * 2;
+              const int i = (cc * 2 + h) * 16 + k * 2;
               const float2 x = fma2(make_float2(X(i), X(i + 1)), c2, a2);
               const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-              part = k == 0 ? e : add2(part, e);
+              part = add2(part, e);
               pk[h * 8 + k] = pack_f16x2(e.x, e.y);
             }
-            sum = fma2(part, make_float2(inv, inv), sum);
+            if (((cc * 2 + h) * 16 + 16) % GRAN == 0) {
+              const float inv = meta[kMetaInv + g * (GRAN / 16)];
+              sum = fma2(part, make_float2(inv, inv), sum);
+              part = make_float2(0.f, 0.f);
+            }
           }
           tmem_st_x16(t_s + cc * 16, pk);
           if (cc == 1) {
@@ -664,7 +672,7 @@ __device__ __forceinline__ void role_convert(const CachedParams& p, const TileBa
   }
 }
 
-template <int TYPE>
+template <int TYPE, int GRAN>
 __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __grid_constant__ CUtensorMap tm_k,
                                                                      const __grid_constant__ CUtensorMap tm_v, const CachedParams p) {
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -735,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
 
   if (warp < 8) {
     reg_alloc<kTRegsSoftmax>();
-    role_tile_softmax(p, bars, smem, ctx, tmem, warp >> 2, tid & 127, lane);
+    role_tile_softmax<GRAN>(p, bars, smem, ctx, tmem, warp >> 2, tid & 127, lane);
   } else {
     reg_dealloc<kTRegsOther>();
     if (warp == 12) {

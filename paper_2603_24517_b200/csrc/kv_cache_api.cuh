@@ -146,6 +146,13 @@ attn_status_t launch_decode(const CachedParams& p, const CUtensorMap& tm_k, cons
   return launch_join<D::kRows>(p, D::kRows, s);
 }
 
+template <int TYPE, int GRAN>
+attn_status_t launch_tile(const CachedParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
+  attn::kv::attn_cached_tile_kernel<TYPE, GRAN><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
+  if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
+  return launch_join<attn::kv::kTileRows>(p, attn::kv::kTileRows / (8 * attn::kv::kJoinRows), s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -233,13 +240,9 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   if (rows == 8) return launch_decode<1>(p, tm_k, tm_v, s);
   if (rows == 16) return launch_decode<2>(p, tm_k, tm_v, s);
   if (rows == 32) return launch_decode<4>(p, tm_k, tm_v, s);
-  if (p.c.type == ATTN_KV_E4M3) {
-    attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
-  } else {
-    attn::kv::attn_cached_tile_kernel<attn::kv::kInt8><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
-  }
-  if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-  return launch_join<attn::kv::kTileRows>(p, attn::kv::kTileRows / (8 * attn::kv::kJoinRows), s);
+  const bool e4m3 = p.c.type == ATTN_KV_E4M3;
+  if (cache->page_size >= 64) return e4m3 ? launch_tile<attn::kv::kE4m3, 64>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 64>(p, tm_k, tm_v, s);
+  return e4m3 ? launch_tile<attn::kv::kE4m3, 16>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 16>(p, tm_k, tm_v, s);
 }
 
 }  // extern "C"
