@@ -149,7 +149,7 @@ DeviceState* device_state(attn_status_t* st) {
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
-      !prepare_decode<1>() || !prepare_decode<2>() || !prepare_decode<4>() ||
+      !prepare_decode<1>() || !prepare_decode<2>() ||
       !prepare_tile<attn::kv::kE4m3, 16>() || !prepare_tile<attn::kv::kE4m3, 64>() ||
       !prepare_tile<attn::kv::kInt8, 16>() || !prepare_tile<attn::kv::kInt8, 64>() ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||

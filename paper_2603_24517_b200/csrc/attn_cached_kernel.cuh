@@ -2,7 +2,7 @@
 //
 //     s_ij = scale k_scale(page of j) q_i . c^K_j,    o_i = sum_j softmax_j(s_ij) v_scale(page of j) c^V_j
 //
-// Bound by HBM: 256 bytes a cached token and key head, read once for all query heads of the group.  A query tile is 8, 16 or 32
+// Bound by HBM: 256 bytes a cached token and key head, read once for all query heads of the group.  A query tile is 8 or 16
 // rows (token, head of the group), heads fastest.  All work is a line of (sequence, key head, query tile, 128 keys) steps, cut
 // into equal contiguous pieces, one a CTA, whatever the lengths are; the cut is computed on the device from the lengths.  A
 // CTA that holds a whole tile's keys writes its result, the others leave fp32 parts, which a second kernel joins in order.
@@ -38,7 +38,7 @@ template <int NB>
 struct Dec {
   static constexpr int kRows = 8 * NB;
   static constexpr int kCtasPerSm = NB == 1 ? 2 : 1;
-  static constexpr int kStages = NB == 1 ? 2 : NB == 2 ? 4 : 2;
+  static constexpr int kStages = NB == 1 ? 2 : 4;
   static constexpr int kRing = kDecWarps * kStages * kWarpStageBytes;
   static constexpr int kMerge = kDecWarps * kRows * kKvDim * 4;
   static constexpr int kStats = kDecWarps * kRows * 8;

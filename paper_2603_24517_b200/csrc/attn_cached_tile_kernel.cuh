@@ -48,7 +48,7 @@ static_assert(kTSmemBars % 8 == 0 && kTSmemMeta % 16 == 0 && kTSmemStats % 16 ==
 static_assert(kHeadDim == kKvDim && kTile == kStepKeys, "one head dimension, one tile");
 
 // What the converters tell the softmax warps about a step.
-enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaGrow = 25, kMetaBad = 26, kMetaValid = 27 };
+enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaBad = 25, kMetaValid = 26 };
 constexpr float kMinRatioLog2 = -60.f;  // V scales below 2^-60 of the largest count as that: nothing in f16
 
 struct TileBarriers {
@@ -81,7 +81,8 @@ constexpr uint32_t kIdescPVf16 = make_idesc_f16(1);
 struct Item {
   int n;            // steps; 0: no more items
   int t_first;      // the first of them
-  bool two;         // the second stage has rows
+  bool two;         // the second stage has rows of its own
+  bool split;       // it has not: the stages take the steps in turn, and their parts are joined at the end
   bool whole;       // all of the tile's steps
   int b, h, tile;
   SeqWork s;
@@ -92,7 +93,7 @@ __device__ __forceinline__ void publish_item(int* box, const CachedParams& p, co
   const bool two = c.tile * kTileRows + kTile < c.s.n * p.group;
   box[0] = n;
   box[1] = c.t;
-  box[2] = (two ? 1 : 0) | (c.t == 0 && n == c.steps ? 2 : 0);
+  box[2] = (two ? 1 : 0) | (c.t == 0 && n == c.steps ? 2 : 0) | (!two && n > 1 ? 4 : 0);
   box[3] = c.b;
   box[4] = c.h;
   box[5] = c.tile;
@@ -115,6 +116,7 @@ __device__ __forceinline__ void read_item(const uint8_t* smem, uint32_t k, Item&
   it.t_first = box[1];
   it.two = (box[2] & 1) != 0;
   it.whole = (box[2] & 2) != 0;
+  it.split = (box[2] & 4) != 0;
   it.b = box[3];
   it.h = box[4];
   it.tile = box[5];
@@ -219,7 +221,6 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
           meta[kMetaInv + lane - 8] = ex2_approx(-ratio);
         } else if (lane == 16) {
           meta[kMetaVref] = ref;
-          meta[kMetaGrow] = vref == ref ? 1.f : __fdividef(vref, ref);
           reinterpret_cast<int*>(meta)[kMetaBad] = bad != 0 ? (__ffs(bad) - 1) * 16 : kStepKeys;
           reinterpret_cast<int*>(meta)[kMetaValid] = now.keys - now.key0;
         }
@@ -314,6 +315,52 @@ __device__ __forceinline__ void role_tile_mma(const TileBarriers& bars, uint8_t*
   for (uint32_t k = 0;; ++k) {
     Item it;
     if (!take_item(bars, smem, k, ctx, kRoleMma, lane, it) || it.n == 0) return;
+    if (it.split) {
+      // The first two steps' scores, then per step j: P V, and the scores of step j + 2 in the place it leaves.  The keys of step
+      // j + 1 are given back only now: the entry of step j + 4 goes by them, and step j's weights have been taken now
+      const uint32_t first = kv_cnt;  // tiles K(j), V(j) are first + 2 j, first + 2 j + 1
+      auto tile_ready = [&](uint32_t t) { return mbar_wait_warp(&bars.kv_full[t % kKvSlots], (t / kKvSlots) & 1, ctx, kRoleMma | kBarKvFull); };
+#pragma unroll 1
+      for (int j = -2; j < it.n; ++j) {
+        const int s = j & 1;  // selected, not indexed: the counters stay in registers
+        const uint32_t q_par = (s ? q_cnt[1] : q_cnt[0]) & 1, sp_par = (s ? sp_cnt[1] : sp_cnt[0]) & 1;
+        const uint32_t vt = first + 2 * j + 1, kt = first + 2 * (j + 2);
+        if (j >= 0) {
+          if (!tile_ready(vt)) return;
+          const uint64_t v_desc = vtile_desc(base + kTSmemKv + (vt % kKvSlots) * kTileBytes);
+          const uint32_t t_o = tmem + 2 * kTile + s * kTile, t_p = tmem + s * kTile;
+          if (j < 2 && !mbar_wait_warp(&bars.o_empty[s], q_par ^ 1, ctx, kRoleMma | kBarOEmpty)) return;
+          if (!mbar_wait_warp(&bars.p_half[s], sp_par, ctx, kRoleMma | kBarPHalf)) return;
+          tc_fence_after_sync();
+          issue_pv_f16(leader, t_o, t_p, v_desc, j >= 2, 0, 4);
+          if (!mbar_wait_warp(&bars.p_full[s], sp_par, ctx, kRoleMma | kBarPFull)) return;
+          if (s) {
+            ++sp_cnt[1];
+          } else {
+            ++sp_cnt[0];
+          }
+          tc_fence_after_sync();
+          issue_pv_f16(leader, t_o, t_p, v_desc, j >= 2, 4, 8);
+          if (leader) {
+            mma_commit(&bars.kv_empty[vt % kKvSlots]);
+            if (j + 1 < it.n) mma_commit(&bars.kv_empty[(vt + 1) % kKvSlots]);
+            if (j + 2 >= it.n) mma_commit(&bars.o_full[s]);
+          }
+        }
+        if (j + 2 < it.n) {
+          if (!tile_ready(kt)) return;
+          if (j < 0 && !mbar_wait_warp(&bars.q_full[s], q_par, ctx, kRoleMma | kBarQFull)) return;
+          tc_fence_after_sync();
+          issue_qk_f16(leader, tmem + s * kTile, s ? q_desc[1] : q_desc[0], kmajor_desc(base + kTSmemKv + (kt % kKvSlots) * kTileBytes));
+          if (leader) mma_commit(&bars.s_full[s]);
+        }
+        if (leader && j == -2) mma_commit(&bars.kv_empty[kt % kKvSlots]);
+      }
+      kv_cnt = first + 2 * it.n;
+      ++q_cnt[0];
+      ++q_cnt[1];
+      continue;
+    }
     {
       const uint32_t slot = kv_cnt % kKvSlots, par = (kv_cnt / kKvSlots) & 1;
       if (!mbar_wait_warp(&bars.kv_full[slot], par, ctx, kRoleMma | kBarKvFull)) return;
@@ -358,6 +405,7 @@ __device__ __forceinline__ void role_tile_mma(const TileBarriers& bars, uint8_t*
           tc_fence_after_sync();
           issue_pv_f16(leader, tmem + 2 * kTile + s * kTile, tmem + s * kTile, v_desc, j > 0, 4, 8);
           if (leader && !has_next) mma_commit(&bars.o_full[s]);
+          if (leader && (s == 1 || !it.two)) mma_commit(&bars.kv_empty[vslot]);
           if (has_next) {
             if (!k_ready) {
               if (!mbar_wait_warp(&bars.kv_full[kslot], kpar, ctx, kRoleMma | kBarKvFull)) return;
@@ -369,10 +417,7 @@ __device__ __forceinline__ void role_tile_mma(const TileBarriers& bars, uint8_t*
           }
         }
       }
-      if (leader) {
-        mma_commit(&bars.kv_empty[vslot]);
-        if (has_next) mma_commit(&bars.kv_empty[kslot]);
-      }
+      if (leader && has_next) mma_commit(&bars.kv_empty[kslot]);
     }
     ++q_cnt[0];
     if (it.two) ++q_cnt[1];
@@ -389,7 +434,9 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
   float* stats = reinterpret_cast<float*>(smem + kTSmemStats) + s * 2 * kTile;
   uint32_t s_cnt = 0, l_cnt = 0, step = 0;
   for (uint32_t k = 0;; ++k) {
-    int n, key0;  // steps left, first key of the step
+    int n, key0;  // steps of the item, first key of the step
+    int first, stride;  // the stage's first step, and from one of its steps to the next
+    bool idle;    // none of the warp's rows is real: it only keeps the barriers going
     int limit;    // keys the row sees; rows that are not real see all
     int clear;    // keys that all rows of the stage see: steps up to there need no mask
     float factor;
@@ -399,15 +446,18 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
       Item it;
       if (!take_item(bars, smem, k, ctx, kRoleSoftmax, lane, it) || it.n == 0) return;
       n = it.n;
-      used = s == 0 || it.two;
+      used = s == 0 || it.two || it.split;
+      first = it.split ? s : 0;
+      stride = it.split ? 2 : 1;
       if (used) {
         // Q: the stage's last product that reads it has completed (its scores have been taken)
-        const int r0 = it.tile * kTileRows + s * kTile;
+        const int r0 = it.tile * kTileRows + (it.two ? s * kTile : 0);
         const TilePlace w = tile_place(p, it.s, it.h, r0 + row);
         limit = w.real ? visible(it.s, w.token, p.causal) : it.s.keys;
         clear = visible(it.s, min(r0 / p.group, it.s.n - 1), p.causal);
-        key0 = it.t_first * kStepKeys;
+        key0 = (it.t_first + first) * kStepKeys;
         seen = limit > key0;
+        idle = !__any_sync(0xffffffffu, w.real);
         // half a warp brings a row, 16 bytes a lane, as it is, and then turns what it has brought into f16 in place
         const long long mine = w.real ? row_offset(p, p.sq, it.b, it.s, w) : -1;
         uint8_t* dst = smem + kTSmemQ + s * kTileBytes + ((lane & 15) >> 3) * kHalfBytes + ((row & ~31) + (lane >> 4)) * 128;
@@ -452,10 +502,20 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
     }
     if (used) {
       float m_used = -INFINITY;  // reference maximum, log2 units
-      float l = 0.f;
-      for (int j = 0; j < n; ++j, ++step, key0 += kStepKeys) {
-        const uint32_t q = step % kMetaSteps;
-        bool ok = mbar_wait(&bars.meta_full[q], (step / kMetaSteps) & 1, ctx, kRoleSoftmax | kBarMeta);
+      float l = 0.f, vref = 0.f;
+      for (int j = first; j < n; j += stride, key0 += stride * kStepKeys) {
+        if (idle) {
+          bool ok = mbar_wait(&bars.s_full[s], s_cnt & 1, ctx, kRoleSoftmax | kBarSFull);
+          if (!__all_sync(0xffffffffu, ok)) return;
+          ++s_cnt;
+          if (lane == 0) {
+            mbar_arrive(&bars.p_half[s]);
+            mbar_arrive(&bars.p_full[s]);
+          }
+          continue;
+        }
+        const uint32_t q = (step + j) % kMetaSteps;
+        bool ok = mbar_wait(&bars.meta_full[q], ((step + j) / kMetaSteps) & 1, ctx, kRoleSoftmax | kBarMeta);
         const float* meta = reinterpret_cast<const float*>(smem + kTSmemMeta) + q * kMetaFloats;
         float cg[kTile / GRAN];
 #pragma unroll
@@ -493,11 +553,12 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
           }
           m_blk = fmaxf(m_blk, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * cg[g]);
         }
-        if (j == 0) {
+        const float v_grow = vref == meta[kMetaVref] ? 1.f : __fdividef(vref, meta[kMetaVref]);
+        vref = meta[kMetaVref];
+        if (j == first) {
           m_used = m_blk == -INFINITY ? 0.f : m_blk;
         } else {
           const float m_new = fmaxf(m_used, m_blk);
-          const float v_grow = meta[kMetaGrow];
           if (__any_sync(0xffffffffu, m_new - m_used > kWeightLag || v_grow != 1.f)) {
             // P V of the step before has completed (S of this one was issued after it): O is quiescent
             const float alpha = ex2_approx(m_used - m_new);
@@ -560,15 +621,11 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
       // a row that has seen no key here has the sum 0 by definition, and no maximum
       stats[row] = seen ? l : 0.f;
       stats[kTile + row] = seen ? m_used : -INFINITY;
-      if (row == 0) {  // the last step's entry: the next one that takes its place needs scores of the next item
-        reinterpret_cast<float*>(smem + kTSmemMisc)[2 + s] =
-            reinterpret_cast<const float*>(smem + kTSmemMeta)[(step - 1) % kMetaSteps * kMetaFloats + kMetaVref];
-      }
+      if (row == 0) reinterpret_cast<float*>(smem + kTSmemMisc)[2 + s] = vref;
       mbar_arrive(&bars.l_full[s]);
       ++l_cnt;
-    } else {
-      step += n;
     }
+    step += n;
   }
 }
 
@@ -591,18 +648,32 @@ __device__ __forceinline__ bool write_item(const CachedParams& p, const TileBarr
 #pragma unroll 1
   for (int s = 0; s < 2; ++s) {
     if (s == 1 && !it.two) continue;
-    const float* stats = reinterpret_cast<const float*>(smem + kTSmemStats) + s * 2 * kTile;
-    bool ok = mbar_wait(&bars.l_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarLFull);
-    ok = __all_sync(0xffffffffu, ok);
-    if (!ok) return false;
-    float l = stats[row];
-    const float m = stats[kTile + row];
-    const float vref = reinterpret_cast<const float*>(smem + kTSmemMisc)[2 + s];
-    mbar_arrive(&bars.l_empty[s]);
-    ok = mbar_wait(&bars.o_full[s], cnt[s] & 1, ctx, kRoleEpilogue | kBarOFull);
-    ok = __all_sync(0xffffffffu, ok);
-    if (!ok) return false;
-    ++cnt[s];
+    float l = 0.f, m = -INFINITY, f[2] = {0.f, 0.f};  // the stage's part, or both stages' joined: O = f[0] O0 + f[1] O1
+    {
+      float lq[2], mq[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (q == 1 && !it.split) break;
+        const float* stats = reinterpret_cast<const float*>(smem + kTSmemStats) + (s + q) * 2 * kTile;
+        const bool ok = mbar_wait(&bars.l_full[s + q], cnt[s + q] & 1, ctx, kRoleEpilogue | kBarLFull);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        lq[q] = stats[row];
+        mq[q] = stats[kTile + row];
+        f[q] = reinterpret_cast<const float*>(smem + kTSmemMisc)[2 + s + q];
+        mbar_arrive(&bars.l_empty[s + q]);
+        m = fmaxf(m, mq[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (q == 1 && !it.split) break;
+        const bool ok = mbar_wait(&bars.o_full[s + q], cnt[s + q] & 1, ctx, kRoleEpilogue | kBarOFull);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        ++cnt[s + q];
+        const float a = mq[q] == -INFINITY ? 0.f : ex2_approx(mq[q] - m);
+        l += mq[q] == -INFINITY ? lq[q] : lq[q] * a;  // the sum of a row that has seen no key is 0
+        f[q] *= a;
+      }
+    }
     tc_fence_after_sync();
     const int r = s * kTile + row;
     const TilePlace w = tile_place(p, it.s, it.h, it.tile * kTileRows + r);
@@ -610,34 +681,42 @@ __device__ __forceinline__ bool write_item(const CachedParams& p, const TileBarr
     if (w.real && it.s.len > it.s.keys && (!p.causal || it.s.len - it.s.n + w.token >= it.s.keys)) l = __int_as_float(0x7fffffff);
     const uint32_t t_o = tmem + lane_sel + 2 * kTile + s * kTile;
     const long long slot = 2ll * blockIdx.x + (it.t_first == 0 ? 1 : 0);
-    const float f = it.whole ? (l == 0.f ? 0.f : __fdividef(vref, l)) : vref;
+    if (it.whole) {
+      const float inv = l == 0.f ? 0.f : __fdividef(1.f, l);
+      f[0] *= inv;
+      f[1] *= inv;
+    }
     uint16_t* out = p.o + row_offset(p, p.so, it.b, it.s, w);
     float* part = p.parts + (slot * kTileRows + r) * kKvDim;
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc) {
-      uint32_t o[32];
-      tmem_ld_x32(t_o + cc * 32, o);
+#pragma unroll 2
+    for (int cc = 0; cc < 8; ++cc) {
+      uint32_t o[16], o1[16];
+      tmem_ld_x16(t_o + cc * 16, o);
+      if (it.split) tmem_ld_x16(t_o + kTile + cc * 16, o1);
       tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float x = __uint_as_float(o[i]) * f[0];
+        if (it.split) x = fmaf(__uint_as_float(o1[i]), f[1], x);
+        o[i] = __float_as_uint(x);
+      }
       if (w.real && it.whole) {
+        uint32_t val[8];
 #pragma unroll
-        for (int ch = 0; ch < 2; ++ch) {
-          uint32_t val[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            val[i] = pack_bf16x2(__uint_as_float(o[ch * 16 + 2 * i]) * f, __uint_as_float(o[ch * 16 + 2 * i + 1]) * f);
-          store_32_bytes(out + cc * 32 + ch * 16, val, p.wide_o);
-        }
+        for (int i = 0; i < 8; ++i) val[i] = pack_bf16x2(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
+        store_32_bytes(out + cc * 16, val, p.wide_o);
       } else if (w.real) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-#pragma unroll
-        for (int ch = 0; ch < 4; ++ch) store_32_bytes(part + cc * 32 + ch * 8, o + ch * 8, true);
+        store_32_bytes(part + cc * 16, o, true);
+        store_32_bytes(part + cc * 16 + 8, o + 8, true);
       }
       __syncwarp();
     }
     tc_fence_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&bars.o_empty[s]);
+    if (lane == 0) {
+      mbar_arrive(&bars.o_empty[s]);
+      if (it.split) mbar_arrive(&bars.o_empty[1]);
+    }
     if (it.whole) {
       if (w.real && p.lse != nullptr)
         p.lse[lse_index(p, it.b, it.s, w)] = l == 0.f ? -INFINITY : (m - kWeightShift + lg2_approx(l)) * kLn2;

@@ -112,10 +112,11 @@ size_t cached_workspace(int ctas, int rows) {
 }
 constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 
-// Rows of a query tile for the longest sequence's (token, head of a group) rows: the smallest tile that holds them.
+// Rows of a query tile for the longest sequence's (token, head of a group) rows.  Decoding, 16 sequences of 12000 tokens, 8 key heads,
+// E4M3: 8 rows 77 us in tiles of 8, 110 of 16; 16 rows 133 and 113.
 int tile_rows(int Hq, int Hkv, int max_new) {
   const long long rows = static_cast<long long>(Hq / Hkv) * max_new;
-  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : attn::kv::kTileRows;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : attn::kv::kTileRows;
 }
 int cached_ctas(int sms, int rows) { return rows == 8 ? sms * attn::kv::Dec<1>::kCtasPerSm : sms; }
 
@@ -239,7 +240,6 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   if (!make_page_map(&tm_k, cache, 0, box, swizzle) || !make_page_map(&tm_v, cache, 1, box, swizzle)) return ATTN_ERR_CUDA;
   if (rows == 8) return launch_decode<1>(p, tm_k, tm_v, s);
   if (rows == 16) return launch_decode<2>(p, tm_k, tm_v, s);
-  if (rows == 32) return launch_decode<4>(p, tm_k, tm_v, s);
   const bool e4m3 = p.c.type == ATTN_KV_E4M3;
   if (cache->page_size >= 64) return e4m3 ? launch_tile<attn::kv::kE4m3, 64>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 64>(p, tm_k, tm_v, s);
   return e4m3 ? launch_tile<attn::kv::kE4m3, 16>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 16>(p, tm_k, tm_v, s);
