@@ -53,6 +53,7 @@ struct CachedParams {
   float* lse;             // [B, Hq, S], or [Hq, S] with starts; may be null
   RowStrides sq, so;
   int Hq, group, causal;
+  int rows_above, rows_up_to;  // the launch is for sequences of more than / at most so many rows (tokens times heads of the group)
   float scale_log2;       // scale * log2(e)
   float* parts;           // [2 ctas][rows][kKvDim], then [2 ctas][rows][2] (reference maximum in log2 units, sum)
   int4* pieces;           // [ctas][2]: {sequence, head, tile, last CTA with a part or -1}, {first row, rows of the sequence} of the
@@ -68,9 +69,12 @@ struct SeqWork {
   int len;           // tokens in all, at least 0
   int keys;          // of them in the table's reach
 };
-__device__ __forceinline__ SeqWork seq_work(const CacheView& c, int b) {
+__device__ __forceinline__ SeqWork seq_work(const CachedParams& p, int b) {
+  const CacheView& c = p.c;
   SeqWork s;
   rows_of(c, b, s.row0, s.n);
+  const int rows = s.n * p.group;
+  if (rows <= p.rows_above || rows > p.rows_up_to) s.n = 0;  // another launch's
   s.len = max(__ldg(c.lens + b), 0);
   s.keys = static_cast<int>(min(static_cast<long long>(s.len), static_cast<long long>(c.max_blocks) << c.page_log2));
   return s;
@@ -93,7 +97,7 @@ struct Cursor {
     steps = steps_of(s, min((tile * ROWS + ROWS - 1) / p.group, s.n - 1), p.causal);
   }
   __device__ __forceinline__ void enter_sequence(const CachedParams& p) {
-    s = seq_work(p.c, b);
+    s = seq_work(p, b);
     tiles = (s.n * p.group + ROWS - 1) / ROWS;
   }
   __device__ __forceinline__ void next_tile(const CachedParams& p) {  // of the head, then the next head, the next sequence
@@ -139,7 +143,7 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   const int per = (p.c.B + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
   const int b0 = static_cast<int>(threadIdx.x) * per, b1 = min(b0 + per, p.c.B);
   long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += head_steps<ROWS>(p, seq_work(p.c, b)) * p.c.Hkv;
+  for (int b = b0; b < b1; ++b) mine += head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
   long long upto = mine;
 #pragma unroll
   for (int m = 1; m < 32; m <<= 1) {
@@ -168,7 +172,7 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   long long from = before + upto - mine;
   if (line.begin >= from && line.begin < from + mine) {
     for (int b = b0; b < b1; ++b) {
-      const long long cost = head_steps<ROWS>(p, seq_work(p.c, b)) * p.c.Hkv;
+      const long long cost = head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
       if (line.begin < from + cost) {
         found[0] = b;
         found[1] = from;

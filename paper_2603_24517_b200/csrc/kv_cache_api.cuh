@@ -111,14 +111,27 @@ size_t cached_workspace(int ctas, int rows) {
   return cached_parts(ctas, rows) * (attn::kv::kKvDim + 2) * sizeof(float) + static_cast<size_t>(ctas) * 2 * sizeof(int4) + 32;
 }
 constexpr int kWorkspaceSms = 160;  // SMs of a device at most
+// In a packed batch with long sequences, single tokens and what else fits 8 rows go to the decoding kernel first (a step of 24
+// sequences, 21 of them single tokens: 343 us all in tiles of 256 rows, 290 so; 4 us where there are none; 16 rows of two
+// tokens stay, 16 sequences of 16 to 32 rows take 88 us together and 112 apart).
+int short_rows(int group) { return group > 8 && group <= 16 ? group : 8; }
 
 // Rows of a query tile for the longest sequence's (token, head of a group) rows.  Decoding, 16 sequences of 12000 tokens, 8 key heads,
-// E4M3: 8 rows 77 us in tiles of 8, 110 of 16; 16 rows 133 and 113.
+// E4M3: 8 rows 77 us in tiles of 8, 110 of 16; 16 rows 133 and 113; 32 rows 208 in tiles of 16, 176 of 256.
 int tile_rows(int Hq, int Hkv, int max_new) {
   const long long rows = static_cast<long long>(Hq / Hkv) * max_new;
   return rows <= 8 ? 8 : rows <= 16 ? 16 : attn::kv::kTileRows;
 }
 int cached_ctas(int sms, int rows) { return rows == 8 ? sms * attn::kv::Dec<1>::kCtasPerSm : sms; }
+
+// Places the parts of a launch at `at`; returns the first byte behind them.
+uintptr_t place_parts(CachedParams* p, uintptr_t at, int sms, int rows) {
+  at = (at + 31) & ~static_cast<uintptr_t>(31);
+  p->ctas = cached_ctas(sms, rows);
+  p->parts = reinterpret_cast<float*>(at);
+  p->pieces = reinterpret_cast<int4*>(p->parts + cached_parts(p->ctas, rows) * (attn::kv::kKvDim + 2));
+  return reinterpret_cast<uintptr_t>(p->pieces + 2 * p->ctas);
+}
 
 // The join as a launch that may begin before the one in front of it has ended (it waits for that one's results on the device).
 template <int ROWS>
@@ -196,7 +209,8 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
 size_t attn_fwd_cached_workspace_bytes(int Hq, int Hkv, int max_new) {
   if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_new <= 0) return 0;
   const int rows = tile_rows(Hq, Hkv, max_new);
-  return cached_workspace(cached_ctas(kWorkspaceSms, rows), rows);
+  const size_t bytes = cached_workspace(cached_ctas(kWorkspaceSms, rows), rows);
+  return rows == attn::kv::kTileRows ? bytes + cached_workspace(cached_ctas(kWorkspaceSms, 8), 8) : bytes;
 }
 
 attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
@@ -227,19 +241,29 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   p.causal = causal ? 1 : 0;
   p.scale_log2 = scale * 1.4426950408889634f;
   const int rows = tile_rows(Hq, cache->Hkv, max_new);
-  p.ctas = cached_ctas(dev->sm_count < kWorkspaceSms ? dev->sm_count : kWorkspaceSms, rows);
-  p.wide_o = !misaligned(o, 31) && p.so.b % 16 == 0 && p.so.s % 16 == 0 && p.so.h % 16 == 0;
+  const int sms = dev->sm_count < kWorkspaceSms ? dev->sm_count : kWorkspaceSms;
   p.status = dev->status;
-  p.parts = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(workspace) + 31) & ~static_cast<uintptr_t>(31));
-  p.pieces = reinterpret_cast<int4*>(p.parts + cached_parts(p.ctas, rows) * (attn::kv::kKvDim + 2));
+  p.wide_o = !misaligned(o, 31) && p.so.b % 16 == 0 && p.so.s % 16 == 0 && p.so.h % 16 == 0;
+  p.rows_above = 0;
+  p.rows_up_to = 0x7fffffff;
+  uintptr_t at = place_parts(&p, reinterpret_cast<uintptr_t>(workspace), sms, rows);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   CUtensorMap tm_k, tm_v;
-  const bool many = rows == attn::kv::kTileRows;
-  const int box = many ? cache->page_size : 16;
-  const CUtensorMapSwizzle swizzle = many ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
-  if (!make_page_map(&tm_k, cache, 0, box, swizzle) || !make_page_map(&tm_v, cache, 1, box, swizzle)) return ATTN_ERR_CUDA;
-  if (rows == 8) return launch_decode<1>(p, tm_k, tm_v, s);
-  if (rows == 16) return launch_decode<2>(p, tm_k, tm_v, s);
+  const bool many = rows == attn::kv::kTileRows, split = many && cache->starts != nullptr && cache->B > 1;
+  if (!many || split) {
+    if (!make_page_map(&tm_k, cache, 0, 16, CU_TENSOR_MAP_SWIZZLE_128B) || !make_page_map(&tm_v, cache, 1, 16, CU_TENSOR_MAP_SWIZZLE_128B))
+      return ATTN_ERR_CUDA;
+    if (rows == 8) return launch_decode<1>(p, tm_k, tm_v, s);
+    if (rows == 16) return launch_decode<2>(p, tm_k, tm_v, s);
+    CachedParams few = p;
+    place_parts(&few, at, sms, 8);
+    few.rows_up_to = p.rows_above = short_rows(p.group);
+    st = launch_decode<1>(few, tm_k, tm_v, s);
+    if (st != ATTN_OK) return st;
+  }
+  if (!make_page_map(&tm_k, cache, 0, cache->page_size, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+      !make_page_map(&tm_v, cache, 1, cache->page_size, CU_TENSOR_MAP_SWIZZLE_NONE))
+    return ATTN_ERR_CUDA;
   const bool e4m3 = p.c.type == ATTN_KV_E4M3;
   if (cache->page_size >= 64) return e4m3 ? launch_tile<attn::kv::kE4m3, 64>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 64>(p, tm_k, tm_v, s);
   return e4m3 ? launch_tile<attn::kv::kE4m3, 16>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 16>(p, tm_k, tm_v, s);

@@ -466,3 +466,16 @@ def test_two_calls_at_once():
         torch.cuda.synchronize()
         for g, w in zip(got, want):
             assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+@pytest.mark.parametrize("group,page,kind", [(4, 32, E4M3), (16, 16, INT8), (1, 128, E4M3)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_and_short_sequences_in_one_batch(group, page, kind, causal):
+    """Prompts next to single tokens, sequences without rows and without tokens: each row is written once, whichever kernel has it."""
+    seqs = [(1, 900), (300, 700), (0, 40), (1, 1), (2, 333), (65, 65), (8, 500), (1, 0), (9, 129), (1, 2500), (17, 17)]
+    b = Batch(seqs, 2, page, kind, seed=group, scale_spread=1.0)
+    q = b.queries(2 * group)
+    o = torch.full_like(q, 7.0)
+    lse = torch.full((2 * group, q.shape[0]), 7.0, device="cuda")
+    lib.attn_fwd_cached(q, b.cache, o, lse, b.table, b.lens, b.starts, max_new=300, causal=causal)
+    check(b, q, o, lse, causal)
