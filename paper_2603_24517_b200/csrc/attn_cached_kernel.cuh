@@ -135,28 +135,8 @@ struct Line {
   __device__ __forceinline__ long long owner(long long step) const { return ((step + 1) * ctas - 1) / total; }
 };
 
-// Cuts the line and finds where this CTA's piece begins.  All threads call; `scratch` holds 3 * (threads / 32) + 2 long longs.
-// A thread's sequences are neighbours, so their sums are scanned once and only the thread that holds the place looks closer.
-template <int ROWS>
-__device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cursor<ROWS>& at, long long* scratch) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int per = (p.c.B + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
-  const int b0 = static_cast<int>(threadIdx.x) * per, b1 = min(b0 + per, p.c.B);
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
-  long long upto = mine;
-#pragma unroll
-  for (int m = 1; m < 32; m <<= 1) {
-    const long long other = __shfl_up_sync(0xffffffffu, upto, m);
-    if (lane >= m) upto += other;
-  }
-  if (lane == 31) scratch[warp] = upto;
-  __syncthreads();
-  long long total = 0, before = 0;
-  for (int w = 0; w < warps; ++w) {
-    if (w == warp) before = total;
-    total += scratch[w];
-  }
+// This CTA's piece of a line of `total` steps; false: it has none.
+__device__ __forceinline__ bool cut_line(const CachedParams& p, Line& line, long long total) {
   line.total = total;
   line.ctas = min(static_cast<long long>(p.ctas), total);
   if (blockIdx.x >= line.ctas) return false;
@@ -168,25 +148,63 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
     line.begin = total * blockIdx.x / line.ctas;
     line.end = total * (blockIdx.x + 1) / line.ctas;
   }
-  long long* found = scratch + warps;  // sequence, its first step
-  long long from = before + upto - mine;
-  if (line.begin >= from && line.begin < from + mine) {
-    for (int b = b0; b < b1; ++b) {
-      const long long cost = head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
-      if (line.begin < from + cost) {
-        found[0] = b;
-        found[1] = from;
-        break;
-      }
-      from += cost;
-    }
+  return true;
+}
+
+// Cuts the line and finds where this CTA's piece begins.  All threads call; `scratch` holds threads / 32 + 2 long longs.  Up to 32
+// sequences a warp does it by itself; beyond, a thread's sequences are neighbours, so their sums are scanned once and only the
+// thread that holds the place looks closer.  False for a CTA without a piece (of all its threads).
+template <int ROWS>
+__device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cursor<ROWS>& at, long long* scratch) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const bool small = p.c.B <= 32;
+  const int threads = small ? 32 : static_cast<int>(blockDim.x), me = small ? lane : static_cast<int>(threadIdx.x);
+  const int per = (p.c.B + threads - 1) / threads;
+  const int b0 = me * per, b1 = min(b0 + per, p.c.B);
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
+  long long upto = mine;
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) {
+    const long long other = __shfl_up_sync(0xffffffffu, upto, m);
+    if (lane >= m) upto += other;
   }
-  __syncthreads();
-  at.b = static_cast<int>(found[0]);
-  long long left = line.begin - found[1];
+  long long found_at = 0;
+  if (small) {
+    if (!cut_line(p, line, __shfl_sync(0xffffffffu, upto, 31))) return false;
+    const unsigned here = __ballot_sync(0xffffffffu, line.begin >= upto - mine && line.begin < upto);
+    at.b = __ffs(here) - 1;
+    found_at = __shfl_sync(0xffffffffu, upto - mine, at.b);
+  } else {
+    if (lane == 31) scratch[warp] = upto;
+    __syncthreads();
+    long long total = 0, before = 0;
+    for (int w = 0; w < warps; ++w) {
+      if (w == warp) before = total;
+      total += scratch[w];
+    }
+    if (!cut_line(p, line, total)) return false;
+    long long* found = scratch + warps;  // sequence, its first step
+    long long from = before + upto - mine;
+    if (line.begin >= from && line.begin < from + mine) {
+      for (int b = b0; b < b1; ++b) {
+        const long long cost = head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
+        if (line.begin < from + cost) {
+          found[0] = b;
+          found[1] = from;
+          break;
+        }
+        from += cost;
+      }
+    }
+    __syncthreads();
+    at.b = static_cast<int>(found[0]);
+    found_at = found[1];
+  }
+  long long left = line.begin - found_at;
   at.enter_sequence(p);
   const long long per_head = head_steps<ROWS>(p, at.s);
-  at.h = total < 1 << 20 ? static_cast<int>(static_cast<uint32_t>(left) / static_cast<uint32_t>(per_head)) : static_cast<int>(left / per_head);
+  at.h = line.total < 1 << 20 ? static_cast<int>(static_cast<uint32_t>(left) / static_cast<uint32_t>(per_head)) : static_cast<int>(left / per_head);
   left -= at.h * per_head;
   at.tile = 0;
   at.enter_tile(p);
@@ -272,6 +290,10 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
   const WaitCtx ctx{abort_flag, p.status, kWaitLimitNs};
 
+  if (threadIdx.x == 0) {
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
   Line line;
   Cursor<kRows> now;
   const bool works = find_piece<kRows>(p, line, now, reinterpret_cast<long long*>(merge));

@@ -782,6 +782,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
     if (tid == 0 && atomicCAS(p.status, 0, kBadSmemAlign) == 0) p.status[1] = static_cast<int>(blockIdx.x);
     return;
   }
+  if (tid == 0) {
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
   Line line;
   Cursor<kTileRows> cur;
   if (!find_piece<kTileRows>(p, line, cur, reinterpret_cast<long long*>(smem))) return;

@@ -113,7 +113,7 @@ size_t cached_workspace(int ctas, int rows) {
 constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 // In a packed batch with long sequences, single tokens and what else fits 8 rows go to the decoding kernel first (a step of 24
 // sequences, 21 of them single tokens: 343 us all in tiles of 256 rows, 290 so; 4 us where there are none; 16 rows of two
-// tokens stay, 16 sequences of 16 to 32 rows take 88 us together and 112 apart).
+// tokens stay, 16 sequences of 16 to 32 rows take 88 us together and 112 apart; nor is it worth a launch where none has over 64).
 int short_rows(int group) { return group > 8 && group <= 16 ? group : 8; }
 
 // Rows of a query tile for the longest sequence's (token, head of a group) rows.  Decoding, 16 sequences of 12000 tokens, 8 key heads,
@@ -249,7 +249,8 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   uintptr_t at = place_parts(&p, reinterpret_cast<uintptr_t>(workspace), sms, rows);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   CUtensorMap tm_k, tm_v;
-  const bool many = rows == attn::kv::kTileRows, split = many && cache->starts != nullptr && cache->B > 1;
+  const bool many = rows == attn::kv::kTileRows;
+  const bool split = many && cache->starts != nullptr && cache->B > 1 && p.group * static_cast<long long>(max_new) > 64;
   if (!many || split) {
     if (!make_page_map(&tm_k, cache, 0, 16, CU_TENSOR_MAP_SWIZZLE_128B) || !make_page_map(&tm_v, cache, 1, 16, CU_TENSOR_MAP_SWIZZLE_128B))
       return ATTN_ERR_CUDA;
