@@ -7,8 +7,10 @@ is missing or fails to load, importing a symbol here raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
+import struct
 from typing import NamedTuple
 
 import torch
@@ -34,6 +36,7 @@ EXPORTED_SYMBOLS = ("attn_fwd", "attn_fwd_strided", "attn_fwd_host", "attn_fwd_n
 
 _lib = None
 _BF16 = torch.bfloat16
+_F32, _I32 = torch.float32, torch.int32
 _LL3 = ctypes.c_longlong * 3
 
 
@@ -113,7 +116,7 @@ def load_library() -> ctypes.CDLL:
     lib.attn_qk_norm_rope_bwd.restype = ci
     lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = []
     lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
-    cache = ctypes.POINTER(_KvCacheStruct)
+    cache = vp  # attn_kv_cache_t: bytes, or a reference to a _KvCacheStruct
     lib.attn_kv_append.argtypes = [cache, vp, vp, ci, ll3, ll3, vp]
     lib.attn_kv_append.restype = ci
     lib.attn_kv_read.argtypes = [cache, vp, vp, ci, ll3, ll3, vp]
@@ -647,14 +650,12 @@ def new_kv_cache(n_pages: int, page_size: int, n_kv_heads: int, dtype=torch.floa
     return KVCache(k, v, k_scale, v_scale)
 
 
-def _page_strides(t):
-    """Byte strides of the (page, slot, head) axes of a [pages, page_size, Hkv, D] tensor of 8-bit codes as a C array."""
-    n, page, heads, D = t.shape
-    a, b, c, _ = t.stride()
-    return _LL3(page * heads * D if n == 1 else a, b, D if heads == 1 else c)
+# attn_kv_cache_t as bytes, which takes less time than filling a ctypes.Structure
+_pack_cache = struct.Struct("7Q6qq7i4x").pack
 
 
-def _kv_cache_struct(cache, block_table, seq_lens, starts):
+def _refuse_cache(cache, block_table, seq_lens, starts):
+    """Names what is not as ``_kv_cache`` needs it."""
     k, v, k_scale, v_scale = cache
     dev, kind, shape = k.device, k.dtype, k.shape
     if dev.type != "cuda" or kind not in _KV_TYPES or len(shape) != 4 or v.shape != shape or v.dtype is not kind \
@@ -662,32 +663,57 @@ def _kv_cache_struct(cache, block_table, seq_lens, starts):
         raise ValueError("a cache's k and v must be cuda tensors [pages, page_size, Hkv, D] of one shape, float8_e4m3fn or int8, "
                          "with a contiguous last axis")
     scales = (shape[0], shape[2])
-    if not (k_scale.dtype is torch.float32 and v_scale.dtype is torch.float32 and k_scale.shape == scales and v_scale.shape == scales
-            and k_scale.is_contiguous() and v_scale.is_contiguous() and k_scale.device == dev and v_scale.device == dev):
-        raise ValueError("a cache's scales must be contiguous float32 tensors [pages, Hkv] on its device")
+    for t in (k_scale, v_scale):
+        if t.dtype is not torch.float32 or t.shape != scales or not t.is_contiguous() or t.device != dev:
+            raise ValueError("a cache's scales must be contiguous float32 tensors [pages, Hkv] on its device")
     if block_table.dtype is not torch.int32 or block_table.dim() != 2 or block_table.device != dev \
             or (block_table.stride(1) != 1 and block_table.shape[1] > 1):
         raise ValueError("block_table must be an int32 tensor [B, blocks] on the cache's device with a contiguous last axis")
-    B, blocks = block_table.shape
+    B = block_table.shape[0]
     if seq_lens.dtype is not torch.int32 or seq_lens.shape != (B,) or not seq_lens.is_contiguous() or seq_lens.device != dev:
         raise ValueError("seq_lens must be a contiguous int32 tensor [B] on the cache's device")
-    if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (B + 1,) or not starts.is_contiguous()
-                               or starts.device != dev):
-        raise ValueError("starts must be a contiguous int32 tensor [B + 1] on the cache's device")
-    return _KvCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
-                          seq_lens.data_ptr(), None if starts is None else starts.data_ptr(), _page_strides(k), _page_strides(v),
-                          block_table.stride(0) if B > 1 else blocks, _KV_TYPES[kind], shape[0], shape[1], shape[2], shape[3], B, blocks)
+    raise ValueError("starts must be a contiguous int32 tensor [B + 1] on the cache's device")
 
 
-def _cached_rows(c, starts, heads, dev, *named):
+def _kv_cache(cache, block_table, seq_lens, starts):
+    """Checks a cache and the sequences of a call: (attn_kv_cache_t as bytes, device index, Hkv, D, B)."""
+    k, v, k_scale, v_scale = cache
+    kind, shape, dev = k.dtype, k.shape, k.get_device()
+    # one expression for the usual call: these checks are a good part of its time
+    if not (dev >= 0 and kind in _KV_TYPES and len(shape) == 4 and v.dtype is kind and v.shape == shape and v.get_device() == dev
+            and block_table.dtype is _I32 and seq_lens.dtype is _I32 and block_table.dim() == 2
+            and block_table.get_device() == dev and seq_lens.get_device() == dev
+            and k_scale.dtype is _F32 and v_scale.dtype is _F32 and k_scale.get_device() == dev and v_scale.get_device() == dev
+            and k_scale.is_contiguous() and v_scale.is_contiguous() and seq_lens.is_contiguous()):
+        _refuse_cache(cache, block_table, seq_lens, starts)
+    n, page, heads, D = shape
+    a, b, c, d = k.stride()
+    e, f, g, h = v.stride()
+    B, blocks = block_table.shape
+    row, one = block_table.stride()
+    scales = (n, heads)
+    if not (d == 1 and h == 1 and (one == 1 or blocks <= 1) and seq_lens.shape == (B,) and k_scale.shape == scales and v_scale.shape == scales
+            and (starts is None or starts.dtype is _I32 and starts.shape == (B + 1,) and starts.is_contiguous()
+                 and starts.get_device() == dev)):
+        _refuse_cache(cache, block_table, seq_lens, starts)
+    if n == 1:  # an axis of extent 1 is never stepped along; torch may report anything there
+        a = e = page * heads * D
+    if heads == 1:
+        c = g = D
+    return (_pack_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                        0 if starts is None else starts.data_ptr(), a, b, c, e, f, g, row if B > 1 else blocks, _KV_TYPES[kind], n, page,
+                        heads, D, B, blocks), dev, heads, D, B)
+
+
+def _cached_rows(D, B, starts, heads, dev, *named):
     """Checks tensors of the call's rows, [B, S, heads, D] or [S, heads, D] with ``starts``; their S."""
     shape = named[0][1].shape
-    if len(shape) != (4 if starts is None else 3) or shape[-1] != c.D or (starts is None and shape[0] != c.B) \
+    if len(shape) != (4 if starts is None else 3) or shape[-1] != D or (starts is None and shape[0] != B) \
             or (heads is not None and shape[-2] != heads):
         raise ValueError(f"{named[0][0]} must be [B, S, heads, D], or [rows, heads, D] with starts, of the cache's D, and keys "
                          "and values of its heads")
     for name, t in named:
-        if t.dtype is not _BF16 or t.shape != shape or t.device != dev or t.stride(-1) != 1:
+        if t.dtype is not _BF16 or t.shape != shape or t.get_device() != dev or t.stride(-1) != 1:
             raise ValueError(f"{name} must be a bfloat16 tensor {list(shape)} with a contiguous last axis on the cache's device")
     return shape[-3]
 
@@ -699,17 +725,24 @@ def _row_strides(t):
     return _strides3(t if t.dim() == 4 else t[None])
 
 
-def _kv_rows_status(name, cache, k, v, block_table, seq_lens, starts, stream):
-    c = _kv_cache_struct(cache, block_table, seq_lens, starts)
-    dev = cache.k.device
-    S = _cached_rows(c, starts, c.Hkv, dev, ("k", k), ("v", v))
-    return _on_device(dev, getattr(load_library(), name), ctypes.byref(c), k.data_ptr(), v.data_ptr(), S, _row_strides(k), _row_strides(v),
-                      _raw_stream(dev, stream))
+def _on_index(dev, fn, *args):
+    """``_on_device`` for a device index."""
+    if torch.cuda.current_device() == dev:
+        return fn(*args)
+    with torch.cuda.device(dev):
+        return fn(*args)
+
+
+def _kv_rows_status(fn, cache, k, v, block_table, seq_lens, starts, stream):
+    c, dev, heads, D, B = _kv_cache(cache, block_table, seq_lens, starts)
+    S = _cached_rows(D, B, starts, heads, dev, ("k", k), ("v", v))
+    return _on_index(dev, fn, c, k.data_ptr(), v.data_ptr(), S, _row_strides(k), _row_strides(v),
+                     torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream)
 
 
 def attn_kv_append_status(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> int:
     """Calls ``attn_kv_append`` on CUDA tensors and returns its raw status code."""
-    return _kv_rows_status("attn_kv_append", cache, k, v, block_table, seq_lens, starts, stream)
+    return _kv_rows_status(load_library().attn_kv_append, cache, k, v, block_table, seq_lens, starts, stream)
 
 
 def attn_kv_append(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> None:
@@ -723,7 +756,7 @@ def attn_kv_append(cache, k, v, block_table, seq_lens, starts=None, stream=None)
 
 def attn_kv_read_status(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> int:
     """Calls ``attn_kv_read`` on CUDA tensors and returns its raw status code."""
-    return _kv_rows_status("attn_kv_read", cache, k, v, block_table, seq_lens, starts, stream)
+    return _kv_rows_status(load_library().attn_kv_read, cache, k, v, block_table, seq_lens, starts, stream)
 
 
 def attn_kv_read(cache, k, v, block_table, seq_lens, starts=None, stream=None) -> None:
@@ -733,31 +766,35 @@ def attn_kv_read(cache, k, v, block_table, seq_lens, starts=None, stream=None) -
         raise AttnError(st, "attn_kv_read")
 
 
+@functools.lru_cache(maxsize=256)
 def attn_fwd_cached_workspace_bytes(Hq: int, Hkv: int, max_new: int) -> int:
     return int(load_library().attn_fwd_cached_workspace_bytes(Hq, Hkv, max_new))
+
+
+def _cached_status(q, cache, o, lse, block_table, seq_lens, starts, max_new, causal, scale, workspace, stream, made_here=False):
+    """``made_here``: o and lse are new tensors of the right kind."""
+    c, dev, heads, D, B = _kv_cache(cache, block_table, seq_lens, starts)
+    S = _cached_rows(D, B, starts, None, dev, ("q", q)) if made_here else _cached_rows(D, B, starts, None, dev, ("q", q), ("o", o))
+    Hq = q.shape[-2]
+    if lse is not None and not made_here and (lse.dtype is not _F32 or not lse.is_contiguous() or lse.get_device() != dev
+                                              or lse.shape != ((B, Hq, S) if starts is None else (Hq, S))):
+        raise ValueError("lse must be a contiguous float32 tensor [B, Hq, S], or [Hq, rows] with starts, on the cache's device")
+    max_new = S if max_new is None else int(max_new)
+    if workspace is None:
+        workspace = _new_workspace(q, max(attn_fwd_cached_workspace_bytes(Hq, heads, max_new), 16), stream)
+    elif not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    return _on_index(dev, load_library().attn_fwd_cached, c, q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), Hq, S,
+                     max_new, 1 if causal else 0, 1.0 / math.sqrt(D) if scale is None else float(scale), _row_strides(q),
+                     None if made_here else _row_strides(o), workspace.data_ptr(), workspace.nbytes,
+                     torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream)
 
 
 def attn_fwd_cached_status(q, cache, o, lse, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale=None,
                            workspace=None, stream=None) -> int:
     """Calls ``attn_fwd_cached`` on CUDA tensors and returns its raw status code.  ``workspace`` is a contiguous cuda tensor
     (allocated here when None)."""
-    c = _kv_cache_struct(cache, block_table, seq_lens, starts)
-    dev = cache.k.device
-    S = _cached_rows(c, starts, None, dev, ("q", q), ("o", o))
-    Hq = q.shape[-2]
-    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.device != dev
-                            or lse.shape != ((c.B, Hq, S) if starts is None else (Hq, S))):
-        raise ValueError("lse must be a contiguous float32 tensor [B, Hq, S], or [Hq, rows] with starts, on the cache's device")
-    max_new = S if max_new is None else int(max_new)
-    lib = load_library()
-    if workspace is None:
-        workspace = _new_workspace(q, max(lib.attn_fwd_cached_workspace_bytes(Hq, c.Hkv, max_new), 16), stream)
-    elif not workspace.is_contiguous() or workspace.device != dev:
-        raise ValueError("workspace must be a contiguous tensor on the cache's device")
-    return _on_device(dev, lib.attn_fwd_cached, ctypes.byref(c), q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), Hq, S,
-                      max_new, 1 if causal else 0,
-                      float(scale) if scale is not None else 1.0 / math.sqrt(c.D), _row_strides(q), _row_strides(o),
-                      workspace.data_ptr(), workspace.nbytes, _raw_stream(dev, stream))
+    return _cached_status(q, cache, o, lse, block_table, seq_lens, starts, max_new, causal, scale, workspace, stream)
 
 
 def attn_fwd_cached(q, cache, o, lse, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale=None, workspace=None,
@@ -888,7 +925,9 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, po
 
 def kv_cache_append(cache, k, v, block_table, seq_lens, starts=None) -> None:
     """Puts new tokens' keys and values into a paged 8-bit cache (see ``attn_kv_append``)."""
-    attn_kv_append(cache, k, v, block_table, seq_lens, starts)
+    st = _kv_rows_status(load_library().attn_kv_append, cache, k, v, block_table, seq_lens, starts, None)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_kv_append")
 
 
 def kv_cache_read(cache, block_table, seq_lens, starts=None, n: int | None = None):
@@ -898,8 +937,11 @@ def kv_cache_read(cache, block_table, seq_lens, starts=None, n: int | None = Non
         raise ValueError("n, the number of rows, must be given and positive")
     heads, D = cache.k.shape[2:]
     shape = (n, heads, D) if starts is not None else (block_table.shape[0], n, heads, D)
-    k, v = (torch.empty(shape, dtype=_BF16, device=cache.k.device) for _ in range(2))
-    attn_kv_read(cache, k, v, block_table, seq_lens, starts)
+    k = cache.k.new_empty(shape, dtype=_BF16)
+    v = torch.empty_like(k)
+    st = _kv_rows_status(load_library().attn_kv_read, cache, k, v, block_table, seq_lens, starts, None)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_kv_read")
     return k, v
 
 
@@ -909,8 +951,9 @@ def attention_cached(q, cache, block_table, seq_lens, starts=None, max_new=None,
     tokens of each sequence, whose keys and values are in the cache already (``kv_cache_append``)."""
     o = _new_like(q)
     lse = None
-    if return_lse:
-        shape = (q.shape[1], q.shape[0]) if starts is not None else (q.shape[0], q.shape[2], q.shape[1])
-        lse = torch.empty(shape, dtype=torch.float32, device=q.device)
-    attn_fwd_cached(q, cache, o, lse, block_table, seq_lens, starts, max_new, causal, scale)
+    if return_lse and q.dim() >= 3:
+        lse = q.new_empty((q.shape[1], q.shape[0]) if starts is not None else (q.shape[0], q.shape[2], q.shape[1]), dtype=_F32)
+    st = _cached_status(q, cache, o, lse, block_table, seq_lens, starts, max_new, causal, scale, None, None, True)
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_fwd_cached")
     return (o, lse) if return_lse else o

@@ -108,6 +108,10 @@ def test_binding_refusals():
 def test_struct_matches_the_header():
     # four pointers, three pointers, 2 x 3 strides, one stride, seven ints
     assert ctypes.sizeof(binding._KvCacheStruct) == 7 * 8 + 6 * 8 + 8 + 7 * 4 + 4
+    # the packed form is the same bytes
+    values = list(range(1, 22))
+    c = binding._KvCacheStruct(*values[:7], (ctypes.c_longlong * 3)(*values[7:10]), (ctypes.c_longlong * 3)(*values[10:13]), *values[13:])
+    assert bytes(c)[:140] == binding._pack_cache(*values)[:140] and len(binding._pack_cache(*values)) == ctypes.sizeof(c)
 
 
 def test_oracle_codes_are_the_types_own():
