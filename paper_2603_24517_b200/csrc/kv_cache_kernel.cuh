@@ -170,7 +170,7 @@ struct RowStrides {
 
 // Grid: (units, 2 Hkv), one CTA of page / 16 warps each.
 template <int TYPE>
-__global__ void __launch_bounds__(256) kv_append_kernel(const CacheView c, const uint16_t* __restrict__ k_rows,
+__global__ void __launch_bounds__(256, 3) kv_append_kernel(const CacheView c, const uint16_t* __restrict__ k_rows,
                                                         const uint16_t* __restrict__ v_rows, const RowStrides ks,
                                                         const RowStrides vs) {
   __shared__ float warp_max[8];
@@ -188,26 +188,27 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const CacheView c, const
   const long long first = max(slot0, static_cast<long long>(max(begin, 0)));
   const long long last = min(slot0 + (1 << c.page_log2), static_cast<long long>(begin) + n);
   if (first >= last) return;
-  const int page = page_of(c, b, static_cast<int>(min(block, 0x7fffffffll)));
-  if (page < 0) return;
   const int lo = static_cast<int>(first - slot0), hi = static_cast<int>(last - slot0);  // slots written: [lo, hi)
 
+  // the rows are on their way while the page is looked up
   const RowStrides st = t ? vs : ks;
   const uint16_t* rows = (t ? v_rows : k_rows) + (c.starts == nullptr ? b * st.b : 0ll) + h * st.h +
                          (row0 + slot0 - begin) * st.s + (lane & 15) * 8;
-  uint8_t* codes = c.codes[t] + page * c.sp[t] + h * c.sh[t] + (lane & 15) * 8;
-  float* scale_at = c.scales[t] + static_cast<long long>(page) * c.Hkv + h;
-  const bool holds = lo > 0;
-  const float before = holds ? *scale_at : 0.f;
-
   uint4 x[8];
   float largest = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int slot = warp * kSlotsPerWarp + 2 * i + (lane >> 4);
     x[i] = make_uint4(0, 0, 0, 0);
-    if (slot >= lo && slot < hi) x[i] = __ldg(reinterpret_cast<const uint4*>(rows + slot * st.s));
+    if (slot >= lo && slot < hi) x[i] = __ldcs(reinterpret_cast<const uint4*>(rows + slot * st.s));
   }
+  const int page = page_of(c, b, static_cast<int>(min(block, 0x7fffffffll)));
+  if (page < 0) return;
+  uint8_t* codes = c.codes[t] + page * c.sp[t] + h * c.sh[t] + (lane & 15) * 8;
+  float* scale_at = c.scales[t] + static_cast<long long>(page) * c.Hkv + h;
+  const bool holds = lo > 0;
+  const float before = holds ? *scale_at : 0.f;
+
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
