@@ -521,7 +521,8 @@ typedef struct {
  * attn_kv_append -- quantises the keys and values of new tokens into their pages.  With A the largest finite magnitude of the
  * new values of a page and head:
  *
- *     E4M3: s = the smallest power of two with A <= 448 s;   INT8: s = A / 127;   s = 0 where A = 0, else at least 2^-100
+ *     E4M3: s = the smallest power of two with A <= 448 s;   INT8: s = A r, r the FP32 number next to 1 / 127 (FP32 product);
+ *     s = 0 where A = 0, else at least 2^-100
  *     s = max(s, the page's scale) if the page holds earlier tokens of the sequence
  *     code = x / s rounded to nearest even, and where s grew, the codes of the page's earlier slots = round(code s_old / s)
  *

@@ -14,7 +14,7 @@ def scale_for(largest: float, int8: bool) -> float:
     if largest == 0.0:
         return 0.0
     if int8:
-        s = float(torch.tensor(largest, dtype=torch.float32) / torch.tensor(127.0, dtype=torch.float32))
+        s = float(torch.tensor(largest, dtype=torch.float32) * (torch.tensor(1.0, dtype=torch.float32) / torch.tensor(127.0, dtype=torch.float32)))
         return max(s, 2.0 ** -100)
     s = 2.0 ** -100
     while largest > 448.0 * s:

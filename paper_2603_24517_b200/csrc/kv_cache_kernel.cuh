@@ -3,7 +3,7 @@
 // Position p of sequence b is slot p % page of page table[b][p / page].  A page and head has one scale s for its keys and one
 // for its values; a code c stands for c s.  With A the largest finite magnitude among the new values of a page and head,
 //
-//     E4M3:  s = the smallest power of two with A <= 448 s       INT8:  s = A / 127       (0 where A = 0)
+//     E4M3:  s = the smallest power of two with A <= 448 s       INT8:  s = A (1 / 127)   (0 where A = 0)
 //     s <- max(s, the page's scale), if the page holds earlier tokens;  c = round(x / s), ties to even
 //
 // and where s grew, the codes the page already holds become round(c s_old / s).  A power of two moves E4M3 codes to a
@@ -128,7 +128,7 @@ __device__ __forceinline__ float scale_for(float a) {
     const int e = static_cast<int>((__float_as_uint(a) + 0x1fffffu) >> 23) - 127 - 8;
     s = e < -100 ? kMinScale : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
   } else {
-    s = __fdiv_rn(a, 127.f);
+    s = __fmul_rn(a, 1.f / 127.f);  // the product defines the scale, not the quotient
   }
   return fmaxf(s, kMinScale);
 }
