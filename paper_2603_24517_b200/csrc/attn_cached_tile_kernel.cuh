@@ -34,13 +34,13 @@ constexpr int kTSmemKv = 2 * kTileBytes;
 constexpr int kTSmemRaw = kTSmemKv + kKvSlots * kTileBytes;      // codes of one K and one V tile
 constexpr int kTSmemStats = kTSmemRaw + 2 * kTile * kKvDim;      // float [2 stages][2][128]
 constexpr int kMetaSteps = 4;
-constexpr int kMetaFloats = 28;
+constexpr int kMetaFloats = 27;
 constexpr int kItemSlots = 5;      // the fetching warp looks two steps (items) ahead of the codes it requests, results follow one behind
 constexpr int kItemInts = 11;
 constexpr int kTSmemMeta = kTSmemStats + 2 * 2 * kTile * 4;
 constexpr int kTSmemItems = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
 constexpr int kTSmemBars = (kTSmemItems + kItemSlots * kItemInts * 4 + 7) / 8 * 8;
-constexpr int kTNumBars = 2 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemSlots;
+constexpr int kTNumBars = 4 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemSlots;
 constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
 constexpr int kTSmemBytes = kTSmemMisc + 16;
 static_assert(kTSmemBytes <= 232448, "shared memory budget of one CTA");
@@ -52,6 +52,7 @@ enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaBad = 2
 constexpr float kMinRatioLog2 = -60.f;  // V scales below 2^-60 of the largest count as that: nothing in f16
 
 struct TileBarriers {
+  uint64_t* q_raw;     // [2] bulk copies: the stage's rows of q as they are -> softmax
   uint64_t* q_full;    // [2] softmax (4 warps): the stage's Q is in shared memory -> MMA
   uint64_t* raw_full;  // [2] TMA: the codes of the keys, of the values -> converters
   uint64_t* raw_empty; // [2] converters (2 warps) -> fetching warp
@@ -424,6 +425,13 @@ __device__ __forceinline__ void role_tile_mma(const TileBarriers& bars, uint8_t*
   }
 }
 
+// An untiled copy of `bytes` (a multiple of 16, both addresses too) to shared memory, counted on `bar`.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
 // ---- softmax: one thread owns one row of stage `s` ------------------------------------------------------------------------
 template <int GRAN>
 __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const TileBarriers& bars, uint8_t* smem, WaitCtx ctx,
@@ -458,41 +466,45 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         key0 = (it.t_first + first) * kStepKeys;
         seen = limit > key0;
         idle = !__any_sync(0xffffffffu, w.real);
-        // half a warp brings a row, 16 bytes a lane, as it is, and then turns what it has brought into f16 in place
-        const long long mine = w.real ? row_offset(p, p.sq, it.b, it.s, w) : -1;
-        uint8_t* dst = smem + kTSmemQ + s * kTileBytes + ((lane & 15) >> 3) * kHalfBytes + ((row & ~31) + (lane >> 4)) * 128;
-        const uint32_t dst32 = smem_u32(dst);
+        // The row as it is, in two copies to where its two halves will stand; then the thread reads all of it, each lane beginning
+        // at another 16 bytes, and writes it back as f16 in the swizzled order (128 bytes of a row are its own either way)
+        uint8_t* mine = smem + kTSmemQ + s * kTileBytes + row * 128;
+        const int rows = __popc(__ballot_sync(0xffffffffu, w.real));
+        if (lane == 0) mbar_arrive_expect_tx(&bars.q_raw[s], rows * kKvDim * 2);
+        __syncwarp();
+        if (w.real) {
+          const uint16_t* src = p.q + row_offset(p, p.sq, it.b, it.s, w);
+          bulk_load(mine, src, 128, &bars.q_raw[s]);
+          bulk_load(mine + kHalfBytes, src + 64, 128, &bars.q_raw[s]);
+        }
+        bool ok = mbar_wait(&bars.q_raw[s], l_cnt & 1, ctx, kRoleSoftmax | kBarQFull);
+        if (!__all_sync(0xffffffffu, ok)) return;
+        uint4 x[16];
+        float largest = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const long long from = __shfl_sync(0xffffffffu, mine, 2 * i + (lane >> 4));
-          const uint32_t at = i * 256 + (((lane & 7) ^ ((2 * i + (lane >> 4)) & 7)) << 4);
-          cp_async16(dst32 + at, p.q + (from >= 0 ? from : 0) + (lane & 15) * 8, from >= 0);
-        }
-        cp_async_wait_all();
-        float my_up = 1.f;
-#pragma unroll 4
-        for (int i = 0; i < 16; ++i) {
-          uint4* at = reinterpret_cast<uint4*>(dst + i * 256 + (((lane & 7) ^ ((2 * i + (lane >> 4)) & 7)) << 4));
-          const uint4 x = *at;
-          const uint32_t words[4] = {x.x, x.y, x.z, x.w};
-          float largest = 0.f;
+          const int c = (i + lane) & 15;
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (w.real) x[i] = *reinterpret_cast<const uint4*>(mine + (c >> 3) * kHalfBytes + ((c & 7) << 4));
+          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const float2 f = unpack_bf16x2(words[m]);
             largest = max3(largest, fabsf(f.x), fabsf(f.y));
           }
+        }
+        const float my_up = row_factor(largest);
 #pragma unroll
-          for (int m = 8; m > 0; m >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, m));
-          const float up = row_factor(largest);
+        for (int i = 0; i < 16; ++i) {
+          const int c = (i + lane) & 15;
+          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
           uint32_t y[4];
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const float2 f = unpack_bf16x2(words[m]);
-            y[m] = pack_f16x2(f.x * up, f.y * up);
+            y[m] = pack_f16x2(f.x * my_up, f.y * my_up);
           }
-          *at = make_uint4(y[0], y[1], y[2], y[3]);
-          const float ups = __shfl_sync(0xffffffffu, up, (lane & 1) << 4);
-          if (lane >> 1 == i) my_up = ups;
+          *reinterpret_cast<uint4*>(mine + (c >> 3) * kHalfBytes + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
         }
         factor = p.scale_log2 / my_up;
         fence_proxy_async_smem();
@@ -757,7 +769,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bar_mem = reinterpret_cast<uint64_t*>(smem + kTSmemBars);
   TileBarriers bars;
-  bars.q_full = bar_mem;
+  bars.q_raw = bar_mem;
+  bars.q_full = bars.q_raw + 2;
   bars.raw_full = bars.q_full + 2;
   bars.raw_empty = bars.raw_full + 2;
   bars.kv_full = bars.raw_empty + 2;
@@ -791,6 +804,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   if (!find_piece<kTileRows>(p, line, cur, reinterpret_cast<long long*>(smem))) return;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.q_raw[i], 4);
       mbar_init(&bars.q_full[i], 4);
       mbar_init(&bars.raw_full[i], 1);
       mbar_init(&bars.raw_empty[i], kConvWarps);
