@@ -40,7 +40,7 @@ constexpr int kItemInts = 11;
 constexpr int kTSmemMeta = kTSmemStats + 2 * 2 * kTile * 4;
 constexpr int kTSmemItems = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
 constexpr int kTSmemBars = (kTSmemItems + kItemSlots * kItemInts * 4 + 7) / 8 * 8;
-constexpr int kTNumBars = 4 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemSlots;
+constexpr int kTNumBars = 2 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemSlots;
 constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
 constexpr int kTSmemBytes = kTSmemMisc + 16;
 static_assert(kTSmemBytes <= 232448, "shared memory budget of one CTA");
@@ -52,7 +52,6 @@ enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaBad = 2
 constexpr float kMinRatioLog2 = -60.f;  // V scales below 2^-60 of the largest count as that: nothing in f16
 
 struct TileBarriers {
-  uint64_t* q_raw;     // [2] bulk copies: the stage's rows of q as they are -> softmax
   uint64_t* q_full;    // [2] softmax (4 warps): the stage's Q is in shared memory -> MMA
   uint64_t* raw_full;  // [2] TMA: the codes of the keys, of the values -> converters
   uint64_t* raw_empty; // [2] converters (2 warps) -> fetching warp
@@ -425,12 +424,11 @@ __device__ __forceinline__ void role_tile_mma(const TileBarriers& bars, uint8_t*
   }
 }
 
-// An untiled copy of `bytes` (a multiple of 16, both addresses too) to shared memory, counted on `bar`.
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-               "l"(src), "r"(bytes), "r"(smem_u32(bar))
-               : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool take) {
+  const int bytes = take ? 16 : 0;  // 0: zeros are written, nothing is read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // ---- softmax: one thread owns one row of stage `s` ------------------------------------------------------------------------
 template <int GRAN>
@@ -466,27 +464,28 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
         key0 = (it.t_first + first) * kStepKeys;
         seen = limit > key0;
         idle = !__any_sync(0xffffffffu, w.real);
-        // The row as it is, in two copies to where its two halves will stand; then the thread reads all of it, each lane beginning
-        // at another 16 bytes, and writes it back as f16 in the swizzled order (128 bytes of a row are its own either way)
-        uint8_t* mine = smem + kTSmemQ + s * kTileBytes + row * 128;
-        const int rows = __popc(__ballot_sync(0xffffffffu, w.real));
-        if (lane == 0) mbar_arrive_expect_tx(&bars.q_raw[s], rows * kKvDim * 2);
-        __syncwarp();
-        if (w.real) {
-          const uint16_t* src = p.q + row_offset(p, p.sq, it.b, it.s, w);
-          bulk_load(mine, src, 128, &bars.q_raw[s]);
-          bulk_load(mine + kHalfBytes, src + 64, 128, &bars.q_raw[s]);
+        // This code runs once an item, so it is never in the instruction cache: short loops take a fifth of the time that the same
+        // work takes unrolled.  Half a warp brings a row, 16 bytes a lane, to its place in the swizzled order; then each
+        // thread reads its own row, every lane beginning at another 16 bytes, and turns it into f16 in place
+        const long long at = w.real ? row_offset(p, p.sq, it.b, it.s, w) : -1;
+        uint8_t* tile = smem + kTSmemQ + s * kTileBytes + (row & ~31) * 128;
+        {
+          const uint32_t dst = smem_u32(tile) + ((lane & 15) >> 3) * kHalfBytes;
+          const uint16_t* q = p.q + (lane & 15) * 8;
+#pragma unroll 2
+          for (int r = lane >> 4; r < 32; r += 2) {
+            const long long from = __shfl_sync(0xffffffffu, at, r);
+            cp_async16(dst + r * 128 + (((lane & 7) ^ (r & 7)) << 4), q + max(from, 0ll), from >= 0);
+          }
+          cp_async_wait_all();
+          __syncwarp();
         }
-        bool ok = mbar_wait(&bars.q_raw[s], l_cnt & 1, ctx, kRoleSoftmax | kBarQFull);
-        if (!__all_sync(0xffffffffu, ok)) return;
-        uint4 x[16];
+        uint8_t* mine = tile + lane * 128;
         float largest = 0.f;
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < 16; ++i) {
-          const int c = (i + lane) & 15;
-          x[i] = make_uint4(0, 0, 0, 0);
-          if (w.real) x[i] = *reinterpret_cast<const uint4*>(mine + (c >> 3) * kHalfBytes + ((c & 7) << 4));
-          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          const uint4 x = *reinterpret_cast<const uint4*>(mine + (i >> 3) * kHalfBytes + (((i + lane) & 7) << 4));
+          const uint32_t words[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const float2 f = unpack_bf16x2(words[m]);
@@ -494,17 +493,18 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
           }
         }
         const float my_up = row_factor(largest);
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < 16; ++i) {
-          const int c = (i + lane) & 15;
-          const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          uint4* place = reinterpret_cast<uint4*>(mine + (i >> 3) * kHalfBytes + (((i + lane) & 7) << 4));
+          const uint4 x = *place;
+          const uint32_t words[4] = {x.x, x.y, x.z, x.w};
           uint32_t y[4];
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const float2 f = unpack_bf16x2(words[m]);
             y[m] = pack_f16x2(f.x * my_up, f.y * my_up);
           }
-          *reinterpret_cast<uint4*>(mine + (c >> 3) * kHalfBytes + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *place = make_uint4(y[0], y[1], y[2], y[3]);
         }
         factor = p.scale_log2 / my_up;
         fence_proxy_async_smem();
@@ -769,8 +769,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bar_mem = reinterpret_cast<uint64_t*>(smem + kTSmemBars);
   TileBarriers bars;
-  bars.q_raw = bar_mem;
-  bars.q_full = bars.q_raw + 2;
+  bars.q_full = bar_mem;
   bars.raw_full = bars.q_full + 2;
   bars.raw_empty = bars.raw_full + 2;
   bars.kv_full = bars.raw_empty + 2;
@@ -804,7 +803,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
   if (!find_piece<kTileRows>(p, line, cur, reinterpret_cast<long long*>(smem))) return;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars.q_raw[i], 4);
       mbar_init(&bars.q_full[i], 4);
       mbar_init(&bars.raw_full[i], 1);
       mbar_init(&bars.raw_empty[i], kConvWarps);
