@@ -88,17 +88,26 @@ __device__ __forceinline__ int steps_of(const SeqWork& s, int i, int causal) {
   return max((visible(s, i, causal) + kStepKeys - 1) / kStepKeys, 1);
 }
 
+template <int ROWS>
+__device__ __forceinline__ int tile_steps(const CachedParams& p, const SeqWork& s, int tile) {
+  return steps_of(s, min((tile * ROWS + ROWS - 1) / p.group, s.n - 1), p.causal);
+}
+template <int ROWS>
+__device__ __forceinline__ int tiles_of(const CachedParams& p, const SeqWork& s) {
+  return (s.n * p.group + ROWS - 1) / ROWS;
+}
+
 // A place on the line of work.
 template <int ROWS>
 struct Cursor {
   int b, h, tile, t, steps, tiles;
   SeqWork s;
   __device__ __forceinline__ void enter_tile(const CachedParams& p) {
-    steps = steps_of(s, min((tile * ROWS + ROWS - 1) / p.group, s.n - 1), p.causal);
+    steps = tile_steps<ROWS>(p, s, tile);
   }
   __device__ __forceinline__ void enter_sequence(const CachedParams& p) {
     s = seq_work(p, b);
-    tiles = (s.n * p.group + ROWS - 1) / ROWS;
+    tiles = tiles_of<ROWS>(p, s);
   }
   __device__ __forceinline__ void next_tile(const CachedParams& p) {  // of the head, then the next head, the next sequence
     t = 0;
@@ -119,12 +128,57 @@ struct Cursor {
 // Steps of one head of a sequence.
 template <int ROWS>
 __device__ __forceinline__ long long head_steps(const CachedParams& p, const SeqWork& s) {
-  const int tiles = (s.n * p.group + ROWS - 1) / ROWS;
+  const int tiles = tiles_of<ROWS>(p, s);
   if (tiles == 0) return 0;
   if (!p.causal) return static_cast<long long>(tiles) * steps_of(s, s.n - 1, 0);
   long long sum = 0;
-  for (int k = 0; k < tiles; ++k) sum += steps_of(s, min((k * ROWS + ROWS - 1) / p.group, s.n - 1), 1);
+  for (int k = 0; k < tiles; ++k) sum += tile_steps<ROWS>(p, s, k);
   return sum;
+}
+// The same by a whole warp (one sequence in all lanes): 8192 tokens of four heads are 128 tiles, 10 us for one lane.
+template <int ROWS>
+__device__ __forceinline__ long long head_steps_warp(const CachedParams& p, const SeqWork& s, int lane) {
+  const int tiles = tiles_of<ROWS>(p, s);
+  if (!p.causal || tiles <= 1) return head_steps<ROWS>(p, s);
+  long long sum = 0;
+  for (int k = lane; k < tiles; k += 32) sum += tile_steps<ROWS>(p, s, k);
+#pragma unroll
+  for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+  return sum;
+}
+// Which tile holds step `left` of a head, and the step within it.
+template <int ROWS>
+__device__ __forceinline__ void find_tile(const CachedParams& p, const SeqWork& s, long long left, int lane, int& tile, int& t) {
+  if (!p.causal) {  // tiles of equal length
+    const int steps = steps_of(s, s.n - 1, 0);
+    tile = static_cast<int>(left / steps);
+    t = static_cast<int>(left - static_cast<long long>(tile) * steps);
+    return;
+  }
+  if (ROWS <= 16) {  // decoding: a tile or two
+    tile = 0;
+    for (int n = tile_steps<ROWS>(p, s, 0); left >= n; n = tile_steps<ROWS>(p, s, ++tile)) left -= n;
+    t = static_cast<int>(left);
+    return;
+  }
+  const int tiles = tiles_of<ROWS>(p, s);
+  for (int k0 = 0;; k0 += 32) {
+    const int mine = k0 + lane < tiles ? tile_steps<ROWS>(p, s, k0 + lane) : 0;
+    long long upto = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const long long other = __shfl_up_sync(0xffffffffu, upto, m);
+      if (lane >= m) upto += other;
+    }
+    const unsigned beyond = __ballot_sync(0xffffffffu, left < upto);
+    if (beyond != 0 || k0 + 32 >= tiles) {
+      const int src = beyond != 0 ? __ffs(beyond) - 1 : 31;
+      tile = k0 + src;
+      t = static_cast<int>(left - __shfl_sync(0xffffffffu, upto - mine, src));
+      return;
+    }
+    left -= __shfl_sync(0xffffffffu, upto, 31);
+  }
 }
 
 // The line of work as one CTA sees it.
@@ -162,7 +216,26 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   const int per = (p.c.B + threads - 1) / threads;
   const int b0 = me * per, b1 = min(b0 + per, p.c.B);
   long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
+  if (small && ROWS > 16) {
+    // lane b has sequence b; those of many tiles are counted by the whole warp, one after another
+    SeqWork s;
+    s.n = s.row0 = s.len = s.keys = 0;
+    if (lane < p.c.B) s = seq_work(p, lane);
+    const bool many = p.causal && tiles_of<ROWS>(p, s) > 8;
+    if (!many) mine = head_steps<ROWS>(p, s) * p.c.Hkv;
+    for (unsigned left = __ballot_sync(0xffffffffu, many); left != 0; left &= left - 1) {
+      const int src = __ffs(left) - 1;
+      SeqWork x;
+      x.row0 = 0;
+      x.n = __shfl_sync(0xffffffffu, s.n, src);
+      x.len = __shfl_sync(0xffffffffu, s.len, src);
+      x.keys = __shfl_sync(0xffffffffu, s.keys, src);
+      const long long sum = head_steps_warp<ROWS>(p, x, lane) * p.c.Hkv;
+      if (lane == src) mine = sum;
+    }
+  } else {
+    for (int b = b0; b < b1; ++b) mine += head_steps<ROWS>(p, seq_work(p, b)) * p.c.Hkv;
+  }
   long long upto = mine;
 #pragma unroll
   for (int m = 1; m < 32; m <<= 1) {
@@ -203,22 +276,11 @@ __device__ __forceinline__ bool find_piece(const CachedParams& p, Line& line, Cu
   }
   long long left = line.begin - found_at;
   at.enter_sequence(p);
-  const long long per_head = head_steps<ROWS>(p, at.s);
+  const long long per_head = ROWS > 16 ? head_steps_warp<ROWS>(p, at.s, lane) : head_steps<ROWS>(p, at.s);
   at.h = line.total < 1 << 20 ? static_cast<int>(static_cast<uint32_t>(left) / static_cast<uint32_t>(per_head)) : static_cast<int>(left / per_head);
   left -= at.h * per_head;
-  at.tile = 0;
+  find_tile<ROWS>(p, at.s, left, lane, at.tile, at.t);
   at.enter_tile(p);
-  if (!p.causal) {  // tiles of equal length
-    at.tile = static_cast<int>(left / at.steps);
-    left -= static_cast<long long>(at.tile) * at.steps;
-  } else {
-    while (left >= at.steps) {
-      left -= at.steps;
-      ++at.tile;
-      at.enter_tile(p);
-    }
-  }
-  at.t = static_cast<int>(left);
   return true;
 }
 // The launch behind this one may start to take its place on the SMs; it waits for this one's results itself.
