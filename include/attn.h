@@ -528,6 +528,7 @@ typedef struct {
  *
  * A page whose slot 0 is written starts afresh: its old scale and codes do not count.  Infinities saturate; NaN becomes the
  * E4M3 NaN, or 0 in INT8.  (A value within 2^-4 of 2^128 may round to that, and is read back as infinity.)  Appending E4M3 to pages filled elsewhere needs their scales to be powers of two.
+ *   S          rows a sequence, or rows in all with starts
  *   k, v       BF16 [B, S, Hkv, D], or [S, Hkv, D] with starts (read); strides {batch, sequence, head} in elements as in
  *              attn_fwd_strided (the batch stride is not used with starts); NULL: contiguous
  * Rows at positions < 0 (seq_lens < n) or without a page are dropped.  The same call on the same cache gives the same bits, once
@@ -540,7 +541,7 @@ attn_status_t attn_kv_append(const attn_kv_cache_t* cache, const void* k, const 
 
 /*
  * attn_kv_read -- the last tokens of each sequence back in BF16: code * scale, rounded once (written; shapes and strides as in
- * attn_kv_append).  Rows at positions < 0 are zeros, rows without a page NaN.  Otherwise as attn_kv_append.
+ * attn_kv_append; rows must not overlap).  Rows at positions < 0 are zeros, rows without a page NaN.  Otherwise as attn_kv_append.
  */
 attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S, const long long* k_strides,
                            const long long* v_strides, void* stream);
@@ -552,7 +553,8 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
  *   q          BF16 [B, S, Hq, D], or [S, Hq, D] with starts (read); Hq % Hkv == 0
  *   o          BF16 like q (written); must not overlap q or the cache
  *   lse        FP32 [B, Hq, S], or [Hq, S] with starts; may be NULL (written)
- *   max_new    at least 1: about how many rows the longest sequence has; chooses the kernel, not the result's meaning
+ *   max_new    at least 1: about how many rows the longest sequence has.  It chooses the kernels (and the workspace): any value
+ *              gives the same attention, a wrong one costs time
  *   causal     non-zero: a row at position p sees the keys 0 .. p; 0: all of its sequence's keys
  *   scale, strides  as in attn_fwd_strided (NULL: contiguous)
  *   workspace  device memory, 16-byte aligned, attn_fwd_cached_workspace_bytes(Hq, Hkv, max_new) bytes; contents undefined
@@ -562,7 +564,9 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
  * Scores and sums accumulate in fp32; queries and codes enter the products exactly (but query values 2^22 times smaller than
  * the row's largest), weights with 11 bits; o is rounded once.  Values whose V scale is 2^-20 of the largest V scale of the
  * sequence, or less, lose bits.  Sums have a fixed order: the same call gives the same bits on the same kind of GPU.
- * Asynchronous on `stream`, no state; calls that may overlap, replays of one captured call too, need workspaces of their own.
+ * Asynchronous on `stream`, no state, 2 launches (4 where a packed batch has long sequences: its single tokens take a kernel of their
+ * own); calls that may overlap, replays of one captured call too, need workspaces of their own.  After a first call on the device
+ * calls can be captured; block_table, seq_lens and starts are read at each replay.
  * Errors: as attn_kv_append, ATTN_ERR_SHAPE also for head counts and max_new, ATTN_ERR_TOO_LARGE for a small workspace.
  */
 size_t attn_fwd_cached_workspace_bytes(int Hq, int Hkv, int max_new); /* 0: arguments attn_fwd_cached refuses */

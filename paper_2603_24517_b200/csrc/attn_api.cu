@@ -902,7 +902,7 @@ const char* attn_status_str(attn_status_t status) {
   return "ATTN_ERR_UNKNOWN";
 }
 
-int attn_version(void) { return 200; }
+int attn_version(void) { return 300; }
 
 namespace {
 

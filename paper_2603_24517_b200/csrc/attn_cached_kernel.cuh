@@ -18,6 +18,11 @@
 // Codes are exact in f16; queries are scaled by a power of two of their row, weights are held as 2^6 exp(s - m) with a maximum
 // that may lag by a factor of 2^8 (so it is reduced over the lanes only when one of them meets a larger score), which leaves
 // f16 its 11 bits of both; V's scale enters as its ratio to the largest one met so far.
+//
+// 64 sequences of up to 8192 tokens (32 / 8 heads, E4M3, 744 MB): 135 us, 5.5 TB/s, 86 % of the copy rate; INT8 codes take 10 %
+// longer.  One token on 512: 9.9 us, all latency (lengths, pages, codes, merge, join).  What a lone warp of a scheduler could not
+// hide bounded the first form (8 warps an SM, 217 us).  Measured slower: tiles of 16 rows at two CTAs an SM (186 us for 16
+// sequences where one CTA takes 112: spills), of 32 rows (213), the merge in loops (9.9 against 9.5 us for the short one).
 #pragma once
 
 #include "attn_fwd_kernel.cuh"
@@ -33,7 +38,8 @@ constexpr int kWarpStageBytes = 2 * 16 * kKvDim;       // K then V
 constexpr float kWeightShift = 6.f;   // weights are held as 2^kWeightShift exp(s - m)
 constexpr float kWeightLag = 8.f;     // log2 units the reference maximum may lag
 
-// Query tiles of 8 NB rows.  8 rows: two CTAs an SM, so that one's start and end run beside the other's steps.
+// Query tiles of 8 NB rows.  8 rows: two CTAs an SM, so that one's start and end run beside the other's steps; 16 rows need
+// 233 registers.
 template <int NB>
 struct Dec {
   static constexpr int kRows = 8 * NB;
