@@ -479,3 +479,46 @@ def test_long_and_short_sequences_in_one_batch(group, page, kind, causal):
     lse = torch.full((2 * group, q.shape[0]), 7.0, device="cuda")
     lib.attn_fwd_cached(q, b.cache, o, lse, b.table, b.lens, b.starts, max_new=300, causal=causal)
     check(b, q, o, lse, causal)
+
+
+def test_many_sequences_on_shared_pages():
+    """4096 sequences of 32768 tokens, all on the same 512 pages (a table whose rows are one): a million steps of work, where the cut
+    needs 64 bits, and more sequences than a warp counts."""
+    b = Batch([(1, 32768)], 1, 64, E4M3, seed=20, spare=0)
+    B = 4096
+    q = (rand(b.g, 4, 8, 128)).bfloat16().repeat(B // 4, 1, 1)[:, None].contiguous()
+    o, lse = lib.attention_cached(q, b.cache, b.table.expand(B, -1), b.lens.expand(B).contiguous())
+    one = Batch.__new__(Batch)
+    one.seqs, one.rows, one.page, one.heads, one.cache, one.ids = [(1, 32768)] * 4, [0, 1, 2, 3, 4], 64, 1, b.cache, b.ids * 4
+    for first in (0, 4, 2048, B - 4):
+        check(one, q[first:first + 4, 0], o[first:first + 4, 0], lse[first:first + 4, :, 0].T.contiguous())
+    # every sequence's result is within the bounds of the same numbers: of those that share a query, none differs by more than both
+    spread = (o.view(B // 4, 4, 8, 128).float().amax(0) - o.view(B // 4, 4, 8, 128).float().amin(0)).max()
+    assert float(spread) <= 2.0 ** -9 * float(b.values(1, 0).abs().max()) + 2.0 ** -6 * float(o.float().abs().max())
+
+
+@pytest.mark.parametrize("kind", [E4M3, INT8])
+def test_forty_long_sequences(kind):
+    """More sequences than a warp counts, in the kernel for many rows, keys and values in different orders in memory."""
+    seqs = [(30 + 7 * i, 200 + 31 * i) for i in range(40)]
+    b = Batch(seqs, 2, 32, kind, seed=21)
+    v = torch.zeros(b.n_pages, 32, 2, 128, dtype=kind, device="cuda")  # slot by slot, the keys head by head
+    v.view(torch.uint8).copy_(b.cache.v.view(torch.uint8))
+    b.cache = lib.KVCache(b.cache.k, v, *b.cache[2:])
+    q = b.queries(6)
+    o, lse = lib.attention_cached(q, b.cache, b.table, b.lens, b.starts, max_new=max(n for n, _ in seqs))
+    check(b, q, o, lse)
+    small, _ = lib.attention_cached(q, b.cache, b.table, b.lens, b.starts, max_new=3)
+    check(b, q, small, None)
+
+
+def test_outputs_that_start_at_16_bytes():
+    """Rows of o at odd multiples of 16 bytes, in the kernel that writes 32 at a time."""
+    b = Batch([(200, 500)], 2, 64, E4M3, seed=22)
+    q = b.queries(4)
+    wide = torch.full((200, 4, 136 * 2), 9.0, dtype=torch.bfloat16, device="cuda")
+    for at in (8, 16):
+        o = wide[:, :, at:at + 128]
+        lib.attn_fwd_cached(q, b.cache, o, None, b.table, b.lens, b.starts)
+        check(b, q, o, None)
+    assert bool((wide[:, :, :8] == 9).all()) and bool((wide[:, :, 144:] == 9).all())
