@@ -95,9 +95,11 @@ bool prepare_decode() {
                               attn::kv::Dec<NB>::kSmem) == cudaSuccess;
 }
 
-template <int TYPE, int GRAN>
+template <int GRAN>
 bool prepare_tile() {
-  return cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<TYPE, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::kTSmemBytes) == cudaSuccess &&
+         cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kInt8, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               attn::kv::kTSmemBytes) == cudaSuccess;
 }
 
@@ -150,8 +152,7 @@ DeviceState* device_state(attn_status_t* st) {
       cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       !prepare_decode<1>() || !prepare_decode<2>() ||
-      !prepare_tile<attn::kv::kE4m3, 16>() || !prepare_tile<attn::kv::kE4m3, 64>() ||
-      !prepare_tile<attn::kv::kInt8, 16>() || !prepare_tile<attn::kv::kInt8, 64>() ||
+      !prepare_tile<16>() || !prepare_tile<32>() || !prepare_tile<64>() ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||
       cudaMalloc(&d.status, 2 * sizeof(int)) != cudaSuccess ||
       cudaMemset(d.status, 0, 2 * sizeof(int)) != cudaSuccess ||

@@ -11,7 +11,7 @@
 //   warps 8-11,  converters: codes exactly to f16 in the swizzled ring of K / V tiles, zeros behind the last token; 8-11 also
 //         14-15  write O / l -> BF16 -> memory, or an fp32 part where the tile's keys are spread over CTAs
 //
-// Scales: 16 keys lie in one page, 64 where pages have 64 slots or more (GRAN, "a granule").  K's scale multiplies the row's
+// Scales: 16 keys lie in one page, 32 or 64 where pages have as many slots (GRAN, "a granule").  K's scale multiplies the row's
 // factor granule by granule, V's enters the exponent as log2 of its ratio to the largest V scale so far, and is taken out of the
 // row sum again granule by granule, so both products run on bare codes.  When the largest V scale grows, O is rescaled as for a
 // grown row maximum.

@@ -160,9 +160,14 @@ attn_status_t launch_decode(const CachedParams& p, const CUtensorMap& tm_k, cons
   return launch_join<D::kRows>(p, D::kRows, s);
 }
 
-template <int TYPE, int GRAN>
+// GRAN: keys that share their scales.  Three prompts of 700 rows on 4700 keys, pages of 32: 206 us by 16 keys, 195 by 32.
+template <int GRAN>
 attn_status_t launch_tile(const CachedParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
-  attn::kv::attn_cached_tile_kernel<TYPE, GRAN><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
+  if (p.c.type == ATTN_KV_E4M3) {
+    attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3, GRAN><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
+  } else {
+    attn::kv::attn_cached_tile_kernel<attn::kv::kInt8, GRAN><<<p.ctas, attn::kThreads, attn::kv::kTSmemBytes, s>>>(tm_k, tm_v, p);
+  }
   if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
   return launch_join<attn::kv::kTileRows>(p, attn::kv::kTileRows / (8 * attn::kv::kJoinRows), s);
 }
@@ -265,9 +270,9 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   if (!make_page_map(&tm_k, cache, 0, cache->page_size, CU_TENSOR_MAP_SWIZZLE_NONE) ||
       !make_page_map(&tm_v, cache, 1, cache->page_size, CU_TENSOR_MAP_SWIZZLE_NONE))
     return ATTN_ERR_CUDA;
-  const bool e4m3 = p.c.type == ATTN_KV_E4M3;
-  if (cache->page_size >= 64) return e4m3 ? launch_tile<attn::kv::kE4m3, 64>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 64>(p, tm_k, tm_v, s);
-  return e4m3 ? launch_tile<attn::kv::kE4m3, 16>(p, tm_k, tm_v, s) : launch_tile<attn::kv::kInt8, 16>(p, tm_k, tm_v, s);
+  if (cache->page_size == 16) return launch_tile<16>(p, tm_k, tm_v, s);
+  if (cache->page_size == 32) return launch_tile<32>(p, tm_k, tm_v, s);
+  return launch_tile<64>(p, tm_k, tm_v, s);
 }
 
 }  // extern "C"
