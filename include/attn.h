@@ -562,8 +562,9 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
  * A row that sees no key has o = 0 and lse = -infinity.  A row that sees a key whose page does not exist has o and lse NaN.
  * Slots behind a sequence's last token may hold anything; the codes and scales of its tokens, and q, must be finite.
  * Scores and sums accumulate in fp32; queries and codes enter the products exactly (but query values 2^22 times smaller than
- * the row's largest), weights with 11 bits; o is rounded once.  Values whose V scale is 2^-20 of the largest V scale of the
- * sequence, or less, lose bits.  Sums have a fixed order: the same call gives the same bits on the same kind of GPU.
+ * the row's largest); o is rounded once.  A key's weight times its V scale is rounded to 11 bits, or by 2^-30 of the largest such
+ * product among the keys that the row sees (where a V scale counts as 2^-64 of the sequence's largest one, and as 2^-84, at least).
+ * Sums have a fixed order: the same call gives the same bits on the same kind of GPU.
  * Asynchronous on `stream`, no state, 2 launches (4 where a packed batch has long sequences: its single tokens take a kernel of their
  * own); calls that may overlap, replays of one captured call too, need workspaces of their own.  After a first call on the device
  * calls can be captured; block_table, seq_lens and starts are read at each replay.

@@ -17,7 +17,7 @@
 // the reads of a 128-byte-swizzled stage meet no bank twice.
 // Codes are exact in f16; queries are scaled by a power of two of their row, weights are held as 2^6 exp(s - m) with a maximum
 // that may lag by a factor of 2^8 (so it is reduced over the lanes only when one of them meets a larger score), which leaves
-// f16 its 11 bits of both; V's scale enters as its ratio to the largest one met so far.
+// f16 its 11 bits of both; V's scale is part of the exponent (below).
 //
 // 64 sequences of up to 8192 tokens (32 / 8 heads, E4M3, 744 MB): 135 us, 5.5 TB/s, 86 % of the copy rate; INT8 codes take 10 %
 // longer.  One token on 512: 9.9 us, all latency (lengths, pages, codes, merge, join).  What a lone warp of a scheduler could not
@@ -37,6 +37,21 @@ constexpr int kStepKeys = 128;                         // keys a CTA takes in on
 constexpr int kWarpStageBytes = 2 * 16 * kKvDim;       // K then V
 constexpr float kWeightShift = 6.f;   // weights are held as 2^kWeightShift exp(s - m)
 constexpr float kWeightLag = 8.f;     // log2 units the reference maximum may lag
+
+// A key's weight in the product with the values is 2^(s_j + log2 vs_j - M): s_j the score in log2 units, vs_j the V scale of its page
+// and head, M a running maximum of s_j + log2 vs_j over the keys that the row sees, rounded up to an integer.  So the weights of
+// what counts most in the row's result have the full f16 precision whatever the scales are, nothing overflows for values near the
+// end of their range, and tokens that the row does not see have no part in it.  The row sum takes the scale out again,
+// l = sum_j 2^(s_j + log2 vs_j - M) / vs_j, and O / l needs no factor.  M is an integer, so that it costs no rounding in the exponents
+// and in the log-sum-exp.
+// Scales of 0 need a number: with R the largest log2 vs so far (at least kScaleLeast), log2 vs counts as R - kScaleZero at least, and as R -
+// kScaleSpan at least in the maximum.  A weight of such a page is then 2^(6 + 8 - 40) at most, which is 0 in f16, while its part of the row
+// sum stays a normal fp32 number.
+constexpr float kScaleLeast = -20.f;
+constexpr float kScaleSpan = 64.f;
+constexpr float kScaleZero = 104.f;
+static_assert(kScaleZero - kScaleSpan - kWeightShift - kWeightLag > 25.f, "weights of scale 0 vanish in f16");
+static_assert(kScaleZero - kScaleLeast < 126.f, "the inverse of the least scale is a normal number");
 
 // Query tiles of 8 NB rows.  8 rows: two CTAs an SM, so that one's start and end run beside the other's steps; 16 rows need
 // 233 registers.
@@ -330,6 +345,21 @@ __device__ __forceinline__ long long lse_index(const CachedParams& p, int b, con
                                : static_cast<long long>(w.head) * p.c.S + s.row0 + w.token;
 }
 
+// x 2^d; d may lie far outside the exponents of one factor.
+__device__ __forceinline__ float times_exp2(float x, float d) {
+  const float h = ex2_approx(0.5f * d);
+  return x * h * h;
+}
+// The row's log-sum-exp from its reference maximum (an integer) and its sum, 0 where it sees no key, NaN where a page was missing.  The
+// sum's exponent is added as an integer, so that the logarithm is one of a number in [1, 2).  Without branches: it runs once an item, so
+// its code is never in the instruction cache (0.6 us of the short single token's 10 with a branch for NaN).
+__device__ __forceinline__ float lse_of(float m, float l) {
+  const uint32_t bits = __float_as_uint(l);
+  const float k = static_cast<float>(static_cast<int>(bits >> 23) - 127);
+  const float z = (m - kWeightShift + k) + lg2_approx(__uint_as_float((bits & 0x7fffffu) | 0x3f800000u));
+  return l == 0.f ? -INFINITY : fmaf(l, 0.f, z * kLn2);
+}
+
 // Transpose of an 8 x 8 matrix of 16-bit numbers that lies over the warp, two a lane.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
@@ -467,7 +497,7 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
     // keys that all rows see: steps up to there need no mask
     const int clear = visible(now.s, min(row_first / p.group, now.s.n - 1), p.causal);
     float acc[NB][8][4];  // d = 16 spread(g) + 2 mt (values 0, 1) and + 1 (2, 3); rows 2 t4 (0, 2) and 2 t4 + 1 (1, 3)
-    float m[NB][2], l[NB][2], vref = 0.f;
+    float m[NB][2], l[NB][2], top_scale = kScaleLeast;  // log2 of the largest V scale
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
@@ -506,14 +536,18 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
             for (int nb = 0; nb < NB; ++nb) mma_f16(s[nb], a, qf[nb][half * 4 + i][0], qf[nb][half * 4 + i][1]);
           }
         }
+        const float lv0 = lg2_approx(v_scale);
+        top_scale = fmaxf(top_scale, lv0);
+        const float lv = fmaxf(lv0, top_scale - kScaleZero), extra = fmaxf(lv, top_scale - kScaleSpan) - lv;
+        const float v_inverse = ex2_approx(-lv), lag = kWeightLag - extra;
         bool grow = false;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const float f = factor[nb][e] * k_scale;
-            s[nb][e] *= f;
-            s[nb][2 + e] *= f;
+            s[nb][e] = fmaf(s[nb][e], f, lv);
+            s[nb][2 + e] = fmaf(s[nb][2 + e], f, lv);
             if (key0 + 16 > clear) {  // warp-uniform
               if (key0 + kr >= limit[nb][e]) s[nb][e] = -INFINITY;
               if (key0 + 8 + kr >= limit[nb][e]) s[nb][2 + e] = -INFINITY;
@@ -521,7 +555,7 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
             } else if (bad) {
               l[nb][e] = __int_as_float(0x7fffffff);
             }
-            grow = grow || fmaxf(s[nb][e], s[nb][2 + e]) > m[nb][e] + kWeightLag;
+            grow = grow || fmaxf(s[nb][e], s[nb][2 + e]) > m[nb][e] + lag;
           }
         }
         if (__any_sync(0xffffffffu, grow)) {
@@ -533,10 +567,11 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
               float top = fmaxf(s[nb][e], s[nb][2 + e]);
 #pragma unroll
               for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-              const float to = fmaxf(m[nb][e], top);
-              a[e] = m[nb][e] == -INFINITY ? 0.f : ex2_approx(m[nb][e] - to);
+              const float to = fmaxf(m[nb][e], ceilf(top + extra));
+              const float h = m[nb][e] == -INFINITY ? 0.f : ex2_approx(0.5f * (m[nb][e] - to));
+              a[e] = h * h;
               m[nb][e] = to;
-              l[nb][e] *= a[e];
+              l[nb][e] = l[nb][e] * h * h;
             }
 #pragma unroll
             for (int mt = 0; mt < 8; ++mt) {
@@ -547,19 +582,6 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
             }
           }
         }
-        if (v_scale > vref) {
-          const float a = __fdividef(vref, v_scale);
-          vref = v_scale;
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-            for (int mt = 0; mt < 8; ++mt) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[nb][mt][e] *= a;
-            }
-          }
-        }
-        const float ratio = vref > 0.f ? __fdividef(v_scale, vref) : 0.f;
         uint32_t pf[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -569,10 +591,10 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
             const float ref = m[nb][e] == -INFINITY ? 0.f : m[nb][e] - kWeightShift;
             x[e] = ex2_approx(s[nb][e] - ref);
             x[2 + e] = ex2_approx(s[nb][2 + e] - ref);
-            l[nb][e] += x[e] + x[2 + e];
+            l[nb][e] = fmaf(x[e] + x[2 + e], v_inverse, l[nb][e]);
           }
-          pf[nb][0] = transpose8x8(pack_f16x2(x[0] * ratio, x[1] * ratio));
-          pf[nb][1] = transpose8x8(pack_f16x2(x[2] * ratio, x[3] * ratio));
+          pf[nb][0] = transpose8x8(pack_f16x2(x[0], x[1]));
+          pf[nb][1] = transpose8x8(pack_f16x2(x[2], x[3]));
         }
         // V^T: inner indices 2 t4, 2 t4 + 1 are keys t4, t4 + 4, and 8 more those + 8; a lane takes d = 16 spread(g) .. + 15 of them
         uint4 w[4];
@@ -625,7 +647,7 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
         float to = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kDecWarps; ++w) to = fmaxf(to, row_stats[w * kRows + r].x);
-        const float a = m[nb][e] == -INFINITY ? 0.f : ex2_approx(m[nb][e] - to) * vref;
+        const float a = m[nb][e] == -INFINITY ? 0.f : ex2_approx(m[nb][e] - to);
         float4* row = reinterpret_cast<float4*>(merge) + (warp * kRows + r) * (kKvDim / 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -640,15 +662,17 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
       const int r = 8 * nb + warp;
       const TilePlace w = tile_place(p, now.s, now.h, row_first + r);
       if (!w.real) break;
-      float to = -INFINITY;
+      // lane i has warp i % 8's maximum and sum
+      const float2 mine = row_stats[(lane & 7) * kRows + r];
+      float to = mine.x;
 #pragma unroll
-      for (int i = 0; i < kDecWarps; ++i) to = fmaxf(to, row_stats[i * kRows + r].x);
-      float sum = 0.f;
+      for (int x = 1; x < kDecWarps; x <<= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, x));
+      float sum = mine.x == -INFINITY ? mine.y : times_exp2(mine.y, mine.x - to);
+#pragma unroll
+      for (int x = 1; x < kDecWarps; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < kDecWarps; ++i) {
-        const float2 ml = row_stats[i * kRows + r];
-        sum += ml.x == -INFINITY ? ml.y : ml.y * ex2_approx(ml.x - to);
         const float4 x = reinterpret_cast<const float4*>(merge)[(i * kRows + r) * (kKvDim / 4) + (lane ^ ((r >> 1 & 3) | (lane >> 4) << 2))];
         o.x += x.x;
         o.y += x.y;
@@ -662,7 +686,7 @@ attn_cached_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
         *reinterpret_cast<uint2*>(p.o + row_offset(p, p.so, now.b, now.s, w) + lane * 4) =
             make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
         if (lane == 0 && p.lse != nullptr)
-          p.lse[lse_index(p, now.b, now.s, w)] = sum == 0.f ? -INFINITY : (to - kWeightShift + log2f(sum)) * kLn2;
+          p.lse[lse_index(p, now.b, now.s, w)] = lse_of(to, sum);
       } else {  // slot 2 i: a tile begun by an earlier CTA; 2 i + 1: one begun here
         const long long slot = 2ll * blockIdx.x + (t_first == 0 ? 1 : 0);
         reinterpret_cast<float4*>(p.parts + (slot * kRows + r) * kKvDim)[lane] = o;
@@ -699,9 +723,10 @@ struct JoinSum {
 };
 __device__ __forceinline__ void join_part(JoinSum& j, const float2 ml, const float4 x) {
   const float to = fmaxf(j.m, ml.x);
-  const float a = j.m == -INFINITY ? 0.f : ex2_approx(j.m - to), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - to);
+  const float g = j.m == -INFINITY ? 0.f : ex2_approx(0.5f * (j.m - to)), h = ml.x == -INFINITY ? 0.f : ex2_approx(0.5f * (ml.x - to));
+  const float a = g * g, f = h * h;
   // a part that has seen no key has the sum 0, or NaN where a page was missing
-  j.l = j.l * (j.m == -INFINITY ? 1.f : a) + ml.y * (ml.x == -INFINITY ? 1.f : f);
+  j.l = (j.m == -INFINITY ? j.l : j.l * g * g) + (ml.x == -INFINITY ? ml.y : ml.y * h * h);
   j.m = to;
   j.o.x = j.o.x * a + x.x * f;
   j.o.y = j.o.y * a + x.y * f;
@@ -713,7 +738,7 @@ __device__ __forceinline__ void join_write(const CachedParams& p, const JoinSum&
   *reinterpret_cast<uint2*>(p.o + row_offset(p, p.so, b, s, w) + lane * 4) =
       make_uint2(pack_bf16x2(j.o.x * inv, j.o.y * inv), pack_bf16x2(j.o.z * inv, j.o.w * inv));
   if (lane == 0 && p.lse != nullptr)
-    p.lse[lse_index(p, b, s, w)] = j.l == 0.f ? -INFINITY : (j.m - kWeightShift + log2f(j.l)) * kLn2;
+    p.lse[lse_index(p, b, s, w)] = lse_of(j.m, j.l);
 }
 
 template <int ROWS>

@@ -12,9 +12,8 @@
 //         14-15  write O / l -> BF16 -> memory, or an fp32 part where the tile's keys are spread over CTAs
 //
 // Scales: 16 keys lie in one page, 32 or 64 where pages have as many slots (GRAN, "a granule").  K's scale multiplies the row's
-// factor granule by granule, V's enters the exponent as log2 of its ratio to the largest V scale so far, and is taken out of the
-// row sum again granule by granule, so both products run on bare codes.  When the largest V scale grows, O is rescaled as for a
-// grown row maximum.
+// factor granule by granule, V's enters the exponent as its log2 and is taken out of the row sum again granule by granule, so both
+// products run on bare codes.
 //
 // Work: the line of (sequence, key head, tile pair, 128 keys) steps cut into equal pieces, as in the decoding kernel.  A tile whose
 // rows fit one stage takes its keys on both stages in turn and joins the two results.
@@ -50,14 +49,13 @@ constexpr int kTSmemItems = kTSmemMeta + kMetaSteps * kMetaFloats * 4;
 constexpr int kTSmemBars = (kTSmemItems + kItemSlots * kItemInts * 4 + 7) / 8 * 8;
 constexpr int kTNumBars = 2 + 4 + 2 * kKvSlots + 2 * 7 + kMetaSteps + 2 * kItemSlots;
 constexpr int kTSmemMisc = kTSmemBars + kTNumBars * 8;
-constexpr int kTSmemBytes = kTSmemMisc + 16;
+constexpr int kTSmemBytes = kTSmemMisc + 8;
 static_assert(kTSmemBytes <= 232448, "shared memory budget of one CTA");
 static_assert(kTSmemBars % 8 == 0 && kTSmemMeta % 16 == 0 && kTSmemStats % 16 == 0 && kTSmemMisc % 8 == 0, "alignment");
 static_assert(kHeadDim == kKvDim && kTile == kStepKeys, "one head dimension, one tile");
 
 // What the converters tell the softmax warps about a step.
-enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaVref = 24, kMetaBad = 25, kMetaValid = 26 };
-constexpr float kMinRatioLog2 = -60.f;  // V scales below 2^-60 of the largest count as that: nothing in f16
+enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaFloor = 24, kMetaBad = 25, kMetaValid = 26 };
 
 struct TileBarriers {
   uint64_t* q_full;    // [2] softmax (4 warps): the stage's Q is in shared memory -> MMA
@@ -200,19 +198,19 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
   };
   StepPlace now = look_up(), next = look_up();
   float scale_now = scale_of(now);
-  float vref = 0.f;
+  float top_scale = kScaleLeast;  // log2 of the largest V scale of the item so far
   const bool asks = lane < 8 && ((lane * 16) & ((1 << c.page_log2) - 1)) == 0;  // one lane a page
   const uint32_t steps = static_cast<uint32_t>(line.end - line.begin);
   for (uint32_t i = 0; i < steps; ++i) {
     const StepPlace after = look_up();
     if (!ok) return;
     const float scale_next = scale_of(next);
-    float top = lane >= 8 && lane < 16 ? scale_now : 0.f;
+    const float lv = lg2_approx(scale_now);
+    float top = lane >= 8 && lane < 16 ? lv : kScaleLeast;
 #pragma unroll
     for (int m = 4; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
     top = __shfl_sync(0xffffffffu, top, 8);
-    if (now.first) vref = 0.f;
-    const float ref = fmaxf(fmaxf(vref, top), 1e-30f);
+    top_scale = fmaxf(now.first ? kScaleLeast : top_scale, top);
     const unsigned bad = __ballot_sync(0xffffffffu, lane < 8 && now.page == -1);
     float* meta = reinterpret_cast<float*>(smem + kTSmemMeta) + (i % kMetaSteps) * kMetaFloats;
 #pragma unroll 1
@@ -224,11 +222,11 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
         if (lane < 8) {
           meta[kMetaK + lane] = scale_now;
         } else if (lane < 16) {
-          const float ratio = now.page >= 0 ? fmaxf(lg2_approx(__fdividef(scale_now, ref)), kMinRatioLog2) : 0.f;
-          meta[kMetaV + lane - 8] = ratio;
-          meta[kMetaInv + lane - 8] = ex2_approx(-ratio);
+          const float counts = now.page >= 0 ? fmaxf(lv, top_scale - kScaleZero) : top_scale;
+          meta[kMetaV + lane - 8] = counts;
+          meta[kMetaInv + lane - 8] = ex2_approx(-counts);
         } else if (lane == 16) {
-          meta[kMetaVref] = ref;
+          meta[kMetaFloor] = top_scale - kScaleSpan;
           reinterpret_cast<int*>(meta)[kMetaBad] = bad != 0 ? (__ffs(bad) - 1) * 16 : kStepKeys;
           reinterpret_cast<int*>(meta)[kMetaValid] = now.keys - now.key0;
         }
@@ -242,7 +240,6 @@ __device__ __forceinline__ void role_fetch(const CachedParams& p, const TileBarr
                     now.h, now.page >= 0 ? now.page : c.n_pages);
       __syncwarp();
     }
-    vref = ref;
     now = next;
     next = after;
     scale_now = scale_next;
@@ -521,8 +518,8 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
       }
     }
     if (used) {
-      float m_used = -INFINITY;  // reference maximum, log2 units
-      float l = 0.f, vref = 0.f;
+      float m_used = -INFINITY;  // reference maximum, log2 units, an integer
+      float l = 0.f;
       for (int j = first; j < n; j += stride, key0 += stride * kStepKeys) {
         if (idle) {
           bool ok = mbar_wait(&bars.s_full[s], s_cnt & 1, ctx, kRoleSoftmax | kBarSFull);
@@ -560,6 +557,7 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
           }
         }
         float m_blk = -INFINITY;
+        const float floor = meta[kMetaFloor];
 #pragma unroll
         for (int g = 0; g < kTile / GRAN; ++g) {
           float top[4];
@@ -571,20 +569,18 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
             for (int k = 3; k + 1 < GRAN / 4; k += 2) top[c] = max3(top[c], X(i + k), X(i + k + 1));
             top[c] = fmaxf(top[c], X(i + GRAN / 4 - 1));
           }
-          m_blk = fmaxf(m_blk, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * cg[g]);
+          m_blk = fmaxf(m_blk, fmaf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), cg[g], fmaxf(meta[kMetaV + g * (GRAN / 16)], floor)));
         }
-        const float v_grow = vref == meta[kMetaVref] ? 1.f : __fdividef(vref, meta[kMetaVref]);
-        vref = meta[kMetaVref];
         if (j == first) {
-          m_used = m_blk == -INFINITY ? 0.f : m_blk;
+          m_used = m_blk == -INFINITY ? 0.f : ceilf(m_blk);
         } else {
-          const float m_new = fmaxf(m_used, m_blk);
-          if (__any_sync(0xffffffffu, m_new - m_used > kWeightLag || v_grow != 1.f)) {
+          if (__any_sync(0xffffffffu, m_blk - m_used > kWeightLag)) {
             // P V of the step before has completed (S of this one was issued after it): O is quiescent
-            const float alpha = ex2_approx(m_used - m_new);
+            const float m_new = fmaxf(m_used, ceilf(m_blk));
+            const float f = ex2_approx(m_used - m_new);
+            l *= f > 0.f ? f : 0x1p-126f;
+            if (f == 0.f) l *= ex2_approx(m_used - m_new + 126.f);  // scales far apart: what is nothing beside O may be most of the row sum
             m_used = m_new;
-            l *= alpha;
-            const float f = alpha * v_grow;
 #pragma unroll
             for (int cc = 0; cc < 8; ++cc) {
               uint32_t o[16];
@@ -641,7 +637,6 @@ __device__ __forceinline__ void role_tile_softmax(const CachedParams& p, const T
       // a row that has seen no key here has the sum 0 by definition, and no maximum
       stats[row] = seen ? l : 0.f;
       stats[kTile + row] = seen ? m_used : -INFINITY;
-      if (row == 0) reinterpret_cast<float*>(smem + kTSmemMisc)[2 + s] = vref;
       mbar_arrive(&bars.l_full[s]);
       ++l_cnt;
     }
@@ -679,7 +674,6 @@ __device__ __forceinline__ bool write_item(const CachedParams& p, const TileBarr
         if (!__all_sync(0xffffffffu, ok)) return false;
         lq[q] = stats[row];
         mq[q] = stats[kTile + row];
-        f[q] = reinterpret_cast<const float*>(smem + kTSmemMisc)[2 + s + q];
         mbar_arrive(&bars.l_empty[s + q]);
         m = fmaxf(m, mq[q]);
       }
@@ -689,9 +683,9 @@ __device__ __forceinline__ bool write_item(const CachedParams& p, const TileBarr
         const bool ok = mbar_wait(&bars.o_full[s + q], cnt[s + q] & 1, ctx, kRoleEpilogue | kBarOFull);
         if (!__all_sync(0xffffffffu, ok)) return false;
         ++cnt[s + q];
-        const float a = mq[q] == -INFINITY ? 0.f : ex2_approx(mq[q] - m);
-        l += mq[q] == -INFINITY ? lq[q] : lq[q] * a;  // the sum of a row that has seen no key is 0
-        f[q] *= a;
+        const float h = mq[q] == -INFINITY ? 0.f : ex2_approx(0.5f * (mq[q] - m));
+        l += mq[q] == -INFINITY ? lq[q] : lq[q] * h * h;  // the sum of a row that has seen no key is 0
+        f[q] = h * h;
       }
     }
     tc_fence_after_sync();
@@ -739,7 +733,7 @@ __device__ __forceinline__ bool write_item(const CachedParams& p, const TileBarr
     }
     if (it.whole) {
       if (w.real && p.lse != nullptr)
-        p.lse[lse_index(p, it.b, it.s, w)] = l == 0.f ? -INFINITY : (m - kWeightShift + lg2_approx(l)) * kLn2;
+        p.lse[lse_index(p, it.b, it.s, w)] = lse_of(m, l);
     } else {
       reinterpret_cast<float2*>(p.parts + 2ll * p.ctas * kTileRows * kKvDim)[slot * kTileRows + r] = make_float2(m, l);
       if (r == 0 && it.t_first == 0) {
