@@ -565,8 +565,8 @@ attn_status_t attn_kv_read(const attn_kv_cache_t* cache, void* k, void* v, int S
  * the row's largest); o is rounded once.  A key's weight times its V scale is rounded to 11 bits, or by 2^-30 of the largest such
  * product among the keys that the row sees (where a V scale counts as 2^-64 of the sequence's largest one, and as 2^-84, at least).
  * Sums have a fixed order: the same call gives the same bits on the same kind of GPU.
- * Asynchronous on `stream`, no state, 2 launches (4 where a packed batch has long sequences: its single tokens take a kernel of their
- * own); calls that may overlap, replays of one captured call too, need workspaces of their own.  After a first call on the device
+ * Asynchronous on `stream`, no state, 2 launches (4 where a packed batch has long sequences and Hq / Hkv is at most 16: its single tokens
+ * take a kernel of their own); calls that may overlap, replays of one captured call too, need workspaces of their own.  After a first call on the device
  * calls can be captured; block_table, seq_lens and starts are read at each replay.
  * Errors: as attn_kv_append, ATTN_ERR_SHAPE also for head counts and max_new, ATTN_ERR_TOO_LARGE for a small workspace.
  */

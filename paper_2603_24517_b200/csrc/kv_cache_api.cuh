@@ -114,7 +114,9 @@ constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 // In a packed batch with long sequences, single tokens and what else fits 8 rows go to the decoding kernel first (a step of 24
 // sequences, 21 of them single tokens: 343 us all in tiles of 256 rows, 290 so; 4 us where there are none; 16 rows of two
 // tokens stay, 16 sequences of 16 to 32 rows take 88 us together and 112 apart; nor is it worth a launch where none has over 64).
-int short_rows(int group) { return group > 8 && group <= 16 ? group : 8; }
+// More than 16 heads a key head: a single token has too many rows itself, so nothing is split off (16 sequences, groups of 32: 60.0 us
+// with the launches for nothing in front, 54.6 without).
+int short_rows(int group) { return group <= 8 ? 8 : group <= 16 ? group : 0; }
 
 // Rows of a query tile for the longest sequence's (token, head of a group) rows.  Decoding, 16 sequences of 12000 tokens, 8 key heads,
 // E4M3: 8 rows 77 us in tiles of 8, 110 of 16; 16 rows 133 and 113; 32 rows 208 in tiles of 16, 176 of 256.
@@ -215,7 +217,7 @@ size_t attn_fwd_cached_workspace_bytes(int Hq, int Hkv, int max_new) {
   if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_new <= 0) return 0;
   const int rows = tile_rows(Hq, Hkv, max_new);
   const size_t bytes = cached_workspace(cached_ctas(kWorkspaceSms, rows), rows);
-  return rows == attn::kv::kTileRows ? bytes + cached_workspace(cached_ctas(kWorkspaceSms, 8), 8) : bytes;
+  return rows == attn::kv::kTileRows && short_rows(Hq / Hkv) > 0 ? bytes + cached_workspace(cached_ctas(kWorkspaceSms, 8), 8) : bytes;
 }
 
 attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
@@ -255,7 +257,7 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   CUtensorMap tm_k, tm_v;
   const bool many = rows == attn::kv::kTileRows;
-  const bool split = many && cache->starts != nullptr && cache->B > 1 && p.group * static_cast<long long>(max_new) > 64;
+  const bool split = many && cache->starts != nullptr && cache->B > 1 && p.group * static_cast<long long>(max_new) > 64 && short_rows(p.group) > 0;
   if (!many || split) {
     if (!make_page_map(&tm_k, cache, 0, 16, CU_TENSOR_MAP_SWIZZLE_128B) || !make_page_map(&tm_v, cache, 1, 16, CU_TENSOR_MAP_SWIZZLE_128B))
       return ATTN_ERR_CUDA;
