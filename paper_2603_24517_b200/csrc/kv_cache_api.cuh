@@ -114,9 +114,12 @@ constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 // In a packed batch with long sequences, single tokens and what else fits 8 rows go to the decoding kernel first (a step of 24
 // sequences, 21 of them single tokens: 343 us all in tiles of 256 rows, 290 so; 4 us where there are none; 16 rows of two
 // tokens stay, 16 sequences of 16 to 32 rows take 88 us together and 112 apart; nor is it worth a launch where none has over 64).
+// Tokens of 9 to 16 rows take tiles of 16, which read their keys once (64 sequences, groups of 16: 314 us in tiles of 8, 305 of 16; 48
+// sequences, groups of 12: 652 and 637; all in tiles of 256 rows 339 and 736, but 24 sequences of 2 key heads 176 where these take 192).
 // More than 16 heads a key head: a single token has too many rows itself, so nothing is split off (16 sequences, groups of 32: 60.0 us
 // with the launches for nothing in front, 54.6 without).
 int short_rows(int group) { return group <= 8 ? 8 : group <= 16 ? group : 0; }
+int short_tile(int group) { return group <= 8 ? 8 : 16; }
 
 // Rows of a query tile for the longest sequence's (token, head of a group) rows.  Decoding, 16 sequences of 12000 tokens, 8 key heads,
 // E4M3: 8 rows 77 us in tiles of 8, 110 of 16; 16 rows 133 and 113; 32 rows 208 in tiles of 16, 176 of 256.
@@ -217,7 +220,9 @@ size_t attn_fwd_cached_workspace_bytes(int Hq, int Hkv, int max_new) {
   if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_new <= 0) return 0;
   const int rows = tile_rows(Hq, Hkv, max_new);
   const size_t bytes = cached_workspace(cached_ctas(kWorkspaceSms, rows), rows);
-  return rows == attn::kv::kTileRows && short_rows(Hq / Hkv) > 0 ? bytes + cached_workspace(cached_ctas(kWorkspaceSms, 8), 8) : bytes;
+  if (rows != attn::kv::kTileRows || short_rows(Hq / Hkv) == 0) return bytes;
+  const int tile = short_tile(Hq / Hkv);
+  return bytes + cached_workspace(cached_ctas(kWorkspaceSms, tile), tile);
 }
 
 attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void* o, float* lse, int Hq, int S, int max_new,
@@ -264,9 +269,10 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
     if (rows == 8) return launch_decode<1>(p, tm_k, tm_v, s);
     if (rows == 16) return launch_decode<2>(p, tm_k, tm_v, s);
     CachedParams few = p;
-    place_parts(&few, at, sms, 8);
+    const int tile = short_tile(p.group);
+    place_parts(&few, at, sms, tile);
     few.rows_up_to = p.rows_above = short_rows(p.group);
-    st = launch_decode<1>(few, tm_k, tm_v, s);
+    st = tile == 8 ? launch_decode<1>(few, tm_k, tm_v, s) : launch_decode<2>(few, tm_k, tm_v, s);
     if (st != ATTN_OK) return st;
   }
   if (!make_page_map(&tm_k, cache, 0, cache->page_size, CU_TENSOR_MAP_SWIZZLE_NONE) ||

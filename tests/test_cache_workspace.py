@@ -22,6 +22,13 @@ def test_large_groups_have_no_launch_for_single_tokens(group):
     assert _bytes(group, 500) < _bytes(16, 500) and _bytes(group, 500) < _bytes(1, 500)
 
 
+@pytest.mark.parametrize("group", [9, 12, 16])
+def test_tokens_of_9_to_16_rows_have_tiles_of_16(group):
+    """16 rows a tile and one CTA an SM instead of 8 and two: the same number of part rows, but half as many pieces (32 bytes each)."""
+    parts = _bytes(group, 500) - _bytes(17, 500)
+    assert parts == _bytes(group, 1) and parts < _bytes(8, 1)
+
+
 def test_sizes_do_not_depend_on_the_length():
     for group in (1, 4, 8, 12, 16):
         assert _bytes(group, 300) == _bytes(group, 300000) == _bytes(group, 300, heads=7)
