@@ -37,6 +37,7 @@ struct DeviceState {
   bool failed = false;
   int sm_count = 0;
   int max_pairs = 0;                 // CTA pairs (clusters of two) that can be resident at once
+  std::atomic<bool> cached_ready{false};  // attn_fwd_cached's kernels have their shared memory
   unsigned int* counters = nullptr;  // [kCounterSlots]
   int* status = nullptr;             // [2]
   unsigned long long* clock_stamps = nullptr;  // [kStampSlots][4], one entry per launch, see FwdParams
@@ -87,22 +88,6 @@ int resident_pairs(int sm_count) {
   return n > 0 ? n : 1;
 }
 
-template <int NB>
-bool prepare_decode() {
-  return cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              attn::kv::Dec<NB>::kSmem) == cudaSuccess &&
-         cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kInt8, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              attn::kv::Dec<NB>::kSmem) == cudaSuccess;
-}
-
-template <int GRAN>
-bool prepare_tile() {
-  return cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              attn::kv::kTSmemBytes) == cudaSuccess &&
-         cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kInt8, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              attn::kv::kTSmemBytes) == cudaSuccess;
-}
-
 // Per-device one-time set-up: architecture check, kernel attribute, scheduler counters and
 // status word.  Returns the state or nullptr (with *st set).
 DeviceState* device_state(attn_status_t* st) {
@@ -151,8 +136,6 @@ DeviceState* device_state(attn_status_t* st) {
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
       cudaFuncSetAttribute(attn::bwd::attn_bwd_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            attn::bwd::kSmemBwdBytes) != cudaSuccess ||
-      !prepare_decode<1>() || !prepare_decode<2>() ||
-      !prepare_tile<16>() || !prepare_tile<32>() || !prepare_tile<64>() ||
       cudaMalloc(&d.counters, kCounterSlots * sizeof(unsigned int)) != cudaSuccess ||
       cudaMalloc(&d.status, 2 * sizeof(int)) != cudaSuccess ||
       cudaMemset(d.status, 0, 2 * sizeof(int)) != cudaSuccess ||

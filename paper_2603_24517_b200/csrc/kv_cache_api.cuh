@@ -138,6 +138,31 @@ uintptr_t place_parts(CachedParams* p, uintptr_t at, int sms, int rows) {
   return reinterpret_cast<uintptr_t>(p->pieces + 2 * p->ctas);
 }
 
+template <int NB>
+bool prepare_decode() {
+  return cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kE4m3, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::Dec<NB>::kSmem) == cudaSuccess &&
+         cudaFuncSetAttribute(attn::kv::attn_cached_decode_kernel<attn::kv::kInt8, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::Dec<NB>::kSmem) == cudaSuccess;
+}
+
+template <int GRAN>
+bool prepare_tile() {
+  return cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kE4m3, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::kTSmemBytes) == cudaSuccess &&
+         cudaFuncSetAttribute(attn::kv::attn_cached_tile_kernel<attn::kv::kInt8, GRAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              attn::kv::kTSmemBytes) == cudaSuccess;
+}
+
+// Done by the first call of attn_fwd_cached on a device: the other entry points neither wait for these ten kernels (the first attn_fwd of a
+// process takes 5.5 ms, with them 6.0) nor fail with them.  Calls at once may both do it.
+bool prepare_cached(DeviceState* dev) {
+  if (dev->cached_ready.load(std::memory_order_acquire)) return true;
+  if (!prepare_decode<1>() || !prepare_decode<2>() || !prepare_tile<16>() || !prepare_tile<32>() || !prepare_tile<64>()) return false;
+  dev->cached_ready.store(true, std::memory_order_release);
+  return true;
+}
+
 // The join as a launch that may begin before the one in front of it has ended (it waits for that one's results on the device).
 template <int ROWS>
 attn_status_t launch_join(const CachedParams& p, int blocks, cudaStream_t s) {
@@ -245,6 +270,7 @@ attn_status_t attn_fwd_cached(const attn_kv_cache_t* cache, const void* q, void*
   if (workspace_bytes < attn_fwd_cached_workspace_bytes(Hq, cache->Hkv, max_new)) return ATTN_ERR_TOO_LARGE;
   DeviceState* dev = device_state(&st);
   if (dev == nullptr) return st;
+  if (!prepare_cached(dev)) return ATTN_ERR_CUDA;
   p.q = static_cast<const uint16_t*>(q);
   p.o = static_cast<uint16_t*>(o);
   p.lse = lse;
