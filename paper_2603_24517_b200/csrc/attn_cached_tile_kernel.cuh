@@ -32,6 +32,7 @@ namespace kv {
 
 constexpr int kTileRows = 256;  // rows of a work item: two stages
 constexpr int kConvWarps = 6;
+constexpr int kItemReaders = 1 + 8 + kConvWarps;  // warps that read an item: MMA, softmax, converters (four of them write results)
 // registers of a thread after the split of the CTA's 64K: 8 softmax, 8 other warps
 constexpr int kTRegsSoftmax = 192, kTRegsOther = 64;
 static_assert(8 * kTRegsSoftmax + 8 * kTRegsOther <= 2048, "register split");
@@ -60,8 +61,8 @@ enum : int { kMetaK = 0, kMetaV = 8, kMetaInv = 16, kMetaFloor = 24, kMetaBad = 
 struct TileBarriers {
   uint64_t* q_full;    // [2] softmax (4 warps): the stage's Q is in shared memory -> MMA
   uint64_t* raw_full;  // [2] TMA: the codes of the keys, of the values -> converters
-  uint64_t* raw_empty; // [2] converters (2 warps) -> fetching warp
-  uint64_t* kv_full;   // [kKvSlots] converters (2 warps) -> MMA
+  uint64_t* raw_empty; // [2] converters (kConvWarps warps) -> fetching warp
+  uint64_t* kv_full;   // [kKvSlots] converters (kConvWarps warps) -> MMA
   uint64_t* kv_empty;  // [kKvSlots] MMA commit -> converters
   uint64_t* s_full;    // [2] MMA commit -> softmax
   uint64_t* p_half;    // [2] softmax (4 warps): the first 64 keys of P -> MMA
@@ -70,9 +71,9 @@ struct TileBarriers {
   uint64_t* o_empty;   // [2] epilogue (4 warps) -> MMA
   uint64_t* l_full;    // [2] softmax (128 threads) -> epilogue
   uint64_t* l_empty;   // [2] epilogue (128 threads) -> softmax
-  uint64_t* meta_full; // [kMetaSteps] fetching warp -> softmax
-  uint64_t* item_full;  // [kItemSlots] fetching warp -> MMA, softmax, epilogue
-  uint64_t* item_empty; // [kItemSlots] those 13 warps -> fetching warp
+  uint64_t* meta_full; // [kMetaSteps] fetching warp -> softmax; converters read the entry too, behind raw_full
+  uint64_t* item_full;  // [kItemSlots] fetching warp -> MMA, softmax, converters
+  uint64_t* item_empty; // [kItemSlots] those kItemReaders warps -> fetching warp
 };
 enum : int { kRoleConvert = 6 << 8, kBarMeta = 20 };
 
@@ -823,7 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_cached_tile_kernel(const __g
     for (int i = 0; i < kMetaSteps; ++i) mbar_init(&bars.meta_full[i], 1);
     for (int i = 0; i < kItemSlots; ++i) {
       mbar_init(&bars.item_full[i], 1);
-      mbar_init(&bars.item_empty[i], kSchedConsumers + 2);
+      mbar_init(&bars.item_empty[i], kItemReaders);
     }
     *abort_flag = 0;
     fence_mbar_init();
