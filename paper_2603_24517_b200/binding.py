@@ -800,8 +800,9 @@ def attn_fwd_cached_status(q, cache, o, lse, block_table, seq_lens, starts=None,
 def attn_fwd_cached(q, cache, o, lse, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale=None, workspace=None,
                     stream=None) -> None:
     """``attn_fwd_cached`` of the C ABI: attention of the rows q [B,S,Hq,D] (or [rows,Hq,D] with ``starts``), the last ones of
-    their sequences, over the cache -> o, lse [B,Hq,S] or [Hq,rows] (lse may be None).  ``max_new``: rows of the longest sequence
-    (a hint; None: all rows of a packed batch)."""
+    their sequences, over the cache -> o, lse [B,Hq,S] or [Hq,rows] (lse may be None).  ``max_new``: rows of the longest sequence,
+    a hint that chooses the kernels.  None takes all rows of the batch for one sequence's, as nothing on the host says more: give it
+    with ``starts`` wherever the longest sequence has fewer, 1 for a decoding step."""
     st = attn_fwd_cached_status(q, cache, o, lse, block_table, seq_lens, starts, max_new, causal, scale, workspace, stream)
     if st != ATTN_OK:
         raise AttnError(st, "attn_fwd_cached")
@@ -948,7 +949,8 @@ def kv_cache_read(cache, block_table, seq_lens, starts=None, n: int | None = Non
 def attention_cached(q, cache, block_table, seq_lens, starts=None, max_new=None, causal: bool = True, scale: float | None = None,
                      return_lse: bool = True):
     """Convenience wrapper: allocates o (and lse) with torch and calls ``attn_fwd_cached``.  q holds the queries of the last
-    tokens of each sequence, whose keys and values are in the cache already (``kv_cache_append``)."""
+    tokens of each sequence, whose keys and values are in the cache already (``kv_cache_append``).  With ``starts`` give ``max_new``, the
+    rows of the longest sequence, too: without it the kernels for long prompts are taken."""
     o = _new_like(q)
     lse = None
     if return_lse and q.dim() >= 3:
