@@ -19,8 +19,8 @@
 // that may lag by a factor of 2^8 (so it is reduced over the lanes only when one of them meets a larger score), which leaves
 // f16 its 11 bits of both; V's scale is part of the exponent (below).
 //
-// 64 sequences of up to 8192 tokens (32 / 8 heads, E4M3, 744 MB): 135 us, 5.5 TB/s, 86 % of the copy rate; INT8 codes take 10 %
-// longer.  One token on 512: 9.9 us, all latency (lengths, pages, codes, merge, join).  What a lone warp of a scheduler could not
+// 64 sequences of up to 8192 tokens (32 / 8 heads, E4M3, 744 MB): 132 us, 5.6 TB/s, 88 % of the copy rate; INT8 codes take 10 %
+// longer.  One token on 512: 10.0 us, all latency (lengths, pages, codes, merge, join).  What a lone warp of a scheduler could not
 // hide bounded the first form (8 warps an SM, 217 us).  Measured slower: tiles of 16 rows at two CTAs an SM (186 us for 16
 // sequences where one CTA takes 112: spills), of 32 rows (213), the merge in loops (9.9 against 9.5 us for the short one).
 #pragma once

@@ -18,11 +18,13 @@
 // Work: the line of (sequence, key head, tile pair, 128 keys) steps cut into equal pieces, as in the decoding kernel.  A tile whose
 // rows fit one stage takes its keys on both stages in turn and joins the two results.
 //
-// Bound by the chain softmax -> P V -> Q K^T of the forward kernel, which the converters beside it and the five roles' instruction
-// fetches lengthen: 8192 rows on 32768 keys (32 / 8 heads, E4M3) 3.22 ms, 1194 TFLOP/s, where the forward kernel takes 2.92 on BF16
-// keys laid out one after another; without the conversion (a timing copy) 6 % less.  A step of a tile pair takes 2.1 us, of one
-// stage's rows 1.9 us.  Code that runs once an item is kept in short loops: straight-line code that is not in the instruction
-// cache takes about 20 clocks an instruction here (an item's switch 14000 clocks, in loops 7000).
+// Bound by the chain softmax -> P V -> Q K^T of the forward kernel, which the converters beside it and the five roles'
+// instruction fetches lengthen: 8192 rows on 32768 keys (32 / 8 heads, E4M3) 3.20 ms, 1200 TFLOP/s, replayed on a GPU with
+// nothing else to do (INT8 3.39), where the forward kernel takes 2.92 on BF16 keys laid out one after another; 3.63 ms, 1060
+// TFLOP/s, in calls one behind the other at the power limit.  Without the conversion (a timing copy) 6 % less.  A step of a tile
+// pair takes 2.1 us, of one stage's rows 1.9 us.  The softmax warps spill 128 to 152 bytes a thread (a row's 128 scores fill the
+// 128 registers the kernel compiles for).  Code that runs once an item is kept in short loops: straight-line code that is not in
+// the instruction cache takes about 20 clocks an instruction here (an item's switch 14000 clocks, in loops 7000).
 #pragma once
 
 #include "attn_cached_kernel.cuh"

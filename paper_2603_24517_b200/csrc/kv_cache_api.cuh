@@ -112,8 +112,8 @@ size_t cached_workspace(int ctas, int rows) {
 }
 constexpr int kWorkspaceSms = 160;  // SMs of a device at most
 // In a packed batch with long sequences, single tokens and what else fits 8 rows go to the decoding kernel first (a step of 24
-// sequences, 21 of them single tokens: 343 us all in tiles of 256 rows, 290 so; 4 us where there are none; 16 rows of two
-// tokens stay, 16 sequences of 16 to 32 rows take 88 us together and 112 apart; nor is it worth a launch where none has over 64).
+// sequences, 21 of them single tokens: 318 us all in tiles of 256 rows, 275 so; 4 us where there are none; 16 rows of two
+// tokens stay, 16 sequences of 16 to 32 rows take a quarter more time apart; nor is it worth a launch where none has over 64).
 // Tokens of 9 to 16 rows take tiles of 16, which read their keys once (64 sequences, groups of 16: 314 us in tiles of 8, 305 of 16; 48
 // sequences, groups of 12: 652 and 637; all in tiles of 256 rows 339 and 736, but 24 sequences of 2 key heads 176 where these take 192).
 // More than 16 heads a key head: a single token has too many rows itself, so nothing is split off (16 sequences, groups of 32: 60.0 us
@@ -122,7 +122,7 @@ int short_rows(int group) { return group <= 8 ? 8 : group <= 16 ? group : 0; }
 int short_tile(int group) { return group <= 8 ? 8 : 16; }
 
 // Rows of a query tile for the longest sequence's (token, head of a group) rows.  Decoding, 16 sequences of 12000 tokens, 8 key heads,
-// E4M3: 8 rows 77 us in tiles of 8, 110 of 16; 16 rows 133 and 113; 32 rows 208 in tiles of 16, 176 of 256.
+// E4M3: 8 rows 76 us in tiles of 8, 106 of 16, 168 of 256; 16 rows 131, 108 and 168; 32 rows 251, 201 and 170.
 int tile_rows(int Hq, int Hkv, int max_new) {
   const long long rows = static_cast<long long>(Hq / Hkv) * max_new;
   return rows <= 8 ? 8 : rows <= 16 ? 16 : attn::kv::kTileRows;
@@ -190,7 +190,7 @@ attn_status_t launch_decode(const CachedParams& p, const CUtensorMap& tm_k, cons
   return launch_join<D::kRows>(p, D::kRows, s);
 }
 
-// GRAN: keys that share their scales.  Three prompts of 700 rows on 4700 keys, pages of 32: 206 us by 16 keys, 195 by 32.
+// GRAN: keys that share their scales.  Three prompts of 700 rows on 4700 keys, pages of 32: 200 us by 16 keys, 191 by 32.
 template <int GRAN>
 attn_status_t launch_tile(const CachedParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
   if (p.c.type == ATTN_KV_E4M3) {

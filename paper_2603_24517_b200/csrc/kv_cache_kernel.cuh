@@ -10,12 +10,13 @@
 // larger scale without a rounding error outside the smallest binades, and x / s is exact; the price is less than one bit of
 // range, which a floating code does not miss.
 //
-// Both directions are bound by HBM: 3 bytes a value.  One CTA owns one page and head of the keys or of the values, a warp 16
-// slots of it, so the largest magnitude is known in the CTA, nobody else touches the scale, and eight 16-byte (codes: 8-byte)
-// accesses are in flight in each lane.  Which page that is follows from the CTA's index alone: sequence b owns the units from
-// starts[b] / page + 2 b on, which is at least as many as it has pages, so a warp finds b by a search over `starts` and no
-// list of pages has to be made first.  32768 tokens of 8 heads: 37.8 us to append, 35.1 to read back, 5.3 and 5.7 TB/s; three CTAs
-// of 256 threads' worth of registers (80, a few spills) against two without spills: 38 and 45 us.
+// Both directions move 3 bytes a value, which bounds them (all but the append in INT8, below).  One CTA owns one page and head
+// of the keys or of the values, a warp 16 slots of it, so the largest magnitude is known in the CTA, nobody else touches the
+// scale, and eight 16-byte (codes: 8-byte) accesses are in flight in each lane.  Which page that is follows from the CTA's index
+// alone: sequence b owns the units from starts[b] / page + 2 b on, which is at least as many as it has pages, so a warp finds b
+// by a search over `starts` and no list of pages has to be made first.  32768 tokens of 8 heads: 37.8 us to append, 35.5 to read
+// back, 5.3 and 5.7 TB/s, in INT8 81.0 (not profiled: the codes take a dozen instructions a value and a branch around a
+// division) and 36.4; three CTAs of 256 threads' worth of registers (80, a few spills) against two without spills: 38 and 45 us.
 #pragma once
 
 #include <cuda_fp16.h>
